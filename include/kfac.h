@@ -446,6 +446,95 @@ int32_t kfac_refresh_due(const kfac_refresh_state *s, int32_t t);
 void kfac_refresh_advance(kfac_refresh_state *s, double ratio_m1, double ratio_m2, double alpha);
 
 /*
+ * Token and expert layers.  What a model whose inputs are tokens, or whose rows are dealt to experts, needs beside the
+ * layers above: segments, embedding, dropout, products grouped by expert, and the Kronecker factors of experts.  An
+ * embedding's factor A is diagonal (the token frequencies); an expert is a fully-connected layer over the rows that it
+ * received, and its factors, inverses and preconditioned gradients go through kfac_invert and kfac_precondition as those of
+ * any layer.  All work goes to the context's stream; the number of launches does not depend on device data, nothing is read
+ * back and nothing is allocated.  Tensors with an ld argument are row-major with rows ld elements apart (a view of a wider
+ * tensor); any alignment to whole elements serves.  Results do not depend on the order in which threads arrive.
+ */
+
+/*
+ * Stable segments.  ids: dev [n] int32 (id_bits = 32) or int64 (64); num >= 1 keys.
+ *   order   [n]        the positions 0 .. n-1 sorted by id, equal ids in the order of their positions; positions whose id is
+ *                      outside [0, num) (padding, a choice beyond an expert's capacity) come last, in order
+ *   offsets [num + 1]  order[offsets[k] .. offsets[k+1]) holds the positions of id k; offsets[num]: positions with an id
+ * n = 0 gives offsets of zero.  Scratch from the workspace: kfac_segments_workspace_bytes (0 for invalid arguments).
+ */
+size_t kfac_segments_workspace_bytes(int32_t n, int32_t num);
+kfac_status kfac_segments(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_bits, int32_t num, int32_t *order, int32_t *offsets);
+
+/*
+ * Embedding lookup with scaling: out[i, :] = scale * table[ids[i], :], zero where ids[i] is outside [0, vocab).
+ * table: dev [vocab, dim] (rows ld_table apart) of table_type, out: dev [n, dim] of out_type (fp32 master weights and bf16
+ * activations go together); the product is formed in fp32 and rounded once.  Needs no workspace.
+ */
+kfac_status kfac_embedding(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_bits, int32_t vocab, int32_t dim, kfac_dtype table_type,
+                           const void *table, int64_t ld_table, float scale, kfac_dtype out_type, void *out, int64_t ld_out);
+
+/*
+ * Gradient of the table, and its Kronecker factor A.  grad_out: dev [n, dim] of `type` (rows ld_grad apart);
+ *   dW[v, :]   = scale * sum_{i: ids[i] = v} grad_out[i, :]      (+ the old dW[v, :] if accumulate != 0; without it rows of
+ *                tokens that do not occur become zero)            dev in/out [vocab, dim] fp32
+ *   A_diag[v] <- decay * A_diag[v] + (1 - decay) * #{i: ids[i] = v} / n    dev in/out [vocab] fp32, or NULL.  For one-hot
+ *                inputs a, A = E[a a^T] has this diagonal and nothing else.  decay = 0 never reads the old contents; n = 0
+ *                leaves A_diag as it is.
+ * Sums in fp32 in an order that depends on n and the ids only (the same inputs give the same bits).  Positions with an id
+ * outside [0, vocab) add nothing (they count in n).  Workspace: kfac_embedding_workspace_bytes (0 for invalid arguments).
+ */
+size_t kfac_embedding_workspace_bytes(int32_t n, int32_t vocab, int32_t dim);
+kfac_status kfac_embedding_grad(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_bits, int32_t vocab, int32_t dim, kfac_dtype type,
+                                const void *grad_out, int64_t ld_grad, float scale, int32_t accumulate, float *dW, float decay, float *A_diag);
+
+/*
+ * Dropout.  x, residual (or NULL), y: dev [rows, cols] of `type`, rows ldx, ldr, ldy apart.
+ *   y = residual + keep * x / (1 - q),   q = round(65536 p) / 65536,  0 <= p <= 1  (p = 1 drops everything)
+ * formed in fp32 and rounded once.  keep is a function of (seed, offset, row * cols + col) alone and is never stored: the
+ * gradient is the same call on the output gradient with the same seed and offset and without a residual.  Element i takes
+ * the 16 bits [16 (i % 2), 16 (i % 2) + 16) of word (i % 8) / 2 of Philox4x32-10 with key (seed low, high) and counter
+ * (i / 8 low, high, offset low, high), and is kept if they are >= 65536 q.  A dropped element gives zero whatever x holds.
+ * Calls that shall be independent differ in seed or offset (layer, step).  y may be x or residual itself (same rows).
+ */
+kfac_status kfac_dropout(kfac_ctx *ctx, int64_t rows, int64_t cols, kfac_dtype type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                         float p, uint64_t seed, uint64_t offset, void *y, int64_t ldy);
+
+/*
+ * Products grouped by expert.  L: one expert as a fully-connected layer (k = 1, stride 1, no padding, h_in = w_in = 1; N is
+ * not used); all experts have its dimensions.  n choices: choice c = t * fan + j sends row t of x to its j-th expert
+ * (fan: experts a row goes to, n a multiple of it).  order, offsets: as kfac_segments makes them of the choices' expert
+ * numbers; order = NULL: choices are sorted already.  Lengths stay on the device; an expert may have none.
+ *   forward      y[c, :]  = W_e x[c / fan, :] (+ b_e)        e the expert of choice c
+ *   grad_input   dx[c, :] = W_e^T dy[c, :]                   (the gradient of x[t, :] is the sum over its fan choices)
+ *   grad_weight  dW_e     = sum_{c of e} dy[c, :] x[c / fan, :]^T, the bias gradient sum dy[c, :] as the last column
+ * x: dev [n / fan, c_in], y, dy: dev [n, c_out], dx: dev [n, c_in], all of `type`, indexed by choice, not by place in `order`;
+ * rows of choices that no expert takes become zero in y and dx.  W: dev [experts, c_out, ldw] of `type`, row o of expert e
+ * at (e * c_out + o) * ldw, its bias (L->bias) in column c_in.  dW: dev [experts, dG, dA] fp32, overwritten, zero for an
+ * expert without rows.  Accumulation in fp32, one rounding at the end; fp32 operands as products of three bf16 planes
+ * (see the rules at the top).  Workspace: kfac_expert_workspace_bytes serves all of them and kfac_stats_expert (0 for
+ * invalid arguments).
+ */
+size_t kfac_expert_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n);
+kfac_status kfac_expert_forward(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type, const int32_t *order,
+                                const int32_t *offsets, const void *x, int64_t ldx, const void *W, int64_t ldw, void *y, int64_t ldy);
+kfac_status kfac_expert_grad_input(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, kfac_dtype type, const int32_t *order,
+                                   const int32_t *offsets, const void *dy, int64_t ldy, const void *W, int64_t ldw, void *dx, int64_t ldx);
+kfac_status kfac_expert_grad_weight(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type,
+                                    const int32_t *order, const int32_t *offsets, const void *x, int64_t ldx, const void *dy, int64_t ldy,
+                                    float *dW);
+
+/*
+ * Factors of experts (Eq. 9 for every expert over the n_e rows that it received) and their running averages:
+ *   A_e <- decay A_e + (1 - decay) / n_e sum x x^T   (x with a constant 1 behind it if L->bias),   A_ema: dev [experts, dA, dA]
+ *   G_e <- decay G_e + (1 - decay) / n_e sum g g^T                                                 G_ema: dev [experts, dG, dG]
+ * x: dev [n / fan, c_in], grad_out: dev [n, c_out] of `in`: per-sample gradients as for kfac_stats.  A_ema or G_ema may be
+ * NULL (that factor is skipped, its input not read).  decay = 0 overwrites; an expert without rows keeps its factors.
+ */
+kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype in, const int32_t *order,
+                              const int32_t *offsets, const void *x, int64_t ldx, const void *grad_out, int64_t ldg, float decay, float *A_ema,
+                              float *G_ema);
+
+/*
  * Optional per-launch timing for benchmarks (not part of the method).  While enabled,
  * every kernel launch of this context is bracketed by HIP events on the context's stream.
  * kfac_profile_read waits for the stream, copies up to max_entries records (in launch
@@ -457,14 +546,16 @@ void kfac_refresh_advance(kfac_refresh_state *s, double ratio_m1, double ratio_m
 typedef enum {
     KFAC_K_GEMM_F32 = 0, KFAC_K_GEMM_BF16 = 1, KFAC_K_GEMM_REDUCE = 2, KFAC_K_PATCH = 3, KFAC_K_TRACE = 4,
     KFAC_K_COPY_DAMP = 5, KFAC_K_LEAF_INVERSE = 6, KFAC_K_ZERO = 7, KFAC_K_BN_UNIT = 8, KFAC_K_BN_REDUCE = 9,
-    KFAC_K_PAD = 10, KFAC_K_ASSEMBLE = 11, KFAC_K_BORDER = 12, KFAC_K_STALENESS = 13, KFAC_K_PACK = 14, KFAC_K_UPDATE = 15, KFAC_K_BN_FULL = 16, KFAC_K_LAYOUT = 17, KFAC_K_GEMM_F32_SPLIT = 18
+    KFAC_K_PAD = 10, KFAC_K_ASSEMBLE = 11, KFAC_K_BORDER = 12, KFAC_K_STALENESS = 13, KFAC_K_PACK = 14, KFAC_K_UPDATE = 15, KFAC_K_BN_FULL = 16, KFAC_K_LAYOUT = 17, KFAC_K_GEMM_F32_SPLIT = 18,
+    KFAC_K_SEGMENTS = 19, KFAC_K_EMBEDDING = 20, KFAC_K_DROPOUT = 21, KFAC_K_EXPERT = 22
 } kfac_kernel;
 
 typedef struct {
     int32_t kernel;    /* kfac_kernel */
     int32_t variant;   /* GEMM: 0 = 128x128 tiles, 1 = 64x64 tiles, 2 / 3 = 32x32 / 64x64 without LDS staging,
-                        * 4 = the displaced products of one image together */
-    int32_t workgroups;
+                        * 4 = the displaced products of one image together.  Embedding: 0 = lookup, 1 .. 3 = the passes of
+                        * its gradient; experts: 0 = forward, 1 = grad_input, 2 = grad_weight, 3 = factors */
+    int32_t workgroups;   /* 0: not reported (token and expert layers) */
     float ms;
     double flops;
     double bytes;

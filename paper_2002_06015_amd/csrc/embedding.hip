@@ -1,0 +1,307 @@
+// Embedding lookup with scaling, and the gradient of its table by sorted tokens.
+//
+// Lookup: out[i] = scale * T[ids[i]].  A wave per 16-byte piece of 64 lanes of a row; reads the distinct rows, writes all.
+//
+// Gradient: dT[v] = scale * sum over the positions of token v, added in fp32 in the order of the positions, without atomics.
+// The positions come sorted by token.  A wave takes a run of `chunk` sorted positions and one 64-lane piece of the columns,
+// keeps the running sum in registers and writes a row where the token changes.  A token whose positions cross runs leaves its
+// part of the sum in scratch, and the join adds the parts in order.  Rows of tokens that do not occur are written by a kernel
+// of their own.  Memory bound: the gradients are read once, the table's gradient is written once.
+#include "token_internal.h"
+
+namespace kfac {
+
+namespace {
+
+typedef unsigned short bf16_t;
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));                     // 16 bytes at an element's alignment
+typedef unsigned short u16x8_u __attribute__((ext_vector_type(8), aligned(2)));
+typedef unsigned short u16x4_u __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ float from_bf16(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
+// to nearest, ties to even; NaN stays NaN
+__device__ __forceinline__ bf16_t to_bf16(float v) { return __builtin_bit_cast(bf16_t, (__bf16)v); }
+
+// W adjacent elements as floats (W = 8: bf16, 4: float), the first `c` of them
+template <typename T, int W>
+__device__ __forceinline__ void load_piece(const T *__restrict__ p, int c, float (&v)[W])
+{
+    if (c >= W) {
+        if constexpr (sizeof(T) == 2 && W == 8) {
+            const u16x8_u r = *(const u16x8_u *)p;
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = from_bf16(r[j]);
+        } else if constexpr (sizeof(T) == 2) {
+            const u16x4_u r = *(const u16x4_u *)p;
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = from_bf16(r[j]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < W / 4; ++q) {
+                const f32x4_u r = *(const f32x4_u *)((const float *)p + 4 * q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[4 * q + j] = r[j];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            v[j] = 0.f;
+            if (j < c) {
+                if constexpr (sizeof(T) == 2) v[j] = from_bf16(p[j]);
+                else v[j] = p[j];
+            }
+        }
+    }
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void store_piece(T *__restrict__ p, int c, const float (&v)[W])
+{
+    if (c >= W) {
+        if constexpr (sizeof(T) == 2 && W == 8) {
+            u16x8_u r;
+#pragma unroll
+            for (int j = 0; j < W; ++j) r[j] = to_bf16(v[j]);
+            *(u16x8_u *)p = r;
+        } else if constexpr (sizeof(T) == 2) {
+            u16x4_u r;
+#pragma unroll
+            for (int j = 0; j < W; ++j) r[j] = to_bf16(v[j]);
+            *(u16x4_u *)p = r;
+        } else {
+#pragma unroll
+            for (int q = 0; q < W / 4; ++q) {
+                f32x4_u r;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = v[4 * q + j];
+                *(f32x4_u *)((float *)p + 4 * q) = r;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            if (j < c) {
+                if constexpr (sizeof(T) == 2) p[j] = to_bf16(v[j]);
+                else p[j] = v[j];
+            }
+    }
+}
+
+// A thread: W adjacent columns of one row.
+template <typename ID, typename TT, typename TO>
+__global__ __launch_bounds__(256) void embedding_kernel(const ID *__restrict__ ids, long long pieces, int per_row, int vocab, int dim,
+                                                        const TT *__restrict__ table, long long ldt, float scale, TO *__restrict__ out,
+                                                        long long ldo)
+{
+    constexpr int W = sizeof(TT) == 2 && sizeof(TO) == 2 ? 8 : 4;
+    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < pieces; u += (long long)gridDim.x * 256) {
+        const long long row = u / per_row;
+        const int c0 = W * (int)(u - row * per_row);
+        const ID id = ids[row];
+        float v[W];
+        if (id >= 0 && id < (ID)vocab) load_piece<TT, W>(table + (long long)id * ldt + c0, dim - c0, v);
+        else
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[j] *= (id >= 0 && id < (ID)vocab) ? scale : 0.f;
+        store_piece<TO, W>(out + row * ldo + c0, dim - c0, v);
+    }
+}
+
+__device__ __forceinline__ int find_key(const int *__restrict__ keys, int n, int key)   // the first position with keys[i] >= key
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = lo + ((hi - lo) >> 1);
+        if (keys[mid] < key) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+// Rows of tokens that do not occur: zero, unless sums are added to what is there.
+constexpr int kAbsentRows = 32;
+__global__ __launch_bounds__(256) void embedding_absent_kernel(const EmbeddingGrad a)
+{
+    __shared__ int absent[kAbsentRows];
+    const int v0 = blockIdx.x * kAbsentRows;
+    if (threadIdx.x < kAbsentRows) {
+        const int v = v0 + threadIdx.x;
+        int none = 0;
+        if (v < a.vocab) {
+            const int i = find_key(a.keys, a.n, v);
+            none = i >= a.n || a.keys[i] != v;
+            if (none && a.A) a.A[v] = a.decay == 0.f ? 0.f : a.decay * a.A[v];
+        }
+        absent[threadIdx.x] = none;
+    }
+    if (a.accumulate) return;
+    __syncthreads();
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r = threadIdx.x >> 6; r < kAbsentRows; r += 4) {
+        if (!absent[r]) continue;
+        float *row = a.dW + (long long)(v0 + r) * a.dim;
+        for (int c = 4 * (threadIdx.x & 63); c < a.dim; c += 256) store_piece<float, 4>(row + c, a.dim - c, zero);
+    }
+}
+
+template <int W>
+__device__ __forceinline__ void write_row(const EmbeddingGrad &a, int key, int count, int c0, const float (&sum)[W])
+{
+    float *row = a.dW + (long long)key * a.dim + c0;
+    float v[W];
+    if (a.accumulate) load_piece<float, W>(row, a.dim - c0, v);
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = a.accumulate ? fmaf(a.scale, sum[j], v[j]) : a.scale * sum[j];
+    store_piece<float, W>(row, a.dim - c0, v);
+    if (c0 == 0 && a.A) a.A[key] = a.decay == 0.f ? a.share * count : fmaf(a.share, (float)count, a.decay * a.A[key]);
+}
+
+// A wave: a run of sorted positions, 64 W columns.
+template <typename T>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingGrad a, int col_tiles, int chunks)
+{
+    constexpr int W = sizeof(T) == 2 ? 8 : 4, AHEAD = 8;
+    const int lane = threadIdx.x & 63;
+    const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = (int)(unit / col_tiles), c0 = ((int)(unit - (long long)c * col_tiles) * 64 + lane) * W;
+    if (c >= chunks) return;
+    const int i0 = c * a.chunk, cnt = min(a.chunk, a.n - i0);
+    // keys and positions of the run, one a lane; neighbours on either side
+    const int mine = min(i0 + min(lane, cnt - 1), a.n - 1);
+    const int my_key = a.keys[mine], my_pos = a.pos[mine];
+    const int before = i0 > 0 ? a.keys[i0 - 1] : -1, after = i0 + cnt < a.n ? a.keys[i0 + cnt] : -1;
+    const T *g = (const T *)a.g;
+    float sum[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) sum[j] = 0.f;
+    int start = 0, key = __builtin_amdgcn_readlane(my_key, 0);
+    if (key >= a.vocab) return;
+    auto flush = [&](int end) {   // positions [start, end) of this run have `key`
+        if (c0 < a.dim) {
+            const bool from = start > 0 || before != key, to = end < cnt || after != key;
+            if (from && to) {
+                write_row<W>(a, key, end - start, c0, sum);
+            } else {   // the part that goes on from the run before, or the one that goes on behind this run
+                store_piece<float, W>(a.partial + ((long long)2 * c + (from ? 1 : 0)) * a.dim + c0, a.dim - c0, sum);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] = 0.f;
+        start = end;
+    };
+    for (int r0 = 0; r0 < cnt; r0 += AHEAD) {
+        float v[AHEAD][W];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int p = __builtin_amdgcn_readlane(my_pos, min(r0 + u, cnt - 1));
+            if (c0 < a.dim) load_piece<T, W>(g + (long long)p * a.ld + c0, a.dim - c0, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (r0 + u >= cnt) break;
+            const int k = __builtin_amdgcn_readlane(my_key, r0 + u);
+            if (k != key) {
+                flush(r0 + u);
+                key = k;
+                if (key >= a.vocab) return;   // sorted: no token from here on
+            }
+#pragma unroll
+            for (int j = 0; j < W; ++j) sum[j] += v[u][j];
+        }
+    }
+    flush(cnt);
+}
+
+// Tokens whose positions cross runs: the workgroup of the run in which such a token starts adds its parts, in order.
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void embedding_join_kernel(const EmbeddingGrad a, int chunks)
+{
+    __shared__ float part[WAVES][64][4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = blockIdx.x, last = min((c + 1) * a.chunk, a.n) - 1;
+    const int key = a.keys[last];
+    if (key >= a.vocab || last + 1 >= a.n || a.keys[last + 1] != key) return;                   // nothing goes on behind this run
+    if (c > 0 && a.keys[c * a.chunk] == key && a.keys[c * a.chunk - 1] == key) return;          // it did not start here
+    const int begin = find_key(a.keys, a.n, key), end = find_key(a.keys, a.n, key + 1);
+    const int c1 = (end - 1) / a.chunk, parts = c1 - c + 1;                                     // parts of the runs c .. c1
+    const int per = (parts + WAVES - 1) / WAVES, p0 = min(wave * per, parts), p1 = min(p0 + per, parts);
+    const int c0 = (blockIdx.y * 64 + lane) * 4;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c0 < a.dim) {
+#pragma unroll 8
+        for (int p = p0; p < p1; ++p) {
+            float v[4];
+            load_piece<float, 4>(a.partial + ((long long)2 * (c + p) + (p == 0 ? 1 : 0)) * a.dim + c0, a.dim - c0, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][lane][j] = sum[j];
+    __syncthreads();
+    if (wave != 0 || c0 >= a.dim) return;
+    for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += part[w][lane][j];
+    write_row<4>(a, key, end - begin, c0, sum);
+}
+
+template <typename ID, typename TT, typename TO>
+hipError_t lookup(const ID *ids, int n, int vocab, int dim, const void *table, long long ldt, float scale, void *out, long long ldo, hipStream_t s)
+{
+    constexpr int W = sizeof(TT) == 2 && sizeof(TO) == 2 ? 8 : 4;
+    const int per_row = (dim + W - 1) / W;
+    const long long pieces = (long long)n * per_row;
+    const long long wgs = (pieces + 255) / 256;
+    embedding_kernel<ID, TT, TO><<<dim3((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20))), dim3(256), 0, s>>>(
+        ids, pieces, per_row, vocab, dim, (const TT *)table, ldt, scale, (TO *)out, ldo);
+    return hipGetLastError();
+}
+
+template <typename ID>
+hipError_t lookup_types(const ID *ids, int n, int vocab, int dim, int table_bf16, const void *table, long long ldt, float scale, int out_bf16,
+                        void *out, long long ldo, hipStream_t s)
+{
+    if (table_bf16) return out_bf16 ? lookup<ID, bf16_t, bf16_t>(ids, n, vocab, dim, table, ldt, scale, out, ldo, s)
+                                    : lookup<ID, bf16_t, float>(ids, n, vocab, dim, table, ldt, scale, out, ldo, s);
+    return out_bf16 ? lookup<ID, float, bf16_t>(ids, n, vocab, dim, table, ldt, scale, out, ldo, s)
+                    : lookup<ID, float, float>(ids, n, vocab, dim, table, ldt, scale, out, ldo, s);
+}
+
+}  // namespace
+
+hipError_t launch_embedding(const void *ids, int id_bits, int n, int vocab, int dim, int table_bf16, const void *table, long long ldt,
+                            float scale, int out_bf16, void *out, long long ldo, hipStream_t s)
+{
+    return id_bits == 64 ? lookup_types((const long long *)ids, n, vocab, dim, table_bf16, table, ldt, scale, out_bf16, out, ldo, s)
+                         : lookup_types((const int *)ids, n, vocab, dim, table_bf16, table, ldt, scale, out_bf16, out, ldo, s);
+}
+
+int embedding_chunk(int n) { return n <= 32768 ? 8 : 32; }
+
+hipError_t launch_embedding_absent(const EmbeddingGrad &a, hipStream_t s)
+{
+    embedding_absent_kernel<<<dim3((a.vocab + kAbsentRows - 1) / kAbsentRows), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s)
+{
+    const int chunks = (a.n + a.chunk - 1) / a.chunk;
+    const int piece = 64 * (a.bf16 ? 8 : 4), col_tiles = (a.dim + piece - 1) / piece;
+    const long long wgs = ((long long)chunks * col_tiles + 3) / 4;
+    if (a.bf16) embedding_sum_kernel<bf16_t><<<dim3((unsigned)wgs), dim3(256), 0, s>>>(a, col_tiles, chunks);
+    else embedding_sum_kernel<float><<<dim3((unsigned)wgs), dim3(256), 0, s>>>(a, col_tiles, chunks);
+    return hipGetLastError();
+}
+
+hipError_t launch_embedding_join(const EmbeddingGrad &a, hipStream_t s)
+{
+    const int chunks = (a.n + a.chunk - 1) / a.chunk;
+    embedding_join_kernel<8><<<dim3(chunks, (a.dim + 255) / 256), dim3(512), 0, s>>>(a, chunks);
+    return hipGetLastError();
+}
+
+}  // namespace kfac

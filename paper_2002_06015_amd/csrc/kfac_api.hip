@@ -4,6 +4,7 @@
 // library; this file only decides what to launch.
 #include "../../include/kfac.h"
 #include "kfac_internal.h"
+#include "token_internal.h"
 
 #include <algorithm>
 #include <climits>
@@ -2853,3 +2854,39 @@ void kfac_refresh_advance(kfac_refresh_state *s, double ratio_m1, double ratio_m
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------- what token_api.hip sees of a context
+namespace kfac {
+
+CtxView ctx_view(const kfac_ctx *ctx) { return CtxView{ctx->stream, ctx->ws, ctx->ws_bytes}; }
+
+bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, double flops, double bytes)
+{
+    if (!ctx->profiling) return true;
+    try {
+        const size_t idx = ctx->prof.size();
+        while (ctx->ev_pool.size() < 2 * (idx + 1)) {
+            ctx->ev_pool.reserve(ctx->ev_pool.size() + 1);   // (throws before the event exists)
+            hipEvent_t ev;
+            if (hipEventCreate(&ev) != hipSuccess) return false;
+            ctx->ev_pool.push_back(ev);
+        }
+        kfac_profile_entry pe{};
+        pe.kernel = kernel;
+        pe.variant = variant;
+        pe.workgroups = workgroups;
+        pe.flops = flops;
+        pe.bytes = bytes;
+        ctx->prof.push_back(pe);
+        return hipEventRecord(ctx->ev_pool[2 * idx], ctx->stream) == hipSuccess;
+    } catch (...) {   // nothing leaves a C entry point
+        return false;
+    }
+}
+
+bool profile_end(kfac_ctx *ctx)
+{
+    return !ctx->profiling || hipEventRecord(ctx->ev_pool[2 * ctx->prof.size() - 1], ctx->stream) == hipSuccess;
+}
+
+}  // namespace kfac

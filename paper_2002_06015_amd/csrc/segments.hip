@@ -1,0 +1,314 @@
+// Stable segments of small keys: order = the positions 0 .. n-1 sorted by key, equal keys in the order of their positions,
+// offsets = where each key starts.  What routing to experts and the gradient of an embedding start from.
+//
+// A counting sort over digits of up to 9 bits, lowest digit first.  The rank of an element among the equal digits of its wave
+// comes from ballots (one a bit: the lanes with the same digit), the count before the wave from LDS, so nothing depends on the
+// order in which atomics arrive.  Up to 8192 positions are sorted by one workgroup whose keys stay in registers and LDS
+// (one launch, bound by the latency of its chain: ballots, an LDS counter, a scan); more take three launches a digit:
+// counts of 2048-position tiles, running sums along the tiles, ranks and scatter.  Reads and writes 16 bytes a position and digit.
+#include "token_internal.h"
+
+namespace kfac {
+
+namespace {
+
+// keys outside [0, num) become num: the last segment, which nobody reads
+template <typename ID>
+__device__ __forceinline__ int seg_key(const ID *ids, int i, int num)
+{
+    const ID v = ids[i];
+    return v >= 0 && v < (ID)num ? (int)v : num;
+}
+
+// Rank of this lane's digit among equal digits of the lanes before it, and their number; `active`: lanes with an element.
+__device__ __forceinline__ int match_digit(int digit, int bits, bool active, int &count)
+{
+    unsigned long long same = __ballot(active);
+    for (int b = 0; b < bits; ++b) {
+        const bool bit = (digit >> b) & 1;
+        const unsigned long long with = __ballot(bit);
+        same &= bit ? with : ~with;
+    }
+    count = __popcll(same);
+    return __popcll(same & ((1ULL << (threadIdx.x & 63)) - 1));
+}
+
+// Ranks of up to ROUNDS x 64 elements of a wave, 64 at a time in order, against counters of the wave in LDS
+template <int ROUNDS>
+__device__ __forceinline__ void rank_wave(const int (&key)[ROUNDS], const bool (&in)[ROUNDS], int rounds, int shift, int bits,
+                                          volatile int *counter, int (&rank)[ROUNDS])
+{
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        if (r >= rounds) break;
+        const int digit = (key[r] >> shift) & ((1 << bits) - 1);
+        int count;
+        const int before = match_digit(digit, bits, in[r], count);
+        const int old = in[r] ? counter[digit] : 0;
+        __builtin_amdgcn_wave_barrier();   // all lanes have read before the first one of each digit counts them
+        rank[r] = old + before;
+        if (in[r] && before == 0) counter[digit] = old + count;
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// counter[w][d] -> elements with a smaller digit, or the same digit in an earlier wave; tmp: [16].  All threads call it.
+template <int WAVES>
+__device__ __forceinline__ void scan_counters(int *counter, int stride, int bins, int *tmp)
+{
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    __syncthreads();
+    int carry = 0;
+    for (int d0 = 0; d0 < bins; d0 += WAVES * 64) {
+        const int d = d0 + t;
+        int sum = 0;
+        if (d < bins)
+            for (int w = 0; w < WAVES; ++w) {
+                const int c = counter[w * stride + d];
+                counter[w * stride + d] = sum;
+                sum += c;
+            }
+        int incl = sum;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 63) tmp[wave] = incl;
+        __syncthreads();
+        int base = carry;
+        for (int w = 0; w < WAVES; ++w) {
+            const int c = tmp[w];
+            if (w < wave) base += c;
+            carry += c;
+        }
+        if (d < bins)
+            for (int w = 0; w < WAVES; ++w) counter[w * stride + d] += base + incl - sum;
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ int lower_bound(const int *keys, int n, int key)
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = lo + ((hi - lo) >> 1);
+        if (keys[mid] < key) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+template <typename ID>
+__global__ __launch_bounds__(1024) void segments_small_kernel(const ID *__restrict__ ids, int n, int num, int passes, int bits,
+                                                              int *__restrict__ order, int *__restrict__ keys, int *__restrict__ offsets)
+{
+    constexpr int WAVES = 16, ROUNDS = kSegSmall / 1024;
+    __shared__ int skey[kSegSmall], spos[kSegSmall];
+    __shared__ int counter[WAVES << kSegBits];
+    __shared__ int tmp[WAVES];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int rounds = (n + 1023) / 1024, first = wave * 64 * rounds + lane;
+    int key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
+    bool in[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int i = first + 64 * r;
+        in[r] = r < rounds && i < n;
+        pos[r] = i;
+        key[r] = in[r] ? seg_key(ids, i, num) : 0;
+        rank[r] = 0;
+    }
+    const int bins = 1 << bits;
+    for (int p = 0; p < passes; ++p) {
+        for (int i = t; i < WAVES * bins; i += 1024) counter[i] = 0;
+        __syncthreads();
+        rank_wave<ROUNDS>(key, in, rounds, p * bits, bits, counter + wave * bins, rank);
+        scan_counters<WAVES>(counter, bins, bins, tmp);
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (in[r]) {
+                const int to = counter[wave * bins + ((key[r] >> (p * bits)) & (bins - 1))] + rank[r];
+                skey[to] = key[r];
+                spos[to] = pos[r];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (in[r]) {
+                key[r] = skey[first + 64 * r];
+                pos[r] = spos[first + 64 * r];
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+        if (in[r]) {
+            order[first + 64 * r] = pos[r];
+            if (keys) keys[first + 64 * r] = key[r];
+        }
+    if (offsets)
+        for (int v = t; v <= num; v += 1024) offsets[v] = lower_bound(skey, n, v);
+}
+
+template <typename ID>
+__global__ __launch_bounds__(256) void segments_count_kernel(const ID *__restrict__ ids, const int *__restrict__ keys, int n, int num, int shift,
+                                                             int bits, int tiles, int *__restrict__ counts)
+{
+    __shared__ int bin[1 << kSegBits];
+    const int bins = 1 << bits, t = threadIdx.x;
+    for (int d = t; d < bins; d += 256) bin[d] = 0;
+    __syncthreads();
+    const int i0 = blockIdx.x * kSegTile;
+#pragma unroll
+    for (int r = 0; r < kSegTile / 256; ++r) {
+        const int i = i0 + t + 256 * r;
+        if (i < n) atomicAdd(&bin[((ids ? seg_key(ids, i, num) : keys[i]) >> shift) & (bins - 1)], 1);
+    }
+    __syncthreads();
+    for (int d = t; d < bins; d += 256) counts[(long long)d * tiles + blockIdx.x] = bin[d];
+}
+
+// one wave a digit: running sums along the tiles, and the digit's total
+__global__ __launch_bounds__(256) void segments_scan_kernel(int *__restrict__ counts, int tiles, int bins, int *__restrict__ totals)
+{
+    const int lane = threadIdx.x & 63, d = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (d >= bins) return;
+    int *row = counts + (long long)d * tiles;
+    int carry = 0;
+    for (int b = 0; b < tiles; b += 64) {
+        const int c = b + lane < tiles ? row[b + lane] : 0;
+        int incl = c;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (b + lane < tiles) row[b + lane] = carry + incl - c;
+        carry += __shfl(incl, 63);
+    }
+    if (lane == 0) totals[d] = carry;
+}
+
+// offsets: given with the only pass, where the digits are the keys
+template <typename ID>
+__global__ __launch_bounds__(256) void segments_scatter_kernel(const ID *__restrict__ ids, const int *__restrict__ keys_in,
+                                                               const int *__restrict__ pos_in, int n, int num, int shift, int bits, int tiles,
+                                                               const int *__restrict__ counts, const int *__restrict__ totals,
+                                                               int *__restrict__ keys_out, int *__restrict__ pos_out, int *__restrict__ offsets)
+{
+    constexpr int WAVES = 4, ROUNDS = kSegTile / 256;
+    __shared__ int counter[WAVES << kSegBits];
+    __shared__ int base[1 << kSegBits];
+    __shared__ int tmp[WAVES];
+    const int bins = 1 << bits, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    for (int i = t; i < WAVES * bins; i += 256) counter[i] = 0;
+    int key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
+    bool in[ROUNDS];
+    const int first = blockIdx.x * kSegTile + wave * 64 * ROUNDS + lane;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int i = first + 64 * r;
+        in[r] = i < n;
+        pos[r] = in[r] ? (pos_in ? pos_in[i] : i) : 0;
+        key[r] = in[r] ? (ids ? seg_key(ids, i, num) : keys_in[i]) : 0;
+        rank[r] = 0;
+    }
+    // where the digits start: a scan of their totals (as if of one wave), plus this tile's place in each
+    __syncthreads();
+    for (int d = t; d < bins; d += 256) counter[d] = totals[d];
+    scan_counters<WAVES>(counter, bins, bins, tmp);      // (the other waves' counters are zero)
+    for (int d = t; d < bins; d += 256) {
+        if (offsets && blockIdx.x == 0 && d <= num) offsets[d] = counter[d];
+        base[d] = counter[d] + counts[(long long)d * tiles + blockIdx.x];
+    }
+    __syncthreads();
+    for (int i = t; i < WAVES * bins; i += 256) counter[i] = 0;
+    __syncthreads();
+    rank_wave<ROUNDS>(key, in, ROUNDS, shift, bits, counter + wave * bins, rank);
+    __syncthreads();
+    for (int d = t; d < bins; d += 256) {
+        int sum = base[d];
+        for (int w = 0; w < WAVES; ++w) {
+            const int c = counter[w * bins + d];
+            counter[w * bins + d] = sum;
+            sum += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+        if (in[r]) {
+            const int to = counter[wave * bins + ((key[r] >> shift) & (bins - 1))] + rank[r];
+            pos_out[to] = pos[r];
+            if (keys_out) keys_out[to] = key[r];
+        }
+}
+
+__global__ __launch_bounds__(256) void segments_offsets_kernel(const int *__restrict__ keys, int n, int num, int *__restrict__ offsets)
+{
+    const int v = blockIdx.x * 256 + threadIdx.x;
+    if (v <= num) offsets[v] = lower_bound(keys, n, v);
+}
+
+template <typename ID>
+hipError_t sort_positions(const ID *ids, int n, int num, const SegmentScratch &w, int *order, const int **keys, int *offsets, hipStream_t s)
+{
+    if (n <= kSegSmall) {
+        const bool here = num < 2 * kSegSmall;   // the offsets of more keys are found by more than one workgroup
+        segments_small_kernel<ID><<<dim3(1), dim3(1024), 0, s>>>(ids, n, num, w.passes, w.bits, order, w.keys[0], here ? offsets : nullptr);
+        if (offsets && !here) segments_offsets_kernel<<<dim3(num / 256 + 1), dim3(256), 0, s>>>(w.keys[0], n, num, offsets);
+        if (keys) *keys = w.keys[0];
+        return hipGetLastError();
+    }
+    const int tiles = (n + kSegTile - 1) / kSegTile, bins = 1 << w.bits;
+    const int *kin = nullptr, *pin = nullptr;
+    for (int p = 0; p < w.passes; ++p) {
+        const bool last = p == w.passes - 1;
+        const ID *from = p == 0 ? ids : nullptr;
+        int *kout = w.keys[p & 1], *pout = last ? order : w.pos[p & 1];
+        segments_count_kernel<ID><<<dim3(tiles), dim3(256), 0, s>>>(from, kin, n, num, p * w.bits, w.bits, tiles, w.counts);
+        segments_scan_kernel<<<dim3((bins + 3) / 4), dim3(256), 0, s>>>(w.counts, tiles, bins, w.totals);
+        segments_scatter_kernel<ID><<<dim3(tiles), dim3(256), 0, s>>>(from, kin, pin, n, num, p * w.bits, w.bits, tiles, w.counts, w.totals,
+                                                                      kout, pout, w.passes == 1 ? offsets : nullptr);
+        kin = kout;
+        pin = pout;
+    }
+    if (keys) *keys = kin;
+    if (offsets && w.passes > 1) segments_offsets_kernel<<<dim3(num / 256 + 1), dim3(256), 0, s>>>(kin, n, num, offsets);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t segment_scratch(char *base, int n, int num, SegmentScratch *out)
+{
+    int bits = 0;
+    while (bits < 31 && ((unsigned)num >> bits)) ++bits;   // keys are 0 .. num
+    SegmentScratch w{};
+    w.passes = (bits + kSegBits - 1) / kSegBits;
+    w.bits = (bits + w.passes - 1) / w.passes;
+    size_t used = 0;
+    auto take = [&](size_t bytes) {
+        char *p = base ? base + used : nullptr;
+        used += (bytes + 255) / 256 * 256;
+        return (int *)p;
+    };
+    const size_t list = sizeof(int) * (size_t)(n > 0 ? n : 1);
+    w.keys[0] = take(list);
+    if (n > kSegSmall) {
+        w.keys[1] = take(list);
+        w.pos[0] = take(list);
+        w.pos[1] = take(list);
+        const size_t tiles = ((size_t)n + kSegTile - 1) / kSegTile;
+        w.counts = take(sizeof(int) * (tiles << w.bits));
+        w.totals = take(sizeof(int) << w.bits);
+    }
+    if (out) *out = w;
+    return used;
+}
+
+hipError_t launch_segments(const void *ids, int id_bits, int n, int num, const SegmentScratch &w, int *order, const int **keys,
+                           int *offsets, hipStream_t s)
+{
+    return id_bits == 64 ? sort_positions((const long long *)ids, n, num, w, order, keys, offsets, s)
+                         : sort_positions((const int *)ids, n, num, w, order, keys, offsets, s);
+}
+
+}  // namespace kfac

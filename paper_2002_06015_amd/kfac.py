@@ -29,10 +29,13 @@ EXPORTS = [
     "kfac_lr_polynomial", "kfac_momentum_coupled", "kfac_update_weights",
     "bn_full_workspace_bytes", "bn_full_precondition", "kfac_nhwc_to_nchw", "kfac_stats_nhwc", "kfac_step_nhwc",
     "kfac_staleness", "kfac_staleness_static", "kfac_next_interval", "kfac_refresh_init", "kfac_refresh_due", "kfac_refresh_advance",
+    "kfac_segments_workspace_bytes", "kfac_segments", "kfac_embedding", "kfac_embedding_workspace_bytes", "kfac_embedding_grad", "kfac_dropout",
+    "kfac_expert_workspace_bytes", "kfac_expert_forward", "kfac_expert_grad_input", "kfac_expert_grad_weight", "kfac_stats_expert",
 ]
 
 KERNEL_NAMES = ["gemm_f32", "gemm_bf16", "gemm_reduce", "patch", "trace", "copy_damp", "leaf_inverse", "zero",
-                "bn_unit", "bn_reduce", "pad", "assemble", "border", "staleness", "pack", "update", "bn_full", "layout", "gemm_f32_split"]
+                "bn_unit", "bn_reduce", "pad", "assemble", "border", "staleness", "pack", "update", "bn_full", "layout", "gemm_f32_split",
+                "segments", "embedding", "dropout", "expert"]
 
 
 class kfac_profile_entry(ctypes.Structure):
@@ -151,6 +154,21 @@ def lib() -> ctypes.CDLL:
         L.kfac_refresh_due.argtypes = [vp, i32]
         L.kfac_refresh_advance.restype = None
         L.kfac_refresh_advance.argtypes = [vp, ctypes.c_double, ctypes.c_double, ctypes.c_double]
+        i64, u64, sz, typ = ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t, ctypes.c_int
+        L.kfac_segments_workspace_bytes.restype = sz
+        L.kfac_segments_workspace_bytes.argtypes = [i32, i32]
+        L.kfac_segments.argtypes = [vp, i32, vp, i32, i32, vp, vp]
+        L.kfac_embedding.argtypes = [vp, i32, vp, i32, i32, i32, typ, vp, i64, f32, typ, vp, i64]
+        L.kfac_embedding_workspace_bytes.restype = sz
+        L.kfac_embedding_workspace_bytes.argtypes = [i32, i32, i32]
+        L.kfac_embedding_grad.argtypes = [vp, i32, vp, i32, i32, i32, typ, vp, i64, f32, i32, vp, f32, vp]
+        L.kfac_dropout.argtypes = [vp, i64, i64, typ, vp, i64, vp, i64, f32, u64, u64, vp, i64]
+        L.kfac_expert_workspace_bytes.restype = sz
+        L.kfac_expert_workspace_bytes.argtypes = [vp, i32, i32]
+        L.kfac_expert_forward.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp, i64]
+        L.kfac_expert_grad_input.argtypes = [vp, vp, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp, i64]
+        L.kfac_expert_grad_weight.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp]
+        L.kfac_stats_expert.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, f32, vp, vp]
         _lib = L
     return _lib
 
@@ -550,6 +568,190 @@ def kfac_refresh_due(state: kfac_refresh_state, t: int) -> bool:
 
 def kfac_refresh_advance(state: kfac_refresh_state, ratio_m1: float, ratio_m2: float, alpha: float) -> None:
     lib().kfac_refresh_advance(ctypes.addressof(state), float(ratio_m1), float(ratio_m2), float(alpha))
+
+
+# ---------------------------------------------------------------- token and expert layers
+_ID_BITS = {torch.int32: 32, torch.int64: 64}
+_KTYPE = {torch.float32: KFAC_F32, torch.bfloat16: KFAC_BF16}
+
+
+def _ids(ids: torch.Tensor, what: str) -> int:
+    if not (ids.is_cuda and ids.is_contiguous() and ids.dim() == 1 and ids.dtype in _ID_BITS):
+        raise ValueError("%s must be a contiguous one-dimensional device tensor of int32 or int64" % what)
+    return _ID_BITS[ids.dtype]
+
+
+def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
+    """The distance of the rows of a [rows, cols] device tensor whose rows are contiguous."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (rows, cols):
+        raise ValueError("%s must be a device tensor of %s and shape [%d, %d], got %s %s" % (what, dtype, rows, cols, t.dtype, tuple(t.shape)))
+    s = t.stride()
+    if (cols > 1 and s[1] != 1) or (rows > 1 and s[0] < cols):
+        raise ValueError("%s must have contiguous rows" % what)
+    return s[0] if rows > 1 else cols
+
+
+def _floats(t: Optional[torch.Tensor], numel: int, what: str):
+    if t is None:
+        return None
+    if not (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.numel() == numel):
+        raise ValueError("%s must be a contiguous float32 device tensor of %d elements" % (what, numel))
+    return t.data_ptr()
+
+
+def _type_of(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _KTYPE:
+        raise ValueError("%s must be float32 or bfloat16" % what)
+    return _KTYPE[t.dtype]
+
+
+def kfac_segments_workspace_bytes(n: int, num: int) -> int:
+    return int(lib().kfac_segments_workspace_bytes(int(n), int(num)))
+
+
+def kfac_segments(ctx: Context, ids: torch.Tensor, num: int, order: torch.Tensor, offsets: torch.Tensor) -> None:
+    """order: int32 [n], the positions sorted by id (stable; ids outside [0, num) last); offsets: int32 [num + 1]."""
+    bits, n = _ids(ids, "ids"), ids.numel()
+    if _ids(order, "order") != 32 or _ids(offsets, "offsets") != 32 or order.numel() != n or offsets.numel() != num + 1:
+        raise ValueError("order must be int32 [%d] and offsets int32 [%d]" % (n, num + 1))
+    st = lib().kfac_segments(ctx.handle, n, ids.data_ptr(), bits, int(num), order.data_ptr(), offsets.data_ptr())
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_segments")
+
+
+def kfac_embedding(ctx: Context, ids: torch.Tensor, table: torch.Tensor, scale: float, out: torch.Tensor) -> None:
+    """out[i] = scale * table[ids[i]]; table and out are float32 or bfloat16 each."""
+    bits, n = _ids(ids, "ids"), ids.numel()
+    if table.dim() != 2:
+        raise ValueError("table must be [vocab, dim]")
+    vocab, dim = table.shape
+    tt, to = _type_of(table, "table"), _type_of(out, "out")
+    st = lib().kfac_embedding(ctx.handle, n, ids.data_ptr(), bits, vocab, dim, tt, table.data_ptr(), _rows_of(table, vocab, dim, table.dtype, "table"),
+                              float(scale), to, out.data_ptr(), _rows_of(out, n, dim, out.dtype, "out"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_embedding")
+
+
+def kfac_embedding_workspace_bytes(n: int, vocab: int, dim: int) -> int:
+    return int(lib().kfac_embedding_workspace_bytes(int(n), int(vocab), int(dim)))
+
+
+def kfac_embedding_grad(ctx: Context, ids: torch.Tensor, grad_out: torch.Tensor, scale: float, dW: torch.Tensor, accumulate: bool = False,
+                        A_diag: Optional[torch.Tensor] = None, decay: float = 0.0) -> None:
+    """dW: float32 [vocab, dim]; A_diag: float32 [vocab], the running average of the token frequencies."""
+    bits, n = _ids(ids, "ids"), ids.numel()
+    if dW.dim() != 2:
+        raise ValueError("dW must be [vocab, dim]")
+    vocab, dim = dW.shape
+    typ = _type_of(grad_out, "grad_out")
+    st = lib().kfac_embedding_grad(ctx.handle, n, ids.data_ptr(), bits, vocab, dim, typ, grad_out.data_ptr(),
+                                   _rows_of(grad_out, n, dim, grad_out.dtype, "grad_out"), float(scale), int(bool(accumulate)),
+                                   _floats(dW, vocab * dim, "dW"), float(decay), _floats(A_diag, vocab, "A_diag"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_embedding_grad")
+
+
+def kfac_dropout(ctx: Context, x: torch.Tensor, p: float, seed: int, offset: int, y: torch.Tensor,
+                 residual: Optional[torch.Tensor] = None) -> None:
+    """y = residual + dropout(x); the gradient is the same call on the output gradient without a residual.  y may be x or residual."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    if not (0 <= int(seed) < 1 << 64 and 0 <= int(offset) < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    rows, cols = x.shape
+    typ = _type_of(x, "x")
+    st = lib().kfac_dropout(ctx.handle, rows, cols, typ, x.data_ptr(), _rows_of(x, rows, cols, x.dtype, "x"),
+                            None if residual is None else residual.data_ptr(),
+                            0 if residual is None else _rows_of(residual, rows, cols, x.dtype, "residual"), float(p), int(seed), int(offset),
+                            y.data_ptr(), _rows_of(y, rows, cols, x.dtype, "y"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_dropout")
+
+
+def _expert(layer, order: Optional[torch.Tensor], offsets: torch.Tensor, n: int):
+    """The layer of one expert, the number of experts and the pointers of the segments."""
+    L = kfac_layer(*[int(v) for v in layer])
+    if _ids(offsets, "offsets") != 32 or offsets.numel() < 2:
+        raise ValueError("offsets must be int32 [experts + 1]")
+    if order is not None and (_ids(order, "order") != 32 or order.numel() != n):
+        raise ValueError("order must be int32 [%d]" % n)
+    return L, offsets.numel() - 1, None if order is None else order.data_ptr(), offsets.data_ptr()
+
+
+def _weights(W: torch.Tensor, L: kfac_layer, experts: int, dtype) -> int:
+    """The distance of the rows of W [experts, c_out, c_in + bias or more]."""
+    if not W.is_cuda or W.dtype != dtype or W.dim() != 3 or W.shape[0] != experts or W.shape[1] != L.c_out or W.shape[2] < L.c_in + L.bias:
+        raise ValueError("W must be a device tensor of %s and shape [%d, %d, at least %d]" % (dtype, experts, L.c_out, L.c_in + L.bias))
+    s = W.stride()
+    if s[2] != 1 or s[1] < L.c_in + L.bias or (experts > 1 and s[0] != L.c_out * s[1]):
+        raise ValueError("W must have contiguous rows, equally far apart over all experts")
+    return s[1]
+
+
+def kfac_expert_workspace_bytes(layer, experts: int, n: int) -> int:
+    L = kfac_layer(*[int(v) for v in layer])
+    return int(lib().kfac_expert_workspace_bytes(ctypes.addressof(L), int(experts), int(n)))
+
+
+def kfac_expert_forward(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, x: torch.Tensor, W: torch.Tensor,
+                        y: torch.Tensor, fan: int = 1) -> None:
+    """y[c] = W_e x[c // fan] for the choices c of every expert e; x [n // fan, c_in], y [n, c_out]."""
+    n = y.shape[0]
+    L, experts, po, pf = _expert(layer, order, offsets, n)
+    typ = _type_of(x, "x")
+    st = lib().kfac_expert_forward(ctx.handle, ctypes.addressof(L), experts, n, int(fan), typ, po, pf, x.data_ptr(),
+                                   _rows_of(x, n // max(1, int(fan)), L.c_in, x.dtype, "x"), W.data_ptr(), _weights(W, L, experts, x.dtype),
+                                   y.data_ptr(), _rows_of(y, n, L.c_out, x.dtype, "y"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_expert_forward")
+
+
+def kfac_expert_grad_input(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, dy: torch.Tensor, W: torch.Tensor,
+                           dx: torch.Tensor) -> None:
+    """dx[c] = W_e^T dy[c]; dy [n, c_out], dx [n, c_in]."""
+    n = dy.shape[0]
+    L, experts, po, pf = _expert(layer, order, offsets, n)
+    typ = _type_of(dy, "dy")
+    st = lib().kfac_expert_grad_input(ctx.handle, ctypes.addressof(L), experts, n, typ, po, pf, dy.data_ptr(), _rows_of(dy, n, L.c_out, dy.dtype, "dy"),
+                                      W.data_ptr(), _weights(W, L, experts, dy.dtype), dx.data_ptr(), _rows_of(dx, n, L.c_in, dy.dtype, "dx"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_expert_grad_input")
+
+
+def kfac_expert_grad_weight(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, x: torch.Tensor, dy: torch.Tensor,
+                            dW: torch.Tensor, fan: int = 1) -> None:
+    """dW_e = sum of dy[c]^T x[c // fan] over the choices of expert e: float32 [experts, c_out, c_in + bias]."""
+    n = dy.shape[0]
+    L, experts, po, pf = _expert(layer, order, offsets, n)
+    typ = _type_of(dy, "dy")
+    st = lib().kfac_expert_grad_weight(ctx.handle, ctypes.addressof(L), experts, n, int(fan), typ, po, pf, x.data_ptr(),
+                                       _rows_of(x, n // max(1, int(fan)), L.c_in, dy.dtype, "x"), dy.data_ptr(),
+                                       _rows_of(dy, n, L.c_out, dy.dtype, "dy"), _floats(dW, experts * L.c_out * (L.c_in + L.bias), "dW"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_expert_grad_weight")
+
+
+def kfac_stats_expert(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, x: Optional[torch.Tensor],
+                      grad_out: Optional[torch.Tensor], decay: float, A_ema: Optional[torch.Tensor], G_ema: Optional[torch.Tensor],
+                      fan: int = 1) -> None:
+    """A_ema: float32 [experts, dA, dA], G_ema: float32 [experts, dG, dG]; a factor that is None is skipped with its input."""
+    fan = int(fan)
+    if (A_ema is not None and x is None) or (G_ema is not None and grad_out is None) or (x is None and grad_out is None):
+        raise ValueError("a factor needs its input")
+    src = x if x is not None else grad_out
+    n = order.numel() if order is not None else grad_out.shape[0] if grad_out is not None else x.shape[0] * fan
+    L, experts, po, pf = _expert(layer, order, offsets, n)
+    typ = _type_of(src, "x")
+    dA = L.c_in + L.bias
+    px = ldx = pg = ldg = None
+    if A_ema is not None:
+        px, ldx = x.data_ptr(), _rows_of(x, n // max(1, fan), L.c_in, src.dtype, "x")
+    if G_ema is not None:
+        pg, ldg = grad_out.data_ptr(), _rows_of(grad_out, n, L.c_out, src.dtype, "grad_out")
+    st = lib().kfac_stats_expert(ctx.handle, ctypes.addressof(L), experts, n, fan, typ, po, pf, px, ldx or 0, pg, ldg or 0, float(decay),
+                                 _floats(A_ema, experts * dA * dA, "A_ema"), _floats(G_ema, experts * L.c_out * L.c_out, "G_ema"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_stats_expert")
 
 
 def kfac_profile_enable(ctx: Context, on: bool) -> None:
