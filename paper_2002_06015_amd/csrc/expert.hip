@@ -15,6 +15,7 @@
 // fp32 operands are the exact sum of three bf16 values; of the nine products the six above 2^-24 are formed (h h, h m, m h,
 // m m, h l, l h), all accumulated in fp32.
 #include "gemm_tiles.h"
+#include "lds_dma.h"
 #include "token_internal.h"
 
 namespace kfac {
@@ -99,28 +100,28 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs &a, int block, int ti
 }
 
 // ---- tiles in LDS --------------------------------------------------------------------------------------
-// 16-byte chunks of 8 elements.  Along k: line = row of the tile, BK / 8 chunks; across k: line = k, 16 chunks of 8 rows.
+// 16-byte chunks of 8 elements.  Along k: line = row of the tile, BK / 8 chunks; across k: line = k, ROWS / 8 chunks of 8 rows.
 // Chunks are permuted inside a line so that the lanes of a read meet different banks.
-template <bool ACROSS, int BK>
+template <bool ACROSS, int BK, int ROWS>
 __device__ __forceinline__ int chunk_at(int line, int pos)
 {
-    if constexpr (ACROSS) return line * 16 + ((((pos >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (pos & 1));
+    if constexpr (ACROSS) return line * (ROWS / 8) + ((((pos >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (pos & 1));
     else if constexpr (BK == 64) return line * 8 + (pos ^ (line & 7));
     else return line * 4 + (pos ^ ((line >> 1) & 3));
 }
 
 // The 16 rows from `row0` (a multiple of 16) of a tile, k = 32 u + 8 (lane / 16) .. + 7: lane -> row lane % 16.
-template <bool ACROSS, int BK>
+template <bool ACROSS, int BK, int ROWS>
 __device__ __forceinline__ bf16x8 fragment(const bf16_t *tile, int row0, int u, int lane)
 {
     if constexpr (ACROSS) {
         const int m = 32 * u + 8 * (lane >> 4) + ((lane & 15) >> 2);
-        const bf16_t *p = tile + 8 * chunk_at<true, BK>(m, row0 / 8) + 4 * (lane & 3);   // (the pair of chunks stays together)
+        const bf16_t *p = tile + 8 * chunk_at<true, BK, ROWS>(m, row0 / 8) + 4 * (lane & 3);   // (the pair of chunks stays together)
         const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)p);
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)(p + 4 * 128));   // k + 4: same permutation
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)(p + 4 * ROWS));   // k + 4: same permutation
         return __builtin_bit_cast(bf16x8, shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     } else {
-        return *(const bf16x8 *)(tile + 8 * chunk_at<false, BK>(row0 + (lane & 15), 4 * u + (lane >> 4)));
+        return *(const bf16x8 *)(tile + 8 * chunk_at<false, BK, ROWS>(row0 + (lane & 15), 4 * u + (lane >> 4)));
     }
 }
 
@@ -237,7 +238,7 @@ struct Staged {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int q = tid + 256 * i;
-            reg[i].store(tile, 128 * BK, chunk_at<ACROSS, BK>(q / PER, q % PER));
+            reg[i].store(tile, 128 * BK, chunk_at<ACROSS, BK, 128>(q / PER, q % PER));
         }
     }
 };
@@ -269,170 +270,115 @@ __device__ __forceinline__ float blend(float decay, float alpha, float old, floa
     return decay == 0.f ? alpha * sum : fmaf(alpha, sum, decay * old);
 }
 
-// Which tile of which factor a workgroup of the statistics forms.
-struct StatsTile {
-    int e, begin, len, ti, tj, dim;
-    bool g;
+// What a workgroup works on: C(i, j) for rows from ti BM and columns from tj BN, i < I, j < J, contraction over K.
+struct Tile {
+    int e, begin, len, ti, tj, I, J, K;
+    bool g;   // statistics: G_e
 };
 
-__device__ __forceinline__ bool find_stats_tile(const ExpertArgs &a, int block, int total, int edge, StatsTile &t)
+// Tiles of BM x BN of the lower triangle of a symmetric matrix (BN = BM or 2 BM): row ti has the columns that reach its diagonal.
+template <int BM, int BN>
+__host__ __device__ __forceinline__ int triangle_tiles(int dim)
 {
-    const int ta = a.A ? (a.ci + edge - 1) / edge : 0, tg = a.G ? (a.co + edge - 1) / edge : 0;
-    const int na = ta * (ta + 1) / 2, per = na + tg * (tg + 1) / 2;
-    const int id = xcd_remap(block, total);
-    t.e = id / per;
-    int local = id - t.e * per;
-    t.g = local >= na;
-    if (t.g) local -= na;
-    tri_decode(local, t.ti, t.tj);
-    t.dim = t.g ? a.co : a.ci;
-    segment(a, t.e, t.begin, t.len);
-    return t.len > 0;
+    const int t = (dim + BM - 1) / BM;
+    return BN == BM ? t * (t + 1) / 2 : (t / 2) * (t / 2 + 1) + (t & 1) * (t / 2 + 1);
 }
 
-template <typename T, int OP>
-__global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
+template <int OP, int BM, int BN>
+__device__ __forceinline__ bool find_work(const ExpertArgs &a, int tiles_j, int total, Tile &t)
 {
-    constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 ? 1 : 3;
-    constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
-    constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
-    constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
-    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
-    constexpr int PLANE = 128 * BK;
-    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * PLANE];
-    bf16_t *tile_a = lds, *tile_b = lds + NP * PLANE;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = wave >> 1, wj = wave & 1;
-
-    int e, begin, len, ti, tj, I, J, K;
-    bool sym_g = false;
+    t.g = false;
     if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
-        if (!find_tile<128>(a, blockIdx.x, tiles_j, e, begin, len, ti, tj)) return;
-        I = len;
-        J = OP == EXPERT_FORWARD ? a.co : a.ci;
-        K = e == a.experts ? 0 : OP == EXPERT_FORWARD ? a.ci : a.co;   // rows of choices that no expert takes are zero
+        if (!find_tile<BM>(a, blockIdx.x, tiles_j, t.e, t.begin, t.len, t.ti, t.tj)) return false;
+        t.I = t.len;
+        t.J = OP == EXPERT_FORWARD ? a.co : a.ci;
+        t.K = t.e == a.experts ? 0 : OP == EXPERT_FORWARD ? a.ci : a.co;   // rows of choices that no expert takes are zero
+        return true;
     } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
         const int per = total / a.experts, id = xcd_remap(blockIdx.x, total);
-        e = id / per;
-        ti = (id - e * per) / tiles_j;
-        tj = (id - e * per) - ti * tiles_j;
-        segment(a, e, begin, len);
-        I = a.co; J = a.ci; K = len;
+        t.e = id / per;
+        t.ti = (id - t.e * per) / tiles_j;
+        t.tj = (id - t.e * per) - t.ti * tiles_j;
+        segment(a, t.e, t.begin, t.len);
+        t.I = a.co; t.J = a.ci; t.K = t.len;
+        return true;
     } else {
-        StatsTile t;
-        if (!find_stats_tile(a, blockIdx.x, total, 128, t)) return;
-        e = t.e; begin = t.begin; len = t.len; ti = t.ti; tj = t.tj; sym_g = t.g;
-        I = J = t.dim; K = len;
-    }
-
-    Staged<T, ACROSS_A, GATHER_A, BK> sa;
-    Staged<T, ACROSS_B, GATHER_B, BK> sb;
-    const T *We = (const T *)a.W + (long long)min(e, a.experts - 1) * a.co * a.ldw;
-    if constexpr (OP == EXPERT_FORWARD) {
-        sa.init(a, (const T *)a.x, a.ldx, a.fan, begin, ti * 128, I, K, tid);
-        sb.init(a, We, a.ldw, 1, 0, tj * 128, J, K, tid);
-    } else if constexpr (OP == EXPERT_GRAD_INPUT) {
-        sa.init(a, (const T *)a.dy, a.ldy, 1, begin, ti * 128, I, K, tid);
-        sb.init(a, We, a.ldw, 1, 0, tj * 128, J, K, tid);
-    } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
-        sa.init(a, (const T *)a.dy, a.ldy, 1, begin, ti * 128, I, K, tid);
-        sb.init(a, (const T *)a.x, a.ldx, a.fan, begin, tj * 128, J, K, tid);
-    } else {
-        sa.init(a, (const T *)(sym_g ? a.dy : a.x), sym_g ? a.ldy : a.ldx, sym_g ? 1 : a.fan, begin, ti * 128, I, K, tid);
-        sb.init(a, (const T *)(sym_g ? a.dy : a.x), sym_g ? a.ldy : a.ldx, sym_g ? 1 : a.fan, begin, tj * 128, J, K, tid);
-    }
-    // sums over k of the rows: the bias column of dW (with the tiles of the first columns), the border of A (with the diagonal)
-    const bool sums = a.bias && ((OP == EXPERT_GRAD_WEIGHT && tj == 0) || (OP == EXPERT_STATS && !sym_g && ti == tj)) && wj == 0;
-    bf16x8 ones;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) ones[q] = (__bf16)1.f;
-
-    floatx4 acc[4][4], row_sum[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    if (K > 0) {
-        sa.load(a, 0, tid);
-        sb.load(a, 0, tid);
-    }
-    for (int k0 = 0; k0 < K; k0 += BK) {
-        if (k0 > 0) __syncthreads();   // every wave has read the step before
-        sa.store(tile_a, tid);
-        sb.store(tile_b, tid);
-        __syncthreads();
-        if (k0 + BK < K) {
-            sa.load(a, k0 + BK, tid);
-            sb.load(a, k0 + BK, tid);
+        const int na = a.A ? triangle_tiles<BM, BN>(a.ci) : 0, per = na + (a.G ? triangle_tiles<BM, BN>(a.co) : 0);
+        const int id = xcd_remap(blockIdx.x, total);
+        t.e = id / per;
+        int local = id - t.e * per;
+        t.g = local >= na;
+        if (t.g) local -= na;
+        if constexpr (BN == BM) {
+            tri_decode(local, t.ti, t.tj);
+        } else {   // rows 2 r and 2 r + 1 have r + 1 tiles each
+            int r = (int)((sqrtf(4.0f * (float)local + 1.0f) - 1.0f) * 0.5f);
+            while (r * (r + 1) > local) --r;
+            while ((r + 1) * (r + 2) <= local) ++r;
+            local -= r * (r + 1);
+            t.ti = 2 * r + (local > r ? 1 : 0);
+            t.tj = local - (local > r ? r + 1 : 0);
         }
-#pragma unroll
-        for (int u = 0; u < BK / 32; ++u) {
-            bf16x8 fa[NP][4], fb[NP][4];
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    fa[p][q] = fragment<ACROSS_A, BK>(tile_a + p * PLANE, wi * 64 + 16 * q, u, lane);
-                    fb[p][q] = fragment<ACROSS_B, BK>(tile_b + p * PLANE, wj * 64 + 16 * q, u, lane);
-                }
-            constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};   // the small products first
-#pragma unroll
-            for (int t = NP == 1 ? 5 : 0; t < 6; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = mfma(fb[pb[t]][j], fa[pa[t]][i], acc[i][j]);
-            if (sums)
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) row_sum[i] = mfma(ones, fa[p][i], row_sum[i]);
-        }
+        segment(a, t.e, t.begin, t.len);
+        t.I = t.J = t.g ? a.co : a.ci;
+        t.K = t.len;
+        return t.len > 0;   // an expert without rows keeps its factors
     }
+}
 
-    // lane -> row i = lane % 16 of a 16 x 16 block, columns 4 (lane / 16) .. + 3
+// Whether a wave adds up its rows over k besides: the bias column of dW, the border of A.
+template <int OP>
+__device__ __forceinline__ bool wants_sums(const ExpertArgs &a, const Tile &t, int wj)
+{
+    return (OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS) && a.bias && !t.g && t.tj == 0 && wj == 0;
+}
+
+// Stores a wave's NI x NJ blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
+template <typename T, int OP, int NI, int NJ>
+__device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[NI][NJ],
+                                           const floatx4 (&row_sum)[NI], int lane)
+{
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = ti * 128 + wi * 64 + 16 * i + (lane & 15);
-        if (row >= I) continue;
+    for (int i = 0; i < NI; ++i) {
+        const int row = i0 + 16 * i + (lane & 15);
+        if (row >= t.I) continue;
         if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
-            const int c = choice_at(a, begin + row);
+            const int c = choice_at(a, t.begin + row);
             if (c < 0) continue;
             T *out = (T *)a.out + (long long)c * a.ldo;
+            const T *bias = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw + a.ci;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = tj * 128 + wj * 64 + 16 * j + 4 * (lane >> 4);
+            for (int j = 0; j < NJ; ++j) {
+                const int col = j0 + 16 * j + 4 * (lane >> 4);
                 floatx4 v = acc[i][j];
-                if (OP == EXPERT_FORWARD && a.bias && e < a.experts)
+                if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (col + r < J) {
-                            const T w = We[(long long)(col + r) * a.ldw + a.ci];
+                        if (col + r < t.J) {
+                            const T w = bias[(long long)(col + r) * a.ldw];
                             if constexpr (sizeof(T) == 2) v[r] += __uint_as_float((unsigned)w << 16);
                             else v[r] += w;
                         }
-                store4<T>(out + col, J - col, v);
+                store4<T>(out + col, t.J - col, v);
             }
         } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
-            float *out = a.dW + ((long long)e * a.co + row) * (a.ci + a.bias);
+            float *out = a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = tj * 128 + wj * 64 + 16 * j + 4 * (lane >> 4);
-                store4<float>(out + col, J - col, acc[i][j]);
+            for (int j = 0; j < NJ; ++j) {
+                const int col = j0 + 16 * j + 4 * (lane >> 4);
+                store4<float>(out + col, t.J - col, acc[i][j]);
             }
             if (sums && lane < 16) out[a.ci] = row_sum[i][0];
         } else {
-            const int d = sym_g ? a.co : a.ci + a.bias;
-            float *M = (sym_g ? a.G : a.A) + (long long)e * d * d;
-            const float alpha = (1.f - a.decay) / (float)len;
+            const int d = t.g ? a.co : a.ci + a.bias;
+            float *M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
+            const float alpha = (1.f - a.decay) / (float)t.len;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int col = tj * 128 + wj * 64 + 16 * j + 4 * (lane >> 4) + r;
-                    if (col > row) continue;               // (off the diagonal all columns are smaller)
+                    const int col = j0 + 16 * j + 4 * (lane >> 4) + r;
+                    if (col > row) continue;               // (the other triangle is the mirror image)
                     float *lo = M + (long long)row * d + col;
                     const float v = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *lo, acc[i][j][r]);
                     *lo = v;
@@ -452,24 +398,339 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
     }
 }
 
-template <typename T>
-hipError_t run(ExpertOp op, const ExpertArgs &a, hipStream_t s, int *workgroups)
+__device__ __forceinline__ bf16x8 ones()
 {
-    long long wgs = 0;
-    int tj = 1;
-    const long long tiles_n = a.n / 128 + (a.n < a.experts + 1 ? a.n : a.experts + 1);   // at most: one ragged tile a segment
-    if (op == EXPERT_FORWARD || op == EXPERT_GRAD_INPUT) {
-        tj = ((op == EXPERT_FORWARD ? a.co : a.ci) + 127) / 128;
-        wgs = tiles_n * tj;
-    } else if (op == EXPERT_GRAD_WEIGHT) {
-        tj = (a.ci + 127) / 128;
-        wgs = (long long)a.experts * ((a.co + 127) / 128) * tj;
-    } else {
-        const long long ta = a.A ? (a.ci + 127) / 128 : 0, tg = a.G ? (a.co + 127) / 128 : 0;
-        wgs = a.experts * (ta * (ta + 1) / 2 + tg * (tg + 1) / 2);
+    bf16x8 v;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = (__bf16)1.f;
+    return v;
+}
+
+template <typename T, int OP>
+__global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
+{
+    constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 ? 1 : 3;
+    constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
+    constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
+    constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
+    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
+    constexpr int PLANE = 128 * BK;
+    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * PLANE];
+    bf16_t *tile_a = lds, *tile_b = lds + NP * PLANE;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave >> 1, wj = wave & 1;
+    Tile t;
+    if (!find_work<OP, 128, 128>(a, tiles_j, total, t)) return;
+
+    Staged<T, ACROSS_A, GATHER_A, BK> sa;
+    Staged<T, ACROSS_B, GATHER_B, BK> sb;
+    const T *We = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw, *x = (const T *)a.x, *dy = (const T *)a.dy;
+    if constexpr (OP == EXPERT_FORWARD) sa.init(a, x, a.ldx, a.fan, t.begin, t.ti * 128, t.I, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) sa.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * 128, t.I, t.K, tid);
+    else sa.init(a, dy, a.ldy, 1, t.begin, t.ti * 128, t.I, t.K, tid);
+    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) sb.init(a, We, a.ldw, 1, 0, t.tj * 128, t.J, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) sb.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * 128, t.J, t.K, tid);
+    else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * 128, t.J, t.K, tid);
+    const bool sums = wants_sums<OP>(a, t, wj);
+
+    floatx4 acc[4][4], row_sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    if (wgs >= (1LL << 30)) return hipErrorInvalidValue;   // (refused by the entry points before)
-    *workgroups = (int)wgs;
+    if (t.K > 0) {
+        sa.load(a, 0, tid);
+        sb.load(a, 0, tid);
+    }
+    for (int k0 = 0; k0 < t.K; k0 += BK) {
+        if (k0 > 0) __syncthreads();   // every wave has read the step before
+        sa.store(tile_a, tid);
+        sb.store(tile_b, tid);
+        __syncthreads();
+        if (k0 + BK < t.K) {
+            sa.load(a, k0 + BK, tid);
+            sb.load(a, k0 + BK, tid);
+        }
+#pragma unroll
+        for (int u = 0; u < BK / 32; ++u) {
+            bf16x8 fa[NP][4], fb[NP][4];
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    fa[p][q] = fragment<ACROSS_A, BK, 128>(tile_a + p * PLANE, wi * 64 + 16 * q, u, lane);
+                    fb[p][q] = fragment<ACROSS_B, BK, 128>(tile_b + p * PLANE, wj * 64 + 16 * q, u, lane);
+                }
+            constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};   // the small products first
+#pragma unroll
+            for (int q = NP == 1 ? 5 : 0; q < 6; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = mfma(fb[pb[q]][j], fa[pa[q]][i], acc[i][j]);
+            if (sums)
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) row_sum[i] = mfma(ones(), fa[p][i], row_sum[i]);
+        }
+    }
+    store_tile<T, OP, 4, 4>(a, t, t.ti * 128 + wi * 64, t.tj * 128 + wj * 64, sums, acc, row_sum, lane);
+}
+
+// ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
+// BM x BN tiles, four waves; steps of 32 k in a ring of three LDS stages.  While a step is multiplied, the fragments of the next
+// one come out of LDS and the loads of the two behind it are on their way; two workgroups share a CU, so that one multiplies
+// while the other waits at a barrier, starts or stores.
+// Offsets in a tensor are 32 bits (the host sees to it); rows and columns beyond the tile's are clamped, they reach no output.
+// What is left of a contraction that is no whole number of steps goes through registers, with zeros behind its end.
+template <bool ACROSS, int GATHER, int ROWS>
+struct Direct {
+    static constexpr int CH = ROWS / 64, PER = ACROSS ? ROWS / 8 : 4;   // chunks a thread and step, chunks a line
+    static constexpr int LINES = 64 / PER;                               // (across k) lines that one load of a wave covers
+    typedef const int __attribute__((address_space(4))) *order_ptr;      // read with scalar loads
+    const char *base;
+    unsigned off[CH];
+    unsigned ld;      // bytes
+    int begin, K, fan;
+    unsigned magic;   // c / fan = (c * magic) >> 32
+    int next[ACROSS && GATHER != 0 ? CH * LINES : 1];   // choices of the step that is loaded next
+
+    __device__ __forceinline__ unsigned row_of(int c) const { return GATHER == 2 && fan > 1 ? __umulhi((unsigned)c, magic) : (unsigned)c; }
+    __device__ __forceinline__ int choice(const ExpertArgs &a, int r) const   // always inside the tensor
+    {
+        return a.order ? min(max(a.order[begin + r], 0), a.n - 1) : begin + r;
+    }
+    __device__ __forceinline__ void fetch_choices(const ExpertArgs &a, int step, int wave)
+    {
+        if constexpr (ACROSS && GATHER != 0) {
+            const order_ptr order = (order_ptr)(unsigned long long)a.order;
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int q = 0; q < LINES; ++q) {
+                    const int r = begin + min(32 * step + (wave + 4 * i) * LINES + q, K - 1);
+                    next[i * LINES + q] = a.order ? order[r] : r;
+                }
+        }
+    }
+    __device__ __forceinline__ void init(const ExpertArgs &a, const void *base_, long long ld_, int fan_, int begin_, int row0, int rows, int K_, int tid)
+    {
+        base = (const char *)base_; ld = (unsigned)(2 * ld_); begin = begin_; K = K_; fan = fan_;
+        magic = fan > 1 ? (unsigned)((0x100000000ULL + fan - 1) / fan) : 0;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int q = tid + 256 * i, line = q / PER, phys = q % PER;
+            if constexpr (ACROSS) {
+                const int pos = ((((phys >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (phys & 1));
+                off[i] = 2u * (unsigned)min(row0 + 8 * pos, rows - 8) + (GATHER == 0 ? (unsigned)line * ld : 0u);
+            } else {
+                int r = min(row0 + line, rows - 1);
+                if constexpr (GATHER != 0) r = (int)row_of(choice(a, r));
+                off[i] = (unsigned)r * ld + 16u * (unsigned)(phys ^ ((line >> 1) & 3));
+            }
+        }
+    }
+    // a whole step's tile into `tile`; the choices of the next step are fetched on the way
+    __device__ __forceinline__ void load(const ExpertArgs &a, bf16_t *tile, int step, int tid, int wave)
+    {
+        const char *from = base;
+        if constexpr (!ACROSS) from += 64LL * step;
+        else if constexpr (GATHER == 0) from += 32LL * step * ld;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            unsigned o = off[i];
+            if constexpr (ACROSS && GATHER != 0) {
+                unsigned r = 0;
+#pragma unroll
+                for (int q = 0; q < LINES; ++q) {
+                    const unsigned at = row_of(min(max(next[i * LINES + q], 0), a.n - 1)) * ld;
+                    r = q == 0 || ((tid & 63) / PER) >= q ? at : r;
+                }
+                o += r;
+            }
+            load_to_lds(from, o, tile + 8 * (64 * wave + 256 * i));
+        }
+        fetch_choices(a, step + 1, wave);
+    }
+    // the last, partial step
+    __device__ __forceinline__ void load_rest(const ExpertArgs &a, bf16_t *tile, int step, int tid) const
+    {
+        const char *from = base;
+        if constexpr (!ACROSS) from += 64LL * step;
+        else if constexpr (GATHER == 0) from += 32LL * step * ld;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int line = (tid + 256 * i) / PER;
+            const int k = ACROSS ? 32 * step + line : 32 * step + 8 * ((tid % PER) ^ ((line >> 1) & 3));
+            uintx4 v = {0, 0, 0, 0};
+            if (k < K) {
+                unsigned o = off[i];
+                if constexpr (ACROSS && GATHER != 0) o += row_of(choice(a, k)) * ld;
+                v = *(const uintx4 *)(from + o);
+            }
+            *(uintx4 *)(tile + 8 * (tid + 256 * i)) = v;
+        }
+    }
+};
+
+template <int OP, int BM, int BN, bool SUMS>
+__global__ __launch_bounds__(256, 2) void expert_direct_kernel(const ExpertArgs a, int tiles_j, int total)
+{
+    constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
+    constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
+    constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
+    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
+    constexpr int NI = BM / 32, NJ = BN / 32, STAGE = (BM + BN) * 32;
+    constexpr int LOADS = BM / 64 + BN / 64;   // a thread's, a step
+    __shared__ __attribute__((aligned(1024))) bf16_t lds[3 * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave >> 1, wj = wave & 1;
+    Tile t;
+    if (!find_work<OP, BM, BN>(a, tiles_j, total, t)) return;
+
+    Direct<ACROSS_A, GATHER_A, BM> da;
+    Direct<ACROSS_B, GATHER_B, BN> db;
+    const bf16_t *We = (const bf16_t *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw;
+    if constexpr (OP == EXPERT_FORWARD) da.init(a, a.x, a.ldx, a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) da.init(a, t.g ? a.dy : a.x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
+    else da.init(a, a.dy, a.ldy, 1, t.begin, t.ti * BM, t.I, t.K, tid);
+    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) db.init(a, We, a.ldw, 1, 0, t.tj * BN, t.J, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) db.init(a, t.g ? a.dy : a.x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
+    else db.init(a, a.x, a.ldx, a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
+    const bool sums = SUMS && wants_sums<OP>(a, t, wj);
+
+    floatx4 acc[NI][NJ], row_sum[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto load = [&](int s, bf16_t *stage) {
+        da.load(a, stage, s, tid, wave);
+        db.load(a, stage + BM * 32, s, tid, wave);
+    };
+    auto read = [&](const bf16_t *stage, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+#pragma unroll
+        for (int q = 0; q < NI; ++q) x[q] = fragment<ACROSS_A, 32, BM>(stage, wi * (BM / 2) + 16 * q, 0, lane);
+#pragma unroll
+        for (int q = 0; q < NJ; ++q) y[q] = fragment<ACROSS_B, 32, BN>(stage + BM * 32, wj * (BN / 2) + 16 * q, 0, lane);
+    };
+    auto multiply = [&](const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ]) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = mfma(y[j], x[i], acc[i][j]);
+        if constexpr (SUMS)
+            if (sums)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) row_sum[i] = mfma(ones(), x[i], row_sum[i]);
+    };
+    const int whole = t.K / 32;
+    if (whole > 0) {
+        bf16x8 fa[2][NI], fb[2][NJ];
+        bf16_t *s0 = lds, *s1 = lds + STAGE, *s2 = lds + 2 * STAGE;   // the stages of this step and the two behind it
+        da.fetch_choices(a, 0, wave);
+        db.fetch_choices(a, 0, wave);
+        load(0, s0);
+        if (whole > 1) load(1, s1);
+        if (whole > 1) wait_loads<LOADS>();
+        else wait_loads<0>();
+        if (whole > 2) load(2, s2);
+        read(s0, fa[0], fb[0]);
+        auto step = [&](int s, const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ], bf16x8 (&nx)[NI], bf16x8 (&ny)[NJ]) {
+            if (s + 1 < whole) {
+                // step s + 1 is there, s + 2 may be on its way, and everyone has read step s
+                if (s + 2 < whole) wait_loads<LOADS>();
+                else wait_loads<0>();
+                if (s + 3 < whole) load(s + 3, s0);
+                read(s1, nx, ny);
+                bf16_t *const free = s0;
+                s0 = s1; s1 = s2; s2 = free;
+            }
+            multiply(x, y);
+        };
+        int s = 0;
+        for (; s + 1 < whole; s += 2) {
+            step(s, fa[0], fb[0], fa[1], fb[1]);
+            step(s + 1, fa[1], fb[1], fa[0], fb[0]);
+        }
+        if (s < whole) multiply(fa[0], fb[0]);
+        __syncthreads();   // everyone has read the last step
+    }
+    if (t.K > 32 * whole) {
+        bf16x8 x[NI], y[NJ];
+        da.load_rest(a, lds, whole, tid);
+        db.load_rest(a, lds + BM * 32, whole, tid);
+        __syncthreads();
+        read(lds, x, y);
+        multiply(x, y);
+    }
+    store_tile<bf16_t, OP, NI, NJ>(a, t, t.ti * BM + wi * (BM / 2), t.tj * BN + wj * (BN / 2), sums, acc, row_sum, lane);
+}
+
+// Operands that go straight to LDS: whole 16-byte chunks, offsets of 32 bits, choices that the division by `fan` is exact for.
+bool chunks(const void *p, long long rows, long long cols, long long ld)
+{
+    return ((uintptr_t)p % 16) == 0 && ld % 8 == 0 && cols % 8 == 0 && cols >= 8 && rows * ld < (1LL << 31);
+}
+bool direct_ok(ExpertOp op, const ExpertArgs &a)
+{
+    if ((long long)a.n * a.fan >= (1LL << 32)) return false;
+    const bool x = chunks(a.x, a.n / a.fan, a.ci, a.ldx), dy = chunks(a.dy, a.n, a.co, a.ldy);
+    switch (op) {
+        case EXPERT_FORWARD: return x && chunks(a.W, a.co, a.ci, a.ldw);
+        case EXPERT_GRAD_INPUT: return dy && chunks(a.W, a.co, a.ci, a.ldw);
+        case EXPERT_GRAD_WEIGHT: return x && dy;
+        case EXPERT_STATS: return (!a.A || x) && (!a.G || dy);
+    }
+    return false;
+}
+
+template <int BM, int BN>
+long long count_tiles(ExpertOp op, const ExpertArgs &a, int &tiles_j)
+{
+    tiles_j = 1;
+    if (op == EXPERT_FORWARD || op == EXPERT_GRAD_INPUT) {   // at most: one ragged tile a segment
+        tiles_j = ((op == EXPERT_FORWARD ? a.co : a.ci) + BN - 1) / BN;
+        return (long long)(a.n / BM + (a.n < a.experts + 1 ? a.n : a.experts + 1)) * tiles_j;
+    }
+    if (op == EXPERT_GRAD_WEIGHT) {
+        tiles_j = (a.ci + BN - 1) / BN;
+        return (long long)a.experts * ((a.co + BM - 1) / BM) * tiles_j;
+    }
+    return (long long)a.experts * ((a.A ? triangle_tiles<BM, BN>(a.ci) : 0) + (a.G ? triangle_tiles<BM, BN>(a.co) : 0));
+}
+
+template <int BM, int BN>
+hipError_t run_direct(ExpertOp op, const ExpertArgs &a, hipStream_t s)
+{
+    int tj;
+    const long long wgs = count_tiles<BM, BN>(op, a, tj);
+    const dim3 grid((unsigned)wgs), block(256);
+    switch (op) {
+        case EXPERT_FORWARD: expert_direct_kernel<EXPERT_FORWARD, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_GRAD_INPUT: expert_direct_kernel<EXPERT_GRAD_INPUT, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_GRAD_WEIGHT:
+            if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            break;
+        case EXPERT_STATS:
+            if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            else expert_direct_kernel<EXPERT_STATS, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            break;
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
+{
+    int tj;
+    const long long wgs = count_tiles<128, 128>(op, a, tj);
     const dim3 grid((unsigned)wgs), block(256);
     switch (op) {
         case EXPERT_FORWARD: expert_general_kernel<T, EXPERT_FORWARD><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
@@ -482,9 +743,11 @@ hipError_t run(ExpertOp op, const ExpertArgs &a, hipStream_t s, int *workgroups)
 
 }  // namespace
 
-hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s, int *workgroups)
+hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s)
 {
-    return bf16 ? run<bf16_t>(op, a, s, workgroups) : run<float>(op, a, s, workgroups);
+    if (!bf16) return run_general<float>(op, a, s);
+    if (direct_ok(op, a)) return run_direct<128, 256>(op, a, s);
+    return run_general<bf16_t>(op, a, s);
 }
 
 }  // namespace kfac

@@ -81,6 +81,6 @@ struct ExpertArgs {
     float decay;
 };
 enum ExpertOp { EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, EXPERT_STATS };
-hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s, int *workgroups);
+hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s);
 
 }  // namespace kfac
