@@ -284,6 +284,16 @@ __host__ __device__ __forceinline__ int triangle_tiles(int dim)
     return BN == BM ? t * (t + 1) / 2 : (t / 2) * (t / 2 + 1) + (t & 1) * (t / 2 + 1);
 }
 
+// Contractions over the rows of an expert take as long as it has rows: every XCD gets an eighth of every expert's tiles.
+// slots: workgroups an expert, a multiple of 8, at least `tiles`.
+__device__ __forceinline__ bool expert_share(int slots, int tiles, int &e, int &local)
+{
+    const int x = blockIdx.x & 7, q = blockIdx.x >> 3, per = slots >> 3;
+    e = q / per;
+    local = x * per + q - e * per;
+    return local < tiles;
+}
+
 template <int OP, int BM, int BN>
 __device__ __forceinline__ bool find_work(const ExpertArgs &a, int tiles_j, int total, Tile &t)
 {
@@ -295,18 +305,21 @@ __device__ __forceinline__ bool find_work(const ExpertArgs &a, int tiles_j, int 
         t.K = t.e == a.experts ? 0 : OP == EXPERT_FORWARD ? a.ci : a.co;   // rows of choices that no expert takes are zero
         return true;
     } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
-        const int per = total / a.experts, id = xcd_remap(blockIdx.x, total);
-        t.e = id / per;
-        t.ti = (id - t.e * per) / tiles_j;
-        t.tj = (id - t.e * per) - t.ti * tiles_j;
+        const int tiles_i = (a.co + BM - 1) / BM;
+        int local;
+        if (!expert_share(total / a.experts, tiles_i * tiles_j, t.e, local)) return false;
+        // bands of 4 rows of tiles, column by column
+        const int band = local / (4 * tiles_j), rows = min(4, tiles_i - 4 * band);
+        local -= band * 4 * tiles_j;
+        t.tj = local / rows;
+        t.ti = 4 * band + local - t.tj * rows;
         segment(a, t.e, t.begin, t.len);
         t.I = a.co; t.J = a.ci; t.K = t.len;
         return true;
     } else {
         const int na = a.A ? triangle_tiles<BM, BN>(a.ci) : 0, per = na + (a.G ? triangle_tiles<BM, BN>(a.co) : 0);
-        const int id = xcd_remap(blockIdx.x, total);
-        t.e = id / per;
-        int local = id - t.e * per;
+        int local;
+        if (!expert_share(total / a.experts, per, t.e, local)) return false;
         t.g = local >= na;
         if (t.g) local -= na;
         if constexpr (BN == BM) {
@@ -336,7 +349,7 @@ __device__ __forceinline__ bool wants_sums(const ExpertArgs &a, const Tile &t, i
 // Stores a wave's NI x NJ blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
 template <typename T, int OP, int NI, int NJ>
 __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[NI][NJ],
-                                           const floatx4 (&row_sum)[NI], int lane)
+                                           const floatx4 (&row_sum)[(NI + 3) / 4], int lane)
 {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -368,7 +381,7 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
                 const int col = j0 + 16 * j + 4 * (lane >> 4);
                 store4<float>(out + col, t.J - col, acc[i][j]);
             }
-            if (sums && lane < 16) out[a.ci] = row_sum[i][0];
+            if (sums && lane < 16) out[a.ci] = row_sum[i / 4][i % 4];
         } else {
             const int d = t.g ? a.co : a.ci + a.bias;
             float *M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
@@ -386,7 +399,7 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
                 }
             if (sums && lane < 16) {
                 float *lo = M + (long long)a.ci * d + row;
-                const float v = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *lo, row_sum[i][0]);
+                const float v = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *lo, row_sum[i / 4][i % 4]);
                 *lo = v;
                 M[(long long)row * d + a.ci] = v;
                 if (row == 0) {
@@ -398,12 +411,12 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
     }
 }
 
-__device__ __forceinline__ bf16x8 ones()
+// Row q of the first operand of a matrix instruction is ones, the others zero: its product adds up the second operand's rows over k
+// into row q of the result.
+__device__ __forceinline__ bf16x8 ones_row(int q, int lane)
 {
-    bf16x8 v;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = (__bf16)1.f;
-    return v;
+    const unsigned v = (lane & 15) == q ? 0x3F803F80u : 0u;
+    return __builtin_bit_cast(bf16x8, uintx4{v, v, v, v});
 }
 
 template <typename T, int OP>
@@ -433,13 +446,11 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
     else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * 128, t.J, t.K, tid);
     const bool sums = wants_sums<OP>(a, t, wj);
 
-    floatx4 acc[4][4], row_sum[4];
+    floatx4 acc[4][4], row_sum[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};   // row_sum[0][i] of lanes 0 .. 15: the rows of block i
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
     if (t.K > 0) {
         sa.load(a, 0, tid);
         sb.load(a, 0, tid);
@@ -474,21 +485,21 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) row_sum[i] = mfma(ones(), fa[p][i], row_sum[i]);
+                    for (int i = 0; i < 4; ++i) row_sum[0] = mfma(ones_row(i, lane), fa[p][i], row_sum[0]);
         }
     }
     store_tile<T, OP, 4, 4>(a, t, t.ti * 128 + wi * 64, t.tj * 128 + wj * 64, sums, acc, row_sum, lane);
 }
 
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
-// BM x BN tiles, four waves; steps of 32 k in a ring of three LDS stages.  While a step is multiplied, the fragments of the next
-// one come out of LDS and the loads of the two behind it are on their way; two workgroups share a CU, so that one multiplies
-// while the other waits at a barrier, starts or stores.
+// BM x BN tiles, WI x WJ waves; steps of 64 k (whole 128-byte lines of operands along k) in two LDS stages.  While one half of a
+// step is multiplied, the fragments of the next half come out of LDS; the loads of a step start when the step before the last one
+// has been read.
 // Offsets in a tensor are 32 bits (the host sees to it); rows and columns beyond the tile's are clamped, they reach no output.
 // What is left of a contraction that is no whole number of steps goes through registers, with zeros behind its end.
-template <bool ACROSS, int GATHER, int ROWS>
+template <bool ACROSS, int GATHER, int ROWS, int THREADS>
 struct Direct {
-    static constexpr int CH = ROWS / 64, PER = ACROSS ? ROWS / 8 : 4;   // chunks a thread and step, chunks a line
+    static constexpr int CH = ROWS * 8 / THREADS, PER = ACROSS ? ROWS / 8 : 8;   // chunks a thread and step, chunks a line
     static constexpr int LINES = 64 / PER;                               // (across k) lines that one load of a wave covers
     typedef const int __attribute__((address_space(4))) *order_ptr;      // read with scalar loads
     const char *base;
@@ -511,7 +522,7 @@ struct Direct {
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int q = 0; q < LINES; ++q) {
-                    const int r = begin + min(32 * step + (wave + 4 * i) * LINES + q, K - 1);
+                    const int r = begin + min(64 * step + (wave + THREADS / 64 * i) * LINES + q, K - 1);
                     next[i * LINES + q] = a.order ? order[r] : r;
                 }
         }
@@ -522,77 +533,76 @@ struct Direct {
         magic = fan > 1 ? (unsigned)((0x100000000ULL + fan - 1) / fan) : 0;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int q = tid + 256 * i, line = q / PER, phys = q % PER;
+            const int q = tid + THREADS * i, line = q / PER, phys = q % PER;
             if constexpr (ACROSS) {
                 const int pos = ((((phys >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (phys & 1));
                 off[i] = 2u * (unsigned)min(row0 + 8 * pos, rows - 8) + (GATHER == 0 ? (unsigned)line * ld : 0u);
             } else {
                 int r = min(row0 + line, rows - 1);
                 if constexpr (GATHER != 0) r = (int)row_of(choice(a, r));
-                off[i] = (unsigned)r * ld + 16u * (unsigned)(phys ^ ((line >> 1) & 3));
+                off[i] = (unsigned)r * ld + 16u * (unsigned)(phys ^ (line & 7));
             }
         }
     }
-    // a whole step's tile into `tile`; the choices of the next step are fetched on the way
-    __device__ __forceinline__ void load(const ExpertArgs &a, bf16_t *tile, int step, int tid, int wave)
+    __device__ __forceinline__ const char *step_base(int step) const
     {
-        const char *from = base;
-        if constexpr (!ACROSS) from += 64LL * step;
-        else if constexpr (GATHER == 0) from += 32LL * step * ld;
+        if constexpr (!ACROSS) return base + 128LL * step;
+        else if constexpr (GATHER == 0) return base + 64LL * step * ld;
+        else return base;
+    }
+    // chunk i of the thread, of a whole step's tile, into `tile`
+    __device__ __forceinline__ void load(const ExpertArgs &a, lds_address tile, int step, int i, int tid, int wave) const
+    {
+        unsigned o = off[i];
+        if constexpr (ACROSS && GATHER != 0) {
+            unsigned r = 0;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            unsigned o = off[i];
-            if constexpr (ACROSS && GATHER != 0) {
-                unsigned r = 0;
-#pragma unroll
-                for (int q = 0; q < LINES; ++q) {
-                    const unsigned at = row_of(min(max(next[i * LINES + q], 0), a.n - 1)) * ld;
-                    r = q == 0 || ((tid & 63) / PER) >= q ? at : r;
-                }
-                o += r;
+            for (int q = 0; q < LINES; ++q) {
+                const unsigned at = row_of(min(max(next[i * LINES + q], 0), a.n - 1)) * ld;
+                r = q == 0 || ((tid & 63) / PER) >= q ? at : r;
             }
-            load_to_lds(from, o, tile + 8 * (64 * wave + 256 * i));
+            o += r;
         }
-        fetch_choices(a, step + 1, wave);
+        load_to_lds(step_base(step), o, tile + 16 * (64 * wave + THREADS * i));
     }
     // the last, partial step
     __device__ __forceinline__ void load_rest(const ExpertArgs &a, bf16_t *tile, int step, int tid) const
     {
-        const char *from = base;
-        if constexpr (!ACROSS) from += 64LL * step;
-        else if constexpr (GATHER == 0) from += 32LL * step * ld;
+        const char *from = step_base(step);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int line = (tid + 256 * i) / PER;
-            const int k = ACROSS ? 32 * step + line : 32 * step + 8 * ((tid % PER) ^ ((line >> 1) & 3));
+            const int line = (tid + THREADS * i) / PER;
+            const int k = ACROSS ? 64 * step + line : 64 * step + 8 * ((tid % PER) ^ (line & 7));
             uintx4 v = {0, 0, 0, 0};
             if (k < K) {
                 unsigned o = off[i];
                 if constexpr (ACROSS && GATHER != 0) o += row_of(choice(a, k)) * ld;
                 v = *(const uintx4 *)(from + o);
             }
-            *(uintx4 *)(tile + 8 * (tid + 256 * i)) = v;
+            *(uintx4 *)(tile + 8 * (tid + THREADS * i)) = v;
         }
     }
 };
 
-template <int OP, int BM, int BN, bool SUMS>
-__global__ __launch_bounds__(256, 2) void expert_direct_kernel(const ExpertArgs a, int tiles_j, int total)
+template <int OP, int BM, int BN, int WI, int WJ, bool SUMS>
+__global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const ExpertArgs a, int tiles_j, int total)
 {
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
-    constexpr int NI = BM / 32, NJ = BN / 32, STAGE = (BM + BN) * 32;
-    constexpr int LOADS = BM / 64 + BN / 64;   // a thread's, a step
-    __shared__ __attribute__((aligned(1024))) bf16_t lds[3 * STAGE];
+    constexpr int THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ, NI = TI / 16, NJ = TJ / 16, STAGE = (BM + BN) * 64;
+    __shared__ __attribute__((aligned(1024))) bf16_t lds[2 * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = wave >> 1, wj = wave & 1;
+    const int wi = wave / WJ, wj = wave % WJ;
     Tile t;
     if (!find_work<OP, BM, BN>(a, tiles_j, total, t)) return;
 
-    Direct<ACROSS_A, GATHER_A, BM> da;
-    Direct<ACROSS_B, GATHER_B, BN> db;
+    typedef Direct<ACROSS_A, GATHER_A, BM, THREADS> DirectA;
+    typedef Direct<ACROSS_B, GATHER_B, BN, THREADS> DirectB;
+    constexpr int LA = DirectA::CH, LB = DirectB::CH;
+    DirectA da;
+    DirectB db;
     const bf16_t *We = (const bf16_t *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw;
     if constexpr (OP == EXPERT_FORWARD) da.init(a, a.x, a.ldx, a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
     else if constexpr (OP == EXPERT_STATS) da.init(a, t.g ? a.dy : a.x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
@@ -602,74 +612,96 @@ __global__ __launch_bounds__(256, 2) void expert_direct_kernel(const ExpertArgs 
     else db.init(a, a.x, a.ldx, a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
     const bool sums = SUMS && wants_sums<OP>(a, t, wj);
 
-    floatx4 acc[NI][NJ], row_sum[NI];
+    floatx4 acc[NI][NJ], row_sum[(NI + 3) / 4];   // row_sum[i / 4][i % 4] of lanes 0 .. 15: the rows of block i
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < (NI + 3) / 4; ++i) row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    auto load = [&](int s, bf16_t *stage) {
-        da.load(a, stage, s, tid, wave);
-        db.load(a, stage + BM * 32, s, tid, wave);
+    const lds_address lds0 = address_in_lds(lds);
+    auto load = [&](int s, int q) {
+        const lds_address stage = lds0 + (s & 1) * (STAGE * 2);
+        if (q < LA) da.load(a, stage, s, q, tid, wave);
+        else db.load(a, stage + BM * 128, s, q - LA, tid, wave);
     };
-    auto read = [&](const bf16_t *stage, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
-#pragma unroll
-        for (int q = 0; q < NI; ++q) x[q] = fragment<ACROSS_A, 32, BM>(stage, wi * (BM / 2) + 16 * q, 0, lane);
-#pragma unroll
-        for (int q = 0; q < NJ; ++q) y[q] = fragment<ACROSS_B, 32, BN>(stage + BM * 32, wj * (BN / 2) + 16 * q, 0, lane);
+    auto fetch = [&](int s) {
+        da.fetch_choices(a, s, wave);
+        db.fetch_choices(a, s, wave);
     };
-    auto multiply = [&](const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ]) {
+    auto read = [&](int s, int u, int q, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+        const bf16_t *stage = lds + (s & 1) * STAGE;
+        if (q < NI) x[q] = fragment<ACROSS_A, 64, BM>(stage, wi * TI + 16 * q, u, lane);
+        else y[q - NI] = fragment<ACROSS_B, 64, BN>(stage + BM * 64, wj * TJ + 16 * (q - NI), u, lane);
+    };
+    auto multiply = [&](const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ], int j) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] = mfma(y[j], x[i], acc[i][j]);
+        for (int i = 0; i < NI; ++i) acc[i][j] = mfma(y[j], x[i], acc[i][j]);
+    };
+    auto add_rows = [&](const bf16x8 (&x)[NI]) {
         if constexpr (SUMS)
             if (sums)
 #pragma unroll
-                for (int i = 0; i < NI; ++i) row_sum[i] = mfma(ones(), x[i], row_sum[i]);
+                for (int i = 0; i < NI; ++i) row_sum[i / 4] = mfma(ones_row(i % 4, lane), x[i], row_sum[i / 4]);
     };
-    const int whole = t.K / 32;
+    const int whole = t.K / 64;
     if (whole > 0) {
         bf16x8 fa[2][NI], fb[2][NJ];
-        bf16_t *s0 = lds, *s1 = lds + STAGE, *s2 = lds + 2 * STAGE;   // the stages of this step and the two behind it
-        da.fetch_choices(a, 0, wave);
-        db.fetch_choices(a, 0, wave);
-        load(0, s0);
-        if (whole > 1) load(1, s1);
-        if (whole > 1) wait_loads<LOADS>();
-        else wait_loads<0>();
-        if (whole > 2) load(2, s2);
-        read(s0, fa[0], fb[0]);
-        auto step = [&](int s, const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ], bf16x8 (&nx)[NI], bf16x8 (&ny)[NJ]) {
-            if (s + 1 < whole) {
-                // step s + 1 is there, s + 2 may be on its way, and everyone has read step s
-                if (s + 2 < whole) wait_loads<LOADS>();
-                else wait_loads<0>();
-                if (s + 3 < whole) load(s + 3, s0);
-                read(s1, nx, ny);
-                bf16_t *const free = s0;
-                s0 = s1; s1 = s2; s2 = free;
-            }
-            multiply(x, y);
-        };
-        int s = 0;
-        for (; s + 1 < whole; s += 2) {
-            step(s, fa[0], fb[0], fa[1], fb[1]);
-            step(s + 1, fa[1], fb[1], fa[0], fb[0]);
+        fetch(0);
+#pragma unroll
+        for (int q = 0; q < LA + LB; ++q) load(0, q);
+        fetch(1);
+        wait_loads<0>();
+        if (whole > 1) {
+#pragma unroll
+            for (int q = 0; q < LA + LB; ++q) load(1, q);
+            fetch(2);
         }
-        if (s < whole) multiply(fa[0], fb[0]);
+#pragma unroll
+        for (int q = 0; q < NI + NJ; ++q) read(0, 0, q, fa[0], fb[0]);
+        constexpr int AHEAD = NJ * 3 / 4;   // the reads before a barrier are done some matrix instructions earlier
+        for (int s = 0; s < whole; ++s) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+                for (int q = min(NI + NJ, (NI + NJ) * j / AHEAD); q < min(NI + NJ, (NI + NJ) * (j + 1) / AHEAD); ++q) read(s, 1, q, fa[1], fb[1]);
+                multiply(fa[0], fb[0], j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            add_rows(fa[0]);
+            wait_loads<0>();   // step s + 1 is there, and everyone has read step s
+            const bool more = s + 2 < whole;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (more)
+#pragma unroll
+                    for (int q = (LA + LB) * j / NJ; q < (LA + LB) * (j + 1) / NJ; ++q) load(s + 2, q);
+#pragma unroll
+                for (int q = (NI + NJ) * j / NJ; q < (NI + NJ) * (j + 1) / NJ; ++q) read(s + 1, 0, q, fa[0], fb[0]);   // (behind the last step: not used)
+                multiply(fa[1], fb[1], j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (more) fetch(s + 3);
+            add_rows(fa[1]);
+        }
         __syncthreads();   // everyone has read the last step
     }
-    if (t.K > 32 * whole) {
-        bf16x8 x[NI], y[NJ];
+    if (t.K > 64 * whole) {
         da.load_rest(a, lds, whole, tid);
-        db.load_rest(a, lds + BM * 32, whole, tid);
+        db.load_rest(a, lds + BM * 64, whole, tid);
         __syncthreads();
-        read(lds, x, y);
-        multiply(x, y);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            bf16x8 x[NI], y[NJ];
+            const int s = 0;
+#pragma unroll
+            for (int q = 0; q < NI + NJ; ++q) read(s, u, q, x, y);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) multiply(x, y, j);
+            add_rows(x);
+        }
     }
-    store_tile<bf16_t, OP, NI, NJ>(a, t, t.ti * BM + wi * (BM / 2), t.tj * BN + wj * (BN / 2), sums, acc, row_sum, lane);
+    store_tile<bf16_t, OP, NI, NJ>(a, t, t.ti * BM + wi * TI, t.tj * BN + wj * TJ, sums, acc, row_sum, lane);
 }
 
 // Operands that go straight to LDS: whole 16-byte chunks, offsets of 32 bits, choices that the division by `fan` is exact for.
@@ -700,27 +732,27 @@ long long count_tiles(ExpertOp op, const ExpertArgs &a, int &tiles_j)
     }
     if (op == EXPERT_GRAD_WEIGHT) {
         tiles_j = (a.ci + BN - 1) / BN;
-        return (long long)a.experts * ((a.co + BM - 1) / BM) * tiles_j;
+        return (long long)a.experts * (((long long)((a.co + BM - 1) / BM) * tiles_j + 7) / 8 * 8);
     }
-    return (long long)a.experts * ((a.A ? triangle_tiles<BM, BN>(a.ci) : 0) + (a.G ? triangle_tiles<BM, BN>(a.co) : 0));
+    return (long long)a.experts * (((a.A ? triangle_tiles<BM, BN>(a.ci) : 0) + (a.G ? triangle_tiles<BM, BN>(a.co) : 0) + 7) / 8 * 8);
 }
 
-template <int BM, int BN>
+template <int BM, int BN, int WI, int WJ>
 hipError_t run_direct(ExpertOp op, const ExpertArgs &a, hipStream_t s)
 {
     int tj;
     const long long wgs = count_tiles<BM, BN>(op, a, tj);
-    const dim3 grid((unsigned)wgs), block(256);
+    const dim3 grid((unsigned)wgs), block(64 * WI * WJ);
     switch (op) {
-        case EXPERT_FORWARD: expert_direct_kernel<EXPERT_FORWARD, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_INPUT: expert_direct_kernel<EXPERT_GRAD_INPUT, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_FORWARD: expert_direct_kernel<EXPERT_FORWARD, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_GRAD_INPUT: expert_direct_kernel<EXPERT_GRAD_INPUT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
         case EXPERT_GRAD_WEIGHT:
-            if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-            else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
             break;
         case EXPERT_STATS:
-            if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-            else expert_direct_kernel<EXPERT_STATS, BM, BN, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+            else expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
             break;
     }
     return hipGetLastError();
@@ -746,7 +778,7 @@ hipError_t run_general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s)
 {
     if (!bf16) return run_general<float>(op, a, s);
-    if (direct_ok(op, a)) return run_direct<128, 256>(op, a, s);
+    if (direct_ok(op, a)) return run_direct<256, 256, 4, 2>(op, a, s);
     return run_general<bf16_t>(op, a, s);
 }
 

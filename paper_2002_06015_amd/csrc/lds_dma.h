@@ -5,14 +5,19 @@
 
 namespace kfac {
 
+// An address in LDS, in bytes.
+typedef unsigned lds_address;
+__device__ __forceinline__ lds_address address_in_lds(void *p)
+{
+    return (unsigned)(unsigned long long)(__attribute__((address_space(3))) void *)p;
+}
+
 // 16 bytes a lane: lane l's, at base + offset (both in bytes), go to lds + 16 l.  base and lds are the same in all lanes of the wave.
 // Written as one block, so that the compiler, which takes every LDS read for a possible reader of every such load in flight and
 // waits for all of them, leaves the waits to the kernel (wait_loads).
-__device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, void *lds)
+__device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, lds_address lds)
 {
-    typedef __attribute__((address_space(3))) void *lds_ptr;
-    const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long long)(lds_ptr)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(offset), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // Waits until at most `newest` loads of this wave are in flight and its LDS accesses are done, then for the other waves.

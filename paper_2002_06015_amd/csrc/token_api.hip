@@ -61,7 +61,7 @@ bool expert_ok(const kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_
     // tiles of one launch, 128 x 128 elements at least
     const long long ti = (L->c_in + 127) / 128, to = (L->c_out + 127) / 128;
     if (((long long)n / 128 + experts + 1) * std::max(ti, to) >= (1LL << 30)) return false;
-    return experts * (ti * to + ti * (ti + 1) / 2 + to * (to + 1) / 2) < (1LL << 30);
+    return experts * (ti * to + ti * (ti + 1) / 2 + to * (to + 1) / 2 + 16) < (1LL << 30);
 }
 
 ExpertArgs expert_args(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, const int32_t *order, const int32_t *offsets)
