@@ -14,6 +14,8 @@
 // 8-byte groups addressed by lanes i / 4, i / 4 + 4, i / 4 + 8, i / 4 + 12).
 // fp32 operands are the exact sum of three bf16 values; of the nine products the six above 2^-24 are formed (h h, h m, m h,
 // m m, h l, l h), all accumulated in fp32.
+#include <type_traits>
+
 #include "gemm_tiles.h"
 #include "lds_dma.h"
 #include "token_internal.h"
@@ -492,14 +494,17 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
 }
 
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
-// BM x BN tiles, WI x WJ waves; steps of 64 k (whole 128-byte lines of operands along k) in two LDS stages.  While one half of a
-// step is multiplied, the fragments of the next half come out of LDS; the loads of a step start when the step before the last one
-// has been read.
+// BM x BN tiles, WI x WJ waves, in halves of 32 k.  Five halves have a place in LDS: while one is multiplied from registers and the
+// fragments of the next one are read, the three behind it are there or on their way.  Loads go out for two halves (64 k, whole
+// 128-byte lines of operands along k) at a time and have three halves' time to arrive: with two stages of 64 k and two halves' time
+// the multiplication waited for them (65536 rows 2048 -> 2048 of 16 experts: 546 us).
 // Offsets in a tensor are 32 bits (the host sees to it); rows and columns beyond the tile's are clamped, they reach no output.
-// What is left of a contraction that is no whole number of steps goes through registers, with zeros behind its end.
+// What is left of a contraction that is no whole number of steps of 64 goes through registers, with zeros behind its end.
+constexpr int kPlaces = 5;
+
 template <bool ACROSS, int GATHER, int ROWS, int THREADS>
 struct Direct {
-    static constexpr int CH = ROWS * 8 / THREADS, PER = ACROSS ? ROWS / 8 : 8;   // chunks a thread and step, chunks a line
+    static constexpr int CH = ROWS * 4 / THREADS, PER = ACROSS ? ROWS / 8 : 4;   // chunks a thread and half, chunks a line
     static constexpr int LINES = 64 / PER;                               // (across k) lines that one load of a wave covers
     typedef const int __attribute__((address_space(4))) *order_ptr;      // read with scalar loads
     const char *base;
@@ -507,7 +512,7 @@ struct Direct {
     unsigned ld;      // bytes
     int begin, K, fan;
     unsigned magic;   // c / fan = (c * magic) >> 32
-    int next[ACROSS && GATHER != 0 ? CH * LINES : 1];   // choices of the step that is loaded next
+    int next[ACROSS && GATHER != 0 ? 2 * CH * LINES : 1];   // choices of the step that is loaded next
 
     __device__ __forceinline__ unsigned row_of(int c) const { return GATHER == 2 && fan > 1 ? __umulhi((unsigned)c, magic) : (unsigned)c; }
     __device__ __forceinline__ int choice(const ExpertArgs &a, int r) const   // always inside the tensor
@@ -519,10 +524,10 @@ struct Direct {
         if constexpr (ACROSS && GATHER != 0) {
             const order_ptr order = (order_ptr)(unsigned long long)a.order;
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < 2 * CH; ++i)
 #pragma unroll
                 for (int q = 0; q < LINES; ++q) {
-                    const int r = begin + min(64 * step + (wave + THREADS / 64 * i) * LINES + q, K - 1);
+                    const int r = begin + min(64 * step + 32 * (i & 1) + (wave + THREADS / 64 * (i >> 1)) * LINES + q, K - 1);
                     next[i * LINES + q] = a.order ? order[r] : r;
                 }
         }
@@ -540,20 +545,20 @@ struct Direct {
             } else {
                 int r = min(row0 + line, rows - 1);
                 if constexpr (GATHER != 0) r = (int)row_of(choice(a, r));
-                off[i] = (unsigned)r * ld + 16u * (unsigned)(phys ^ (line & 7));
+                off[i] = (unsigned)r * ld + 16u * (unsigned)(phys ^ ((line >> 1) & 3));
             }
         }
     }
-    __device__ __forceinline__ const char *step_base(int step) const
+    __device__ __forceinline__ const char *half_base(int step, int u) const
     {
-        if constexpr (!ACROSS) return base + 128LL * step;
-        else if constexpr (GATHER == 0) return base + 64LL * step * ld;
+        if constexpr (!ACROSS) return base + 128LL * step + 64 * u;
+        else if constexpr (GATHER == 0) return base + (64LL * step + 32 * u) * ld;
         else return base;
     }
-    // chunk i of the thread, of a whole step's tile, into `tile`
+    // load i of the thread's 2 CH of a step: chunk i / 2 of half i % 2, into the tile of that half
     __device__ __forceinline__ void load(const ExpertArgs &a, lds_address tile, int step, int i, int tid, int wave) const
     {
-        unsigned o = off[i];
+        unsigned o = off[i >> 1];
         if constexpr (ACROSS && GATHER != 0) {
             unsigned r = 0;
 #pragma unroll
@@ -563,16 +568,16 @@ struct Direct {
             }
             o += r;
         }
-        load_to_lds(step_base(step), o, tile + 16 * (64 * wave + THREADS * i));
+        load_to_lds(half_base(step, i & 1), o, tile + 16 * (64 * wave + THREADS * (i >> 1)));
     }
-    // the last, partial step
-    __device__ __forceinline__ void load_rest(const ExpertArgs &a, bf16_t *tile, int step, int tid) const
+    // half u of the last, partial step
+    __device__ __forceinline__ void load_rest(const ExpertArgs &a, bf16_t *tile, int step, int u, int tid) const
     {
-        const char *from = step_base(step);
+        const char *from = half_base(step, u);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int line = (tid + THREADS * i) / PER;
-            const int k = ACROSS ? 64 * step + line : 64 * step + 8 * ((tid % PER) ^ (line & 7));
+            const int k = 64 * step + 32 * u + (ACROSS ? line : 8 * ((tid % PER) ^ ((line >> 1) & 3)));
             uintx4 v = {0, 0, 0, 0};
             if (k < K) {
                 unsigned o = off[i];
@@ -591,8 +596,8 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
-    constexpr int THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ, NI = TI / 16, NJ = TJ / 16, STAGE = (BM + BN) * 64;
-    __shared__ __attribute__((aligned(1024))) bf16_t lds[2 * STAGE];
+    constexpr int THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ, NI = TI / 16, NJ = TJ / 16, PLACE = (BM + BN) * 32;
+    __shared__ __attribute__((aligned(1024))) bf16_t lds[kPlaces * PLACE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
     Tile t;
@@ -600,7 +605,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
 
     typedef Direct<ACROSS_A, GATHER_A, BM, THREADS> DirectA;
     typedef Direct<ACROSS_B, GATHER_B, BN, THREADS> DirectB;
-    constexpr int LA = DirectA::CH, LB = DirectB::CH;
+    constexpr int LA = 2 * DirectA::CH, LOADS = LA + 2 * DirectB::CH;   // a thread's, a step
     DirectA da;
     DirectB db;
     const bf16_t *We = (const bf16_t *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw;
@@ -620,23 +625,19 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     const lds_address lds0 = address_in_lds(lds);
-    auto load = [&](int s, int q) {
-        const lds_address stage = lds0 + (s & 1) * (STAGE * 2);
-        if (q < LA) da.load(a, stage, s, q, tid, wave);
-        else db.load(a, stage + BM * 128, s, q - LA, tid, wave);
+    auto load = [&](int s, int place, int q) {   // place: of the step's first half
+        const int at = place + (q & 1) < kPlaces ? place + (q & 1) : place + (q & 1) - kPlaces;
+        if (q < LA) da.load(a, lds0 + at * (2 * PLACE), s, q, tid, wave);
+        else db.load(a, lds0 + at * (2 * PLACE) + BM * 64, s, q - LA, tid, wave);
     };
     auto fetch = [&](int s) {
         da.fetch_choices(a, s, wave);
         db.fetch_choices(a, s, wave);
     };
-    auto read = [&](int s, int u, int q, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
-        const bf16_t *stage = lds + (s & 1) * STAGE;
-        if (q < NI) x[q] = fragment<ACROSS_A, 64, BM>(stage, wi * TI + 16 * q, u, lane);
-        else y[q - NI] = fragment<ACROSS_B, 64, BN>(stage + BM * 64, wj * TJ + 16 * (q - NI), u, lane);
-    };
-    auto multiply = [&](const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ], int j) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) acc[i][j] = mfma(y[j], x[i], acc[i][j]);
+    auto read = [&](int place, int q, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+        const bf16_t *half = lds + place * PLACE;
+        if (q < NI) x[q] = fragment<ACROSS_A, 32, BM>(half, wi * TI + 16 * q, 0, lane);
+        else y[q - NI] = fragment<ACROSS_B, 32, BN>(half + BM * 32, wj * TJ + 16 * (q - NI), 0, lane);
     };
     auto add_rows = [&](const bf16x8 (&x)[NI]) {
         if constexpr (SUMS)
@@ -647,57 +648,65 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     const int whole = t.K / 64;
     if (whole > 0) {
         bf16x8 fa[2][NI], fb[2][NJ];
+        int place = 0;   // of the first half of the step that is multiplied
+        auto behind = [&](int n) { return place + n < kPlaces ? place + n : place + n - kPlaces; };
         fetch(0);
 #pragma unroll
-        for (int q = 0; q < LA + LB; ++q) load(0, q);
+        for (int q = 0; q < LOADS; ++q) load(0, 0, q);
         fetch(1);
-        wait_loads<0>();
         if (whole > 1) {
 #pragma unroll
-            for (int q = 0; q < LA + LB; ++q) load(1, q);
+            for (int q = 0; q < LOADS; ++q) load(1, 2, q);
             fetch(2);
+            wait_loads<LOADS>();
+        } else {
+            wait_loads<0>();
         }
 #pragma unroll
-        for (int q = 0; q < NI + NJ; ++q) read(0, 0, q, fa[0], fb[0]);
-        constexpr int AHEAD = NJ * 3 / 4;   // the reads before a barrier are done some matrix instructions earlier
+        for (int q = 0; q < NI + NJ; ++q) read(0, q, fa[0], fb[0]);
+        // One half of a step: x y is multiplied; the fragments of the next half are read from `from`, and the loads of step s + 2 are
+        // started if there is one, an access behind every few matrix instructions, which run meanwhile.
+        auto half = [&](const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ], int from, bf16x8 (&nx)[NI], bf16x8 (&ny)[NJ], auto first, bool more, int s, int to) {
+            constexpr int MM = NI * NJ, NR = NI + NJ, EVERY = MM * 3 / 4 / NR, APART = MM / LOADS;   // (before a barrier the reads end earlier)
+#pragma unroll
+            for (int m = 0; m < MM; ++m) {
+                acc[m % NI][m / NI] = mfma(y[m / NI], x[m % NI], acc[m % NI][m / NI]);
+                if (m % EVERY == 0 && m / EVERY < NR) read(from, m / EVERY, nx, ny);
+                if constexpr (first)
+                    if (m % APART == 1 && m / APART < LOADS)
+                        if (more) load(s + 2, to, m / APART);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            add_rows(x);
+        };
         for (int s = 0; s < whole; ++s) {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-#pragma unroll
-                for (int q = min(NI + NJ, (NI + NJ) * j / AHEAD); q < min(NI + NJ, (NI + NJ) * (j + 1) / AHEAD); ++q) read(s, 1, q, fa[1], fb[1]);
-                multiply(fa[0], fb[0], j);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            add_rows(fa[0]);
-            wait_loads<0>();   // step s + 1 is there, and everyone has read step s
             const bool more = s + 2 < whole;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                if (more)
-#pragma unroll
-                    for (int q = (LA + LB) * j / NJ; q < (LA + LB) * (j + 1) / NJ; ++q) load(s + 2, q);
-#pragma unroll
-                for (int q = (NI + NJ) * j / NJ; q < (NI + NJ) * (j + 1) / NJ; ++q) read(s + 1, 0, q, fa[0], fb[0]);   // (behind the last step: not used)
-                multiply(fa[1], fb[1], j);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (more) fetch(s + 3);
-            add_rows(fa[1]);
+            wait_lds();   // everyone has read the first half of step s: its place and the one before it are free
+            half(fa[0], fb[0], behind(1), fa[1], fb[1], std::true_type{}, more, s, behind(4));
+            fetch(s + 3);
+            if (more) wait_loads<LOADS>();   // step s + 1 is there
+            else wait_loads<0>();
+            half(fa[1], fb[1], behind(2), fa[0], fb[0], std::false_type{}, false, s, 0);   // (what is read behind the last step is not used)
+            place = behind(2);
         }
         __syncthreads();   // everyone has read the last step
     }
     if (t.K > 64 * whole) {
-        da.load_rest(a, lds, whole, tid);
-        db.load_rest(a, lds + BM * 64, whole, tid);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            da.load_rest(a, lds + u * PLACE, whole, u, tid);
+            db.load_rest(a, lds + u * PLACE + BM * 32, whole, u, tid);
+        }
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             bf16x8 x[NI], y[NJ];
-            const int s = 0;
 #pragma unroll
-            for (int q = 0; q < NI + NJ; ++q) read(s, u, q, x, y);
+            for (int q = 0; q < NI + NJ; ++q) read(u, q, x, y);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) multiply(x, y, j);
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) acc[i][j] = mfma(y[j], x[i], acc[i][j]);
             add_rows(x);
         }
     }

@@ -27,4 +27,10 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(newest) : "memory");
 }
 
+// The same without a wait for loads.
+__device__ __forceinline__ void wait_lds()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
 }  // namespace kfac
