@@ -348,13 +348,31 @@ __device__ __forceinline__ bool wants_sums(const ExpertArgs &a, const Tile &t, i
     return (OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS) && a.bias && !t.g && t.tj == 0 && wj == 0;
 }
 
-// Stores a wave's NI x NJ blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
-template <typename T, int OP, int NI, int NJ>
-__device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[NI][NJ],
-                                           const floatx4 (&row_sum)[(NI + 3) / 4], int lane)
+// Row and column ci of A_e, and its corner: the bias.
+__device__ __forceinline__ void store_border(const ExpertArgs &a, const Tile &t, int row, float sum)
+{
+    const int d = a.ci + a.bias;
+    float *M = a.A + (long long)t.e * d * d, *lo = M + (long long)a.ci * d + row;
+    const float v = blend(a.decay, (1.f - a.decay) / (float)t.len, a.decay == 0.f ? 0.f : *lo, sum);
+    *lo = v;
+    M[(long long)row * d + a.ci] = v;
+    if (row == 0) {
+        float *corner = M + (long long)a.ci * d + a.ci;
+        *corner = blend(a.decay, 1.f - a.decay, a.decay == 0.f ? 0.f : *corner, 1.f);
+    }
+}
+
+__device__ __forceinline__ float value(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
+__device__ __forceinline__ float value(float v) { return v; }
+
+// Stores a wave's 4 x 4 blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
+// row_sum[i] of lanes 0 .. 15: the rows of block i, added up over k.
+template <typename T, int OP>
+__device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[4][4],
+                                           const floatx4 &row_sum, int lane)
 {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const int row = i0 + 16 * i + (lane & 15);
         if (row >= t.I) continue;
         if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
@@ -363,33 +381,29 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
             T *out = (T *)a.out + (long long)c * a.ldo;
             const T *bias = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw + a.ci;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const int col = j0 + 16 * j + 4 * (lane >> 4);
                 floatx4 v = acc[i][j];
                 if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (col + r < t.J) {
-                            const T w = bias[(long long)(col + r) * a.ldw];
-                            if constexpr (sizeof(T) == 2) v[r] += __uint_as_float((unsigned)w << 16);
-                            else v[r] += w;
-                        }
+                        if (col + r < t.J) v[r] += value(bias[(long long)(col + r) * a.ldw]);
                 store4<T>(out + col, t.J - col, v);
             }
         } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
             float *out = a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const int col = j0 + 16 * j + 4 * (lane >> 4);
                 store4<float>(out + col, t.J - col, acc[i][j]);
             }
-            if (sums && lane < 16) out[a.ci] = row_sum[i / 4][i % 4];
+            if (sums && lane < 16) out[a.ci] = row_sum[i];
         } else {
             const int d = t.g ? a.co : a.ci + a.bias;
             float *M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
             const float alpha = (1.f - a.decay) / (float)t.len;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int col = j0 + 16 * j + 4 * (lane >> 4) + r;
@@ -399,16 +413,7 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
                     *lo = v;
                     if (col < row) M[(long long)col * d + row] = v;
                 }
-            if (sums && lane < 16) {
-                float *lo = M + (long long)a.ci * d + row;
-                const float v = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *lo, row_sum[i / 4][i % 4]);
-                *lo = v;
-                M[(long long)row * d + a.ci] = v;
-                if (row == 0) {
-                    float *corner = M + (long long)a.ci * d + a.ci;
-                    *corner = blend(a.decay, 1.f - a.decay, a.decay == 0.f ? 0.f : *corner, 1.f);
-                }
-            }
+            if (sums && lane < 16) store_border(a, t, row, row_sum[i]);
         }
     }
 }
@@ -448,7 +453,7 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
     else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * 128, t.J, t.K, tid);
     const bool sums = wants_sums<OP>(a, t, wj);
 
-    floatx4 acc[4][4], row_sum[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};   // row_sum[0][i] of lanes 0 .. 15: the rows of block i
+    floatx4 acc[4][4], row_sum = {0.f, 0.f, 0.f, 0.f};   // row_sum[i] of lanes 0 .. 15: the rows of block i
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -487,10 +492,10 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) row_sum[0] = mfma(ones_row(i, lane), fa[p][i], row_sum[0]);
+                    for (int i = 0; i < 4; ++i) row_sum = mfma(ones_row(i, lane), fa[p][i], row_sum);
         }
     }
-    store_tile<T, OP, 4, 4>(a, t, t.ti * 128 + wi * 64, t.tj * 128 + wj * 64, sums, acc, row_sum, lane);
+    store_tile<T, OP>(a, t, t.ti * 128 + wi * 64, t.tj * 128 + wj * 64, sums, acc, row_sum, lane);
 }
 
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
@@ -501,6 +506,27 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
 // Offsets in a tensor are 32 bits (the host sees to it); rows and columns beyond the tile's are clamped, they reach no output.
 // What is left of a contraction that is no whole number of steps of 64 goes through registers, with zeros behind its end.
 constexpr int kPlaces = 5;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// The 32 rows from `row0` (a multiple of 32) of a half, k = 16 u + 8 (lane / 32) .. + 7: lane -> row lane % 32.
+template <bool ACROSS, int ROWS>
+__device__ __forceinline__ bf16x8 fragment32(const bf16_t *tile, int row0, int u, int lane)
+{
+    if constexpr (ACROSS) {
+        const int m = 16 * u + 8 * (lane >> 5) + ((lane & 15) >> 2), pair = (row0 >> 4) + ((lane >> 4) & 1);
+        const bf16_t *p = tile + m * ROWS + 16 * (pair ^ ((m & 3) << 1)) + 4 * (lane & 3);
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)p);
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)(p + 4 * ROWS));   // k + 4: same permutation
+        return __builtin_bit_cast(bf16x8, shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    } else {
+        const int line = row0 + (lane & 31);
+        return *(const bf16x8 *)(tile + 32 * line + 8 * ((2 * u + (lane >> 5)) ^ ((line >> 1) & 3)));
+    }
+}
+__device__ __forceinline__ floatx16 mfma32(const bf16x8 &j, const bf16x8 &i, const floatx16 &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(j, i, c, 0, 0, 0);
+}
 
 template <bool ACROSS, int GATHER, int ROWS, int THREADS>
 struct Direct {
@@ -540,7 +566,7 @@ struct Direct {
         for (int i = 0; i < CH; ++i) {
             const int q = tid + THREADS * i, line = q / PER, phys = q % PER;
             if constexpr (ACROSS) {
-                const int pos = ((((phys >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (phys & 1));
+                const int pos = (((phys >> 1) ^ ((line & 3) << 1)) << 1) | (phys & 1);
                 off[i] = 2u * (unsigned)min(row0 + 8 * pos, rows - 8) + (GATHER == 0 ? (unsigned)line * ld : 0u);
             } else {
                 int r = min(row0 + line, rows - 1);
@@ -596,7 +622,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
-    constexpr int THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ, NI = TI / 16, NJ = TJ / 16, PLACE = (BM + BN) * 32;
+    constexpr int THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ, NI = TI / 32, NJ = TJ / 32, PLACE = (BM + BN) * 32;
     __shared__ __attribute__((aligned(1024))) bf16_t lds[kPlaces * PLACE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
@@ -617,13 +643,16 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     else db.init(a, a.x, a.ldx, a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
     const bool sums = SUMS && wants_sums<OP>(a, t, wj);
 
-    floatx4 acc[NI][NJ], row_sum[(NI + 3) / 4];   // row_sum[i / 4][i % 4] of lanes 0 .. 15: the rows of block i
+    floatx16 acc[NI][NJ];
+    float row_sum[NI];
 #pragma unroll
-    for (int i = 0; i < (NI + 3) / 4; ++i) row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NI; ++i) {
+        row_sum[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    }
     const lds_address lds0 = address_in_lds(lds);
     auto load = [&](int s, int place, int q) {   // place: of the step's first half
         const int at = place + (q & 1) < kPlaces ? place + (q & 1) : place + (q & 1) - kPlaces;
@@ -634,20 +663,30 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
         da.fetch_choices(a, s, wave);
         db.fetch_choices(a, s, wave);
     };
-    auto read = [&](int place, int q, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+    // fragment q of a half: first those of its first 16 k
+    auto read = [&](int place, int q, bf16x8 (&x)[2][NI], bf16x8 (&y)[2][NJ]) {
         const bf16_t *half = lds + place * PLACE;
-        if (q < NI) x[q] = fragment<ACROSS_A, 32, BM>(half, wi * TI + 16 * q, 0, lane);
-        else y[q - NI] = fragment<ACROSS_B, 32, BN>(half + BM * 32, wj * TJ + 16 * (q - NI), 0, lane);
+        const int u = q / (NI + NJ), n = q % (NI + NJ);
+        if (n < NI) x[u][n] = fragment32<ACROSS_A, BM>(half, wi * TI + 32 * n, u, lane);
+        else y[u][n - NI] = fragment32<ACROSS_B, BN>(half + BM * 32, wj * TJ + 32 * (n - NI), u, lane);
     };
-    auto add_rows = [&](const bf16x8 (&x)[NI]) {
+    auto multiply = [&](const bf16x8 (&x)[2][NI], const bf16x8 (&y)[2][NJ], int m) {
+        const int u = m / (NI * NJ), j = m / NI % NJ, i = m % NI;
+        acc[i][j] = mfma32(y[u][j], x[u][i], acc[i][j]);
+    };
+    auto add_rows = [&](const bf16x8 (&x)[2][NI]) {
         if constexpr (SUMS)
             if (sums)
 #pragma unroll
-                for (int i = 0; i < NI; ++i) row_sum[i / 4] = mfma(ones_row(i % 4, lane), x[i], row_sum[i / 4]);
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) row_sum[i] += (float)x[u][i][q];
     };
     const int whole = t.K / 64;
     if (whole > 0) {
-        bf16x8 fa[2][NI], fb[2][NJ];
+        bf16x8 fa[2][2][NI], fb[2][2][NJ];   // [half][first or second 16 k]
         int place = 0;   // of the first half of the step that is multiplied
         auto behind = [&](int n) { return place + n < kPlaces ? place + n : place + n - kPlaces; };
         fetch(0);
@@ -663,18 +702,22 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
             wait_loads<0>();
         }
 #pragma unroll
-        for (int q = 0; q < NI + NJ; ++q) read(0, q, fa[0], fb[0]);
+        for (int q = 0; q < 2 * (NI + NJ); ++q) read(0, q, fa[0], fb[0]);
         // One half of a step: x y is multiplied; the fragments of the next half are read from `from`, and the loads of step s + 2 are
         // started if there is one, an access behind every few matrix instructions, which run meanwhile.
-        auto half = [&](const bf16x8 (&x)[NI], const bf16x8 (&y)[NJ], int from, bf16x8 (&nx)[NI], bf16x8 (&ny)[NJ], auto first, bool more, int s, int to) {
-            constexpr int MM = NI * NJ, NR = NI + NJ, EVERY = MM * 3 / 4 / NR, APART = MM / LOADS;   // (before a barrier the reads end earlier)
+        auto half = [&](const bf16x8 (&x)[2][NI], const bf16x8 (&y)[2][NJ], int from, bf16x8 (&nx)[2][NI], bf16x8 (&ny)[2][NJ], auto first, bool more, int s,
+                        int to) {
+            constexpr int MM = 2 * NI * NJ, NR = 2 * (NI + NJ);
 #pragma unroll
             for (int m = 0; m < MM; ++m) {
-                acc[m % NI][m / NI] = mfma(y[m / NI], x[m % NI], acc[m % NI][m / NI]);
-                if (m % EVERY == 0 && m / EVERY < NR) read(from, m / EVERY, nx, ny);
+                multiply(x, y, m);
+                // the reads end some instructions before the barrier
+#pragma unroll
+                for (int q = min(NR, NR * m / (MM * 3 / 4)); q < min(NR, NR * (m + 1) / (MM * 3 / 4)); ++q) read(from, q, nx, ny);
                 if constexpr (first)
-                    if (m % APART == 1 && m / APART < LOADS)
-                        if (more) load(s + 2, to, m / APART);
+                    if (more)
+#pragma unroll
+                        for (int q = LOADS * m / MM; q < LOADS * (m + 1) / MM; ++q) load(s + 2, to, q);
                 __builtin_amdgcn_sched_barrier(0);
             }
             add_rows(x);
@@ -700,17 +743,110 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            bf16x8 x[NI], y[NJ];
+            bf16x8 x[2][NI], y[2][NJ];
 #pragma unroll
-            for (int q = 0; q < NI + NJ; ++q) read(u, q, x, y);
+            for (int q = 0; q < 2 * (NI + NJ); ++q) read(u, q, x, y);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int i = 0; i < NI; ++i) acc[i][j] = mfma(y[j], x[i], acc[i][j]);
+            for (int m = 0; m < 2 * NI * NJ; ++m) multiply(x, y, m);
             add_rows(x);
         }
     }
-    store_tile<bf16_t, OP, NI, NJ>(a, t, t.ti * BM + wi * TI, t.tj * BN + wj * TJ, sums, acc, row_sum, lane);
+    if constexpr (SUMS)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) row_sum[i] += __shfl_xor(row_sum[i], 32);   // the other 8 of 16 k
+    // The sums go out through LDS, so that a wave stores whole pieces of rows: straight from the registers a store would
+    // touch 16 bytes of each of 32 rows (65536 rows 2048 -> 2048: 26 us a tile instead of 34 us a tile's products).
+    // lane -> row lane % 32 of a block, columns 8 g + 4 (lane / 32) .. + 3 for its 16 sums in fours.
+    const int i0 = t.ti * BM, j0 = t.tj * BN;
+    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
+        constexpr int LD = BN + 8;
+        static_assert(BM * LD <= kPlaces * PLACE, "the tile has to fit");
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = wj * TJ + 32 * j + 8 * g + 4 * (lane >> 5);
+                float add[4] = {0.f, 0.f, 0.f, 0.f};
+                if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (j0 + col + r < t.J) add[r] = value(We[(long long)(j0 + col + r) * a.ldw + a.ci]);
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    floatx4 v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * g + r] + add[r];
+                    store4<bf16_t>(lds + (wi * TI + 32 * i + (lane & 31)) * LD + col, 4, v);
+                }
+            }
+        __syncthreads();
+        constexpr int PER_ROW = BN / 8, ROWS = THREADS / PER_ROW;
+        const int col = 8 * (tid % PER_ROW), left = t.J - j0 - col;
+        for (int r = tid / PER_ROW; r < BM && i0 + r < t.I; r += ROWS) {
+            const int c = choice_at(a, t.begin + i0 + r);
+            if (c < 0) continue;
+            const uintx4 v = *(const uintx4 *)(lds + r * LD + col);
+            bf16_t *out = (bf16_t *)a.out + (long long)c * a.ldo + j0 + col;
+            if (left >= 8) {
+                *(uintx4_u *)out = v;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q < left) out[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
+            }
+        }
+    } else {   // fp32 results, a part of the tile's rows at a time
+        constexpr int LD = BN + 4, PART = BM * LD * 4 <= kPlaces * PLACE * 2 ? BM : BM / 2;
+        static_assert(PART * LD * 4 <= kPlaces * PLACE * 2 && PART % TI == 0, "the part has to fit");
+        float *const part = (float *)lds;
+        const bool w = OP == EXPERT_GRAD_WEIGHT;
+        const int d = w ? a.ci + a.bias : t.g ? a.co : a.ci + a.bias;
+        float *const M = w ? a.dW + (long long)t.e * a.co * d : (t.g ? a.G : a.A) + (long long)t.e * d * d;
+        const float alpha = w ? 1.f : (1.f - a.decay) / (float)t.len;
+        for (int p0 = 0; p0 < BM; p0 += PART) {
+            __syncthreads();
+            if (wi * TI >= p0 && wi * TI < p0 + PART)
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const floatx4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                            *(floatx4 *)(part + (wi * TI - p0 + 32 * i + (lane & 31)) * LD + wj * TJ + 32 * j + 8 * g + 4 * (lane >> 5)) = v;
+                        }
+            __syncthreads();
+            constexpr int PER_ROW = BN / 4, ROWS = THREADS / PER_ROW;
+            const int col = 4 * (tid % PER_ROW);
+            for (int r = tid / PER_ROW; r < PART && i0 + p0 + r < t.I; r += ROWS) {
+                const int row = i0 + p0 + r, left = (w ? t.J : min(t.J, row + 1)) - j0 - col;   // (of factors the lower triangle)
+                if (left <= 0) continue;
+                float *out = M + (long long)row * d + j0 + col;
+                floatx4 v = *(const floatx4 *)(part + r * LD + col);
+                if (!w) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = blend(a.decay, alpha, a.decay != 0.f && q < left ? out[q] : 0.f, v[q]);
+                    *(floatx4 *)(part + r * LD + col) = v;
+                }
+                store4<float>(out, left, v);
+            }
+            if (w) continue;
+            __syncthreads();
+            // the mirror image: a wave's lanes along the rows
+            for (int c = tid / 64; c < BN && j0 + c < t.J; c += THREADS / 64)
+                for (int r = lane; r < PART && i0 + p0 + r < t.I; r += 64)
+                    if (i0 + p0 + r > j0 + c) M[(long long)(j0 + c) * d + i0 + p0 + r] = part[r * LD + c];
+        }
+        if (sums && lane < 32)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int row = i0 + wi * TI + 32 * i + lane;
+                if (row >= t.I) continue;
+                if (w) M[(long long)row * d + a.ci] = row_sum[i];
+                else store_border(a, t, row, row_sum[i]);
+            }
+    }
 }
 
 // Operands that go straight to LDS: whole 16-byte chunks, offsets of 32 bits, choices that the division by `fan` is exact for.
