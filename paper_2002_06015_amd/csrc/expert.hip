@@ -107,7 +107,8 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs &a, int block, int ti
 template <bool ACROSS, int BK, int ROWS>
 __device__ __forceinline__ int chunk_at(int line, int pos)
 {
-    if constexpr (ACROSS) return line * (ROWS / 8) + ((((pos >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (pos & 1));
+    if constexpr (ACROSS && ROWS == 64) return line * 8 + ((((pos >> 1) ^ (((line >> 1) & 1) | ((line >> 2) & 2))) << 1) | (pos & 1));
+    else if constexpr (ACROSS) return line * (ROWS / 8) + ((((pos >> 1) ^ ((line & 3) | ((line >> 1) & 4))) << 1) | (pos & 1));
     else if constexpr (BK == 64) return line * 8 + (pos ^ (line & 7));
     else return line * 4 + (pos ^ ((line >> 1) & 3));
 }
@@ -177,9 +178,9 @@ struct Chunk {
 // One operand of a tile.  Along k: rows [0, rows) from `line`; across k: columns col0 .. of `cols`, k < K.
 // GATHER: 0: line r is base + r ld;  1: base + choice_at(begin + r) ld;  2: base + choice_at(begin + r) / fan * ld
 // (fan: 1 where the rows are those of the choices)
-template <typename T, bool ACROSS, int GATHER, int BK>
+template <typename T, bool ACROSS, int GATHER, int BK, int EDGE>
 struct Staged {
-    static constexpr int CH = BK / 16, PER = ACROSS ? 16 : BK / 8;
+    static constexpr int CH = BK * EDGE / 2048, PER = ACROSS ? EDGE / 8 : BK / 8;
     const T *base;
     long long ld;
     int begin, K, cols, col0;
@@ -240,7 +241,7 @@ struct Staged {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int q = tid + 256 * i;
-            reg[i].store(tile, 128 * BK, chunk_at<ACROSS, BK, 128>(q / PER, q % PER));
+            reg[i].store(tile, EDGE * BK, chunk_at<ACROSS, BK, EDGE>(q / PER, q % PER));
         }
     }
 };
@@ -365,14 +366,14 @@ __device__ __forceinline__ void store_border(const ExpertArgs &a, const Tile &t,
 __device__ __forceinline__ float value(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
 __device__ __forceinline__ float value(float v) { return v; }
 
-// Stores a wave's 4 x 4 blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
+// Stores a wave's NB x NB blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
 // row_sum[i] of lanes 0 .. 15: the rows of block i, added up over k.
-template <typename T, int OP>
-__device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[4][4],
+template <typename T, int OP, int NB>
+__device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[NB][NB],
                                            const floatx4 &row_sum, int lane)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NB; ++i) {
         const int row = i0 + 16 * i + (lane & 15);
         if (row >= t.I) continue;
         if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
@@ -381,7 +382,7 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
             T *out = (T *)a.out + (long long)c * a.ldo;
             const T *bias = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw + a.ci;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < NB; ++j) {
                 const int col = j0 + 16 * j + 4 * (lane >> 4);
                 floatx4 v = acc[i][j];
                 if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts)
@@ -393,7 +394,7 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
         } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
             float *out = a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < NB; ++j) {
                 const int col = j0 + 16 * j + 4 * (lane >> 4);
                 store4<float>(out + col, t.J - col, acc[i][j]);
             }
@@ -403,7 +404,7 @@ __device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, i
             float *M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
             const float alpha = (1.f - a.decay) / (float)t.len;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int col = j0 + 16 * j + 4 * (lane >> 4) + r;
@@ -426,38 +427,38 @@ __device__ __forceinline__ bf16x8 ones_row(int q, int lane)
     return __builtin_bit_cast(bf16x8, uintx4{v, v, v, v});
 }
 
-template <typename T, int OP>
-__global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
+template <typename T, int OP, int EDGE>
+__global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
 {
     constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 ? 1 : 3;
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
-    constexpr int PLANE = 128 * BK;
+    constexpr int PLANE = EDGE * BK, NB = EDGE / 32;   // NB x NB blocks of 16 x 16 a wave
     __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * PLANE];
     bf16_t *tile_a = lds, *tile_b = lds + NP * PLANE;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave >> 1, wj = wave & 1;
     Tile t;
-    if (!find_work<OP, 128, 128>(a, tiles_j, total, t)) return;
+    if (!find_work<OP, EDGE, EDGE>(a, tiles_j, total, t)) return;
 
-    Staged<T, ACROSS_A, GATHER_A, BK> sa;
-    Staged<T, ACROSS_B, GATHER_B, BK> sb;
+    Staged<T, ACROSS_A, GATHER_A, BK, EDGE> sa;
+    Staged<T, ACROSS_B, GATHER_B, BK, EDGE> sb;
     const T *We = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw, *x = (const T *)a.x, *dy = (const T *)a.dy;
-    if constexpr (OP == EXPERT_FORWARD) sa.init(a, x, a.ldx, a.fan, t.begin, t.ti * 128, t.I, t.K, tid);
-    else if constexpr (OP == EXPERT_STATS) sa.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * 128, t.I, t.K, tid);
-    else sa.init(a, dy, a.ldy, 1, t.begin, t.ti * 128, t.I, t.K, tid);
-    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) sb.init(a, We, a.ldw, 1, 0, t.tj * 128, t.J, t.K, tid);
-    else if constexpr (OP == EXPERT_STATS) sb.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * 128, t.J, t.K, tid);
-    else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * 128, t.J, t.K, tid);
+    if constexpr (OP == EXPERT_FORWARD) sa.init(a, x, a.ldx, a.fan, t.begin, t.ti * EDGE, t.I, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) sa.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * EDGE, t.I, t.K, tid);
+    else sa.init(a, dy, a.ldy, 1, t.begin, t.ti * EDGE, t.I, t.K, tid);
+    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) sb.init(a, We, a.ldw, 1, 0, t.tj * EDGE, t.J, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) sb.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * EDGE, t.J, t.K, tid);
+    else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * EDGE, t.J, t.K, tid);
     const bool sums = wants_sums<OP>(a, t, wj);
 
-    floatx4 acc[4][4], row_sum = {0.f, 0.f, 0.f, 0.f};   // row_sum[i] of lanes 0 .. 15: the rows of block i
+    floatx4 acc[NB][NB], row_sum = {0.f, 0.f, 0.f, 0.f};   // row_sum[i] of lanes 0 .. 15: the rows of block i
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     if (t.K > 0) {
         sa.load(a, 0, tid);
         sb.load(a, 0, tid);
@@ -473,29 +474,29 @@ __global__ __launch_bounds__(256, 2) void expert_general_kernel(const ExpertArgs
         }
 #pragma unroll
         for (int u = 0; u < BK / 32; ++u) {
-            bf16x8 fa[NP][4], fb[NP][4];
+            bf16x8 fa[NP][NB], fb[NP][NB];
 #pragma unroll
             for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    fa[p][q] = fragment<ACROSS_A, BK, 128>(tile_a + p * PLANE, wi * 64 + 16 * q, u, lane);
-                    fb[p][q] = fragment<ACROSS_B, BK, 128>(tile_b + p * PLANE, wj * 64 + 16 * q, u, lane);
+                for (int q = 0; q < NB; ++q) {
+                    fa[p][q] = fragment<ACROSS_A, BK, EDGE>(tile_a + p * PLANE, wi * (EDGE / 2) + 16 * q, u, lane);
+                    fb[p][q] = fragment<ACROSS_B, BK, EDGE>(tile_b + p * PLANE, wj * (EDGE / 2) + 16 * q, u, lane);
                 }
             constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};   // the small products first
 #pragma unroll
             for (int q = NP == 1 ? 5 : 0; q < 6; ++q)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < NB; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = mfma(fb[pb[q]][j], fa[pa[q]][i], acc[i][j]);
+                    for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fb[pb[q]][j], fa[pa[q]][i], acc[i][j]);
             if (sums)
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) row_sum = mfma(ones_row(i, lane), fa[p][i], row_sum);
+                    for (int i = 0; i < NB; ++i) row_sum = mfma(ones_row(i, lane), fa[p][i], row_sum);
         }
     }
-    store_tile<T, OP>(a, t, t.ti * 128 + wi * 64, t.tj * 128 + wj * 64, sums, acc, row_sum, lane);
+    store_tile<T, OP, NB>(a, t, t.ti * EDGE + wi * (EDGE / 2), t.tj * EDGE + wj * (EDGE / 2), sums, acc, row_sum, lane);
 }
 
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
@@ -903,17 +904,17 @@ hipError_t run_direct(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, int EDGE>
 hipError_t run_general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
 {
     int tj;
-    const long long wgs = count_tiles<128, 128>(op, a, tj);
+    const long long wgs = count_tiles<EDGE, EDGE>(op, a, tj);
     const dim3 grid((unsigned)wgs), block(256);
     switch (op) {
-        case EXPERT_FORWARD: expert_general_kernel<T, EXPERT_FORWARD><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_INPUT: expert_general_kernel<T, EXPERT_GRAD_INPUT><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_WEIGHT: expert_general_kernel<T, EXPERT_GRAD_WEIGHT><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_STATS: expert_general_kernel<T, EXPERT_STATS><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_FORWARD: expert_general_kernel<T, EXPERT_FORWARD, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_GRAD_INPUT: expert_general_kernel<T, EXPERT_GRAD_INPUT, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_GRAD_WEIGHT: expert_general_kernel<T, EXPERT_GRAD_WEIGHT, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_STATS: expert_general_kernel<T, EXPERT_STATS, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
     }
     return hipGetLastError();
 }
@@ -922,9 +923,16 @@ hipError_t run_general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
 
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s)
 {
-    if (!bf16) return run_general<float>(op, a, s);
-    if (direct_ok(op, a)) return run_direct<256, 256, 4, 2>(op, a, s);
-    return run_general<bf16_t>(op, a, s);
+    int tj;
+    if (bf16 && direct_ok(op, a)) {
+        // 256 x 256 tiles need half the traffic, but one of them fills a CU: only where there is one for each of 256
+        if (count_tiles<256, 256>(op, a, tj) >= 256) return run_direct<256, 256, 4, 2>(op, a, s);
+        return run_direct<128, 128, 2, 2>(op, a, s);
+    }
+    // 128 x 128 tiles where there are two for each CU; the smaller ones finish a step in a third of the time
+    const bool large = count_tiles<128, 128>(op, a, tj) >= 512;
+    if (bf16) return large ? run_general<bf16_t, 128>(op, a, s) : run_general<bf16_t, 64>(op, a, s);
+    return large ? run_general<float, 128>(op, a, s) : run_general<float, 64>(op, a, s);
 }
 
 }  // namespace kfac

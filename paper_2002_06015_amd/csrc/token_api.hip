@@ -58,9 +58,9 @@ bool expert_ok(const kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_
     if (kfac_layer_dims(L, nullptr, nullptr, nullptr, nullptr) != KFAC_OK) return false;
     if (L->k != 1 || L->stride != 1 || L->pad != 0 || L->h_in != 1 || L->w_in != 1) return false;
     if (experts < 1 || experts > kMaxExperts || n < 0 || n > kMaxPositions || fan < 1 || n % fan != 0) return false;
-    // tiles of one launch, 128 x 128 elements at least
-    const long long ti = (L->c_in + 127) / 128, to = (L->c_out + 127) / 128;
-    if (((long long)n / 128 + experts + 1) * std::max(ti, to) >= (1LL << 30)) return false;
+    // tiles of one launch, 64 x 64 elements at least
+    const long long ti = (L->c_in + 63) / 64, to = (L->c_out + 63) / 64;
+    if (((long long)n / 64 + experts + 1) * std::max(ti, to) >= (1LL << 30)) return false;
     return experts * (ti * to + ti * (ti + 1) / 2 + to * (to + 1) / 2 + 16) < (1LL << 30);
 }
 
