@@ -366,57 +366,88 @@ __device__ __forceinline__ void store_border(const ExpertArgs &a, const Tile &t,
 __device__ __forceinline__ float value(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
 __device__ __forceinline__ float value(float v) { return v; }
 
-// Stores a wave's NB x NB blocks of 16 x 16 from (i0, j0).  lane -> row i = lane % 16 of a block, columns 4 (lane / 16) .. + 3.
-// row_sum[i] of lanes 0 .. 15: the rows of block i, added up over k.
-template <typename T, int OP, int NB>
-__device__ __forceinline__ void store_tile(const ExpertArgs &a, const Tile &t, int i0, int j0, bool sums, const floatx4 (&acc)[NB][NB],
-                                           const floatx4 &row_sum, int lane)
+// Stores a BM x BN tile whose sums are spread over the workgroup's registers.  They go out through LDS, PART rows at a time, so
+// that a wave stores whole pieces of rows: straight from the registers a store would touch 16 to 32 bytes of each of 16 or 32 rows
+// (65536 rows 64 -> 2048 in bf16: 213 us instead of 92).  put(p0): brings rows p0 .. p0 + PART - 1 into `part`, rows LD apart, with
+// what put_quad gives for four adjacent sums.
+template <typename T, int OP, int BM, int BN, int PART, int THREADS, typename Put>
+__device__ __forceinline__ void store_rows(const ExpertArgs &a, const Tile &t, void *memory, int tid, Put put)
 {
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        const int row = i0 + 16 * i + (lane & 15);
-        if (row >= t.I) continue;
-        if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
-            const int c = choice_at(a, t.begin + row);
-            if (c < 0) continue;
-            T *out = (T *)a.out + (long long)c * a.ldo;
-            const T *bias = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw + a.ci;
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                const int col = j0 + 16 * j + 4 * (lane >> 4);
-                floatx4 v = acc[i][j];
-                if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts)
+    const int i0 = t.ti * BM, j0 = t.tj * BN;
+    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
+        constexpr int E = 16 / sizeof(T), LD = BN + E, PER_ROW = BN / E, ROWS = THREADS / PER_ROW;   // 16-byte pieces
+        T *const part = (T *)memory;
+        const int col = E * (tid % PER_ROW), left = t.J - j0 - col;
+        for (int p0 = 0; p0 < BM && i0 + p0 < t.I; p0 += PART) {
+            __syncthreads();
+            put(p0, [&](int row, int c, const floatx4 &v) {
+                floatx4 w = v;
+                if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts) {
+                    const T *bias = (const T *)a.W + ((long long)t.e * a.co + j0 + c) * a.ldw + a.ci;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (col + r < t.J) v[r] += value(bias[(long long)(col + r) * a.ldw]);
-                store4<T>(out + col, t.J - col, v);
-            }
-        } else if constexpr (OP == EXPERT_GRAD_WEIGHT) {
-            float *out = a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                const int col = j0 + 16 * j + 4 * (lane >> 4);
-                store4<float>(out + col, t.J - col, acc[i][j]);
-            }
-            if (sums && lane < 16) out[a.ci] = row_sum[i];
-        } else {
-            const int d = t.g ? a.co : a.ci + a.bias;
-            float *M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
-            const float alpha = (1.f - a.decay) / (float)t.len;
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int col = j0 + 16 * j + 4 * (lane >> 4) + r;
-                    if (col > row) continue;               // (the other triangle is the mirror image)
-                    float *lo = M + (long long)row * d + col;
-                    const float v = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *lo, acc[i][j][r]);
-                    *lo = v;
-                    if (col < row) M[(long long)col * d + row] = v;
+                        if (j0 + c + r < t.J) w[r] += value(bias[(long long)r * a.ldw]);
                 }
-            if (sums && lane < 16) store_border(a, t, row, row_sum[i]);
+                store4<T>(part + (row - p0) * LD + c, 4, w);
+            });
+            __syncthreads();
+#pragma unroll 4
+            for (int r = tid / PER_ROW; r < PART; r += ROWS) {
+                if (i0 + p0 + r >= t.I) break;
+                const int c = choice_at(a, t.begin + i0 + p0 + r);
+                const uintx4 v = *(const uintx4 *)(part + r * LD + col);
+                T *out = (T *)a.out + (long long)c * a.ldo + j0 + col;
+                if (c >= 0 && left >= E) {
+                    *(uintx4_u *)out = v;
+                } else if (c >= 0) {
+#pragma unroll
+                    for (int q = 0; q < E; ++q)
+                        if (q < left) out[q] = part[r * LD + col + q];
+                }
+            }
+        }
+    } else {
+        constexpr int LD = BN + 4, PER_ROW = BN / 4, ROWS = THREADS / PER_ROW;
+        constexpr bool w = OP == EXPERT_GRAD_WEIGHT;
+        float *const part = (float *)memory;
+        const int d = w ? a.ci + a.bias : t.g ? a.co : a.ci + a.bias;
+        float *const M = w ? a.dW + (long long)t.e * a.co * d : (t.g ? a.G : a.A) + (long long)t.e * d * d;
+        const float alpha = w ? 1.f : (1.f - a.decay) / (float)t.len;
+        const int col = 4 * (tid % PER_ROW);
+        for (int p0 = 0; p0 < BM && i0 + p0 < t.I; p0 += PART) {
+            __syncthreads();
+            put(p0, [&](int row, int c, const floatx4 &v) { *(floatx4 *)(part + (row - p0) * LD + c) = v; });
+            __syncthreads();
+            for (int r = tid / PER_ROW; r < PART && i0 + p0 + r < t.I; r += ROWS) {
+                const int row = i0 + p0 + r, left = (w ? t.J : min(t.J, row + 1)) - j0 - col;   // (of factors the lower triangle)
+                if (left <= 0) continue;
+                float *out = M + (long long)row * d + j0 + col;
+                floatx4 v = *(const floatx4 *)(part + r * LD + col);
+                if constexpr (!w) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = blend(a.decay, alpha, a.decay != 0.f && q < left ? out[q] : 0.f, v[q]);
+                    *(floatx4 *)(part + r * LD + col) = v;
+                }
+                store4<float>(out, left, v);
+            }
+            if constexpr (!w) {   // the mirror image: lanes along the rows
+                __syncthreads();
+                for (int u = tid; u < BN * PART; u += THREADS) {
+                    const int r = u % PART, c = u / PART, row = i0 + p0 + r;
+                    if (row < t.I && row > j0 + c) M[(long long)(j0 + c) * d + row] = part[r * LD + c];
+                }
+            }
         }
     }
+}
+
+// The sum of a row over k: the bias column of dW, or the border of A_e.
+template <int OP>
+__device__ __forceinline__ void store_sum(const ExpertArgs &a, const Tile &t, int row, float sum)
+{
+    if (row >= t.I) return;
+    if constexpr (OP == EXPERT_GRAD_WEIGHT) a.dW[((long long)t.e * a.co + row) * (a.ci + a.bias) + a.ci] = sum;
+    else if constexpr (OP == EXPERT_STATS) store_border(a, t, row, sum);
 }
 
 // Row q of the first operand of a matrix instruction is ones, the others zero: its product adds up the second operand's rows over k
@@ -436,8 +467,9 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
     constexpr int PLANE = EDGE * BK, NB = EDGE / 32;   // NB x NB blocks of 16 x 16 a wave
-    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * PLANE];
-    bf16_t *tile_a = lds, *tile_b = lds + NP * PLANE;
+    // small tiles have two LDS stages: a step's operands are converted and stored while the step before it is multiplied
+    constexpr int STAGES = EDGE == 64 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) bf16_t lds[STAGES * 2 * NP * PLANE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave >> 1, wj = wave & 1;
     Tile t;
@@ -459,19 +491,18 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
     for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (t.K > 0) {
-        sa.load(a, 0, tid);
-        sb.load(a, 0, tid);
-    }
-    for (int k0 = 0; k0 < t.K; k0 += BK) {
-        if (k0 > 0) __syncthreads();   // every wave has read the step before
-        sa.store(tile_a, tid);
-        sb.store(tile_b, tid);
-        __syncthreads();
-        if (k0 + BK < t.K) {
-            sa.load(a, k0 + BK, tid);
-            sb.load(a, k0 + BK, tid);
+    auto store = [&](int stage) {
+        sa.store(lds + stage * 2 * NP * PLANE, tid);
+        sb.store(lds + stage * 2 * NP * PLANE + NP * PLANE, tid);
+    };
+    auto load = [&](int k0) {
+        if (k0 < t.K) {
+            sa.load(a, k0, tid);
+            sb.load(a, k0, tid);
         }
+    };
+    auto multiply = [&](int stage) {
+        const bf16_t *tile_a = lds + stage * 2 * NP * PLANE, *tile_b = tile_a + NP * PLANE;
 #pragma unroll
         for (int u = 0; u < BK / 32; ++u) {
             bf16x8 fa[NP][NB], fb[NP][NB];
@@ -495,8 +526,42 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
 #pragma unroll
                     for (int i = 0; i < NB; ++i) row_sum = mfma(ones_row(i, lane), fa[p][i], row_sum);
         }
+    };
+    load(0);
+    if constexpr (STAGES == 2) {
+        if (t.K > 0) store(0);
+        load(BK);
+        for (int k0 = 0, stage = 0; k0 < t.K; k0 += BK, stage ^= 1) {
+            __syncthreads();   // the step is there, and every wave has read the one before it
+            if (k0 + BK < t.K) store(stage ^ 1);
+            load(k0 + 2 * BK);
+            multiply(stage);
+        }
+    } else {
+        for (int k0 = 0; k0 < t.K; k0 += BK) {
+            if (k0 > 0) __syncthreads();   // every wave has read the step before
+            store(0);
+            __syncthreads();
+            load(k0 + BK);
+            multiply(0);
+        }
     }
-    store_tile<T, OP, NB>(a, t, t.ti * EDGE + wi * (EDGE / 2), t.tj * EDGE + wj * (EDGE / 2), sums, acc, row_sum, lane);
+    // lane -> row lane % 16 of a block, columns 4 (lane / 16) .. + 3
+    constexpr bool SAME = OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT;   // results of the operands' type
+    constexpr int PART = EDGE == 64 ? 64 : sizeof(T) == 2 && !SAME ? 32 : 64;
+    static_assert(PART * (EDGE + 8) * (SAME ? sizeof(T) : 4) <= sizeof(lds), "the part has to fit");
+    store_rows<T, OP, EDGE, EDGE, PART, 256>(a, t, lds, tid, [&](int p0, auto put_quad) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int row = wi * (EDGE / 2) + 16 * i;
+            if (row < p0 || row >= p0 + PART) continue;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) put_quad(row + (lane & 15), wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4), acc[i][j]);
+        }
+    });
+    if (sums && lane < 16)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) store_sum<OP>(a, t, t.ti * EDGE + wi * (EDGE / 2) + 16 * i + lane, row_sum[i]);
 }
 
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
@@ -755,99 +820,26 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     if constexpr (SUMS)
 #pragma unroll
         for (int i = 0; i < NI; ++i) row_sum[i] += __shfl_xor(row_sum[i], 32);   // the other 8 of 16 k
-    // The sums go out through LDS, so that a wave stores whole pieces of rows: straight from the registers a store would
-    // touch 16 bytes of each of 32 rows (65536 rows 2048 -> 2048: 26 us a tile instead of 34 us a tile's products).
-    // lane -> row lane % 32 of a block, columns 8 g + 4 (lane / 32) .. + 3 for its 16 sums in fours.
-    const int i0 = t.ti * BM, j0 = t.tj * BN;
-    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) {
-        constexpr int LD = BN + 8;
-        static_assert(BM * LD <= kPlaces * PLACE, "the tile has to fit");
-        __syncthreads();
+    // lane -> row lane % 32 of a block, columns 8 g + 4 (lane / 32) .. + 3 for its 16 sums in fours
+    constexpr int SIZE = OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT ? 2 : 4;
+    constexpr int PART = BM * (BN + 8) * SIZE <= (int)sizeof(lds) ? BM : BM / 2;
+    static_assert(PART * (BN + 8) * SIZE <= sizeof(lds), "the part has to fit");
+    store_rows<bf16_t, OP, BM, BN, PART, THREADS>(a, t, lds, tid, [&](int p0, auto put_quad) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+        for (int i = 0; i < NI; ++i) {
+            const int row = wi * TI + 32 * i;
+            if (row < p0 || row >= p0 + PART) continue;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = wj * TJ + 32 * j + 8 * g + 4 * (lane >> 5);
-                float add[4] = {0.f, 0.f, 0.f, 0.f};
-                if (OP == EXPERT_FORWARD && a.bias && t.e < a.experts)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (j0 + col + r < t.J) add[r] = value(We[(long long)(j0 + col + r) * a.ldw + a.ci]);
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    floatx4 v;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * g + r] + add[r];
-                    store4<bf16_t>(lds + (wi * TI + 32 * i + (lane & 31)) * LD + col, 4, v);
-                }
-            }
-        __syncthreads();
-        constexpr int PER_ROW = BN / 8, ROWS = THREADS / PER_ROW;
-        const int col = 8 * (tid % PER_ROW), left = t.J - j0 - col;
-        for (int r = tid / PER_ROW; r < BM && i0 + r < t.I; r += ROWS) {
-            const int c = choice_at(a, t.begin + i0 + r);
-            if (c < 0) continue;
-            const uintx4 v = *(const uintx4 *)(lds + r * LD + col);
-            bf16_t *out = (bf16_t *)a.out + (long long)c * a.ldo + j0 + col;
-            if (left >= 8) {
-                *(uintx4_u *)out = v;
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (q < left) out[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
-            }
+                for (int g = 0; g < 4; ++g)
+                    put_quad(row + (lane & 31), wj * TJ + 32 * j + 8 * g + 4 * (lane >> 5),
+                             floatx4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
         }
-    } else {   // fp32 results, a part of the tile's rows at a time
-        constexpr int LD = BN + 4, PART = BM * LD * 4 <= kPlaces * PLACE * 2 ? BM : BM / 2;
-        static_assert(PART * LD * 4 <= kPlaces * PLACE * 2 && PART % TI == 0, "the part has to fit");
-        float *const part = (float *)lds;
-        const bool w = OP == EXPERT_GRAD_WEIGHT;
-        const int d = w ? a.ci + a.bias : t.g ? a.co : a.ci + a.bias;
-        float *const M = w ? a.dW + (long long)t.e * a.co * d : (t.g ? a.G : a.A) + (long long)t.e * d * d;
-        const float alpha = w ? 1.f : (1.f - a.decay) / (float)t.len;
-        for (int p0 = 0; p0 < BM; p0 += PART) {
-            __syncthreads();
-            if (wi * TI >= p0 && wi * TI < p0 + PART)
+    });
+    if (sums && lane < 32)
 #pragma unroll
-                for (int i = 0; i < NI; ++i)
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const floatx4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                            *(floatx4 *)(part + (wi * TI - p0 + 32 * i + (lane & 31)) * LD + wj * TJ + 32 * j + 8 * g + 4 * (lane >> 5)) = v;
-                        }
-            __syncthreads();
-            constexpr int PER_ROW = BN / 4, ROWS = THREADS / PER_ROW;
-            const int col = 4 * (tid % PER_ROW);
-            for (int r = tid / PER_ROW; r < PART && i0 + p0 + r < t.I; r += ROWS) {
-                const int row = i0 + p0 + r, left = (w ? t.J : min(t.J, row + 1)) - j0 - col;   // (of factors the lower triangle)
-                if (left <= 0) continue;
-                float *out = M + (long long)row * d + j0 + col;
-                floatx4 v = *(const floatx4 *)(part + r * LD + col);
-                if (!w) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = blend(a.decay, alpha, a.decay != 0.f && q < left ? out[q] : 0.f, v[q]);
-                    *(floatx4 *)(part + r * LD + col) = v;
-                }
-                store4<float>(out, left, v);
-            }
-            if (w) continue;
-            __syncthreads();
-            // the mirror image: a wave's lanes along the rows
-            for (int c = tid / 64; c < BN && j0 + c < t.J; c += THREADS / 64)
-                for (int r = lane; r < PART && i0 + p0 + r < t.I; r += 64)
-                    if (i0 + p0 + r > j0 + c) M[(long long)(j0 + c) * d + i0 + p0 + r] = part[r * LD + c];
-        }
-        if (sums && lane < 32)
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int row = i0 + wi * TI + 32 * i + lane;
-                if (row >= t.I) continue;
-                if (w) M[(long long)row * d + a.ci] = row_sum[i];
-                else store_border(a, t, row, row_sum[i]);
-            }
-    }
+        for (int i = 0; i < NI; ++i) store_sum<OP>(a, t, t.ti * BM + wi * TI + 32 * i + lane, row_sum[i]);
 }
 
 // Operands that go straight to LDS: whole 16-byte chunks, offsets of 32 bits, choices that the division by `fan` is exact for.
