@@ -57,8 +57,17 @@ __device__ __forceinline__ int choice_at(const ExpertArgs &a, int s)
     return c >= 0 && c < a.n ? c : -1;
 }
 
-// Tile `block` of those of all experts with BM rows and tiles_j columns of tiles each; false: there are fewer.  Consecutive
-// tiles share a panel of W; every XCD works through one contiguous share.  All threads of a wave call it.
+// Tiles in bands of 4 rows, column by column: the 32 that an XCD works on at one time are 4 x 8 and touch 12 panels of operands.
+__device__ __forceinline__ void banded(int local, int rows, int tiles_j, int &ti, int &tj)
+{
+    const int band = local / (4 * tiles_j), high = min(4, rows - 4 * band);
+    local -= band * 4 * tiles_j;
+    tj = local / high;
+    ti = 4 * band + local - tj * high;
+}
+
+// Tile `block` of those of all experts with BM rows and tiles_j columns of tiles each; false: there are fewer.  Every XCD works through
+// one contiguous share.  All threads of a wave call it.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const ExpertArgs &a, int block, int tiles_j, int &e, int &begin, int &len, int &ti, int &tj)
 {
@@ -90,10 +99,7 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs &a, int block, int ti
             e = __builtin_amdgcn_readfirstlane(e0 + who);
             begin = __builtin_amdgcn_readlane(b, who);
             len = __builtin_amdgcn_readlane(l, who);
-            const int rows = (len + BM - 1) / BM;
-            const int local = id - before - (__builtin_amdgcn_readlane(incl, who) - __builtin_amdgcn_readlane(t, who));
-            tj = local / rows;
-            ti = local - tj * rows;
+            banded(id - before - (__builtin_amdgcn_readlane(incl, who) - __builtin_amdgcn_readlane(t, who)), (len + BM - 1) / BM, tiles_j, ti, tj);
             return true;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
@@ -311,11 +317,7 @@ __device__ __forceinline__ bool find_work(const ExpertArgs &a, int tiles_j, int 
         const int tiles_i = (a.co + BM - 1) / BM;
         int local;
         if (!expert_share(total / a.experts, tiles_i * tiles_j, t.e, local)) return false;
-        // bands of 4 rows of tiles, column by column
-        const int band = local / (4 * tiles_j), rows = min(4, tiles_i - 4 * band);
-        local -= band * 4 * tiles_j;
-        t.tj = local / rows;
-        t.ti = 4 * band + local - t.tj * rows;
+        banded(local, tiles_i, tiles_j, t.ti, t.tj);
         segment(a, t.e, t.begin, t.len);
         t.I = a.co; t.J = a.ci; t.K = t.len;
         return true;
