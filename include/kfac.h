@@ -553,7 +553,7 @@ typedef enum {
 typedef struct {
     int32_t kernel;    /* kfac_kernel */
     int32_t variant;   /* GEMM: 0 = 128x128 tiles, 1 = 64x64 tiles, 2 / 3 = 32x32 / 64x64 without LDS staging,
-                        * 4 = the displaced products of one image together.  Embedding: 0 = lookup, 1 .. 3 = the passes of
+                        * 4 = the displaced products of one image together.  Embedding: 0 = lookup, 1 and 2 = the passes of
                         * its gradient; experts: 0 = forward, 1 = grad_input, 2 = grad_weight, 3 = factors */
     int32_t workgroups;   /* 0: not reported (token and expert layers) */
     float ms;

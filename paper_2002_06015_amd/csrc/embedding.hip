@@ -5,8 +5,9 @@
 // Gradient: dT[v] = scale * sum over the positions of token v, added in fp32 in the order of the positions, without atomics.
 // The positions come sorted by token.  A wave takes a run of `chunk` sorted positions and one 64-lane piece of the columns,
 // keeps the running sum in registers and writes a row where the token changes.  A token whose positions cross runs leaves its
-// part of the sum in scratch, and the join adds the parts in order.  Rows of tokens that do not occur are written by a kernel
-// of their own.  Memory bound: the gradients are read once, the table's gradient is written once.
+// part of the sum in scratch, and the join adds the parts in order.  Rows of tokens that do not occur are zeros, which the sort's
+// launches write beside the sort.  Memory bound: the gradients are read once, the table's gradient is written once, rows of tokens
+// that occur twice.
 #include "token_internal.h"
 
 namespace kfac {
@@ -120,32 +121,6 @@ __device__ __forceinline__ int find_key(const int *__restrict__ keys, int n, int
     return lo;
 }
 
-// Rows of tokens that do not occur: zero, unless sums are added to what is there.
-constexpr int kAbsentRows = 32;
-__global__ __launch_bounds__(256) void embedding_absent_kernel(const EmbeddingGrad a)
-{
-    __shared__ int absent[kAbsentRows];
-    const int v0 = blockIdx.x * kAbsentRows;
-    if (threadIdx.x < kAbsentRows) {
-        const int v = v0 + threadIdx.x;
-        int none = 0;
-        if (v < a.vocab) {
-            const int i = find_key(a.keys, a.n, v);
-            none = i >= a.n || a.keys[i] != v;
-            if (none && a.A) a.A[v] = a.decay == 0.f ? 0.f : a.decay * a.A[v];
-        }
-        absent[threadIdx.x] = none;
-    }
-    if (a.accumulate) return;
-    __syncthreads();
-    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r = threadIdx.x >> 6; r < kAbsentRows; r += 4) {
-        if (!absent[r]) continue;
-        float *row = a.dW + (long long)(v0 + r) * a.dim;
-        for (int c = 4 * (threadIdx.x & 63); c < a.dim; c += 256) store_piece<float, 4>(row + c, a.dim - c, zero);
-    }
-}
-
 template <int W>
 __device__ __forceinline__ void write_row(const EmbeddingGrad &a, int key, int count, int c0, const float (&sum)[W])
 {
@@ -155,7 +130,7 @@ __device__ __forceinline__ void write_row(const EmbeddingGrad &a, int key, int c
 #pragma unroll
     for (int j = 0; j < W; ++j) v[j] = a.accumulate ? fmaf(a.scale, sum[j], v[j]) : a.scale * sum[j];
     store_piece<float, W>(row, a.dim - c0, v);
-    if (c0 == 0 && a.A) a.A[key] = a.decay == 0.f ? a.share * count : fmaf(a.share, (float)count, a.decay * a.A[key]);
+    if (c0 == 0 && a.A) a.A[key] = fmaf(a.share, (float)count, a.A[key]);
 }
 
 // A wave: a run of sorted positions, 64 W columns.
@@ -214,38 +189,64 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingGrad 
     flush(cnt);
 }
 
-// Tokens whose positions cross runs: the workgroup of the run in which such a token starts adds its parts, in order.
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void embedding_join_kernel(const EmbeddingGrad a, int chunks)
+// Tokens whose positions cross runs: a wave for every run in which such a token starts and 256 columns adds its parts, in order.
+// A token of more than kLongParts parts is left to the whole workgroup, which adds up a share of the parts in each wave.
+constexpr int kJoinWaves = 8, kLongParts = 24;
+__global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const EmbeddingGrad a, int chunks)
 {
-    __shared__ float part[WAVES][64][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = blockIdx.x, last = min((c + 1) * a.chunk, a.n) - 1;
-    const int key = a.keys[last];
-    if (key >= a.vocab || last + 1 >= a.n || a.keys[last + 1] != key) return;                   // nothing goes on behind this run
-    if (c > 0 && a.keys[c * a.chunk] == key && a.keys[c * a.chunk - 1] == key) return;          // it did not start here
-    const int begin = find_key(a.keys, a.n, key), end = find_key(a.keys, a.n, key + 1);
-    const int c1 = (end - 1) / a.chunk, parts = c1 - c + 1;                                     // parts of the runs c .. c1
-    const int per = (parts + WAVES - 1) / WAVES, p0 = min(wave * per, parts), p1 = min(p0 + per, parts);
+    __shared__ float part[kJoinWaves][64][4];
+    __shared__ int is_long[kJoinWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c0 = (blockIdx.y * 64 + lane) * 4;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c0 < a.dim) {
+    // parts of the token that goes on behind run c and starts in it; 0: there is none
+    auto look = [&](int c, int &key) {
+        if (c >= chunks) return 0;
+        const int last = min((c + 1) * a.chunk, a.n) - 1;
+        key = a.keys[last];
+        if (key >= a.vocab || last + 1 >= a.n || a.keys[last + 1] != key) return 0;
+        if (c > 0 && a.keys[c * a.chunk] == key && a.keys[c * a.chunk - 1] == key) return 0;
+        return (find_key(a.keys, a.n, key + 1) - 1) / a.chunk - c + 1;
+    };
+    auto add = [&](int c, int p0, int p1, float (&sum)[4]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = 0.f;
+        if (c0 < a.dim) {
 #pragma unroll 8
-        for (int p = p0; p < p1; ++p) {
-            float v[4];
-            load_piece<float, 4>(a.partial + ((long long)2 * (c + p) + (p == 0 ? 1 : 0)) * a.dim + c0, a.dim - c0, v);
+            for (int p = p0; p < p1; ++p) {
+                float v[4];
+                load_piece<float, 4>(a.partial + ((long long)2 * (c + p) + (p == 0 ? 1 : 0)) * a.dim + c0, a.dim - c0, v);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += v[j];
+                for (int j = 0; j < 4; ++j) sum[j] += v[j];
+            }
         }
+    };
+    auto write = [&](int key, const float (&sum)[4]) {
+        if (c0 < a.dim) write_row<4>(a, key, find_key(a.keys, a.n, key + 1) - find_key(a.keys, a.n, key), c0, sum);
+    };
+    int key = 0;
+    float sum[4];
+    const int mine = blockIdx.x * kJoinWaves + wave, parts = look(mine, key);
+    if (lane == 0) is_long[wave] = parts > kLongParts;
+    if (parts > 0 && parts <= kLongParts) {
+        add(mine, 0, parts, sum);
+        write(key, sum);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) part[wave][lane][j] = sum[j];
     __syncthreads();
-    if (wave != 0 || c0 >= a.dim) return;
-    for (int w = 1; w < WAVES; ++w)
+    for (int w = 0; w < kJoinWaves; ++w) {
+        if (!is_long[w]) continue;
+        const int c = blockIdx.x * kJoinWaves + w, all = look(c, key), per = (all + kJoinWaves - 1) / kJoinWaves;
+        add(c, min(wave * per, all), min(wave * per + per, all), sum);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] += part[w][lane][j];
-    write_row<4>(a, key, end - begin, c0, sum);
+        for (int j = 0; j < 4; ++j) part[wave][lane][j] = sum[j];
+        __syncthreads();
+        if (wave == 0) {
+            for (int q = 1; q < kJoinWaves; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += part[q][lane][j];
+            write(key, sum);
+        }
+        __syncthreads();
+    }
 }
 
 template <typename ID, typename TT, typename TO>
@@ -281,12 +282,6 @@ hipError_t launch_embedding(const void *ids, int id_bits, int n, int vocab, int 
 
 int embedding_chunk(int n) { return n <= 32768 ? 8 : 32; }
 
-hipError_t launch_embedding_absent(const EmbeddingGrad &a, hipStream_t s)
-{
-    embedding_absent_kernel<<<dim3((a.vocab + kAbsentRows - 1) / kAbsentRows), dim3(256), 0, s>>>(a);
-    return hipGetLastError();
-}
-
 hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s)
 {
     const int chunks = (a.n + a.chunk - 1) / a.chunk;
@@ -300,7 +295,7 @@ hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s)
 hipError_t launch_embedding_join(const EmbeddingGrad &a, hipStream_t s)
 {
     const int chunks = (a.n + a.chunk - 1) / a.chunk;
-    embedding_join_kernel<8><<<dim3(chunks, (a.dim + 255) / 256), dim3(512), 0, s>>>(a, chunks);
+    embedding_join_kernel<<<dim3((chunks + kJoinWaves - 1) / kJoinWaves, (a.dim + 255) / 256), dim3(64 * kJoinWaves), 0, s>>>(a, chunks);
     return hipGetLastError();
 }
 

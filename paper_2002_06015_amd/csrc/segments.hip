@@ -4,8 +4,9 @@
 // A counting sort over digits of up to 9 bits, lowest digit first.  The rank of an element among the equal digits of its wave
 // comes from ballots (one a bit: the lanes with the same digit), the count before the wave from LDS, so nothing depends on the
 // order in which atomics arrive.  Up to 8192 positions are sorted by one workgroup whose keys stay in registers and LDS
-// (one launch, bound by the latency of its chain: ballots, an LDS counter, a scan); more take three launches a digit:
-// counts of 2048-position tiles, running sums along the tiles, ranks and scatter.  Reads and writes 16 bytes a position and digit.
+// (one launch, bound by the latency of its chain: ballots, an LDS counter, a scan), up to 32768 if the key is one digit.  More take
+// two launches a digit: counts of 2048-position tiles, then ranks and scatter, where every tile adds up the counts of those before
+// it (beyond 256 tiles a launch between them does).  Reads and writes 16 bytes a position and digit.
 #include "token_internal.h"
 
 namespace kfac {
@@ -52,7 +53,7 @@ __device__ __forceinline__ void rank_wave(const int (&key)[ROUNDS], const bool (
     }
 }
 
-// counter[w][d] -> elements with a smaller digit, or the same digit in an earlier wave; tmp: [16].  All threads call it.
+// counter[w][d] -> elements with a smaller digit, or the same digit in an earlier wave; tmp: [WAVES].  All threads call it.
 template <int WAVES>
 __device__ __forceinline__ void scan_counters(int *counter, int stride, int bins, int *tmp)
 {
@@ -61,13 +62,11 @@ __device__ __forceinline__ void scan_counters(int *counter, int stride, int bins
     int carry = 0;
     for (int d0 = 0; d0 < bins; d0 += WAVES * 64) {
         const int d = d0 + t;
-        int sum = 0;
-        if (d < bins)
-            for (int w = 0; w < WAVES; ++w) {
-                const int c = counter[w * stride + d];
-                counter[w * stride + d] = sum;
-                sum += c;
-            }
+        int c[WAVES], sum = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) c[w] = d < bins ? counter[w * stride + d] : 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += c[w];
         int incl = sum;
         for (int o = 1; o < 64; o <<= 1) {
             const int up = __shfl_up(incl, o);
@@ -75,17 +74,40 @@ __device__ __forceinline__ void scan_counters(int *counter, int stride, int bins
         }
         if (lane == 63) tmp[wave] = incl;
         __syncthreads();
-        int base = carry;
+        int base = carry + incl - sum;
+#pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const int c = tmp[w];
-            if (w < wave) base += c;
-            carry += c;
+            const int v = tmp[w];
+            if (w < wave) base += v;
+            carry += v;
         }
         if (d < bins)
-            for (int w = 0; w < WAVES; ++w) counter[w * stride + d] += base + incl - sum;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                counter[w * stride + d] = base;
+                base += c[w];
+            }
         __syncthreads();
     }
 }
+
+// Share `block` of `blocks` of the work beside a sort.
+__device__ __forceinline__ void fill_share(const Fill &f, long long block, long long blocks, int threads)
+{
+    const long long first = block * threads + threadIdx.x, step = blocks * threads;
+    if (f.data) {   // 16 bytes a lane from the first aligned element on
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        long long head = (4 - (((unsigned long long)f.data >> 2) & 3)) & 3;
+        if (head > f.count) head = f.count;
+        const long long quads = (f.count - head) / 4;
+        for (long long i = first; i < quads; i += step) *(f32x4 *)(f.data + head + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
+        const long long rest = f.count - 4 * quads;   // head and tail
+        for (long long i = first; i < rest; i += step) f.data[i < head ? i : i + 4 * quads] = 0.f;
+    }
+    for (long long i = first; i < f.n_decayed; i += step) f.decayed[i] = f.decay == 0.f ? 0.f : f.decay * f.decayed[i];
+}
+
+__global__ __launch_bounds__(1024) void fill_kernel(const Fill f) { fill_share(f, blockIdx.x, gridDim.x, 1024); }
 
 __device__ __forceinline__ int lower_bound(const int *keys, int n, int key)
 {
@@ -99,8 +121,13 @@ __device__ __forceinline__ int lower_bound(const int *keys, int n, int key)
 
 template <typename ID>
 __global__ __launch_bounds__(1024) void segments_small_kernel(const ID *__restrict__ ids, int n, int num, int passes, int bits,
-                                                              int *__restrict__ order, int *__restrict__ keys, int *__restrict__ offsets)
+                                                              int *__restrict__ order, int *__restrict__ keys, int *__restrict__ offsets,
+                                                              const Fill fill)
 {
+    if (blockIdx.x > 0) {
+        fill_share(fill, blockIdx.x - 1, gridDim.x - 1, 1024);
+        return;
+    }
     constexpr int WAVES = 16, ROUNDS = kSegSmall / 1024;
     __shared__ int skey[kSegSmall], spos[kSegSmall];
     __shared__ int counter[WAVES << kSegBits];
@@ -148,10 +175,50 @@ __global__ __launch_bounds__(1024) void segments_small_kernel(const ID *__restri
         for (int v = t; v <= num; v += 1024) offsets[v] = lower_bound(skey, n, v);
 }
 
+// One workgroup, keys of one digit: counts, then ranks.
+template <typename ID>
+__global__ __launch_bounds__(1024) void segments_one_kernel(const ID *__restrict__ ids, int n, int num, int bits, int *__restrict__ order,
+                                                            int *__restrict__ offsets)
+{
+    constexpr int WAVES = 16, ROUNDS = 8;
+    __shared__ int counter[WAVES << kSegBits];
+    __shared__ int tmp[WAVES];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, bins = 1 << bits;
+    const int per_wave = (n + 64 * WAVES - 1) / (64 * WAVES) * 64, i0 = wave * per_wave, i1 = min(i0 + per_wave, n);
+    for (int i = t; i < WAVES * bins; i += 1024) counter[i] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int i = i0 + lane; i < i1; i += 64) atomicAdd(&counter[wave * bins + seg_key(ids, i, num)], 1);
+    scan_counters<WAVES>(counter, bins, bins, tmp);
+    if (offsets)
+        for (int v = t; v <= num; v += 1024) offsets[v] = counter[v];   // (where the first wave's start)
+    __syncthreads();
+    for (int b0 = i0; b0 < i1; b0 += 64 * ROUNDS) {
+        int key[ROUNDS], rank[ROUNDS];
+        bool in[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int i = b0 + 64 * r + lane;
+            in[r] = i < i1;
+            key[r] = in[r] ? seg_key(ids, i, num) : 0;
+            rank[r] = 0;
+        }
+        rank_wave<ROUNDS>(key, in, min(ROUNDS, (i1 - b0 + 63) / 64), 0, bits, counter + wave * bins, rank);   // (the counters hold the places)
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (in[r]) order[rank[r]] = b0 + 64 * r + lane;
+    }
+}
+
+// counts: [tiles][bins]
 template <typename ID>
 __global__ __launch_bounds__(256) void segments_count_kernel(const ID *__restrict__ ids, const int *__restrict__ keys, int n, int num, int shift,
-                                                             int bits, int tiles, int *__restrict__ counts)
+                                                             int bits, int tiles, int *__restrict__ counts, const Fill fill)
 {
+    if ((int)blockIdx.x >= tiles) {
+        fill_share(fill, blockIdx.x - tiles, gridDim.x - tiles, 256);
+        return;
+    }
     __shared__ int bin[1 << kSegBits];
     const int bins = 1 << bits, t = threadIdx.x;
     for (int d = t; d < bins; d += 256) bin[d] = 0;
@@ -163,27 +230,27 @@ __global__ __launch_bounds__(256) void segments_count_kernel(const ID *__restric
         if (i < n) atomicAdd(&bin[((ids ? seg_key(ids, i, num) : keys[i]) >> shift) & (bins - 1)], 1);
     }
     __syncthreads();
-    for (int d = t; d < bins; d += 256) counts[(long long)d * tiles + blockIdx.x] = bin[d];
+    for (int d = t; d < bins; d += 256) counts[(long long)blockIdx.x * bins + d] = bin[d];
 }
 
-// one wave a digit: running sums along the tiles, and the digit's total
-__global__ __launch_bounds__(256) void segments_scan_kernel(int *__restrict__ counts, int tiles, int bins, int *__restrict__ totals)
+// running sums along the tiles, and the digits' totals
+constexpr int kScanTiles = 256;   // beyond so many a launch of its own adds them up
+__global__ __launch_bounds__(64) void segments_scan_kernel(int *__restrict__ counts, int tiles, int bins, int *__restrict__ totals)
 {
-    const int lane = threadIdx.x & 63, d = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int d = blockIdx.x * 64 + threadIdx.x;
     if (d >= bins) return;
-    int *row = counts + (long long)d * tiles;
     int carry = 0;
-    for (int b = 0; b < tiles; b += 64) {
-        const int c = b + lane < tiles ? row[b + lane] : 0;
-        int incl = c;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int up = __shfl_up(incl, o);
-            if (lane >= o) incl += up;
+    for (int b0 = 0; b0 < tiles; b0 += 16) {
+        int c[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) c[q] = b0 + q < tiles ? counts[(long long)(b0 + q) * bins + d] : 0;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            if (b0 + q < tiles) counts[(long long)(b0 + q) * bins + d] = carry;
+            carry += c[q];
         }
-        if (b + lane < tiles) row[b + lane] = carry + incl - c;
-        carry += __shfl(incl, 63);
     }
-    if (lane == 0) totals[d] = carry;
+    totals[d] = carry;
 }
 
 // offsets: given with the only pass, where the digits are the keys
@@ -191,8 +258,13 @@ template <typename ID>
 __global__ __launch_bounds__(256) void segments_scatter_kernel(const ID *__restrict__ ids, const int *__restrict__ keys_in,
                                                                const int *__restrict__ pos_in, int n, int num, int shift, int bits, int tiles,
                                                                const int *__restrict__ counts, const int *__restrict__ totals,
-                                                               int *__restrict__ keys_out, int *__restrict__ pos_out, int *__restrict__ offsets)
+                                                               int *__restrict__ keys_out, int *__restrict__ pos_out, int *__restrict__ offsets,
+                                                               const Fill fill)
 {
+    if ((int)blockIdx.x >= tiles) {
+        fill_share(fill, blockIdx.x - tiles, gridDim.x - tiles, 256);
+        return;
+    }
     constexpr int WAVES = 4, ROUNDS = kSegTile / 256;
     __shared__ int counter[WAVES << kSegBits];
     __shared__ int base[1 << kSegBits];
@@ -210,13 +282,32 @@ __global__ __launch_bounds__(256) void segments_scatter_kernel(const ID *__restr
         key[r] = in[r] ? (ids ? seg_key(ids, i, num) : keys_in[i]) : 0;
         rank[r] = 0;
     }
-    // where the digits start: a scan of their totals (as if of one wave), plus this tile's place in each
     __syncthreads();
-    for (int d = t; d < bins; d += 256) counter[d] = totals[d];
+    // where the digits start: a scan of their totals (as if of one wave), plus this tile's place in each
+    for (int d = t; d < bins; d += 256) {
+        int before = 0, total = 0;
+        if (tiles > kScanTiles) {
+            before = counts[(long long)blockIdx.x * bins + d];
+            total = totals[d];
+        } else {
+            for (int b0 = 0; b0 < tiles; b0 += 16) {
+                int c[16];
+#pragma unroll
+                for (int q = 0; q < 16; ++q) c[q] = b0 + q < tiles ? counts[(long long)(b0 + q) * bins + d] : 0;
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    if (b0 + q < (int)blockIdx.x) before += c[q];
+                    total += c[q];
+                }
+            }
+        }
+        counter[d] = total;
+        base[d] = before;
+    }
     scan_counters<WAVES>(counter, bins, bins, tmp);      // (the other waves' counters are zero)
     for (int d = t; d < bins; d += 256) {
         if (offsets && blockIdx.x == 0 && d <= num) offsets[d] = counter[d];
-        base[d] = counter[d] + counts[(long long)d * tiles + blockIdx.x];
+        base[d] += counter[d];
     }
     __syncthreads();
     for (int i = t; i < WAVES * bins; i += 256) counter[i] = 0;
@@ -224,11 +315,13 @@ __global__ __launch_bounds__(256) void segments_scatter_kernel(const ID *__restr
     rank_wave<ROUNDS>(key, in, ROUNDS, shift, bits, counter + wave * bins, rank);
     __syncthreads();
     for (int d = t; d < bins; d += 256) {
-        int sum = base[d];
+        int sum = base[d], c[WAVES];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) c[w] = counter[w * bins + d];
+#pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const int c = counter[w * bins + d];
             counter[w * bins + d] = sum;
-            sum += c;
+            sum += c[w];
         }
     }
     __syncthreads();
@@ -247,12 +340,35 @@ __global__ __launch_bounds__(256) void segments_offsets_kernel(const int *__rest
     if (v <= num) offsets[v] = lower_bound(keys, n, v);
 }
 
-template <typename ID>
-hipError_t sort_positions(const ID *ids, int n, int num, const SegmentScratch &w, int *order, const int **keys, int *offsets, hipStream_t s)
+// Part i of `parts` of the work beside a sort, and the workgroups of `threads` that do it (at most 4 for each CU).
+Fill part_of(const Fill *fill, int i, int parts, int threads, int *wgs)
 {
+    Fill f{};
+    *wgs = 0;
+    if (!fill) return f;
+    f = *fill;
+    const long long per = (f.count / parts + 3) / 4 * 4, from = per * i < f.count ? per * i : f.count;
+    f.count = i == parts - 1 || f.count - from < per ? f.count - from : per;
+    if (f.data) f.data += from;
+    if (i > 0) f.n_decayed = 0;
+    const long long work = (f.data ? f.count / 4 : 0) + f.n_decayed;
+    if (work > 0) *wgs = (int)(work / threads < 1024 * 256 / threads ? work / threads + 1 : 1024 * 256 / threads);
+    return f;
+}
+
+template <typename ID>
+hipError_t sort_positions(const ID *ids, int n, int num, const SegmentScratch &w, int *order, const int **keys, int *offsets,
+                          const Fill *fill, hipStream_t s)
+{
+    int extra;
+    if (w.passes == 1 && n > kSegSmall && n <= kSegOne && !keys && !fill) {
+        segments_one_kernel<ID><<<dim3(1), dim3(1024), 0, s>>>(ids, n, num, w.bits, order, offsets);
+        return hipGetLastError();
+    }
     if (n <= kSegSmall) {
         const bool here = num < 2 * kSegSmall;   // the offsets of more keys are found by more than one workgroup
-        segments_small_kernel<ID><<<dim3(1), dim3(1024), 0, s>>>(ids, n, num, w.passes, w.bits, order, w.keys[0], here ? offsets : nullptr);
+        const Fill f = part_of(fill, 0, 1, 1024, &extra);
+        segments_small_kernel<ID><<<dim3(1 + extra), dim3(1024), 0, s>>>(ids, n, num, w.passes, w.bits, order, w.keys[0], here ? offsets : nullptr, f);
         if (offsets && !here) segments_offsets_kernel<<<dim3(num / 256 + 1), dim3(256), 0, s>>>(w.keys[0], n, num, offsets);
         if (keys) *keys = w.keys[0];
         return hipGetLastError();
@@ -263,10 +379,12 @@ hipError_t sort_positions(const ID *ids, int n, int num, const SegmentScratch &w
         const bool last = p == w.passes - 1;
         const ID *from = p == 0 ? ids : nullptr;
         int *kout = w.keys[p & 1], *pout = last ? order : w.pos[p & 1];
-        segments_count_kernel<ID><<<dim3(tiles), dim3(256), 0, s>>>(from, kin, n, num, p * w.bits, w.bits, tiles, w.counts);
-        segments_scan_kernel<<<dim3((bins + 3) / 4), dim3(256), 0, s>>>(w.counts, tiles, bins, w.totals);
-        segments_scatter_kernel<ID><<<dim3(tiles), dim3(256), 0, s>>>(from, kin, pin, n, num, p * w.bits, w.bits, tiles, w.counts, w.totals,
-                                                                      kout, pout, w.passes == 1 ? offsets : nullptr);
+        Fill f = part_of(fill, 2 * p, 2 * w.passes, 256, &extra);
+        segments_count_kernel<ID><<<dim3(tiles + extra), dim3(256), 0, s>>>(from, kin, n, num, p * w.bits, w.bits, tiles, w.counts, f);
+        if (tiles > kScanTiles) segments_scan_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, s>>>(w.counts, tiles, bins, w.totals);
+        f = part_of(fill, 2 * p + 1, 2 * w.passes, 256, &extra);
+        segments_scatter_kernel<ID><<<dim3(tiles + extra), dim3(256), 0, s>>>(from, kin, pin, n, num, p * w.bits, w.bits, tiles, w.counts, w.totals,
+                                                                              kout, pout, w.passes == 1 ? offsets : nullptr, f);
         kin = kout;
         pin = pout;
     }
@@ -305,10 +423,18 @@ size_t segment_scratch(char *base, int n, int num, SegmentScratch *out)
 }
 
 hipError_t launch_segments(const void *ids, int id_bits, int n, int num, const SegmentScratch &w, int *order, const int **keys,
-                           int *offsets, hipStream_t s)
+                           int *offsets, const Fill *fill, hipStream_t s)
 {
-    return id_bits == 64 ? sort_positions((const long long *)ids, n, num, w, order, keys, offsets, s)
-                         : sort_positions((const int *)ids, n, num, w, order, keys, offsets, s);
+    return id_bits == 64 ? sort_positions((const long long *)ids, n, num, w, order, keys, offsets, fill, s)
+                         : sort_positions((const int *)ids, n, num, w, order, keys, offsets, fill, s);
+}
+
+hipError_t launch_fill(const Fill &fill, hipStream_t s)
+{
+    int wgs;
+    const Fill f = part_of(&fill, 0, 1, 1024, &wgs);
+    if (wgs > 0) fill_kernel<<<dim3(wgs), dim3(1024), 0, s>>>(f);
+    return hipGetLastError();
 }
 
 }  // namespace kfac

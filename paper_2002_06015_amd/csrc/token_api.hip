@@ -97,7 +97,7 @@ kfac_status kfac_segments(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_
     SegmentScratch w;
     if (segment_scratch(c.ws, n, num, &w) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
     return timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, (double)in.size + o.size + f.size,
-                 [&] { return launch_segments(ids, id_bits, n, num, w, order, nullptr, offsets, c.stream); }) ? KFAC_OK : KFAC_ERR_DEVICE;
+                 [&] { return launch_segments(ids, id_bits, n, num, w, order, nullptr, offsets, nullptr, c.stream); }) ? KFAC_OK : KFAC_ERR_DEVICE;
 }
 
 kfac_status kfac_embedding(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_bits, int32_t vocab, int32_t dim, kfac_dtype table_type,
@@ -142,20 +142,22 @@ kfac_status kfac_embedding_grad(kfac_ctx *ctx, int32_t n, const void *ids, int32
     a.n = n; a.vocab = vocab; a.dim = dim;
     a.g = grad_out; a.ld = ld_grad; a.bf16 = type == KFAC_BF16;
     a.accumulate = accumulate != 0;
-    a.scale = scale; a.decay = decay; a.share = n > 0 ? (1.f - decay) / (float)n : 0.f;
-    a.dW = dW; a.A = n > 0 ? A_diag : nullptr;   // no positions: no mean to add
+    a.scale = scale; a.share = n > 0 ? (1.f - decay) / (float)n : 0.f;
+    a.dW = dW; a.A = A_diag;
     a.chunk = embedding_chunk(n);
-    const double moved = (double)n * dim * esize(type) + 4.0 * vocab * dim;
-    bool ok = true;
+    Fill fill{};
+    if (!accumulate) { fill.data = dW; fill.count = (long long)vocab * dim; }
+    if (A_diag && n > 0) { fill.decayed = A_diag; fill.n_decayed = vocab; fill.decay = decay; }   // no positions: no mean to add
+    const double moved = (double)n * dim * esize(type), written = 4.0 * vocab * dim;
+    bool ok;
     if (n > 0) {
         const int *keys = nullptr;
-        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, 2.0 * in.size, [&] { return launch_segments(ids, id_bits, n, vocab, seg, pos, &keys, nullptr, c.stream); });
+        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, 2.0 * in.size + written, [&] { return launch_segments(ids, id_bits, n, vocab, seg, pos, &keys, nullptr, &fill, c.stream); });
         a.keys = keys;
-    }
-    ok = ok && timed(ctx, KFAC_K_EMBEDDING, 1, 0, 0.0, 0.0, [&] { return launch_embedding_absent(a, c.stream); });
-    if (n > 0) {
-        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 2, 0, (double)n * dim, moved, [&] { return launch_embedding_sum(a, c.stream); });
-        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 3, 0, 0.0, 0.0, [&] { return launch_embedding_join(a, c.stream); });
+        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 1, 0, (double)n * dim, moved, [&] { return launch_embedding_sum(a, c.stream); });
+        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 2, 0, 0.0, 0.0, [&] { return launch_embedding_join(a, c.stream); });
+    } else {
+        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, written, [&] { return launch_fill(fill, c.stream); });
     }
     return ok ? KFAC_OK : KFAC_ERR_DEVICE;
 }

@@ -22,9 +22,9 @@ bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, doubl
 bool profile_end(kfac_ctx *ctx);
 
 // ---- segments: a stable sort of positions by a small key ----------------------------------------------
-// One workgroup sorts up to kSegSmall positions in LDS; more go through passes of a counting sort over tiles of
-// kSegTile positions, kSegBits bits of the key a pass at most.
-constexpr int kSegSmall = 8192, kSegTile = 2048, kSegBits = 9;
+// One workgroup sorts up to kSegSmall positions in LDS, or up to kSegOne by a key of one digit; more go through passes of a counting
+// sort over tiles of kSegTile positions, kSegBits bits of the key a pass at most.
+constexpr int kSegSmall = 8192, kSegOne = 32768, kSegTile = 2048, kSegBits = 9;
 struct SegmentScratch {
     int *keys[2], *pos[2];   // [n] each: sorted keys and positions; pos[1] is not needed for n <= kSegSmall
     int *counts, *totals;    // [tiles << bits], [1 << bits]
@@ -32,9 +32,19 @@ struct SegmentScratch {
 };
 // Carves the scratch from `base` (nullptr: only counts); returns the bytes.
 size_t segment_scratch(char *base, int n, int num, SegmentScratch *out);
-// order: dev [n]; keys: the sorted keys end up there; offsets: dev [num + 1] or nullptr
+// Work that shares the sort's launches: data[0 .. count) <- 0 (unless nullptr), decayed[0 .. n_decayed) *= decay (without reading
+// it for 0).  The sort keeps few CUs busy; the rest writes meanwhile.
+struct Fill {
+    float *data;
+    long long count;
+    float *decayed;
+    int n_decayed;
+    float decay;
+};
+// order: dev [n]; keys: the sorted keys end up there; offsets: dev [num + 1] or nullptr; fill: or nullptr
 hipError_t launch_segments(const void *ids, int id_bits, int n, int num, const SegmentScratch &w, int *order, const int **keys,
-                           int *offsets, hipStream_t s);
+                           int *offsets, const Fill *fill, hipStream_t s);
+hipError_t launch_fill(const Fill &fill, hipStream_t s);
 
 // ---- embedding -----------------------------------------------------------------------------------------
 hipError_t launch_embedding(const void *ids, int id_bits, int n, int vocab, int dim, int table_bf16, const void *table, long long ldt,
@@ -45,13 +55,12 @@ struct EmbeddingGrad {
     const void *g;
     long long ld;
     int bf16, accumulate;
-    float scale, decay, share;   // share: (1 - decay) / n
-    float *dW, *A;           // A may be nullptr
+    float scale, share;      // share: (1 - decay) / n
+    float *dW, *A;           // rows of zeros unless accumulate; decayed already, or nullptr
     float *partial;          // [2 * chunks][dim]
     int chunk;               // sorted positions that one wave adds up
 };
 int embedding_chunk(int n);
-hipError_t launch_embedding_absent(const EmbeddingGrad &a, hipStream_t s);
 hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s);
 hipError_t launch_embedding_join(const EmbeddingGrad &a, hipStream_t s);
 

@@ -586,7 +586,7 @@ def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
     if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (rows, cols):
         raise ValueError("%s must be a device tensor of %s and shape [%d, %d], got %s %s" % (what, dtype, rows, cols, t.dtype, tuple(t.shape)))
     s = t.stride()
-    if (cols > 1 and s[1] != 1) or (rows > 1 and s[0] < cols):
+    if rows > 0 and ((cols > 1 and s[1] != 1) or (rows > 1 and s[0] < cols)):
         raise ValueError("%s must have contiguous rows" % what)
     return s[0] if rows > 1 else cols
 

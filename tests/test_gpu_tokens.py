@@ -251,3 +251,49 @@ def test_dropout_beyond_32_bit_elements():
     last = x[rows - 1].float().cpu().numpy() != 0
     assert np.array_equal(last, T.dropout_keep((rows - 1) * cols, cols, 0.5, 11, 0))
     ctx.close()
+
+
+@pytest.mark.parametrize("n,num", [(32768, 31), (32769, 31), (32768, 300), (600000, 20), (600000, 70000), (2 ** 21 + 5, 100000)])
+def test_segments_of_many_positions(n, num):
+    """One workgroup and many tiles, on both sides of the rules that choose between them."""
+    ids = np.random.default_rng(n).integers(-1, num, n)
+    order, offsets = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(num + 1, dtype=torch.int32, device="cuda")
+    ctx = _ctx(kfac.kfac_segments_workspace_bytes(n, num))
+    kfac.kfac_segments(ctx, torch.from_numpy(ids).cuda(), num, order, offsets)
+    ref_order, ref_offsets = T.segments(ids, num)
+    assert np.array_equal(order.cpu().numpy(), ref_order) and np.array_equal(offsets.cpu().numpy(), ref_offsets)
+    ctx.close()
+
+
+def test_embedding_grad_of_unaligned_tables():
+    """dW and A_diag that start at any element: the zeros are written around the aligned pieces."""
+    rng = np.random.default_rng(8)
+    for shift in range(4):
+        for n, vocab, dim in ((40, 300, 7), (9000, 500, 3), (0, 5, 3), (1, 1, 1)):
+            ids = rng.integers(0, vocab, n)
+            g = torch.from_numpy(rng.standard_normal((n, dim))).float().cuda()
+            buf, abuf = torch.full((vocab * dim + 8,), 9.0, device="cuda"), torch.full((vocab + 8,), 9.0, device="cuda")
+            dW, A = buf[shift:shift + vocab * dim].view(vocab, dim), abuf[shift:shift + vocab]
+            ctx = _ctx(kfac.kfac_embedding_workspace_bytes(n, vocab, dim))
+            kfac.kfac_embedding_grad(ctx, torch.from_numpy(ids).cuda(), g, 1.0, dW, False, A, 0.0)
+            ref, counts, mag = T.embedding_grad(ids, _values(g), 1.0, vocab)
+            assert np.all(np.abs(_values(dW) - ref) <= (counts[:, None] + 4) * 2.0 ** -24 * mag)
+            assert n == 0 or np.allclose(_values(A), counts / n, rtol=8 * 2.0 ** -24, atol=0)
+            for b, size in ((buf, vocab * dim), (abuf, vocab)):
+                assert bool((b[:shift] == 9.0).all()) and bool((b[shift + size:] == 9.0).all())
+            ctx.close()
+
+
+@pytest.mark.parametrize("n,share", [(3000, 0.5), (20000, 0.3), (70000, 0.9)])
+def test_embedding_grad_of_one_frequent_token(n, share):
+    """A token of more parts than one wave adds up, between others, at places that are no whole runs."""
+    rng = np.random.default_rng(n)
+    vocab, dim = 900, 300
+    ids = np.where(rng.random(n) < share, 450, rng.integers(-1, vocab, n))
+    g = torch.from_numpy(rng.standard_normal((n, dim))).to(BF16).cuda()
+    dW = torch.empty(vocab, dim, device="cuda")
+    ctx = _ctx(kfac.kfac_embedding_workspace_bytes(n, vocab, dim))
+    kfac.kfac_embedding_grad(ctx, torch.from_numpy(ids).int().cuda(), g, 1.0, dW)
+    ref, counts, mag = T.embedding_grad(ids, _values(g), 1.0, vocab)
+    assert np.all(np.abs(_values(dW) - ref) <= (counts[:, None] + 4) * 2.0 ** -24 * mag)
+    ctx.close()
