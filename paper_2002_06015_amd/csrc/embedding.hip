@@ -23,13 +23,13 @@ __device__ __forceinline__ float from_bf16(bf16_t v) { return __uint_as_float((u
 // to nearest, ties to even; NaN stays NaN
 __device__ __forceinline__ bf16_t to_bf16(float v) { return __builtin_bit_cast(bf16_t, (__bf16)v); }
 
-// W adjacent elements as floats (W = 8: bf16, 4: float), the first `c` of them
-template <typename T, int W>
+// W adjacent elements as floats (W = 8: bf16, 4: float), the first `c` of them; ONCE: nobody reads them again
+template <typename T, int W, bool ONCE = false>
 __device__ __forceinline__ void load_piece(const T *__restrict__ p, int c, float (&v)[W])
 {
     if (c >= W) {
         if constexpr (sizeof(T) == 2 && W == 8) {
-            const u16x8_u r = *(const u16x8_u *)p;
+            const u16x8_u r = ONCE ? __builtin_nontemporal_load((const u16x8_u *)p) : *(const u16x8_u *)p;
 #pragma unroll
             for (int j = 0; j < W; ++j) v[j] = from_bf16(r[j]);
         } else if constexpr (sizeof(T) == 2) {
@@ -39,7 +39,8 @@ __device__ __forceinline__ void load_piece(const T *__restrict__ p, int c, float
         } else {
 #pragma unroll
             for (int q = 0; q < W / 4; ++q) {
-                const f32x4_u r = *(const f32x4_u *)((const float *)p + 4 * q);
+                const f32x4_u *at = (const f32x4_u *)((const float *)p + 4 * q);
+                const f32x4_u r = ONCE ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[4 * q + j] = r[j];
             }
@@ -111,16 +112,6 @@ __global__ __launch_bounds__(256) void embedding_kernel(const ID *__restrict__ i
     }
 }
 
-__device__ __forceinline__ int find_key(const int *__restrict__ keys, int n, int key)   // the first position with keys[i] >= key
-{
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = lo + ((hi - lo) >> 1);
-        if (keys[mid] < key) lo = mid + 1; else hi = mid;
-    }
-    return lo;
-}
-
 template <int W>
 __device__ __forceinline__ void write_row(const EmbeddingGrad &a, int key, int count, int c0, const float (&sum)[W])
 {
@@ -171,7 +162,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingGrad 
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int p = __builtin_amdgcn_readlane(my_pos, min(r0 + u, cnt - 1));
-            if (c0 < a.dim) load_piece<T, W>(g + (long long)p * a.ld + c0, a.dim - c0, v[u]);
+            if (c0 < a.dim) load_piece<T, W, true>(g + (long long)p * a.ld + c0, a.dim - c0, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
@@ -198,14 +189,28 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
     __shared__ int is_long[kJoinWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c0 = (blockIdx.y * 64 + lane) * 4;
-    // parts of the token that goes on behind run c and starts in it; 0: there is none
-    auto look = [&](int c, int &key) {
+    // Parts of the token that goes on behind run c and starts in it (0: there is none), and its positions.  The lanes look at the ends of
+    // 64 runs at a time: a search through all keys would be a chain of a dozen loads.
+    auto look = [&](int c, int &key, int &count) {
         if (c >= chunks) return 0;
-        const int last = min((c + 1) * a.chunk, a.n) - 1;
+        const int first = c * a.chunk, last = min(first + a.chunk, a.n) - 1;
         key = a.keys[last];
-        if (key >= a.vocab || last + 1 >= a.n || a.keys[last + 1] != key) return 0;
-        if (c > 0 && a.keys[c * a.chunk] == key && a.keys[c * a.chunk - 1] == key) return 0;
-        return (find_key(a.keys, a.n, key + 1) - 1) / a.chunk - c + 1;
+        const int mine = a.keys[min(first + lane, last)], next = a.keys[min(last + 1, a.n - 1)], before = a.keys[max(first - 1, 0)];
+        if (key >= a.vocab || last + 1 >= a.n || next != key) return 0;
+        const int here = __popcll(__ballot(first + lane <= last && mine == key));
+        if (here == last + 1 - first && c > 0 && before == key) return 0;                     // it came from before
+        int parts = 1;   // runs that the token fills to their end
+        for (;;) {
+            const int end = (c + parts + lane + 1) * a.chunk - 1;
+            const unsigned long long through = __ballot(end < a.n && a.keys[min(end, a.n - 1)] == key);
+            if (through == ~0ULL) { parts += 64; continue; }
+            parts += __ffsll(~through) - 1;
+            break;
+        }
+        const int tail = (c + parts) * a.chunk;
+        const int there = __popcll(__ballot(lane < a.chunk && tail + lane < a.n && a.keys[min(tail + lane, a.n - 1)] == key));
+        count = here + (parts - 1) * a.chunk + there;
+        return there > 0 ? parts + 1 : parts;
     };
     auto add = [&](int c, int p0, int p1, float (&sum)[4]) {
 #pragma unroll
@@ -220,21 +225,21 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
             }
         }
     };
-    auto write = [&](int key, const float (&sum)[4]) {
-        if (c0 < a.dim) write_row<4>(a, key, find_key(a.keys, a.n, key + 1) - find_key(a.keys, a.n, key), c0, sum);
+    auto write = [&](int key, int count, const float (&sum)[4]) {
+        if (c0 < a.dim) write_row<4>(a, key, count, c0, sum);
     };
-    int key = 0;
+    int key = 0, count = 0;
     float sum[4];
-    const int mine = blockIdx.x * kJoinWaves + wave, parts = look(mine, key);
+    const int mine = blockIdx.x * kJoinWaves + wave, parts = look(mine, key, count);
     if (lane == 0) is_long[wave] = parts > kLongParts;
     if (parts > 0 && parts <= kLongParts) {
         add(mine, 0, parts, sum);
-        write(key, sum);
+        write(key, count, sum);
     }
     __syncthreads();
     for (int w = 0; w < kJoinWaves; ++w) {
         if (!is_long[w]) continue;
-        const int c = blockIdx.x * kJoinWaves + w, all = look(c, key), per = (all + kJoinWaves - 1) / kJoinWaves;
+        const int c = blockIdx.x * kJoinWaves + w, all = look(c, key, count), per = (all + kJoinWaves - 1) / kJoinWaves;
         add(c, min(wave * per, all), min(wave * per + per, all), sum);
 #pragma unroll
         for (int j = 0; j < 4; ++j) part[wave][lane][j] = sum[j];
@@ -243,7 +248,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
             for (int q = 1; q < kJoinWaves; ++q)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum[j] += part[q][lane][j];
-            write(key, sum);
+            write(key, count, sum);
         }
         __syncthreads();
     }

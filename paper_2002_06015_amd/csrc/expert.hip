@@ -576,13 +576,17 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
 constexpr int kPlaces = 5;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
+// Which pairs of chunks of line m change places, so that the lanes of a transposing read meet different banks.
+template <int ROWS>
+__device__ __forceinline__ int swap_pairs(int m) { return ROWS == 64 ? m & 2 : (m & 3) << 1; }
+
 // The 32 rows from `row0` (a multiple of 32) of a half, k = 16 u + 8 (lane / 32) .. + 7: lane -> row lane % 32.
 template <bool ACROSS, int ROWS>
 __device__ __forceinline__ bf16x8 fragment32(const bf16_t *tile, int row0, int u, int lane)
 {
     if constexpr (ACROSS) {
         const int m = 16 * u + 8 * (lane >> 5) + ((lane & 15) >> 2), pair = (row0 >> 4) + ((lane >> 4) & 1);
-        const bf16_t *p = tile + m * ROWS + 16 * (pair ^ ((m & 3) << 1)) + 4 * (lane & 3);
+        const bf16_t *p = tile + m * ROWS + 16 * (pair ^ swap_pairs<ROWS>(m)) + 4 * (lane & 3);
         const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)p);
         const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_ptr)(p + 4 * ROWS));   // k + 4: same permutation
         return __builtin_bit_cast(bf16x8, shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
@@ -634,7 +638,7 @@ struct Direct {
         for (int i = 0; i < CH; ++i) {
             const int q = tid + THREADS * i, line = q / PER, phys = q % PER;
             if constexpr (ACROSS) {
-                const int pos = (((phys >> 1) ^ ((line & 3) << 1)) << 1) | (phys & 1);
+                const int pos = (((phys >> 1) ^ swap_pairs<ROWS>(line)) << 1) | (phys & 1);
                 off[i] = 2u * (unsigned)min(row0 + 8 * pos, rows - 8) + (GATHER == 0 ? (unsigned)line * ld : 0u);
             } else {
                 int r = min(row0 + line, rows - 1);
@@ -921,6 +925,9 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t
     if (bf16 && direct_ok(op, a)) {
         // 256 x 256 tiles need half the traffic, but one of them fills a CU: only where there is one for each of 256
         if (count_tiles<256, 256>(op, a, tj) >= 256) return run_direct<256, 256, 4, 2>(op, a, s);
+        // few rows an expert: 64 x 64, more of them in flight (a decoding step of 8 choices 1024 -> 4096: 14 us, 17 with 128 x 128; 2048
+        // rows 1024 -> 1024 of 8 experts: 13 and 17; 4096 of 16: 21 and 19).  Gradients of weights have as many tiles whatever the rows.
+        if ((op == EXPERT_FORWARD || op == EXPERT_GRAD_INPUT) && count_tiles<128, 128>(op, a, tj) <= 320) return run_direct<64, 64, 2, 2>(op, a, s);
         return run_direct<128, 128, 2, 2>(op, a, s);
     }
     // 128 x 128 tiles where there are two for each CU; the smaller ones finish a step in a third of the time

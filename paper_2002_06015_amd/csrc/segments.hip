@@ -4,7 +4,7 @@
 // A counting sort over digits of up to 9 bits, lowest digit first.  The rank of an element among the equal digits of its wave
 // comes from ballots (one a bit: the lanes with the same digit), the count before the wave from LDS, so nothing depends on the
 // order in which atomics arrive.  Up to 8192 positions are sorted by one workgroup whose keys stay in registers and LDS
-// (one launch, bound by the latency of its chain: ballots, an LDS counter, a scan), up to 32768 if the key is one digit.  More take
+// (one launch, bound by the instructions of its ballots on one CU: 16384 positions would take longer than in tiles).  More take
 // two launches a digit: counts of 2048-position tiles, then ranks and scatter, where every tile adds up the counts of those before
 // it (beyond 256 tiles a launch between them does).  Reads and writes 16 bytes a position and digit.
 #include "token_internal.h"
@@ -21,15 +21,22 @@ __device__ __forceinline__ int seg_key(const ID *ids, int i, int num)
     return v >= 0 && v < (ID)num ? (int)v : num;
 }
 
+typedef volatile __attribute__((address_space(3))) int *lds_counter;
+
 // Rank of this lane's digit among equal digits of the lanes before it, and their number; `active`: lanes with an element.
 __device__ __forceinline__ int match_digit(int digit, int bits, bool active, int &count)
 {
-    unsigned long long same = __ballot(active);
-    for (int b = 0; b < bits; ++b) {
-        const bool bit = (digit >> b) & 1;
-        const unsigned long long with = __ballot(bit);
-        same &= bit ? with : ~with;
+    const unsigned long long in = __ballot(active);
+    unsigned lo = (unsigned)in, hi = (unsigned)(in >> 32);
+#pragma unroll
+    for (int b = 0; b < kSegBits; ++b) {
+        if (b >= bits) break;
+        const int mine = (int)((unsigned)digit << (31 - b)) >> 31;   // all ones where the bit is set
+        const unsigned long long with = __ballot(mine != 0);
+        lo &= ~((unsigned)with ^ (unsigned)mine);
+        hi &= ~((unsigned)(with >> 32) ^ (unsigned)mine);
     }
+    const unsigned long long same = (unsigned long long)hi << 32 | lo;
     count = __popcll(same);
     return __popcll(same & ((1ULL << (threadIdx.x & 63)) - 1));
 }
@@ -37,7 +44,7 @@ __device__ __forceinline__ int match_digit(int digit, int bits, bool active, int
 // Ranks of up to ROUNDS x 64 elements of a wave, 64 at a time in order, against counters of the wave in LDS
 template <int ROUNDS>
 __device__ __forceinline__ void rank_wave(const int (&key)[ROUNDS], const bool (&in)[ROUNDS], int rounds, int shift, int bits,
-                                          volatile int *counter, int (&rank)[ROUNDS])
+                                          lds_counter counter, int (&rank)[ROUNDS])
 {
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
@@ -49,6 +56,21 @@ __device__ __forceinline__ void rank_wave(const int (&key)[ROUNDS], const bool (
         __builtin_amdgcn_wave_barrier();   // all lanes have read before the first one of each digit counts them
         rank[r] = old + before;
         if (in[r] && before == 0) counter[digit] = old + count;
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// The counts alone: no two lanes add to the same counter at once.
+template <int ROUNDS>
+__device__ __forceinline__ void count_wave(const int (&key)[ROUNDS], const bool (&in)[ROUNDS], int rounds, int shift, int bits, lds_counter counter)
+{
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        if (r >= rounds) break;
+        const int digit = (key[r] >> shift) & ((1 << bits) - 1);
+        int count;
+        const int before = match_digit(digit, bits, in[r], count);
+        if (in[r] && before == 0) counter[digit] += count;
         __builtin_amdgcn_wave_barrier();
     }
 }
@@ -148,7 +170,7 @@ __global__ __launch_bounds__(1024) void segments_small_kernel(const ID *__restri
     for (int p = 0; p < passes; ++p) {
         for (int i = t; i < WAVES * bins; i += 1024) counter[i] = 0;
         __syncthreads();
-        rank_wave<ROUNDS>(key, in, rounds, p * bits, bits, counter + wave * bins, rank);
+        rank_wave<ROUNDS>(key, in, rounds, p * bits, bits, (lds_counter)(counter + wave * bins), rank);
         scan_counters<WAVES>(counter, bins, bins, tmp);
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r)
@@ -175,41 +197,6 @@ __global__ __launch_bounds__(1024) void segments_small_kernel(const ID *__restri
         for (int v = t; v <= num; v += 1024) offsets[v] = lower_bound(skey, n, v);
 }
 
-// One workgroup, keys of one digit: counts, then ranks.
-template <typename ID>
-__global__ __launch_bounds__(1024) void segments_one_kernel(const ID *__restrict__ ids, int n, int num, int bits, int *__restrict__ order,
-                                                            int *__restrict__ offsets)
-{
-    constexpr int WAVES = 16, ROUNDS = 8;
-    __shared__ int counter[WAVES << kSegBits];
-    __shared__ int tmp[WAVES];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, bins = 1 << bits;
-    const int per_wave = (n + 64 * WAVES - 1) / (64 * WAVES) * 64, i0 = wave * per_wave, i1 = min(i0 + per_wave, n);
-    for (int i = t; i < WAVES * bins; i += 1024) counter[i] = 0;
-    __syncthreads();
-#pragma unroll 8
-    for (int i = i0 + lane; i < i1; i += 64) atomicAdd(&counter[wave * bins + seg_key(ids, i, num)], 1);
-    scan_counters<WAVES>(counter, bins, bins, tmp);
-    if (offsets)
-        for (int v = t; v <= num; v += 1024) offsets[v] = counter[v];   // (where the first wave's start)
-    __syncthreads();
-    for (int b0 = i0; b0 < i1; b0 += 64 * ROUNDS) {
-        int key[ROUNDS], rank[ROUNDS];
-        bool in[ROUNDS];
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const int i = b0 + 64 * r + lane;
-            in[r] = i < i1;
-            key[r] = in[r] ? seg_key(ids, i, num) : 0;
-            rank[r] = 0;
-        }
-        rank_wave<ROUNDS>(key, in, min(ROUNDS, (i1 - b0 + 63) / 64), 0, bits, counter + wave * bins, rank);   // (the counters hold the places)
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r)
-            if (in[r]) order[rank[r]] = b0 + 64 * r + lane;
-    }
-}
-
 // counts: [tiles][bins]
 template <typename ID>
 __global__ __launch_bounds__(256) void segments_count_kernel(const ID *__restrict__ ids, const int *__restrict__ keys, int n, int num, int shift,
@@ -219,18 +206,27 @@ __global__ __launch_bounds__(256) void segments_count_kernel(const ID *__restric
         fill_share(fill, blockIdx.x - tiles, gridDim.x - tiles, 256);
         return;
     }
-    __shared__ int bin[1 << kSegBits];
-    const int bins = 1 << bits, t = threadIdx.x;
-    for (int d = t; d < bins; d += 256) bin[d] = 0;
-    __syncthreads();
-    const int i0 = blockIdx.x * kSegTile;
+    constexpr int WAVES = 4, ROUNDS = kSegTile / 256;
+    __shared__ int counter[WAVES << kSegBits];
+    const int bins = 1 << bits, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    for (int i = t; i < WAVES * bins; i += 256) counter[i] = 0;
+    int key[ROUNDS];
+    bool in[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kSegTile / 256; ++r) {
-        const int i = i0 + t + 256 * r;
-        if (i < n) atomicAdd(&bin[((ids ? seg_key(ids, i, num) : keys[i]) >> shift) & (bins - 1)], 1);
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int i = blockIdx.x * kSegTile + wave * 64 * ROUNDS + 64 * r + lane;
+        in[r] = i < n;
+        key[r] = in[r] ? (ids ? seg_key(ids, i, num) : keys[i]) : 0;
     }
     __syncthreads();
-    for (int d = t; d < bins; d += 256) counts[(long long)blockIdx.x * bins + d] = bin[d];
+    count_wave<ROUNDS>(key, in, ROUNDS, shift, bits, (lds_counter)(counter + wave * bins));
+    __syncthreads();
+    for (int d = t; d < bins; d += 256) {
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += counter[w * bins + d];
+        counts[(long long)blockIdx.x * bins + d] = sum;
+    }
 }
 
 // running sums along the tiles, and the digits' totals
@@ -284,25 +280,26 @@ __global__ __launch_bounds__(256) void segments_scatter_kernel(const ID *__restr
     }
     __syncthreads();
     // where the digits start: a scan of their totals (as if of one wave), plus this tile's place in each
-    for (int d = t; d < bins; d += 256) {
-        int before = 0, total = 0;
-        if (tiles > kScanTiles) {
-            before = counts[(long long)blockIdx.x * bins + d];
-            total = totals[d];
-        } else {
-            for (int b0 = 0; b0 < tiles; b0 += 16) {
-                int c[16];
+    if (tiles > kScanTiles) {
+        for (int d = t; d < bins; d += 256) {
+            counter[d] = totals[d];
+            base[d] = counts[(long long)blockIdx.x * bins + d];
+        }
+    } else if (2 * t < bins) {   // two digits a thread
+        int before[2] = {0, 0}, total[2] = {0, 0};
+        constexpr int AHEAD = 32;
+        for (int b0 = 0; b0 < tiles; b0 += AHEAD) {
+            int2 c[AHEAD];
 #pragma unroll
-                for (int q = 0; q < 16; ++q) c[q] = b0 + q < tiles ? counts[(long long)(b0 + q) * bins + d] : 0;
+            for (int q = 0; q < AHEAD; ++q) c[q] = *(const int2 *)(counts + (long long)min(b0 + q, tiles - 1) * bins + 2 * t);
 #pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    if (b0 + q < (int)blockIdx.x) before += c[q];
-                    total += c[q];
-                }
+            for (int q = 0; q < AHEAD; ++q) {
+                if (b0 + q < (int)blockIdx.x) { before[0] += c[q].x; before[1] += c[q].y; }
+                if (b0 + q < tiles) { total[0] += c[q].x; total[1] += c[q].y; }
             }
         }
-        counter[d] = total;
-        base[d] = before;
+        counter[2 * t] = total[0]; counter[2 * t + 1] = total[1];
+        base[2 * t] = before[0]; base[2 * t + 1] = before[1];
     }
     scan_counters<WAVES>(counter, bins, bins, tmp);      // (the other waves' counters are zero)
     for (int d = t; d < bins; d += 256) {
@@ -312,7 +309,7 @@ __global__ __launch_bounds__(256) void segments_scatter_kernel(const ID *__restr
     __syncthreads();
     for (int i = t; i < WAVES * bins; i += 256) counter[i] = 0;
     __syncthreads();
-    rank_wave<ROUNDS>(key, in, ROUNDS, shift, bits, counter + wave * bins, rank);
+    rank_wave<ROUNDS>(key, in, ROUNDS, shift, bits, (lds_counter)(counter + wave * bins), rank);
     __syncthreads();
     for (int d = t; d < bins; d += 256) {
         int sum = base[d], c[WAVES];
@@ -361,10 +358,6 @@ hipError_t sort_positions(const ID *ids, int n, int num, const SegmentScratch &w
                           const Fill *fill, hipStream_t s)
 {
     int extra;
-    if (w.passes == 1 && n > kSegSmall && n <= kSegOne && !keys && !fill) {
-        segments_one_kernel<ID><<<dim3(1), dim3(1024), 0, s>>>(ids, n, num, w.bits, order, offsets);
-        return hipGetLastError();
-    }
     if (n <= kSegSmall) {
         const bool here = num < 2 * kSegSmall;   // the offsets of more keys are found by more than one workgroup
         const Fill f = part_of(fill, 0, 1, 1024, &extra);
@@ -400,6 +393,7 @@ size_t segment_scratch(char *base, int n, int num, SegmentScratch *out)
     int bits = 0;
     while (bits < 31 && ((unsigned)num >> bits)) ++bits;   // keys are 0 .. num
     SegmentScratch w{};
+    if (bits < 1) bits = 1;
     w.passes = (bits + kSegBits - 1) / kSegBits;
     w.bits = (bits + w.passes - 1) / w.passes;
     size_t used = 0;

@@ -22,9 +22,9 @@ bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, doubl
 bool profile_end(kfac_ctx *ctx);
 
 // ---- segments: a stable sort of positions by a small key ----------------------------------------------
-// One workgroup sorts up to kSegSmall positions in LDS, or up to kSegOne by a key of one digit; more go through passes of a counting
-// sort over tiles of kSegTile positions, kSegBits bits of the key a pass at most.
-constexpr int kSegSmall = 8192, kSegOne = 32768, kSegTile = 2048, kSegBits = 9;
+// One workgroup sorts up to kSegSmall positions in LDS; more go through passes of a counting sort over tiles of kSegTile positions,
+// kSegBits bits of the key a pass at most.
+constexpr int kSegSmall = 8192, kSegTile = 2048, kSegBits = 9;
 struct SegmentScratch {
     int *keys[2], *pos[2];   // [n] each: sorted keys and positions; pos[1] is not needed for n <= kSegSmall
     int *counts, *totals;    // [tiles << bits], [1 << bits]
