@@ -299,3 +299,98 @@ def test_experts_under_the_natural_gradient():
         assert np.abs(_values(U[e]) - ref).max() <= 1e-3 * np.abs(ref).max()
     ctx.close()
     c.ctx.close()
+
+
+@pytest.mark.parametrize("ci,co,bias,dtype", [(1032, 1032, 0, BF16), (1032, 1040, 1, BF16), (1033, 1030, 0, BF16), (1033, 1030, 1, F32)])
+def test_many_tiles(ci, co, bias, dtype):
+    """Enough rows and columns for the largest tiles; ragged segments, choices that no expert takes, gathered rows two to a token."""
+    tokens, fan, E = 5000, 2, 16
+    c = Case(tokens, fan, E, ci, co, bias, dtype, "drop", 0, seed=2)
+    n = c.n
+    choice = torch.from_numpy(c.choice).cuda()
+    y, dx, dW = c.out(co, 0), torch.full((n, ci), 5.0, dtype=dtype, device="cuda"), torch.full((E, co, ci + bias), 5.0, device="cuda")
+    A, G = torch.full((E, ci + bias, ci + bias), 1.0, device="cuda"), torch.full((E, co, co), 1.0, device="cuda")
+    kfac.kfac_expert_forward(c.ctx, c.layer, c.order, c.offsets, c.x, c.W, y, fan=fan)
+    kfac.kfac_expert_grad_input(c.ctx, c.layer, c.order, c.offsets, c.dy, c.W, dx)
+    kfac.kfac_expert_grad_weight(c.ctx, c.layer, c.order, c.offsets, c.x, c.dy, dW, fan=fan)
+    kfac.kfac_stats_expert(c.ctx, c.layer, c.order, c.offsets, c.x, c.dy, 0.5, A, G, fan=fan)
+    torch.cuda.synchronize()
+    assert c.untouched(co)
+
+    def check(got, ref, mag, m, out, what):
+        bound = (m + 8) * 2.0 ** -24 * mag + (2.0 ** -8 * ref.abs() if out == BF16 else 0.0) + 1e-40
+        bad = ~((got.double() - ref).abs() <= bound)
+        assert not bool(bad.any()), "%s: %d values" % (what, int(bad.sum()))
+
+    free = (choice < 0) | (choice >= E)
+    assert not bool(y[free].any()) and not bool(dx[free].any()) and bool(free.any())
+    for e in range(E):
+        mine = torch.nonzero(choice == e).reshape(-1)
+        m = mine.numel()
+        x, d, W = c.x[mine // fan].double(), c.dy[mine].double(), c.W[e, :, :ci].double()
+        b = c.W[e, :, ci].double() if bias else torch.zeros(co, dtype=torch.float64, device="cuda")
+        check(y[mine], x @ W.T + b, x.abs() @ W.abs().T + b.abs(), ci + 1, dtype, "y")
+        check(dx[mine], d @ W, d.abs() @ W.abs(), co, dtype, "dx")
+        if bias:
+            x = torch.cat([x, torch.ones(m, 1, dtype=torch.float64, device="cuda")], 1)
+        check(dW[e], d.T @ x, d.abs().T @ x.abs(), m, F32, "dW")
+        check(A[e], 0.5 + 0.5 * (x.T @ x) / m, 0.5 + 0.5 * (x.abs().T @ x.abs()) / m, m, F32, "A")
+        check(G[e], 0.5 + 0.5 * (d.T @ d) / m, 0.5 + 0.5 * (d.abs().T @ d.abs()) / m, m, F32, "G")
+    assert torch.equal(A, A.transpose(1, 2)) and torch.equal(G, G.transpose(1, 2))
+    c.ctx.close()
+
+
+def test_rows_of_all_lengths_of_a_contraction():
+    """Weight gradients over segments of 0 .. 200 rows: every length of the last, partial step, whole steps and none."""
+    E, ci, co = 201, 72, 40
+    lengths = np.arange(E)
+    np.random.default_rng(0).shuffle(lengths)
+    choice = np.repeat(np.arange(E), lengths).astype(np.int32)
+    n = len(choice)
+    for dtype in (F32, BF16):
+        c = Case(n, 1, E, ci, co, 0, dtype, "even")
+        kfac.kfac_segments(c.ctx, torch.from_numpy(choice).cuda(), E, c.order, c.offsets)
+        dW = torch.full((E, co, ci), 5.0, device="cuda")
+        kfac.kfac_expert_grad_weight(c.ctx, c.layer, c.order, c.offsets, c.x, c.dy, dW)
+        ref, mag = T.expert_grad_weight(choice, _values(c.x), _values(c.dy), E, 0, 1)
+        _close(dW, ref, mag, 200, F32, "dW")
+        c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_captured_in_a_graph(dtype):
+    """The calls in a HIP graph, replayed with other inputs and with eager work between the replays."""
+    stream = torch.cuda.Stream()
+    layer = _layer(128, 64, 0)
+    n, E = 300, 4
+    with torch.cuda.stream(stream):
+        ctx = kfac.Context([layer], workspace_bytes=max(kfac.kfac_segments_workspace_bytes(n, E), kfac.kfac_embedding_workspace_bytes(n, 50, 128)), stream=stream)
+        choice = torch.zeros(n, dtype=torch.int32, device="cuda")
+        x, W, dy = (torch.randn(*s, device="cuda").to(dtype) for s in ((n, 128), (E, 64, 128), (n, 64)))
+        order, offsets = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(E + 1, dtype=torch.int32, device="cuda")
+        y, dW, dT = torch.empty(n, 64, dtype=dtype, device="cuda"), torch.empty(E, 64, 128, device="cuda"), torch.empty(50, 128, device="cuda")
+        h = torch.empty_like(x)
+
+        def run():
+            kfac.kfac_segments(ctx, choice, E, order, offsets)
+            kfac.kfac_dropout(ctx, x, 0.3, 5, 6, h)
+            kfac.kfac_expert_forward(ctx, layer, order, offsets, h, W, y)
+            kfac.kfac_expert_grad_weight(ctx, layer, order, offsets, h, dy, dW)
+            kfac.kfac_embedding_grad(ctx, choice, h, 1.0, dT)
+
+        run()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            run()
+        for k in range(4):
+            choice.copy_(torch.randint(-1, E, (n,), device="cuda"))
+            x.copy_(torch.randn(n, 128, device="cuda"))
+            graph.replay()
+            stream.synchronize()
+            got = [t.clone() for t in (order, offsets, y, dW, dT)]
+            run()
+            stream.synchronize()
+            for a, b in zip(got, (order, offsets, y, dW, dT)):
+                assert torch.equal(a, b)
+        ctx.close()
