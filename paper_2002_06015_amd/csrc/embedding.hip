@@ -125,7 +125,7 @@ __device__ __forceinline__ void write_row(const EmbeddingGrad &a, int key, int c
 }
 
 // A wave: a run of sorted positions, 64 W columns.
-template <typename T>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingGrad a, int col_tiles, int chunks)
 {
     constexpr int W = sizeof(T) == 2 ? 8 : 4, AHEAD = 8;
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingGrad 
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int p = __builtin_amdgcn_readlane(my_pos, min(r0 + u, cnt - 1));
-            if (c0 < a.dim) load_piece<T, W, true>(g + (long long)p * a.ld + c0, a.dim - c0, v[u]);
+            if (c0 < a.dim) load_piece<T, W, ONCE>(g + (long long)p * a.ld + c0, a.dim - c0, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
@@ -285,6 +285,7 @@ hipError_t launch_embedding(const void *ids, int id_bits, int n, int vocab, int 
                          : lookup_types((const int *)ids, n, vocab, dim, table_bf16, table, ldt, scale, out_bf16, out, ldo, s);
 }
 
+// Short runs where there are few positions, so that there are waves enough; long ones leave fewer parts to join.
 int embedding_chunk(int n) { return n <= 32768 ? 8 : 32; }
 
 hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s)
@@ -292,8 +293,17 @@ hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s)
     const int chunks = (a.n + a.chunk - 1) / a.chunk;
     const int piece = 64 * (a.bf16 ? 8 : 4), col_tiles = (a.dim + piece - 1) / piece;
     const long long wgs = ((long long)chunks * col_tiles + 3) / 4;
-    if (a.bf16) embedding_sum_kernel<bf16_t><<<dim3((unsigned)wgs), dim3(256), 0, s>>>(a, col_tiles, chunks);
-    else embedding_sum_kernel<float><<<dim3((unsigned)wgs), dim3(256), 0, s>>>(a, col_tiles, chunks);
+    const dim3 grid((unsigned)wgs), block(256);
+    // gradients that the caches cannot hold are read past them, which leaves the caches to the rows that are written (131071 x 1024 bf16:
+    // 89 us, 125 through them); smaller ones may still be there from their writing (8191 x 1024: 11 us, 13 past them)
+    const bool once = (long long)a.n * a.dim * (a.bf16 ? 2 : 4) > (64LL << 20);
+    if (a.bf16) {
+        if (once) embedding_sum_kernel<bf16_t, true><<<grid, block, 0, s>>>(a, col_tiles, chunks);
+        else embedding_sum_kernel<bf16_t, false><<<grid, block, 0, s>>>(a, col_tiles, chunks);
+    } else {
+        if (once) embedding_sum_kernel<float, true><<<grid, block, 0, s>>>(a, col_tiles, chunks);
+        else embedding_sum_kernel<float, false><<<grid, block, 0, s>>>(a, col_tiles, chunks);
+    }
     return hipGetLastError();
 }
 
