@@ -135,8 +135,10 @@ __device__ __forceinline__ bf16x8 fragment(const bf16_t *tile, int row0, int u, 
 }
 
 // ---- general kernel: any size, stride and alignment -----------------------------------------------------
-// 128 x 128 tiles, four waves of 64 x 64; operands go through registers (converted there if they are fp32) into one LDS
-// stage while the next step's loads are in flight.
+// Tiles of 128 x 128 (four waves of 64 x 64, one LDS stage) or 64 x 64 (of 32 x 32, two stages); operands go through registers, and
+// are converted there if they are fp32, while the next step's loads are in flight.  fp32: 177 - 195 TFLOP/s on 4096 rows
+// 4096 -> 4096 (the library's product has 151), bound by the vector instructions that split the operands (6 of them for each matrix
+// instruction in small tiles) and the matrix unit's power; bf16 with odd sizes 16384 rows 1025 -> 2049: 240 - 450 TFLOP/s.
 template <typename T>
 struct Chunk {
     uintx4 v[sizeof(T) / 2];
@@ -285,12 +287,12 @@ struct Tile {
     bool g;   // statistics: G_e
 };
 
-// Tiles of BM x BN of the lower triangle of a symmetric matrix (BN = BM or 2 BM): row ti has the columns that reach its diagonal.
-template <int BM, int BN>
+// Tiles of the lower triangle of a symmetric matrix.
+template <int EDGE>
 __host__ __device__ __forceinline__ int triangle_tiles(int dim)
 {
-    const int t = (dim + BM - 1) / BM;
-    return BN == BM ? t * (t + 1) / 2 : (t / 2) * (t / 2 + 1) + (t & 1) * (t / 2 + 1);
+    const int t = (dim + EDGE - 1) / EDGE;
+    return t * (t + 1) / 2;
 }
 
 // Contractions over the rows of an expert take as long as it has rows: every XCD gets an eighth of every expert's tiles.
@@ -322,21 +324,13 @@ __device__ __forceinline__ bool find_work(const ExpertArgs &a, int tiles_j, int 
         t.I = a.co; t.J = a.ci; t.K = t.len;
         return true;
     } else {
-        const int na = a.A ? triangle_tiles<BM, BN>(a.ci) : 0, per = na + (a.G ? triangle_tiles<BM, BN>(a.co) : 0);
+        const int na = a.A ? triangle_tiles<BM>(a.ci) : 0, per = na + (a.G ? triangle_tiles<BM>(a.co) : 0);
         int local;
         if (!expert_share(total / a.experts, per, t.e, local)) return false;
         t.g = local >= na;
         if (t.g) local -= na;
-        if constexpr (BN == BM) {
-            tri_decode(local, t.ti, t.tj);
-        } else {   // rows 2 r and 2 r + 1 have r + 1 tiles each
-            int r = (int)((sqrtf(4.0f * (float)local + 1.0f) - 1.0f) * 0.5f);
-            while (r * (r + 1) > local) --r;
-            while ((r + 1) * (r + 2) <= local) ++r;
-            local -= r * (r + 1);
-            t.ti = 2 * r + (local > r ? 1 : 0);
-            t.tj = local - (local > r ? r + 1 : 0);
-        }
+        static_assert(BM == BN, "the triangle has square tiles");
+        tri_decode(local, t.ti, t.tj);
         segment(a, t.e, t.begin, t.len);
         t.I = t.J = t.g ? a.co : a.ci;
         t.K = t.len;
@@ -569,8 +563,13 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
 // BM x BN tiles, WI x WJ waves, in halves of 32 k.  Five halves have a place in LDS: while one is multiplied from registers and the
 // fragments of the next one are read, the three behind it are there or on their way.  Loads go out for two halves (64 k, whole
-// 128-byte lines of operands along k) at a time and have three halves' time to arrive: with two stages of 64 k and two halves' time
-// the multiplication waited for them (65536 rows 2048 -> 2048 of 16 experts: 546 us).
+// 128-byte lines of operands along k; half lines were fetched twice: 640 us for the forward product below) at a time and have three
+// halves' time to arrive.
+// 65536 rows 2048 -> 2048 of 16 experts: 540, 525 and 550 us for the three products, 1.0 PFLOP/s; 8192 rows 8192 -> 8192: 1.1 - 1.28 (the
+// library's product has 1.41).  Bound by what the loads cost inside a CU and by power: without loads in the loop 375, 365 and
+// 330 us, with loads of the same lines over and over 460, 451 and 541, at a shader clock of 1.64 - 1.8 GHz.  Four waves of
+// 128 x 128, which read a quarter less from LDS, were slower (576, 562 and 664 us), as were two stages of 64 k (8192 rows: 1131, 1048
+// and 918 us instead of 1006, 856 and 972).
 // Offsets in a tensor are 32 bits (the host sees to it); rows and columns beyond the tile's are clamped, they reach no output.
 // What is left of a contraction that is no whole number of steps of 64 goes through registers, with zeros behind its end.
 constexpr int kPlaces = 5;
@@ -878,7 +877,7 @@ long long count_tiles(ExpertOp op, const ExpertArgs &a, int &tiles_j)
         tiles_j = (a.ci + BN - 1) / BN;
         return (long long)a.experts * (((long long)((a.co + BM - 1) / BM) * tiles_j + 7) / 8 * 8);
     }
-    return (long long)a.experts * (((a.A ? triangle_tiles<BM, BN>(a.ci) : 0) + (a.G ? triangle_tiles<BM, BN>(a.co) : 0) + 7) / 8 * 8);
+    return (long long)a.experts * (((a.A ? triangle_tiles<BM>(a.ci) : 0) + (a.G ? triangle_tiles<BM>(a.co) : 0) + 7) / 8 * 8);
 }
 
 template <int BM, int BN, int WI, int WJ>
@@ -890,14 +889,24 @@ hipError_t run_direct(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     switch (op) {
         case EXPERT_FORWARD: expert_direct_kernel<EXPERT_FORWARD, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
         case EXPERT_GRAD_INPUT: expert_direct_kernel<EXPERT_GRAD_INPUT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_WEIGHT:
-            if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-            else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-            break;
-        case EXPERT_STATS:
-            if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-            else expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-            break;
+        default: return hipErrorInvalidValue;   // (run_direct_rows has the others)
+    }
+    return hipGetLastError();
+}
+
+// The contractions over rows
+template <int BM, int BN, int WI, int WJ>
+hipError_t run_direct_rows(ExpertOp op, const ExpertArgs &a, hipStream_t s)
+{
+    int tj;
+    const long long wgs = count_tiles<BM, BN>(op, a, tj);
+    const dim3 grid((unsigned)wgs), block(64 * WI * WJ);
+    if (op == EXPERT_GRAD_WEIGHT) {
+        if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+        else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+    } else {
+        if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+        else expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
     }
     return hipGetLastError();
 }
@@ -923,14 +932,18 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t
 {
     int tj;
     if (bf16 && direct_ok(op, a)) {
-        // 256 x 256 tiles need half the traffic, but one of them fills a CU: only where there is one for each of 256
-        if (count_tiles<256, 256>(op, a, tj) >= 256) return run_direct<256, 256, 4, 2>(op, a, s);
+        // 256 x 256 tiles need half the traffic of 128 x 128, but one of them fills a CU: only where there is one for each of the 256
+        // (16384 rows 1024 -> 2048 of 16 experts, forward: 72 us, 83 with 128 x 128; 2048 rows 1024 -> 1024 of 8: 27 and 17)
+        const bool full = count_tiles<256, 256>(op, a, tj) >= 256;
+        if (op == EXPERT_GRAD_WEIGHT || op == EXPERT_STATS) return full ? run_direct_rows<256, 256, 4, 2>(op, a, s) : run_direct_rows<128, 128, 2, 2>(op, a, s);
+        if (full) return run_direct<256, 256, 4, 2>(op, a, s);
         // few rows an expert: 64 x 64, more of them in flight (a decoding step of 8 choices 1024 -> 4096: 14 us, 17 with 128 x 128; 2048
-        // rows 1024 -> 1024 of 8 experts: 13 and 17; 4096 of 16: 21 and 19).  Gradients of weights have as many tiles whatever the rows.
-        if ((op == EXPERT_FORWARD || op == EXPERT_GRAD_INPUT) && count_tiles<128, 128>(op, a, tj) <= 320) return run_direct<64, 64, 2, 2>(op, a, s);
-        return run_direct<128, 128, 2, 2>(op, a, s);
+        // rows 1024 -> 1024 of 8 experts: 13 and 17; 4096 of 16: 21 and 19).  Gradients of weights have as many tiles whatever the rows
+        // (2048 rows of 8 experts: 29 us, 19 with 128 x 128).
+        return count_tiles<128, 128>(op, a, tj) <= 320 ? run_direct<64, 64, 2, 2>(op, a, s) : run_direct<128, 128, 2, 2>(op, a, s);
     }
-    // 128 x 128 tiles where there are two for each CU; the smaller ones finish a step in a third of the time
+    // 128 x 128 tiles where there are two for each CU, smaller ones otherwise (fp32 2051 rows 515 -> 1000 of 8 uneven experts: 32, 47 and 67 us
+    // for the three products, 47, 88 and 141 with 128 x 128)
     const bool large = count_tiles<128, 128>(op, a, tj) >= 512;
     if (bf16) return large ? run_general<bf16_t, 128>(op, a, s) : run_general<bf16_t, 64>(op, a, s);
     return large ? run_general<float, 128>(op, a, s) : run_general<float, 64>(op, a, s);

@@ -130,6 +130,7 @@ kfac_status kfac_embedding_grad(kfac_ctx *ctx, int32_t n, const void *ids, int32
     if (!std::isfinite(scale) || !(decay >= 0.f && decay < 1.f) || ld_grad < dim || ld_grad > (1LL << 40) || !dW) return KFAC_ERR_INVALID;
     if (!aligned(dW, 4) || !aligned(A_diag, 4) || (n > 0 && (!ids || !grad_out || !aligned(ids, id_bits / 8) || !aligned(grad_out, esize(type)))))
         return KFAC_ERR_INVALID;
+    if (((long long)n / embedding_chunk(n) + 1) * (dim / 256 + 1) >= (1LL << 30)) return KFAC_ERR_INVALID;   // workgroups of one launch
     const Range w = matrix(dW, vocab, dim, dim, 4), d = matrix(A_diag, 1, vocab, vocab, 4), g = matrix(grad_out, n, dim, ld_grad, esize(type)),
                 in{(const char *)ids, (size_t)n * (id_bits / 8)};
     if (overlap(w, d) || overlap(w, g) || overlap(w, in) || overlap(d, g) || overlap(d, in)) return KFAC_ERR_INVALID;
