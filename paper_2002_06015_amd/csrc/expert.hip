@@ -135,8 +135,8 @@ __device__ __forceinline__ bf16x8 fragment(const bf16_t *tile, int row0, int u, 
 }
 
 // ---- general kernel: any size, stride and alignment -----------------------------------------------------
-// Tiles of 128 x 128 (four waves of 64 x 64, one LDS stage) or 64 x 64 (of 32 x 32, two stages); operands go through registers, and
-// are converted there if they are fp32, while the next step's loads are in flight.  fp32: 177 - 195 TFLOP/s on 4096 rows
+// Tiles of 128 x 128 (four waves of 64 x 64) or 64 x 64 (of 32 x 32, several groups of waves that share the contraction); operands go
+// through registers, and are converted there if they are fp32, while the next step's loads are in flight.  fp32: 177 - 195 TFLOP/s on 4096 rows
 // 4096 -> 4096 (the library's product has 151), bound by the vector instructions that split the operands (6 of them for each matrix
 // instruction in small tiles) and the matrix unit's power; bf16 with odd sizes 16384 rows 1025 -> 2049: 240 - 450 TFLOP/s.
 template <typename T>
@@ -211,8 +211,8 @@ struct Staged {
             choice[i] = k < K ? choice_at(a, begin + k) : -1;
         }
     }
-    // rows: of the tile's first row on (along k); cols and K as above
-    __device__ __forceinline__ void init(const ExpertArgs &a, const T *base_, long long ld_, int fan_, int begin_, int row0, int rows, int K_, int tid)
+    // rows: of the tile's first row on (along k); cols and K as above; k0: the first step
+    __device__ __forceinline__ void init(const ExpertArgs &a, const T *base_, long long ld_, int fan_, int begin_, int row0, int rows, int K_, int k0, int tid)
     {
         base = base_; ld = ld_; fan = (unsigned)fan_; begin = begin_; K = K_; cols = rows; col0 = row0;
         if constexpr (!ACROSS) {
@@ -224,10 +224,10 @@ struct Staged {
                 line_ptr[i] = r < rows && c >= 0 ? line(r, c) : nullptr;
             }
         } else if constexpr (GATHER != 0) {
-            next_choices(a, 0, tid);
+            next_choices(a, k0, tid);
         }
     }
-    __device__ __forceinline__ void load(const ExpertArgs &a, int k0, int tid)
+    __device__ __forceinline__ void load(const ExpertArgs &a, int k0, int apart, int tid)   // the next one: apart further
     {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -242,7 +242,7 @@ struct Staged {
                 reg[i].load(there ? line(k, c) + col0 + pos : base, there ? cols - col0 - pos : 0);
             }
         }
-        if constexpr (ACROSS && GATHER != 0) next_choices(a, k0 + BK, tid);
+        if constexpr (ACROSS && GATHER != 0) next_choices(a, k0 + apart, tid);
     }
     __device__ __forceinline__ void store(bf16_t *tile, int tid) const
     {
@@ -454,8 +454,9 @@ __device__ __forceinline__ bf16x8 ones_row(int q, int lane)
     return __builtin_bit_cast(bf16x8, uintx4{v, v, v, v});
 }
 
-template <typename T, int OP, int EDGE>
-__global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
+// GROUPS of four waves share a tile: each takes every GROUPS-th step of the contraction, the sums are added up in the groups' order.
+template <typename T, int OP, int EDGE, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
 {
     constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 ? 1 : 3;
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
@@ -463,23 +464,23 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
     constexpr int PLANE = EDGE * BK, NB = EDGE / 32;   // NB x NB blocks of 16 x 16 a wave
-    // small tiles have two LDS stages: a step's operands are converted and stored while the step before it is multiplied
-    constexpr int STAGES = EDGE == 64 ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) bf16_t lds[STAGES * 2 * NP * PLANE];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ __attribute__((aligned(16))) bf16_t lds[GROUPS * 2 * NP * PLANE];
+    const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0, first = group * BK;
     const int wi = wave >> 1, wj = wave & 1;
+    bf16_t *const tile_a = lds + group * 2 * NP * PLANE, *const tile_b = tile_a + NP * PLANE;
     Tile t;
     if (!find_work<OP, EDGE, EDGE>(a, tiles_j, total, t)) return;
 
     Staged<T, ACROSS_A, GATHER_A, BK, EDGE> sa;
     Staged<T, ACROSS_B, GATHER_B, BK, EDGE> sb;
     const T *We = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw, *x = (const T *)a.x, *dy = (const T *)a.dy;
-    if constexpr (OP == EXPERT_FORWARD) sa.init(a, x, a.ldx, a.fan, t.begin, t.ti * EDGE, t.I, t.K, tid);
-    else if constexpr (OP == EXPERT_STATS) sa.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * EDGE, t.I, t.K, tid);
-    else sa.init(a, dy, a.ldy, 1, t.begin, t.ti * EDGE, t.I, t.K, tid);
-    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) sb.init(a, We, a.ldw, 1, 0, t.tj * EDGE, t.J, t.K, tid);
-    else if constexpr (OP == EXPERT_STATS) sb.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * EDGE, t.J, t.K, tid);
-    else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * EDGE, t.J, t.K, tid);
+    if constexpr (OP == EXPERT_FORWARD) sa.init(a, x, a.ldx, a.fan, t.begin, t.ti * EDGE, t.I, t.K, first, tid);
+    else if constexpr (OP == EXPERT_STATS) sa.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * EDGE, t.I, t.K, first, tid);
+    else sa.init(a, dy, a.ldy, 1, t.begin, t.ti * EDGE, t.I, t.K, first, tid);
+    if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) sb.init(a, We, a.ldw, 1, 0, t.tj * EDGE, t.J, t.K, first, tid);
+    else if constexpr (OP == EXPERT_STATS) sb.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * EDGE, t.J, t.K, first, tid);
+    else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * EDGE, t.J, t.K, first, tid);
     const bool sums = wants_sums<OP>(a, t, wj);
 
     floatx4 acc[NB][NB], row_sum = {0.f, 0.f, 0.f, 0.f};   // row_sum[i] of lanes 0 .. 15: the rows of block i
@@ -487,18 +488,13 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
     for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto store = [&](int stage) {
-        sa.store(lds + stage * 2 * NP * PLANE, tid);
-        sb.store(lds + stage * 2 * NP * PLANE + NP * PLANE, tid);
-    };
     auto load = [&](int k0) {
         if (k0 < t.K) {
-            sa.load(a, k0, tid);
-            sb.load(a, k0, tid);
+            sa.load(a, k0, GROUPS * BK, tid);
+            sb.load(a, k0, GROUPS * BK, tid);
         }
     };
-    auto multiply = [&](int stage) {
-        const bf16_t *tile_a = lds + stage * 2 * NP * PLANE, *tile_b = tile_a + NP * PLANE;
+    auto multiply = [&]() {
 #pragma unroll
         for (int u = 0; u < BK / 32; ++u) {
             bf16x8 fa[NP][NB], fb[NP][NB];
@@ -523,30 +519,48 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
                     for (int i = 0; i < NB; ++i) row_sum = mfma(ones_row(i, lane), fa[p][i], row_sum);
         }
     };
-    load(0);
-    if constexpr (STAGES == 2) {
-        if (t.K > 0) store(0);
-        load(BK);
-        for (int k0 = 0, stage = 0; k0 < t.K; k0 += BK, stage ^= 1) {
-            __syncthreads();   // the step is there, and every wave has read the one before it
-            if (k0 + BK < t.K) store(stage ^ 1);
-            load(k0 + 2 * BK);
-            multiply(stage);
+    load(first);
+    for (int k0 = 0; k0 < t.K; k0 += GROUPS * BK) {
+        if (k0 > 0) __syncthreads();   // every wave has read the step before
+        if (k0 + first < t.K) {
+            sa.store(tile_a, tid);
+            sb.store(tile_b, tid);
         }
-    } else {
-        for (int k0 = 0; k0 < t.K; k0 += BK) {
-            if (k0 > 0) __syncthreads();   // every wave has read the step before
-            store(0);
+        __syncthreads();
+        load(k0 + first + GROUPS * BK);
+        if (k0 + first < t.K) multiply();
+    }
+    if constexpr (GROUPS > 1) {
+        constexpr int LD = EDGE + 4;
+        static_assert((EDGE * LD + EDGE) * 4 <= sizeof(lds), "a group's sums have to fit");
+        float *const part = (float *)lds, *const part_rows = part + EDGE * LD;
+        for (int g = 1; g < GROUPS; ++g) {
             __syncthreads();
-            load(k0 + BK);
-            multiply(0);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const int row = wi * (EDGE / 2) + 16 * i + (lane & 15);
+                if (group == g && sums && lane < 16) part_rows[row] = row_sum[i];
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (group == g) *(floatx4 *)(part + row * LD + wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4)) = acc[i][j];
+            }
+            __syncthreads();
+            if (group == 0)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    const int row = wi * (EDGE / 2) + 16 * i + (lane & 15);
+                    if (sums && lane < 16) row_sum[i] += part_rows[row];
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) acc[i][j] += *(const floatx4 *)(part + row * LD + wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4));
+                }
         }
     }
     // lane -> row lane % 16 of a block, columns 4 (lane / 16) .. + 3
     constexpr bool SAME = OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT;   // results of the operands' type
     constexpr int PART = EDGE == 64 ? 64 : sizeof(T) == 2 && !SAME ? 32 : 64;
     static_assert(PART * (EDGE + 8) * (SAME ? sizeof(T) : 4) <= sizeof(lds), "the part has to fit");
-    store_rows<T, OP, EDGE, EDGE, PART, 256>(a, t, lds, tid, [&](int p0, auto put_quad) {
+    store_rows<T, OP, EDGE, EDGE, PART, 256 * GROUPS>(a, t, lds, threadIdx.x, [&](int p0, auto put_quad) {
+        if (group > 0) return;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             const int row = wi * (EDGE / 2) + 16 * i;
@@ -555,7 +569,7 @@ __global__ __launch_bounds__(256, EDGE == 128 ? 2 : 4) void expert_general_kerne
             for (int j = 0; j < NB; ++j) put_quad(row + (lane & 15), wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4), acc[i][j]);
         }
     });
-    if (sums && lane < 16)
+    if (sums && group == 0 && lane < 16)
 #pragma unroll
         for (int i = 0; i < NB; ++i) store_sum<OP>(a, t, t.ti * EDGE + wi * (EDGE / 2) + 16 * i + lane, row_sum[i]);
 }
@@ -911,19 +925,39 @@ hipError_t run_direct_rows(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T, int EDGE>
-hipError_t run_general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
+template <typename T, ExpertOp OP, int EDGE, int GROUPS>
+hipError_t run_general(const ExpertArgs &a, hipStream_t s)
 {
     int tj;
-    const long long wgs = count_tiles<EDGE, EDGE>(op, a, tj);
-    const dim3 grid((unsigned)wgs), block(256);
-    switch (op) {
-        case EXPERT_FORWARD: expert_general_kernel<T, EXPERT_FORWARD, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_INPUT: expert_general_kernel<T, EXPERT_GRAD_INPUT, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_WEIGHT: expert_general_kernel<T, EXPERT_GRAD_WEIGHT, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_STATS: expert_general_kernel<T, EXPERT_STATS, EDGE><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-    }
+    const long long wgs = count_tiles<EDGE, EDGE>(OP, a, tj);
+    expert_general_kernel<T, OP, EDGE, GROUPS><<<dim3((unsigned)wgs), dim3(256 * GROUPS), 0, s>>>(a, tj, (int)wgs);
     return hipGetLastError();
+}
+
+// 128 x 128 tiles where there are two for each CU, smaller ones otherwise (fp32 2051 rows 515 -> 1000 of 8 uneven experts: 47, 88 and
+// 141 us for the three products with the large ones, 32, 49 and 66 with the small ones and one group, 36, 38 and 46 with two).
+// Contractions over rows of few tiles are chains as long as the longest expert: four groups (512 tiles at most; fp32 factors of 2053
+// rows, 448 tiles: 55, 36 and 27 us with one, two and four; of 2048 rows, 1376 tiles: 42 with two, 59 with four).
+template <typename T, ExpertOp OP>
+hipError_t general(const ExpertArgs &a, hipStream_t s)
+{
+    int tj;
+    if (count_tiles<128, 128>(OP, a, tj) >= 512) return run_general<T, OP, 128, 1>(a, s);
+    if constexpr (OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS)
+        if (count_tiles<64, 64>(OP, a, tj) <= 512) return run_general<T, OP, 64, 4>(a, s);
+    return run_general<T, OP, 64, 2>(a, s);
+}
+
+template <typename T>
+hipError_t general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
+{
+    switch (op) {
+        case EXPERT_FORWARD: return general<T, EXPERT_FORWARD>(a, s);
+        case EXPERT_GRAD_INPUT: return general<T, EXPERT_GRAD_INPUT>(a, s);
+        case EXPERT_GRAD_WEIGHT: return general<T, EXPERT_GRAD_WEIGHT>(a, s);
+        case EXPERT_STATS: return general<T, EXPERT_STATS>(a, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -942,11 +976,7 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t
         // (2048 rows of 8 experts: 29 us, 19 with 128 x 128).
         return count_tiles<128, 128>(op, a, tj) <= 320 ? run_direct<64, 64, 2, 2>(op, a, s) : run_direct<128, 128, 2, 2>(op, a, s);
     }
-    // 128 x 128 tiles where there are two for each CU, smaller ones otherwise (fp32 2051 rows 515 -> 1000 of 8 uneven experts: 32, 47 and 67 us
-    // for the three products, 47, 88 and 141 with 128 x 128)
-    const bool large = count_tiles<128, 128>(op, a, tj) >= 512;
-    if (bf16) return large ? run_general<bf16_t, 128>(op, a, s) : run_general<bf16_t, 64>(op, a, s);
-    return large ? run_general<float, 128>(op, a, s) : run_general<float, 64>(op, a, s);
+    return bf16 ? general<bf16_t>(op, a, s) : general<float>(op, a, s);
 }
 
 }  // namespace kfac
