@@ -187,7 +187,7 @@ constexpr int kJoinWaves = 8, kLongParts = 24;
 __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const EmbeddingGrad a, int chunks)
 {
     __shared__ float part[kJoinWaves][64][4];
-    __shared__ int long_parts[kJoinWaves], long_key[kJoinWaves], long_count[kJoinWaves];
+    __shared__ int is_long[kJoinWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c0 = (blockIdx.y * 64 + lane) * 4;
     // Parts of the token that goes on behind run c and starts in it (0: there is none), and its positions.  The lanes look at the ends of
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = 0.f;
         if (c0 < a.dim) {
-#pragma unroll 12
+#pragma unroll 8
             for (int p = p0; p < p1; ++p) {
                 float v[4];
                 load_piece<float, 4>(a.partial + ((long long)2 * (c + p) + (p == 0 ? 1 : 0)) * a.dim + c0, a.dim - c0, v);
@@ -232,19 +232,15 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
     int key = 0, count = 0;
     float sum[4];
     const int mine = blockIdx.x * kJoinWaves + wave, parts = look(mine, key, count);
-    if (lane == 0) {
-        long_parts[wave] = parts > kLongParts ? parts : 0;
-        long_key[wave] = key;
-        long_count[wave] = count;
-    }
+    if (lane == 0) is_long[wave] = parts > kLongParts;
     if (parts > 0 && parts <= kLongParts) {
         add(mine, 0, parts, sum);
         write(key, count, sum);
     }
     __syncthreads();
     for (int w = 0; w < kJoinWaves; ++w) {
-        const int c = blockIdx.x * kJoinWaves + w, all = long_parts[w], per = (all + kJoinWaves - 1) / kJoinWaves;
-        if (all == 0) continue;
+        if (!is_long[w]) continue;
+        const int c = blockIdx.x * kJoinWaves + w, all = look(c, key, count), per = (all + kJoinWaves - 1) / kJoinWaves;
         add(c, min(wave * per, all), min(wave * per + per, all), sum);
 #pragma unroll
         for (int j = 0; j < 4; ++j) part[wave][lane][j] = sum[j];
@@ -253,7 +249,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
             for (int q = 1; q < kJoinWaves; ++q)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum[j] += part[q][lane][j];
-            write(long_key[w], long_count[w], sum);
+            write(key, count, sum);
         }
         __syncthreads();
     }
