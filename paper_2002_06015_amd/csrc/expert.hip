@@ -446,12 +446,12 @@ __device__ __forceinline__ void store_sum(const ExpertArgs &a, const Tile &t, in
     else if constexpr (OP == EXPERT_STATS) store_border(a, t, row, sum);
 }
 
-// Row q of the first operand of a matrix instruction is ones, the others zero: its product adds up the second operand's rows over k
-// into row q of the result.
-__device__ __forceinline__ bf16x8 ones_row(int q, int lane)
+// The product with ones adds up the second operand's rows over k, into every row of the result.  (Ones in one row and zeros in the
+// others would let several blocks share a result, but a zero times an infinity or a NaN is a NaN in the sums of another block.)
+__device__ __forceinline__ floatx4 add_up(const bf16x8 &i, const floatx4 &c)
 {
-    const unsigned v = (lane & 15) == q ? 0x3F803F80u : 0u;
-    return __builtin_bit_cast(bf16x8, uintx4{v, v, v, v});
+    constexpr unsigned one = 0x3F803F80u;
+    return mfma(__builtin_bit_cast(bf16x8, uintx4{one, one, one, one}), i, c);
 }
 
 // GROUPS of four waves share a tile: each takes every GROUPS-th step of the contraction, the sums are added up in the groups' order.
@@ -483,11 +483,13 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
     else sb.init(a, x, a.ldx, a.fan, t.begin, t.tj * EDGE, t.J, t.K, first, tid);
     const bool sums = wants_sums<OP>(a, t, wj);
 
-    floatx4 acc[NB][NB], row_sum = {0.f, 0.f, 0.f, 0.f};   // row_sum[i] of lanes 0 .. 15: the rows of block i
+    floatx4 acc[NB][NB], row_sum[NB];   // row_sum[i][0] of lanes 0 .. 15: the rows of block i
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < NB; ++i) {
+        row_sum[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
     auto load = [&](int k0) {
         if (k0 < t.K) {
             sa.load(a, k0, GROUPS * BK, tid);
@@ -516,7 +518,7 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int i = 0; i < NB; ++i) row_sum = mfma(ones_row(i, lane), fa[p][i], row_sum);
+                    for (int i = 0; i < NB; ++i) row_sum[i] = add_up(fa[p][i], row_sum[i]);
         }
     };
     load(first);
@@ -539,7 +541,7 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 const int row = wi * (EDGE / 2) + 16 * i + (lane & 15);
-                if (group == g && sums && lane < 16) part_rows[row] = row_sum[i];
+                if (group == g && sums && lane < 16) part_rows[row] = row_sum[i][0];
 #pragma unroll
                 for (int j = 0; j < NB; ++j)
                     if (group == g) *(floatx4 *)(part + row * LD + wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4)) = acc[i][j];
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {
                     const int row = wi * (EDGE / 2) + 16 * i + (lane & 15);
-                    if (sums && lane < 16) row_sum[i] += part_rows[row];
+                    if (sums && lane < 16) row_sum[i][0] += part_rows[row];
 #pragma unroll
                     for (int j = 0; j < NB; ++j) acc[i][j] += *(const floatx4 *)(part + row * LD + wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4));
                 }
@@ -571,7 +573,7 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
     });
     if (sums && group == 0 && lane < 16)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) store_sum<OP>(a, t, t.ti * EDGE + wi * (EDGE / 2) + 16 * i + lane, row_sum[i]);
+        for (int i = 0; i < NB; ++i) store_sum<OP>(a, t, t.ti * EDGE + wi * (EDGE / 2) + 16 * i + lane, row_sum[i][0]);
 }
 
 // ---- bf16, rows of whole 16-byte chunks: operands straight to LDS --------------------------------------
