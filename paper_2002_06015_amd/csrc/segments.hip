@@ -349,7 +349,7 @@ Fill part_of(const Fill *fill, int i, int parts, int threads, int *wgs)
     f.count = i == parts - 1 || f.count - from < per ? f.count - from : per;
     if (f.data) f.data += from;
     if (i > 0) f.n_decayed = 0;
-    const long long work = (f.data ? f.count / 4 : 0) + f.n_decayed;
+    const long long work = (f.data ? (f.count + 3) / 4 : 0) + f.n_decayed;   // (a part may have fewer than four elements)
     if (work > 0) *wgs = (int)(work / threads < 1024 * 256 / threads ? work / threads + 1 : 1024 * 256 / threads);
     return f;
 }
