@@ -511,7 +511,8 @@ kfac_status kfac_dropout(kfac_ctx *ctx, int64_t rows, int64_t cols, kfac_dtype t
  * rows of choices that no expert takes become zero in y and dx.  W: dev [experts, c_out, ldw] of `type`, row o of expert e
  * at (e * c_out + o) * ldw, its bias (L->bias) in column c_in.  dW: dev [experts, dG, dA] fp32, overwritten, zero for an
  * expert without rows.  Accumulation in fp32, one rounding at the end; fp32 operands as products of three bf16 planes
- * (see the rules at the top).  Workspace: kfac_expert_workspace_bytes serves all of them and kfac_stats_expert (0 for
+ * each, or, in a context created with KFAC_PRODUCTS_FP32_MFMA, through the fp32 matrix instruction (ranges as in the
+ * rules at the top; kfac_stats_expert likewise).  Workspace: kfac_expert_workspace_bytes serves all of them and kfac_stats_expert (0 for
  * invalid arguments).
  */
 size_t kfac_expert_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n);

@@ -13,7 +13,7 @@
 // instruction through the transposing LDS read (ds_read_b64_tr_b16: among 16 lanes, lane i receives element i % 4 of the four
 // 8-byte groups addressed by lanes i / 4, i / 4 + 4, i / 4 + 8, i / 4 + 12).
 // fp32 operands are the exact sum of three bf16 values; of the nine products the six above 2^-24 are formed (h h, h m, m h,
-// m m, h l, l h), all accumulated in fp32.
+// m m, h l, l h), all accumulated in fp32.  Contexts that ask for the fp32 matrix instruction get it.
 #include <type_traits>
 
 #include "gemm_tiles.h"
@@ -41,6 +41,7 @@ __device__ __forceinline__ floatx4 mfma(const bf16x8 &j, const bf16x8 &i, const 
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(j, i, c, 0, 0, 0);
 }
+__device__ __forceinline__ floatx4 mfma(float j, float i, const floatx4 &c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(j, i, c, 0, 0, 0); }
 
 // ---- segments ------------------------------------------------------------------------------------------
 __device__ __forceinline__ int segment_begin(const ExpertArgs &a, int e) { return min(max(a.offsets[e], 0), a.n); }
@@ -134,11 +135,35 @@ __device__ __forceinline__ bf16x8 fragment(const bf16_t *tile, int row0, int u, 
     }
 }
 
+// fp32 tiles of the fp32 matrix instruction: 32 k.  Where element (line, at) of a tile is; eight (along k: four) adjacent ones stay
+// together, and the lanes of a read meet different banks.
+template <bool ACROSS, int ROWS>
+__device__ __forceinline__ int float_at(int line, int at)
+{
+    if constexpr (ACROSS) return line * ROWS + (at ^ (line & 12) << 2);
+    else return line * 32 + (at ^ (line & 7) << 2);
+}
+
+// The 16 rows from `row0` of such a tile, k = 16 u + 4 (lane / 16) .. + 3: lane -> row lane % 16.
+template <bool ACROSS, int ROWS>
+__device__ __forceinline__ floatx4 fragment(const float *tile, int row0, int u, int lane)
+{
+    const int k = 16 * u + 4 * (lane >> 4), row = row0 + (lane & 15);
+    if constexpr (ACROSS) {
+        const float *p = tile + float_at<true, ROWS>(k, row);   // (the four lines are permuted alike)
+        return floatx4{p[0], p[ROWS], p[2 * ROWS], p[3 * ROWS]};
+    } else {
+        return *(const floatx4 *)(tile + float_at<false, ROWS>(row, k));
+    }
+}
+
 // ---- general kernel: any size, stride and alignment -----------------------------------------------------
 // Tiles of 128 x 128 (four waves of 64 x 64) or 64 x 64 (of 32 x 32, several groups of waves that share the contraction); operands go
 // through registers, and are converted there if they are fp32, while the next step's loads are in flight.  fp32: 177 - 195 TFLOP/s on 4096 rows
 // 4096 -> 4096 (the library's product has 151), bound by the vector instructions that split the operands (6 of them for each matrix
 // instruction in small tiles) and the matrix unit's power; bf16 with odd sizes 16384 rows 1025 -> 2049: 240 - 450 TFLOP/s.
+// The fp32 instruction: 118 TFLOP/s of its 157 there (1160 us instead of 700 - 750), and 42, 48 and 45 us for the products of 2051 rows
+// 515 -> 1000 of 8 even experts (34, 37 and 33 through planes): for its range, not for its speed.
 template <typename T>
 struct Chunk {
     uintx4 v[sizeof(T) / 2];
@@ -180,6 +205,13 @@ struct Chunk {
             *(uintx4 *)(tile + plane + 8 * at) = m;
             *(uintx4 *)(tile + 2 * plane + 8 * at) = l;
         }
+    }
+    // into a tile of the fp32 instruction, four elements at each place
+    __device__ __forceinline__ void store(float *at0, float *at1) const
+    {
+        static_assert(sizeof(T) == 4, "fp32 operands");
+        *(uintx4 *)at0 = v[0];
+        *(uintx4 *)at1 = v[1];
     }
 };
 
@@ -250,6 +282,14 @@ struct Staged {
         for (int i = 0; i < CH; ++i) {
             const int q = tid + 256 * i;
             reg[i].store(tile, EDGE * BK, chunk_at<ACROSS, BK, EDGE>(q / PER, q % PER));
+        }
+    }
+    __device__ __forceinline__ void store(float *tile, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int q = tid + 256 * i, line = q / PER, at = 8 * (q % PER);
+            reg[i].store(tile + float_at<ACROSS, EDGE>(line, at), tile + float_at<ACROSS, EDGE>(line, at + 4));
         }
     }
 };
@@ -455,20 +495,22 @@ __device__ __forceinline__ floatx4 add_up(const bf16x8 &i, const floatx4 &c)
 }
 
 // GROUPS of four waves share a tile: each takes every GROUPS-th step of the contraction, the sums are added up in the groups' order.
-template <typename T, int OP, int EDGE, int GROUPS>
+// FP32: with the fp32 matrix instruction, whose four k of step v are 16 u + 4 q + v of the lanes 16 q .. 16 q + 15.
+template <typename T, bool FP32, int OP, int EDGE, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
 {
-    constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 ? 1 : 3;
+    typedef std::conditional_t<FP32, float, bf16_t> E;   // what is in LDS
+    constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 || FP32 ? 1 : 3;
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
     constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
     constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
     constexpr int PLANE = EDGE * BK, NB = EDGE / 32;   // NB x NB blocks of 16 x 16 a wave
-    __shared__ __attribute__((aligned(16))) bf16_t lds[GROUPS * 2 * NP * PLANE];
+    __shared__ __attribute__((aligned(16))) E lds[GROUPS * 2 * NP * PLANE];
     const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0, first = group * BK;
     const int wi = wave >> 1, wj = wave & 1;
-    bf16_t *const tile_a = lds + group * 2 * NP * PLANE, *const tile_b = tile_a + NP * PLANE;
+    E *const tile_a = lds + group * 2 * NP * PLANE, *const tile_b = tile_a + NP * PLANE;
     Tile t;
     if (!find_work<OP, EDGE, EDGE>(a, tiles_j, total, t)) return;
 
@@ -497,28 +539,50 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
         }
     };
     auto multiply = [&]() {
+        if constexpr (FP32) {
 #pragma unroll
-        for (int u = 0; u < BK / 32; ++u) {
-            bf16x8 fa[NP][NB], fb[NP][NB];
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
+            for (int u = 0; u < BK / 16; ++u) {
+                floatx4 fa[NB], fb[NB];
 #pragma unroll
                 for (int q = 0; q < NB; ++q) {
-                    fa[p][q] = fragment<ACROSS_A, BK, EDGE>(tile_a + p * PLANE, wi * (EDGE / 2) + 16 * q, u, lane);
-                    fb[p][q] = fragment<ACROSS_B, BK, EDGE>(tile_b + p * PLANE, wj * (EDGE / 2) + 16 * q, u, lane);
+                    fa[q] = fragment<ACROSS_A, EDGE>(tile_a, wi * (EDGE / 2) + 16 * q, u, lane);
+                    fb[q] = fragment<ACROSS_B, EDGE>(tile_b, wj * (EDGE / 2) + 16 * q, u, lane);
                 }
-            constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};   // the small products first
 #pragma unroll
-            for (int q = NP == 1 ? 5 : 0; q < 6; ++q)
+                for (int v = 0; v < 4; ++v) {
 #pragma unroll
-                for (int i = 0; i < NB; ++i)
+                    for (int i = 0; i < NB; ++i)
 #pragma unroll
-                    for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fb[pb[q]][j], fa[pa[q]][i], acc[i][j]);
-            if (sums)
+                        for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fb[j][v], fa[i][v], acc[i][j]);
+                    if (sums)
 #pragma unroll
-                for (int p = NP - 1; p >= 0; --p)
+                        for (int i = 0; i < NB; ++i) row_sum[i] = mfma(1.f, fa[i][v], row_sum[i]);
+                }
+            }
+        } else {
 #pragma unroll
-                    for (int i = 0; i < NB; ++i) row_sum[i] = add_up(fa[p][i], row_sum[i]);
+            for (int u = 0; u < BK / 32; ++u) {
+                bf16x8 fa[NP][NB], fb[NP][NB];
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+#pragma unroll
+                    for (int q = 0; q < NB; ++q) {
+                        fa[p][q] = fragment<ACROSS_A, BK, EDGE>(tile_a + p * PLANE, wi * (EDGE / 2) + 16 * q, u, lane);
+                        fb[p][q] = fragment<ACROSS_B, BK, EDGE>(tile_b + p * PLANE, wj * (EDGE / 2) + 16 * q, u, lane);
+                    }
+                constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};   // the small products first
+#pragma unroll
+                for (int q = NP == 1 ? 5 : 0; q < 6; ++q)
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fb[pb[q]][j], fa[pa[q]][i], acc[i][j]);
+                if (sums)
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                        for (int i = 0; i < NB; ++i) row_sum[i] = add_up(fa[p][i], row_sum[i]);
+            }
         }
     };
     load(first);
@@ -559,7 +623,7 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
     }
     // lane -> row lane % 16 of a block, columns 4 (lane / 16) .. + 3
     constexpr bool SAME = OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT;   // results of the operands' type
-    constexpr int PART = EDGE == 64 ? 64 : sizeof(T) == 2 && !SAME ? 32 : 64;
+    constexpr int PART = EDGE == 128 && (FP32 || (sizeof(T) == 2 && !SAME)) ? 32 : 64;
     static_assert(PART * (EDGE + 8) * (SAME ? sizeof(T) : 4) <= sizeof(lds), "the part has to fit");
     store_rows<T, OP, EDGE, EDGE, PART, 256 * GROUPS>(a, t, lds, threadIdx.x, [&](int p0, auto put_quad) {
         if (group > 0) return;
@@ -927,12 +991,12 @@ hipError_t run_direct_rows(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T, ExpertOp OP, int EDGE, int GROUPS>
+template <typename T, bool FP32, ExpertOp OP, int EDGE, int GROUPS>
 hipError_t run_general(const ExpertArgs &a, hipStream_t s)
 {
     int tj;
     const long long wgs = count_tiles<EDGE, EDGE>(OP, a, tj);
-    expert_general_kernel<T, OP, EDGE, GROUPS><<<dim3((unsigned)wgs), dim3(256 * GROUPS), 0, s>>>(a, tj, (int)wgs);
+    expert_general_kernel<T, FP32, OP, EDGE, GROUPS><<<dim3((unsigned)wgs), dim3(256 * GROUPS), 0, s>>>(a, tj, (int)wgs);
     return hipGetLastError();
 }
 
@@ -940,31 +1004,31 @@ hipError_t run_general(const ExpertArgs &a, hipStream_t s)
 // 141 us for the three products with the large ones, 32, 49 and 66 with the small ones and one group, 36, 38 and 46 with two).
 // Contractions over rows of few tiles are chains as long as the longest expert: four groups (512 tiles at most; fp32 factors of 2053
 // rows, 448 tiles: 55, 36 and 27 us with one, two and four; of 2048 rows, 1376 tiles: 42 with two, 59 with four).
-template <typename T, ExpertOp OP>
+template <typename T, bool FP32, ExpertOp OP>
 hipError_t general(const ExpertArgs &a, hipStream_t s)
 {
     int tj;
-    if (count_tiles<128, 128>(OP, a, tj) >= 512) return run_general<T, OP, 128, 1>(a, s);
+    if (count_tiles<128, 128>(OP, a, tj) >= 512) return run_general<T, FP32, OP, 128, 1>(a, s);
     if constexpr (OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS)
-        if (count_tiles<64, 64>(OP, a, tj) <= 512) return run_general<T, OP, 64, 4>(a, s);
-    return run_general<T, OP, 64, 2>(a, s);
+        if (count_tiles<64, 64>(OP, a, tj) <= 512) return run_general<T, FP32, OP, 64, 4>(a, s);
+    return run_general<T, FP32, OP, 64, 2>(a, s);
 }
 
-template <typename T>
+template <typename T, bool FP32>
 hipError_t general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
 {
     switch (op) {
-        case EXPERT_FORWARD: return general<T, EXPERT_FORWARD>(a, s);
-        case EXPERT_GRAD_INPUT: return general<T, EXPERT_GRAD_INPUT>(a, s);
-        case EXPERT_GRAD_WEIGHT: return general<T, EXPERT_GRAD_WEIGHT>(a, s);
-        case EXPERT_STATS: return general<T, EXPERT_STATS>(a, s);
+        case EXPERT_FORWARD: return general<T, FP32, EXPERT_FORWARD>(a, s);
+        case EXPERT_GRAD_INPUT: return general<T, FP32, EXPERT_GRAD_INPUT>(a, s);
+        case EXPERT_GRAD_WEIGHT: return general<T, FP32, EXPERT_GRAD_WEIGHT>(a, s);
+        case EXPERT_STATS: return general<T, FP32, EXPERT_STATS>(a, s);
     }
     return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s)
+hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s)
 {
     int tj;
     if (bf16 && direct_ok(op, a)) {
@@ -978,7 +1042,8 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t
         // (2048 rows of 8 experts: 29 us, 19 with 128 x 128).
         return count_tiles<128, 128>(op, a, tj) <= 320 ? run_direct<64, 64, 2, 2>(op, a, s) : run_direct<128, 128, 2, 2>(op, a, s);
     }
-    return bf16 ? general<bf16_t>(op, a, s) : general<float>(op, a, s);
+    if (bf16) return general<bf16_t, false>(op, a, s);
+    return planes ? general<float, false>(op, a, s) : general<float, true>(op, a, s);
 }
 
 }  // namespace kfac

@@ -2858,7 +2858,7 @@ void kfac_refresh_advance(kfac_refresh_state *s, double ratio_m1, double ratio_m
 // ---------------------------------------------------------------- what token_api.hip sees of a context
 namespace kfac {
 
-CtxView ctx_view(const kfac_ctx *ctx) { return CtxView{ctx->stream, ctx->ws, ctx->ws_bytes}; }
+CtxView ctx_view(const kfac_ctx *ctx) { return CtxView{ctx->stream, ctx->ws, ctx->ws_bytes, ctx->tun.split != 0}; }
 
 bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, double flops, double bytes)
 {

@@ -75,7 +75,8 @@ ExpertArgs expert_args(const kfac_layer *L, int32_t experts, int32_t n, int32_t 
 
 bool run_expert(kfac_ctx *ctx, ExpertOp op, const ExpertArgs &a, kfac_dtype type, double flops, double bytes)
 {
-    return timed(ctx, KFAC_K_EXPERT, (int)op, 0, flops, bytes, [&] { return launch_expert(op, a, type == KFAC_BF16, ctx_view(ctx).stream); });
+    const CtxView c = ctx_view(ctx);
+    return timed(ctx, KFAC_K_EXPERT, (int)op, 0, flops, bytes, [&] { return launch_expert(op, a, type == KFAC_BF16, c.fp32_planes, c.stream); });
 }
 
 }  // namespace

@@ -15,6 +15,7 @@ struct CtxView {
     hipStream_t stream;
     char *ws;
     size_t ws_bytes;
+    bool fp32_planes;   // fp32 products: planes, or the fp32 matrix instruction
 };
 CtxView ctx_view(const kfac_ctx *ctx);
 // around one launch: records its times while profiling is on (nothing otherwise); false: a HIP call failed
@@ -90,6 +91,7 @@ struct ExpertArgs {
     float decay;
 };
 enum ExpertOp { EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, EXPERT_STATS };
-hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, hipStream_t s);
+// planes: how fp32 operands are multiplied (bf16 != 0: not used)
+hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s);
 
 }  // namespace kfac
