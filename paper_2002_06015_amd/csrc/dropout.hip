@@ -128,7 +128,7 @@ hipError_t run(DropoutArgs a, hipStream_t s)
     // blocks of the generator that a row can touch
     const unsigned long long per_row = a.rows == 1 || a.cols % 8 == 0 ? (a.cols + 7) / 8 : (a.cols + 7) / 8 + 1;
     const unsigned long long units = per_row * a.rows, wgs = (units + 255) / 256;
-    const dim3 grid((unsigned)(wgs < (1 << 24) ? wgs : (1 << 24)));
+    const dim3 grid((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)));   // a launch takes less than 2^32 threads; the kernel goes on from there
     if (a.r) dropout_kernel<T, true><<<grid, dim3(256), 0, s>>>(a, (unsigned)per_row, units);
     else dropout_kernel<T, false><<<grid, dim3(256), 0, s>>>(a, (unsigned)per_row, units);
     return hipGetLastError();
