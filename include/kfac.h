@@ -460,7 +460,8 @@ void kfac_refresh_advance(kfac_refresh_state *s, double ratio_m1, double ratio_m
  *   order   [n]        the positions 0 .. n-1 sorted by id, equal ids in the order of their positions; positions whose id is
  *                      outside [0, num) (padding, a choice beyond an expert's capacity) come last, in order
  *   offsets [num + 1]  order[offsets[k] .. offsets[k+1]) holds the positions of id k; offsets[num]: positions with an id
- * n = 0 gives offsets of zero.  Scratch from the workspace: kfac_segments_workspace_bytes (0 for invalid arguments).
+ * n = 0 gives offsets of zero.  Scratch from the workspace: kfac_segments_workspace_bytes (0 for invalid arguments;
+ * never less for more positions or more keys).
  */
 size_t kfac_segments_workspace_bytes(int32_t n, int32_t num);
 kfac_status kfac_segments(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_bits, int32_t num, int32_t *order, int32_t *offsets);
@@ -481,7 +482,8 @@ kfac_status kfac_embedding(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id
  *                inputs a, A = E[a a^T] has this diagonal and nothing else.  decay = 0 never reads the old contents; n = 0
  *                leaves A_diag as it is.
  * Sums in fp32 in an order that depends on n and the ids only (the same inputs give the same bits).  Positions with an id
- * outside [0, vocab) add nothing (they count in n).  Workspace: kfac_embedding_workspace_bytes (0 for invalid arguments).
+ * outside [0, vocab) add nothing (they count in n).  Workspace: kfac_embedding_workspace_bytes (0 for invalid arguments; never
+ * less for larger n, vocab or dim: the size for the largest batch serves all others).
  */
 size_t kfac_embedding_workspace_bytes(int32_t n, int32_t vocab, int32_t dim);
 kfac_status kfac_embedding_grad(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_bits, int32_t vocab, int32_t dim, kfac_dtype type,

@@ -287,7 +287,13 @@ hipError_t launch_embedding(const void *ids, int id_bits, int n, int vocab, int 
 }
 
 // Short runs where there are few positions, so that there are waves enough; long ones leave fewer parts to join.
-int embedding_chunk(int n) { return n <= 32768 ? 8 : 32; }
+constexpr int kShortRuns = 32768;
+int embedding_chunk(int n) { return n <= kShortRuns ? 8 : 32; }
+int embedding_most_chunks(int n)
+{
+    const int here = (n + embedding_chunk(n) - 1) / embedding_chunk(n);
+    return n <= kShortRuns || here > kShortRuns / 8 ? here : kShortRuns / 8;
+}
 
 hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s)
 {

@@ -397,6 +397,7 @@ size_t segment_scratch(char *base, int n, int num, SegmentScratch *out)
     if (bits < 1) bits = 1;
     w.passes = (bits + kSegBits - 1) / kSegBits;
     w.bits = (bits + w.passes - 1) / w.passes;
+    const int widest = bits < kSegBits ? bits : kSegBits;   // digit of any number of keys up to this one: more keys never need less scratch
     size_t used = 0;
     auto take = [&](size_t bytes) {
         char *p = base ? base + used : nullptr;
@@ -410,8 +411,8 @@ size_t segment_scratch(char *base, int n, int num, SegmentScratch *out)
         w.pos[0] = take(list);
         w.pos[1] = take(list);
         const size_t tiles = ((size_t)n + kSegTile - 1) / kSegTile;
-        w.counts = take(sizeof(int) * (tiles << w.bits));
-        w.totals = take(sizeof(int) << w.bits);
+        w.counts = take(sizeof(int) * (tiles << widest));
+        w.totals = take(sizeof(int) << widest);
     }
     if (out) *out = w;
     return used;

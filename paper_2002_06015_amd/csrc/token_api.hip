@@ -44,8 +44,7 @@ size_t embedding_grad_scratch(char *base, int n, int vocab, int dim, SegmentScra
         return p;
     };
     char *order = take(sizeof(int) * (size_t)std::max(n, 1));
-    const size_t chunks = ((size_t)n + embedding_chunk(n) - 1) / embedding_chunk(n);
-    char *part = take(2 * chunks * (size_t)dim * sizeof(float));
+    char *part = take(2 * (size_t)embedding_most_chunks(n) * (size_t)dim * sizeof(float));
     if (pos) *pos = (int *)order;
     if (partial) *partial = (float *)part;
     return used;

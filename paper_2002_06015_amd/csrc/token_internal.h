@@ -28,10 +28,10 @@ bool profile_end(kfac_ctx *ctx);
 constexpr int kSegSmall = 8192, kSegTile = 2048, kSegBits = 9;
 struct SegmentScratch {
     int *keys[2], *pos[2];   // [n] each: sorted keys and positions; pos[1] is not needed for n <= kSegSmall
-    int *counts, *totals;    // [tiles << bits], [1 << bits]
+    int *counts, *totals;    // [tiles << bits], [1 << bits] at least
     int passes, bits;        // of the counting sort
 };
-// Carves the scratch from `base` (nullptr: only counts); returns the bytes.
+// Carves the scratch from `base` (nullptr: only counts); returns the bytes, which never fall as n or num grows.
 size_t segment_scratch(char *base, int n, int num, SegmentScratch *out);
 // Work that shares the sort's launches: data[0 .. count) <- 0 (unless nullptr), decayed[0 .. n_decayed) *= decay (without reading
 // it for 0).  The sort keeps few CUs busy; the rest writes meanwhile.
@@ -58,10 +58,11 @@ struct EmbeddingGrad {
     int bf16, accumulate;
     float scale, share;      // share: (1 - decay) / n
     float *dW, *A;           // rows of zeros unless accumulate; decayed already, or nullptr
-    float *partial;          // [2 * chunks][dim]
+    float *partial;          // [2 * chunks][dim] at least
     int chunk;               // sorted positions that one wave adds up
 };
 int embedding_chunk(int n);
+int embedding_most_chunks(int n);   // runs of any number of positions up to n
 hipError_t launch_embedding_sum(const EmbeddingGrad &a, hipStream_t s);
 hipError_t launch_embedding_join(const EmbeddingGrad &a, hipStream_t s);
 
