@@ -24,6 +24,12 @@ Range matrix(const void *p, long long rows, long long cols, long long ld, size_t
     return Range{(const char *)p, p && rows > 0 ? (size_t)((rows - 1) * ld + cols) * es : 0};
 }
 bool overlap(const Range &a, const Range &b) { return a.size && b.size && a.p < b.p + b.size && b.p < a.p + a.size; }
+// rows that lie ld elements apart: offsets, in bytes too, stay far inside 64 bits
+bool spread_ok(long long rows, long long ld)
+{
+    constexpr long long most = 1LL << 40;
+    return ld <= most && (rows <= 1 || ld <= most / rows);
+}
 bool aligned(const void *p, size_t es) { return (uintptr_t)p % es == 0; }
 
 // One launch between the profiler's events
@@ -105,7 +111,7 @@ kfac_status kfac_embedding(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id
 {
     if (!ctx || !segments_ok(n, vocab) || dim < 1 || dim > kMaxDim || (id_bits != 32 && id_bits != 64)) return KFAC_ERR_INVALID;
     if (!type_ok(table_type) || !type_ok(out_type) || !std::isfinite(scale)) return KFAC_ERR_INVALID;
-    if (ld_table < dim || ld_out < dim || ld_table > (1LL << 40) || ld_out > (1LL << 40)) return KFAC_ERR_INVALID;
+    if (ld_table < dim || ld_out < dim || !spread_ok(vocab, ld_table) || !spread_ok(n, ld_out)) return KFAC_ERR_INVALID;
     if (n == 0) return KFAC_OK;
     if (!ids || !table || !out || !aligned(ids, id_bits / 8) || !aligned(table, esize(table_type)) || !aligned(out, esize(out_type))) return KFAC_ERR_INVALID;
     const Range o = matrix(out, n, dim, ld_out, esize(out_type));
@@ -127,7 +133,7 @@ kfac_status kfac_embedding_grad(kfac_ctx *ctx, int32_t n, const void *ids, int32
                                 const void *grad_out, int64_t ld_grad, float scale, int32_t accumulate, float *dW, float decay, float *A_diag)
 {
     if (!ctx || !segments_ok(n, vocab) || dim < 1 || dim > kMaxDim || (id_bits != 32 && id_bits != 64) || !type_ok(type)) return KFAC_ERR_INVALID;
-    if (!std::isfinite(scale) || !(decay >= 0.f && decay < 1.f) || ld_grad < dim || ld_grad > (1LL << 40) || !dW) return KFAC_ERR_INVALID;
+    if (!std::isfinite(scale) || !(decay >= 0.f && decay < 1.f) || ld_grad < dim || !spread_ok(n, ld_grad) || !dW) return KFAC_ERR_INVALID;
     if (!aligned(dW, 4) || !aligned(A_diag, 4) || (n > 0 && (!ids || !grad_out || !aligned(ids, id_bits / 8) || !aligned(grad_out, esize(type)))))
         return KFAC_ERR_INVALID;
     if (((long long)n / embedding_chunk(n) + 1) * (dim / 256 + 1) >= (1LL << 30)) return KFAC_ERR_INVALID;   // workgroups of one launch
@@ -169,8 +175,8 @@ kfac_status kfac_dropout(kfac_ctx *ctx, int64_t rows, int64_t cols, kfac_dtype t
     constexpr int64_t most = (int64_t)1 << 40;
     if (!ctx || !type_ok(type) || rows < 0 || cols < 0 || rows > most || cols > most || !(p >= 0.f && p <= 1.f)) return KFAC_ERR_INVALID;
     if (rows == 0 || cols == 0) return KFAC_OK;
-    if (rows > most / cols || ldx < cols || ldy < cols || (residual && ldr < cols) || ldx > most || ldy > most || ldr > most) return KFAC_ERR_INVALID;
-    if (rows > 1 && (ldx > most / rows || ldy > most / rows || (residual && ldr > most / rows))) return KFAC_ERR_INVALID;
+    if (rows > most / cols || ldx < cols || ldy < cols || (residual && ldr < cols) || ldr > most) return KFAC_ERR_INVALID;
+    if (!spread_ok(rows, ldx) || !spread_ok(rows, ldy) || (residual && !spread_ok(rows, ldr))) return KFAC_ERR_INVALID;
     if (rows > 1 && cols > ((int64_t)1 << 32)) return KFAC_ERR_INVALID;
     if (!x || !y || !aligned(x, esize(type)) || !aligned(y, esize(type)) || !aligned(residual, esize(type))) return KFAC_ERR_INVALID;
     const Range out = matrix(y, rows, cols, ldy, esize(type)), in = matrix(x, rows, cols, ldx, esize(type)),

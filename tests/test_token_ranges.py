@@ -1,0 +1,28 @@
+"""CPU-only: what the token and expert entry points accept and refuse at the ends of their ranges."""
+import ctypes
+
+import pytest
+
+from paper_2002_06015_amd import kfac, workloads as wl
+
+INV, WS = kfac.KFAC_ERR_INVALID, kfac.KFAC_ERR_WORKSPACE
+P, Q, R, S = ((a << 44) for a in (1, 2, 3, 4))     # made-up addresses, 16 TiB apart, never dereferenced
+
+
+@pytest.fixture()
+def h():
+    handle = ctypes.c_void_p()
+    assert kfac.lib().kfac_create(ctypes.addressof(handle), None, ctypes.c_void_p(0x100000), 256) == kfac.KFAC_OK
+    yield handle.value
+    kfac.lib().kfac_destroy(handle)
+
+
+def test_distances_of_rows_that_no_tensor_has(h):
+    """Rows times their distance beyond 2^40 elements are refused: products of the two that pass 64 bits among them."""
+    far = (1 << 40) - 8
+    embedding = lambda n, vocab, ldt, ldo: kfac.lib().kfac_embedding(h, n, P, 64, vocab, 16, 0, Q, ldt, 1.0, 0, R, ldo)  # noqa: E731
+    assert embedding(8, 1 << 29, far, 16) == INV and embedding(1 << 29, 10, 16, far) == INV
+    assert embedding(8, 1 << 24, 1 << 17, 16) == INV and embedding(8, 1 << 23, 1 << 40, 16) == INV and embedding(1 << 24, 10, 16, 1 << 17) == INV
+    grad = lambda n, ld: kfac.lib().kfac_embedding_grad(h, n, P, 64, 10, 16, 0, Q, ld, 1.0, 0, R, 0.5, S)  # noqa: E731
+    assert grad(1 << 29, far) == INV and grad(1 << 24, 1 << 17) == INV
+    assert grad(1, far) == WS and grad(1 << 20, 1 << 20) == WS                  # no reason to refuse these: 256 bytes hold no lists
