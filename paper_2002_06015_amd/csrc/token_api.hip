@@ -15,15 +15,28 @@ constexpr int kMaxPositions = 1 << 30, kMaxDim = 1 << 20, kMaxExperts = 1 << 16;
 bool type_ok(kfac_dtype t) { return t == KFAC_F32 || t == KFAC_BF16; }
 size_t esize(kfac_dtype t) { return t == KFAC_BF16 ? 2 : 4; }
 
-struct Range {   // bytes [p, p + size); empty: touches nothing
+// Bytes that a call touches: one piece of `row` bytes every `ld` bytes from p to p + size; ld = 0: one piece.  Empty: touches nothing.
+struct Range {
     const char *p;
-    size_t size;
+    size_t size, row, ld;
+    Range(const void *p_ = nullptr, size_t size_ = 0, size_t row_ = 0, size_t ld_ = 0) : p((const char *)p_), size(size_), row(ld_ ? row_ : size_), ld(ld_) {}
 };
 Range matrix(const void *p, long long rows, long long cols, long long ld, size_t es)
 {
-    return Range{(const char *)p, p && rows > 0 ? (size_t)((rows - 1) * ld + cols) * es : 0};
+    if (!p || rows <= 0) return Range();
+    return Range(p, (size_t)((rows - 1) * ld + cols) * es, (size_t)cols * es, rows > 1 && ld > cols ? (size_t)ld * es : 0);
 }
-bool overlap(const Range &a, const Range &b) { return a.size && b.size && a.p < b.p + b.size && b.p < a.p + a.size; }
+// Columns beside each other in one wider tensor are apart though their ranges meet: with the same distance of rows (or one piece on
+// one side) the two sets of pieces are compared inside one distance.
+bool overlap(const Range &a, const Range &b)
+{
+    if (!a.size || !b.size || a.p >= b.p + b.size || b.p >= a.p + a.size) return false;
+    if (a.ld != b.ld && a.ld && b.ld) return true;
+    const size_t ld = a.ld ? a.ld : b.ld;
+    if (!ld) return true;
+    const size_t at = a.p <= b.p ? (size_t)(b.p - a.p) % ld : (ld - (size_t)(a.p - b.p) % ld) % ld;   // of b's pieces behind a's
+    return at < a.row || at + b.row > ld;
+}
 // rows that lie ld elements apart: offsets, in bytes too, stay far inside 64 bits
 bool spread_ok(long long rows, long long ld)
 {
@@ -115,7 +128,7 @@ kfac_status kfac_embedding(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id
     if (n == 0) return KFAC_OK;
     if (!ids || !table || !out || !aligned(ids, id_bits / 8) || !aligned(table, esize(table_type)) || !aligned(out, esize(out_type))) return KFAC_ERR_INVALID;
     const Range o = matrix(out, n, dim, ld_out, esize(out_type));
-    if (overlap(o, matrix(table, vocab, dim, ld_table, esize(table_type))) || overlap(o, Range{(const char *)ids, (size_t)n * (id_bits / 8)}))
+    if (overlap(o, matrix(table, vocab, dim, ld_table, esize(table_type))) || overlap(o, Range{ids, (size_t)n * (id_bits / 8)}))
         return KFAC_ERR_INVALID;
     return timed(ctx, KFAC_K_EMBEDDING, 0, 0, (double)n * dim, (double)n * dim * (esize(table_type) + esize(out_type)), [&] {
         return launch_embedding(ids, id_bits, n, vocab, dim, table_type == KFAC_BF16, table, ld_table, scale, out_type == KFAC_BF16, out, ld_out,

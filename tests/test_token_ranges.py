@@ -26,3 +26,18 @@ def test_distances_of_rows_that_no_tensor_has(h):
     grad = lambda n, ld: kfac.lib().kfac_embedding_grad(h, n, P, 64, 10, 16, 0, Q, ld, 1.0, 0, R, 0.5, S)  # noqa: E731
     assert grad(1 << 29, far) == INV and grad(1 << 24, 1 << 17) == INV
     assert grad(1, far) == WS and grad(1 << 20, 1 << 20) == WS                  # no reason to refuse these: 256 bytes hold no lists
+
+
+def test_columns_that_overlap_are_refused(h):
+    """Views of one tensor whose columns meet, or whose rows lie differently far apart."""
+    L = ctypes.addressof(kfac.kfac_layer(*wl.fc_layer(1, 16, 16)))
+    dropout = lambda y, ldy=64, x=P, ldx=64: kfac.lib().kfac_dropout(h, 4, 16, 0, x, ldx, None, 0, 0.1, 1, 2, y, ldy)  # noqa: E731
+    for at in (4, 60, 64 * 4 - 4, 64 * 4 + 4, 2 * 64 * 4 - 60):                 # bytes: rows are 256 bytes apart and 64 long
+        assert dropout(P + at) == INV and dropout(P, x=P + at) == INV, at
+    assert dropout(P + 64, ldy=65) == INV and dropout(P + 64, ldy=16) == INV
+    forward = lambda y, x=P, W=Q: kfac.lib().kfac_expert_forward(h, L, 2, 8, 1, 0, None, S, x, 64, W, 64, y, 64)  # noqa: E731
+    for at in (4, 60, 252, 260):
+        assert forward(P + at) == INV and forward(Q + at) == INV and forward(P, x=P + at) == INV, at
+    # a list of ids inside the rows of the output, and one that is longer than what lies between them
+    lookup = lambda ids, n: kfac.lib().kfac_embedding(h, n, ids, 64, 10, 16, 0, Q, 16, 1.0, 0, R, 64)  # noqa: E731
+    assert lookup(R + 32, 8) == INV and lookup(R + 64, 40) == INV
