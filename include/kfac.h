@@ -452,7 +452,8 @@ void kfac_refresh_advance(kfac_refresh_state *s, double ratio_m1, double ratio_m
  * received, and its factors, inverses and preconditioned gradients go through kfac_invert and kfac_precondition as those of
  * any layer.  All work goes to the context's stream; the number of launches does not depend on device data, nothing is read
  * back and nothing is allocated.  Tensors with an ld argument are row-major with rows ld elements apart (a view of a wider
- * tensor; its columns beside those of another argument do not overlap it); any alignment to whole elements serves.  Results do not depend on the order in which threads arrive.
+ * tensor; its columns beside those of another argument do not overlap it); any alignment to whole elements serves.  Results
+ * do not depend on the order in which threads arrive.
  */
 
 /*

@@ -682,10 +682,11 @@ def _weights(W: torch.Tensor, L: kfac_layer, experts: int, dtype) -> int:
     """The distance of the rows of W [experts, c_out, c_in + bias or more]."""
     if not W.is_cuda or W.dtype != dtype or W.dim() != 3 or W.shape[0] != experts or W.shape[1] != L.c_out or W.shape[2] < L.c_in + L.bias:
         raise ValueError("W must be a device tensor of %s and shape [%d, %d, at least %d]" % (dtype, experts, L.c_out, L.c_in + L.bias))
-    s = W.stride()
-    if s[2] != 1 or s[1] < L.c_in + L.bias or (experts > 1 and s[0] != L.c_out * s[1]):
+    s, cols = W.stride(), L.c_in + L.bias
+    ld = s[1] if L.c_out > 1 else s[0] if experts > 1 else cols     # (strides of length-one dimensions say nothing)
+    if (W.shape[2] > 1 and s[2] != 1) or ld < cols or (experts > 1 and s[0] != L.c_out * ld):
         raise ValueError("W must have contiguous rows, equally far apart over all experts")
-    return s[1]
+    return ld
 
 
 def kfac_expert_workspace_bytes(layer, experts: int, n: int) -> int:
