@@ -69,17 +69,22 @@ size_t embedding_grad_scratch(char *base, int n, int vocab, int dim, SegmentScra
     return used;
 }
 
-// What the four expert calls share.  x_rows: rows of x.
-bool expert_ok(const kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type, const int32_t *offsets)
+// Experts that the calls take.
+bool experts_ok(const kfac_layer *L, int32_t experts, int32_t n)
 {
-    if (!ctx || !L || !offsets || !aligned(offsets, 4) || !type_ok(type)) return false;
-    if (kfac_layer_dims(L, nullptr, nullptr, nullptr, nullptr) != KFAC_OK) return false;
+    if (!L || kfac_layer_dims(L, nullptr, nullptr, nullptr, nullptr) != KFAC_OK) return false;
     if (L->k != 1 || L->stride != 1 || L->pad != 0 || L->h_in != 1 || L->w_in != 1) return false;
-    if (experts < 1 || experts > kMaxExperts || n < 0 || n > kMaxPositions || fan < 1 || n % fan != 0) return false;
+    if (experts < 1 || experts > kMaxExperts || n < 0 || n > kMaxPositions) return false;
     // tiles of one launch, 64 x 64 elements at least
     const long long ti = (L->c_in + 63) / 64, to = (L->c_out + 63) / 64;
     if (((long long)n / 64 + experts + 1) * std::max(ti, to) >= (1LL << 30)) return false;
     return experts * (ti * to + ti * (ti + 1) / 2 + to * (to + 1) / 2 + 16) < (1LL << 30);
+}
+
+// What the four expert calls share.
+bool expert_ok(const kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type, const int32_t *offsets)
+{
+    return ctx && offsets && aligned(offsets, 4) && type_ok(type) && experts_ok(L, experts, n) && fan >= 1 && n % fan == 0;
 }
 
 ExpertArgs expert_args(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, const int32_t *order, const int32_t *offsets)
@@ -211,8 +216,7 @@ kfac_status kfac_dropout(kfac_ctx *ctx, int64_t rows, int64_t cols, kfac_dtype t
 
 size_t kfac_expert_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n)
 {
-    if (!L || kfac_layer_dims(L, nullptr, nullptr, nullptr, nullptr) != KFAC_OK || experts < 1 || experts > kMaxExperts || n < 0 || n > kMaxPositions) return 0;
-    return 256;
+    return experts_ok(L, experts, n) ? 256 : 0;   // (they use none; 0 is for what they refuse)
 }
 
 kfac_status kfac_expert_forward(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type, const int32_t *order,
@@ -282,7 +286,7 @@ kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t expert
     a.x = x; a.ldx = ldx; a.dy = grad_out; a.ldy = ldg;
     a.A = A_ema; a.G = G_ema; a.decay = decay;
     const double fa = A_ema ? (double)dA * dA : 0.0, fg = G_ema ? (double)dG * dG : 0.0;
-    return run_expert(ctx, EXPERT_STATS, a, in, n * (fa + fg), es * ((double)rx.size + rg.size) / es + 4.0 * experts * (fa + fg)) ? KFAC_OK
+    return run_expert(ctx, EXPERT_STATS, a, in, n * (fa + fg), (double)rx.size + rg.size + 4.0 * experts * (fa + fg)) ? KFAC_OK
                                                                                                                                : KFAC_ERR_DEVICE;
 }
 

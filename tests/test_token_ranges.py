@@ -41,3 +41,11 @@ def test_columns_that_overlap_are_refused(h):
     # a list of ids inside the rows of the output, and one that is longer than what lies between them
     lookup = lambda ids, n: kfac.lib().kfac_embedding(h, n, ids, 64, 10, 16, 0, Q, 16, 1.0, 0, R, 64)  # noqa: E731
     assert lookup(R + 32, 8) == INV and lookup(R + 64, 40) == INV
+
+
+def test_workspace_of_experts_that_the_calls_refuse():
+    """No size for what no call of the experts takes: layers that are not fully connected, more tiles than a launch has."""
+    size = kfac.kfac_expert_workspace_bytes
+    assert size(wl.fc_layer(1, 64, 32), 4, 100) > 0 and size(wl.fc_layer(1, 64, 32, 1), 1 << 16, 0) > 0
+    assert size(wl.conv_layer(1, 64, 32, 3, 1, 1, 8), 4, 100) == 0 and size(wl.conv_layer(1, 64, 32, 1, 1, 0, 8), 4, 100) == 0
+    assert size(wl.fc_layer(1, 64, 1 << 20), 1 << 16, 1 << 30) == 0
