@@ -1,6 +1,7 @@
 // Embedding lookup with scaling, and the gradient of its table by sorted tokens.
 //
-// Lookup: out[i] = scale * T[ids[i]].  A wave per 16-byte piece of 64 lanes of a row; reads the distinct rows, writes all.
+// Lookup: out[i] = scale * T[ids[i]].  A thread takes a piece of a row, eight elements where both are bf16 and four otherwise; the
+// pieces of all rows follow each other.  Reads the distinct rows, writes all.
 //
 // Gradient: dT[v] = scale * sum over the positions of token v, added in fp32 in the order of the positions, without atomics.
 // The positions come sorted by token.  A wave takes a run of `chunk` sorted positions and one 64-lane piece of the columns,
@@ -286,7 +287,9 @@ hipError_t launch_embedding(const void *ids, int id_bits, int n, int vocab, int 
                          : lookup_types((const int *)ids, n, vocab, dim, table_bf16, table, ldt, scale, out_bf16, out, ldo, s);
 }
 
-// Short runs where there are few positions, so that there are waves enough; long ones leave fewer parts to join.
+// Short runs where there are few positions, so that there are waves enough; long ones leave fewer parts to join.  The whole gradient of a
+// table of 32000 tokens in bf16, runs of 8 and of 32 positions: 256 wide 36 and 47 us for 8192 positions, 59 and 62 for 32768, 75 and 68
+// for 65536; 1024 wide 40 and 50, 87 and 79, 122 and 105.  (In fp32 34 and 39, 59 and 58, 75 and 62; 40 and 41, 96 and 89, 143 and 122.)
 constexpr int kShortRuns = 32768;
 int embedding_chunk(int n) { return n <= kShortRuns ? 8 : 32; }
 int embedding_most_chunks(int n)

@@ -1000,10 +1000,13 @@ hipError_t run_general(const ExpertArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-// 128 x 128 tiles where there are two for each CU, smaller ones otherwise (fp32 2051 rows 515 -> 1000 of 8 uneven experts: 47, 88 and
-// 141 us for the three products with the large ones, 32, 49 and 66 with the small ones and one group, 36, 38 and 46 with two).
-// Contractions over rows of few tiles are chains as long as the longest expert: four groups (512 tiles at most; fp32 factors of 2053
-// rows, 448 tiles: 55, 36 and 27 us with one, two and four; of 2048 rows, 1376 tiles: 42 with two, 59 with four).
+// 128 x 128 tiles where there are two for each CU, smaller ones otherwise: fp32 2051 rows 515 -> 1000 of 8 uneven experts take 47, 88 and
+// 141 us for the three products with the large ones (200, 125 and 320 tiles), 32, 49 and 66 with the small ones and one group, 36, 38 and
+// 46 with two.  Even experts, small with two groups and large: forward 135 and 150 us at 657 large tiles, 249 and 230 at 1241; weights 21.5
+// and 21.8 at 512, 88 and 112 at 640, 55 and 53 at 1408; factors 27 and 28 at 512, 117 and 130 at 896.
+// Contractions over rows of few tiles are chains as long as the longest expert: four groups up to 512 small tiles.  Uneven experts, fp32
+// factors of 2053 rows, 448 tiles: 55, 36 and 27 us with one, two and four; of 2048 rows, 1376 tiles: 42 with two, 59 with four.  Even
+// experts, four and two: weights 15 and 20 us at 64 tiles, 11 and 13 at 256, 19 and 15.5 at 512, 32 and 25 at 832.
 template <typename T, bool FP32, ExpertOp OP>
 hipError_t general(const ExpertArgs &a, hipStream_t s)
 {
@@ -1033,7 +1036,10 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes
     int tj;
     if (bf16 && direct_ok(op, a)) {
         // 256 x 256 tiles need half the traffic of 128 x 128, but one of them fills a CU: only where there is one for each of the 256
-        // (16384 rows 1024 -> 2048 of 16 experts, forward: 72 us, 83 with 128 x 128; 2048 rows 1024 -> 1024 of 8: 27 and 17)
+        // (16384 rows 1024 -> 2048 of 16 even experts, forward: 72 us, 83 with 128 x 128; uneven ones, whose last round is partial: 92 and
+        // 86; 4096 rows 2048 -> 2048, 264 tiles: 54 and 56; 2048 rows 1024 -> 1024 of 8, 68 tiles: 28 and 17).  Weights of 16384 rows,
+        // uneven: 113 and 103 us at 128 tiles, 69 and 78 at 256, 96 and 144 at 512; factors 137 and 136 at 192, 107 and 119 at 384, 218 and
+        // 268 at 768.
         const bool full = count_tiles<256, 256>(op, a, tj) >= 256;
         if (op == EXPERT_GRAD_WEIGHT || op == EXPERT_STATS) return full ? run_direct_rows<256, 256, 4, 2>(op, a, s) : run_direct_rows<128, 128, 2, 2>(op, a, s);
         if (full) return run_direct<256, 256, 4, 2>(op, a, s);

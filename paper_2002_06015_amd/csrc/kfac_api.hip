@@ -2860,7 +2860,7 @@ namespace kfac {
 
 CtxView ctx_view(const kfac_ctx *ctx) { return CtxView{ctx->stream, ctx->ws, ctx->ws_bytes, ctx->tun.split != 0}; }
 
-bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, double flops, double bytes)
+bool profile_begin(kfac_ctx *ctx, int kernel, int variant, double flops, double bytes)
 {
     if (!ctx->profiling) return true;
     try {
@@ -2874,7 +2874,6 @@ bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, doubl
         kfac_profile_entry pe{};
         pe.kernel = kernel;
         pe.variant = variant;
-        pe.workgroups = workgroups;
         pe.flops = flops;
         pe.bytes = bytes;
         ctx->prof.push_back(pe);

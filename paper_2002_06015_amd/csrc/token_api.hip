@@ -47,9 +47,9 @@ bool aligned(const void *p, size_t es) { return (uintptr_t)p % es == 0; }
 
 // One launch between the profiler's events
 template <typename F>
-bool timed(kfac_ctx *ctx, int kernel, int variant, int workgroups, double flops, double bytes, F launch)
+bool timed(kfac_ctx *ctx, int kernel, int variant, double flops, double bytes, F launch)
 {
-    return profile_begin(ctx, kernel, variant, workgroups, flops, bytes) && launch() == hipSuccess && profile_end(ctx);
+    return profile_begin(ctx, kernel, variant, flops, bytes) && launch() == hipSuccess && profile_end(ctx);
 }
 
 bool segments_ok(int32_t n, int32_t num) { return n >= 0 && n <= kMaxPositions && num >= 1 && num < (1 << 30); }
@@ -99,7 +99,7 @@ ExpertArgs expert_args(const kfac_layer *L, int32_t experts, int32_t n, int32_t 
 bool run_expert(kfac_ctx *ctx, ExpertOp op, const ExpertArgs &a, kfac_dtype type, double flops, double bytes)
 {
     const CtxView c = ctx_view(ctx);
-    return timed(ctx, KFAC_K_EXPERT, (int)op, 0, flops, bytes, [&] { return launch_expert(op, a, type == KFAC_BF16, c.fp32_planes, c.stream); });
+    return timed(ctx, KFAC_K_EXPERT, (int)op, flops, bytes, [&] { return launch_expert(op, a, type == KFAC_BF16, c.fp32_planes, c.stream); });
 }
 
 }  // namespace
@@ -120,7 +120,7 @@ kfac_status kfac_segments(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id_
     const CtxView c = ctx_view(ctx);
     SegmentScratch w;
     if (segment_scratch(c.ws, n, num, &w) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
-    return timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, (double)in.size + o.size + f.size,
+    return timed(ctx, KFAC_K_SEGMENTS, 0, 0.0, (double)in.size + o.size + f.size,
                  [&] { return launch_segments(ids, id_bits, n, num, w, order, nullptr, offsets, nullptr, c.stream); }) ? KFAC_OK : KFAC_ERR_DEVICE;
 }
 
@@ -135,7 +135,7 @@ kfac_status kfac_embedding(kfac_ctx *ctx, int32_t n, const void *ids, int32_t id
     const Range o = matrix(out, n, dim, ld_out, esize(out_type));
     if (overlap(o, matrix(table, vocab, dim, ld_table, esize(table_type))) || overlap(o, Range{ids, (size_t)n * (id_bits / 8)}))
         return KFAC_ERR_INVALID;
-    return timed(ctx, KFAC_K_EMBEDDING, 0, 0, (double)n * dim, (double)n * dim * (esize(table_type) + esize(out_type)), [&] {
+    return timed(ctx, KFAC_K_EMBEDDING, 0, (double)n * dim, (double)n * dim * (esize(table_type) + esize(out_type)), [&] {
         return launch_embedding(ids, id_bits, n, vocab, dim, table_type == KFAC_BF16, table, ld_table, scale, out_type == KFAC_BF16, out, ld_out,
                                 ctx_view(ctx).stream);
     }) ? KFAC_OK : KFAC_ERR_DEVICE;
@@ -177,12 +177,12 @@ kfac_status kfac_embedding_grad(kfac_ctx *ctx, int32_t n, const void *ids, int32
     bool ok;
     if (n > 0) {
         const int *keys = nullptr;
-        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, 2.0 * in.size + written, [&] { return launch_segments(ids, id_bits, n, vocab, seg, pos, &keys, nullptr, &fill, c.stream); });
+        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0.0, 2.0 * in.size + written, [&] { return launch_segments(ids, id_bits, n, vocab, seg, pos, &keys, nullptr, &fill, c.stream); });
         a.keys = keys;
-        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 1, 0, (double)n * dim, moved, [&] { return launch_embedding_sum(a, c.stream); });
-        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 2, 0, 0.0, 0.0, [&] { return launch_embedding_join(a, c.stream); });
+        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 1, (double)n * dim, moved, [&] { return launch_embedding_sum(a, c.stream); });
+        ok = ok && timed(ctx, KFAC_K_EMBEDDING, 2, 0.0, 0.0, [&] { return launch_embedding_join(a, c.stream); });
     } else {
-        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0, 0.0, written, [&] { return launch_fill(fill, c.stream); });
+        ok = timed(ctx, KFAC_K_SEGMENTS, 0, 0.0, written, [&] { return launch_fill(fill, c.stream); });
     }
     return ok ? KFAC_OK : KFAC_ERR_DEVICE;
 }
@@ -210,7 +210,7 @@ kfac_status kfac_dropout(kfac_ctx *ctx, int64_t rows, int64_t cols, kfac_dtype t
     a.factor = a.threshold < 65536u ? (float)(65536.0 / (65536.0 - a.threshold)) : 0.f;
     a.seed = seed; a.offset = offset;
     const double e = (double)rows * cols;
-    return timed(ctx, KFAC_K_DROPOUT, 0, 0, 0.0, e * esize(type) * (residual ? 3 : 2),
+    return timed(ctx, KFAC_K_DROPOUT, 0, 0.0, e * esize(type) * (residual ? 3 : 2),
                  [&] { return launch_dropout(a, type == KFAC_BF16, ctx_view(ctx).stream); }) ? KFAC_OK : KFAC_ERR_DEVICE;
 }
 

@@ -18,8 +18,8 @@ struct CtxView {
     bool fp32_planes;   // fp32 products: planes, or the fp32 matrix instruction
 };
 CtxView ctx_view(const kfac_ctx *ctx);
-// around one launch: records its times while profiling is on (nothing otherwise); false: a HIP call failed
-bool profile_begin(kfac_ctx *ctx, int kernel, int variant, int workgroups, double flops, double bytes);
+// around one entry of the profile: records its times while profiling is on (nothing otherwise); false: a HIP call failed
+bool profile_begin(kfac_ctx *ctx, int kernel, int variant, double flops, double bytes);
 bool profile_end(kfac_ctx *ctx);
 
 // ---- segments: a stable sort of positions by a small key ----------------------------------------------
