@@ -1,0 +1,580 @@
+"""Performance cases of what surrounds the products of experts: routing, the join of their results, the norm in front of them, and
+activations kept in 8 bits for the backward pass and the statistics.
+
+A case names one operator as a training or serving program calls it:
+
+  route        tokens to their experts: scores, choice, gates
+  route_training   the same and the gradient of the logits from that of the gates
+  combine      every token's results of its experts, weighted by the gates, added to the residual stream
+  combine_training   the same and the gradients of the results and of the gates
+  norm         a branch added to the residual stream, root-mean-square norm of the sum
+  norm_training    the same, with the activations kept in 8 bits beside the norm's output or without them, the gradient of the
+               stream, the gradient of the norm's scale and its diagonal factor
+  keep         activations brought into 8 bits with a scale for 32 adjacent ones, and back
+  kept_weights gradient of the weights of experts whose inputs were kept in 8 bits
+  kept_factor  Kronecker factors A of experts whose inputs were kept in 8 bits
+
+`pad` is the number of elements by which rows are further apart than they are long.  8 bits: e4m3 values (four significant bits,
+448 at most) under a power-of-two scale 2^(byte - 127), the smallest that keeps the largest of its 32 values within 448.  With `own`
+false the operators are computed from elementary torch operations in 32 bits, the order of experts in 64.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+BYTES = {"f32": 4, "bf16": 2}
+KINDS = ("route", "route_training", "combine", "combine_training", "norm", "norm_training", "keep", "kept_weights", "kept_factor")
+EPS = 1e-5
+
+
+def _named(case, name):
+    return dict(case, name=name) if name else case
+
+
+def _route(kind, tokens, experts, fan, scores, dtype, groups=1, top_groups=1, group_best=1, bias=0, renormalise=1, scale=1.0, padding=0.0,
+           closed=0.0, pad=0, name=None):
+    return _named({"kind": kind, "tokens": tokens, "experts": experts, "fan": fan, "scores": scores, "dtype": dtype, "groups": groups,
+                   "top_groups": top_groups, "group_best": group_best, "bias": bias, "renormalise": renormalise, "scale": scale,
+                   "padding": padding, "closed": closed, "pad": pad}, name)
+
+
+def _combine(kind, tokens, fan, dim, dtype, stream, pad=0, name=None):
+    return _named({"kind": kind, "tokens": tokens, "fan": fan, "dim": dim, "dtype": dtype, "stream": stream, "pad": pad}, name)
+
+
+def _norm(kind, tokens, dim, dtype, stream, kept=0, pad=0, name=None):
+    return _named({"kind": kind, "tokens": tokens, "dim": dim, "dtype": dtype, "stream": stream, "kept": kept, "pad": pad}, name)
+
+
+def _keep(tokens, dim, dtype, pad=0, name=None):
+    return _named({"kind": "keep", "tokens": tokens, "dim": dim, "dtype": dtype, "pad": pad}, name)
+
+
+def _kept(kind, tokens, fan, experts, c_in, c_out, bias, dtype, skew=0.5, name=None):
+    return _named({"kind": kind, "tokens": tokens, "fan": fan, "experts": experts, "c_in": c_in, "c_out": c_out, "bias": bias, "dtype": dtype,
+                   "skew": skew}, name)
+
+
+def listed():
+    return [
+        # A decoding step of four sequences: nothing but latency.
+        _route("route", 4, 64, 2, "softmax", "bf16", name="route_4x64_bf16"),
+        # A training batch of a small layer, fp32 logits in a wider tensor, some padding tokens and closed experts.
+        _route("route_training", 8191, 16, 2, "softmax", "f32", padding=0.01, closed=0.02, pad=3, name="route_8191x16_f32"),
+        # Long sequences, many experts in groups, a bias that balances them.
+        _route("route_training", 65536, 256, 8, "sigmoid", "bf16", 8, 4, 2, 1, 1, 2.5, name="route_65536x256_bf16"),
+        # The join of a decoding step.
+        _combine("combine", 4, 2, 1024, "bf16", "bf16", name="combine_4x2_1024_bf16"),
+        # Odd rows, further apart than they are long, four experts a token.
+        _combine("combine_training", 2051, 4, 1001, "f32", "f32", 7, name="combine_2051x4_1001_f32"),
+        # The join of a large training batch, forward and backward.
+        _combine("combine_training", 32768, 2, 2048, "bf16", "bf16", name="combine_32768x2_2048_bf16"),
+        # The norm of a decoding step.
+        _norm("norm", 4, 1024, "bf16", "bf16", name="norm_4x1024_bf16"),
+        # A small fp32 layer with odd rows, further apart than they are long.
+        _norm("norm_training", 2053, 1001, "f32", "f32", 0, 7, name="norm_2053x1001_f32"),
+        # One training batch: bf16 activations, an fp32 residual stream, the norm's output kept in 8 bits too.
+        _norm("norm_training", 16384, 2048, "bf16", "f32", 1, name="norm_16384x2048_bf16_f32_kept"),
+        # The activations of a batch into 8 bits and back.
+        _keep(16384, 2048, "bf16", name="keep_16384x2048_bf16"),
+        # Gradient of the weights of one training batch of an expert layer.
+        _kept("kept_weights", 8192, 2, 16, 1024, 2048, 0, "bf16", name="kept_weights_8192x2_1024_2048_bf16"),
+        # Factors of the inputs of an expert layer with a bias.
+        _kept("kept_factor", 16384, 2, 16, 1024, 2048, 1, "bf16", name="kept_factor_16384x2_1024_bf16"),
+    ]
+
+
+# ---------------------------------------------------------------------------------------------- the range
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _width(rng, lo, hi):
+    c = _log_int(rng, lo, hi)
+    if rng.random() < 0.6 and c >= 64:   # most widths are whole numbers of blocks, the others any
+        c = c // 64 * 64
+    return c
+
+
+def _seconds(case):
+    """A rough time of a case, to bound what draw() gives."""
+    w = work(case)
+    return w["flops"] / (6e14 if case["kind"].startswith("kept") and case["dtype"] == "bf16" else 1e14) + w["bytes"] / 4e12
+
+
+def draw(rng):
+    most = max(_seconds(c) for c in listed())
+    while True:
+        kind = rng.choice(KINDS)
+        dtype = rng.choice(("f32", "bf16", "bf16"))
+        pad = rng.choice((0, 0, 0, 8, 3))
+        if kind.startswith("route"):
+            tokens = _log_int(rng, 1, 512) if kind == "route" else _log_int(rng, 64, 65536)
+            experts = rng.choice((4, 8, 16, 32, 60, 64, 128, 160, 256, 384, 512))
+            groups = rng.choice((1, 1, 2, 4, 8)) if experts >= 16 and experts % 8 == 0 else 1
+            top = rng.randint(max(1, groups // 4), groups)
+            fan = min(rng.choice((1, 2, 2, 4, 6, 8)), top * (experts // groups))
+            case = _route(kind, tokens, experts, fan, rng.choice(("softmax", "softmax", "sigmoid")), dtype, groups, top, rng.choice((1, 2)),
+                          int(rng.random() < 0.5), int(fan > 1 and rng.random() < 0.7), rng.choice((1.0, 1.0, 2.5)), rng.choice((0.0, 0.0, 0.02)),
+                          rng.choice((0.0, 0.0, 0.05)), pad)
+        elif kind.startswith("combine"):
+            tokens = _log_int(rng, 1, 512) if kind == "combine" else _log_int(rng, 64, 32768)
+            case = _combine(kind, tokens, rng.choice((1, 2, 2, 4, 6, 8)), _width(rng, 64, 8192), dtype, rng.choice((dtype, "f32")), pad)
+        elif kind.startswith("norm"):
+            tokens = _log_int(rng, 1, 512) if kind == "norm" else _log_int(rng, 64, 32768)
+            case = _norm(kind, tokens, _width(rng, 64, 8192), dtype, rng.choice((dtype, "f32")), int(kind == "norm_training" and rng.random() < 0.5), pad)
+        elif kind == "keep":
+            case = _keep(_log_int(rng, 1, 65536), _width(rng, 33, 8192), dtype, pad)
+        else:
+            experts = rng.choice((1, 4, 8, 16, 16, 32))
+            case = _kept(kind, _log_int(rng, 64, 16384), rng.choice((1, 2, 2, 4)) if experts > 2 else 1, experts, _width(rng, 64, 2048), _width(rng, 64, 2048),
+                         int(rng.random() < 0.4), dtype, rng.choice((0.25, 0.5, 1.0)))
+            longest = min(case["tokens"], case["tokens"] * case["fan"] * (1.0 + 4.0 * case["skew"]) / experts + 8)
+            if experts * longest * max(case["c_in"], case["c_out"]) > 1 << 29:
+                continue   # the padded plain form has to fit
+        if _seconds(case) <= most:
+            return case
+
+
+# ---------------------------------------------------------------------------------------------- what a pass has to move
+def work(case):
+    kind, s = case["kind"], BYTES[case["dtype"]]
+    if kind.startswith("route"):
+        n, E, k = case["tokens"], case["experts"], case["fan"]
+        nbytes, flops = n * E * s + 8 * n * k, 4.0 * n * E
+        if kind == "route_training":
+            nbytes, flops = nbytes + n * E * s + 4 * n * k, flops + 4.0 * n * E
+        return {"bytes": nbytes, "flops": flops}
+    if kind.startswith("combine"):
+        n, k, d, t = case["tokens"], case["fan"], case["dim"], BYTES[case["stream"]]
+        nbytes, flops = n * k * d * s + 2 * n * d * t + 4 * n * k, 2.0 * n * k * d
+        if kind == "combine_training":
+            nbytes, flops = nbytes + n * k * d * s + n * d * t + 4 * n * k, flops + 3.0 * n * k * d
+        return {"bytes": nbytes, "flops": flops}
+    if kind.startswith("norm"):
+        n, d, t = case["tokens"], case["dim"], BYTES[case["stream"]]
+        nbytes, flops = n * d * (2 * s + 2 * t) + 4 * d, 5.0 * n * d
+        if kind == "norm_training":
+            nbytes, flops = nbytes + n * d * (s + 2 * t) + 8 * d, flops + 12.0 * n * d
+            if case["kept"]:
+                nbytes += n * d * (1 + 1 / 32 + 2)
+        return {"bytes": nbytes, "flops": flops}
+    if kind == "keep":
+        e = case["tokens"] * case["dim"]
+        return {"bytes": e * (2 * s + 1 + 1 / 32), "flops": 3.0 * e}
+    T, n, E, ci, co, b = case["tokens"], case["tokens"] * case["fan"], case["experts"], case["c_in"], case["c_out"], case["bias"]
+    x = T * ci * (1 + 1 / 32)
+    if kind == "kept_weights":
+        return {"bytes": 4 * n + x + n * co * s + 4 * E * co * (ci + b), "flops": 2.0 * n * (ci + b) * co}
+    return {"bytes": 4 * n + x + 4 * E * (ci + b) ** 2, "flops": 1.0 * n * (ci + b) ** 2}
+
+
+# ---------------------------------------------------------------------------------------------- inputs
+def _rows(g, rows, cols, dtype, pad=0, scale=1.0):
+    """[rows, cols], the rows cols + pad elements apart."""
+    return torch.randn(rows, cols + pad, generator=g, device="cuda").mul_(scale).to(dtype)[:, :cols]
+
+
+def _activations(g, rows, cols, dtype, pad=0):
+    """Values of a few channels ten times as large as those of the others."""
+    loud = torch.where(torch.rand(cols + pad, generator=g, device="cuda") < 0.02, 10.0, 1.0)
+    return torch.randn(rows, cols + pad, generator=g, device="cuda").mul_(loud).to(dtype)[:, :cols]
+
+
+def _to_8_bits(x):
+    """(e4m3 [rows, cols], scale bytes [rows, blocks of 32]) of values in 32 bits."""
+    rows, cols = x.shape
+    blocks = (cols + 31) // 32
+    v = torch.nn.functional.pad(x, (0, 32 * blocks - cols)).view(rows, blocks, 32)
+    m, k = torch.frexp(v.abs().amax(2))                     # amax = m 2^k, 1/2 <= m < 1; 448 = 7/8 2^9
+    e = torch.where(m > 0.875, k - 8, k - 9)
+    e = torch.where(m == 0, -117, e).clamp(-117, 119)
+    q = torch.ldexp(v, -e[:, :, None]).clamp(-448, 448).to(torch.float8_e4m3fn)
+    return q.view(rows, -1)[:, :cols], (e + 127).to(torch.uint8)
+
+
+def _from_8_bits(q, scales):
+    rows, cols = q.shape
+    e = (scales.to(torch.int32) - 127).repeat_interleave(32, 1)[:, :cols]
+    return torch.ldexp(q.float(), e)
+
+
+def _inputs(case, seed):
+    """The tensors of a case, from the seed alone."""
+    kind, dtype = case["kind"], TYPES[case["dtype"]]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1000003 * seed + 29)
+    rand = lambda *shape: torch.rand(*shape, generator=g, device="cuda")  # noqa: E731
+    if kind.startswith("route"):
+        n, E, k = case["tokens"], case["experts"], case["fan"]
+        logits = torch.randn(n, E + case["pad"], generator=g, device="cuda") + 0.5 * torch.randn(E + case["pad"], generator=g, device="cuda")
+        if case["closed"] > 0:
+            logits = logits.masked_fill(rand(*logits.shape) < case["closed"], -math.inf)
+        if case["padding"] > 0:
+            logits = logits.masked_fill(rand(n, 1) < case["padding"], -math.inf)
+        s = {"logits": logits.to(dtype)[:, :E], "bias": 0.1 * torch.randn(E, generator=g, device="cuda") if case["bias"] else None}
+        if kind == "route_training":
+            s["dgate"] = torch.randn(n, k, generator=g, device="cuda")
+        return s
+    if kind.startswith("combine"):
+        n, k, d, stream, pad = case["tokens"], case["fan"], case["dim"], TYPES[case["stream"]], case["pad"]
+        s = {"y": _rows(g, n * k, d, dtype, pad), "gate": torch.softmax(torch.randn(n, k, generator=g, device="cuda"), 1),
+             "residual": _rows(g, n, d, stream, pad)}
+        if kind == "combine_training":
+            s["dout"] = _rows(g, n, d, stream, pad, 1e-3)
+        return s
+    if kind.startswith("norm"):
+        n, d, stream, pad = case["tokens"], case["dim"], TYPES[case["stream"]], case["pad"]
+        s = {"x": _rows(g, n, d, dtype, pad), "residual": _activations(g, n, d, stream, pad), "gamma": 1.0 + 0.2 * torch.randn(d, generator=g, device="cuda")}
+        if kind == "norm_training":
+            s["dy"], s["dstream"] = _rows(g, n, d, dtype, pad, 1e-3), _rows(g, n, d, stream, pad, 1e-3)
+        return s
+    if kind == "keep":
+        return {"x": _activations(g, case["tokens"], case["dim"], dtype, case["pad"])}
+    T, fan, E = case["tokens"], case["fan"], case["experts"]
+    score = case["skew"] * torch.randn(E, generator=g, device="cuda") - torch.log(-torch.log(rand(T, E).clamp_(1e-7, 1 - 1e-7)))
+    choice = score.topk(fan, dim=1).indices.reshape(-1)
+    s = {"choice": choice, "order": torch.sort(choice, stable=True).indices.to(torch.int32)}
+    counts = torch.bincount(choice, minlength=E)
+    s["offsets"] = torch.nn.functional.pad(torch.cumsum(counts, 0), (1, 0)).to(torch.int32)
+    s["longest"] = max(1, int(counts.max()))
+    s["q"], s["scales"] = _to_8_bits(_activations(g, T, case["c_in"], dtype).float())
+    s["q"] = s["q"].contiguous()
+    if kind == "kept_weights":
+        s["dy"] = _rows(g, T * fan, case["c_out"], dtype, 0, 1e-3)
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s["case"] = case
+    if own:   # what a program that uses the library keeps: outputs, a context with its workspace
+        from paper_2002_06015_amd import kfac
+        s["lib"] = kfac
+        kind, dtype = case["kind"], TYPES[case["dtype"]]
+        new = dict(device="cuda")
+        need, layer = 256, (1, 1, 1, 1, 1, 0, 1, 1, 0)
+        if kind.startswith("route"):
+            n, E, k = case["tokens"], case["experts"], case["fan"]
+            s["router"] = kfac.router(E, k, groups=case["groups"], top_groups=case["top_groups"], group_best=case["group_best"],
+                                      scores=kfac.KFAC_ROUTE_SIGMOID if case["scores"] == "sigmoid" else kfac.KFAC_ROUTE_SOFTMAX,
+                                      renormalise=case["renormalise"], scale=case["scale"])
+            s["choice"], s["gate"] = torch.empty(n * k, dtype=torch.int32, **new), torch.empty(n, k, **new)
+            s["dlogits"] = torch.empty(n, E, dtype=dtype, **new)
+        elif kind.startswith("combine"):
+            n, k, d = case["tokens"], case["fan"], case["dim"]
+            s["out"] = torch.empty(n, d, dtype=TYPES[case["stream"]], **new)
+            if kind == "combine_training":
+                s["dresult"], s["dgate"] = torch.empty(n * k, d, dtype=dtype, **new), torch.empty(n, k, **new)
+        elif kind.startswith("norm"):
+            n, d = case["tokens"], case["dim"]
+            s["h"], s["out"] = torch.empty(n, d, dtype=TYPES[case["stream"]], **new), torch.empty(n, d, dtype=dtype, **new)
+            s["q"] = s["scales"] = None
+            if kind == "norm_training":
+                need = kfac.kfac_rms_norm_workspace_bytes(n, d)
+                s["dh"], s["dgamma"], s["F"] = torch.empty(n, d, dtype=TYPES[case["stream"]], **new), torch.empty(d, **new), torch.empty(d, **new)
+                if case["kept"]:
+                    s["q"] = torch.empty(n, d, dtype=torch.float8_e4m3fn, **new)
+                    s["scales"], s["back"] = torch.empty(n, (d + 31) // 32, dtype=torch.uint8, **new), torch.empty(n, d, dtype=torch.bfloat16, **new)
+        elif kind == "keep":
+            n, d = case["tokens"], case["dim"]
+            s["q"], s["scales"] = torch.empty(n, d, dtype=torch.float8_e4m3fn, **new), torch.empty(n, (d + 31) // 32, dtype=torch.uint8, **new)
+            s["back"] = torch.empty(n, d, dtype=dtype, **new)
+        else:
+            E, ci, co, b = case["experts"], case["c_in"], case["c_out"], case["bias"]
+            layer = (1, ci, co, 1, 1, 0, 1, 1, b)
+            need = kfac.kfac_kept_workspace_bytes(layer, E, case["tokens"] * case["fan"])
+            if kind == "kept_weights":
+                s["dW"] = torch.empty(E, co, ci + b, **new)
+            else:
+                s["A"] = torch.zeros(E, ci + b, ci + b, **new)
+        s["layer"] = layer
+        s["ctx"] = kfac.Context([layer], workspace_bytes=max(256, need))
+    return s
+
+
+# ---------------------------------------------------------------------------------------------- the pass
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+def _run_own(s):
+    kfac, case, ctx = s["lib"], s["case"], s["ctx"]
+    kind = case["kind"]
+    if kind.startswith("route"):
+        kfac.kfac_route(ctx, s["router"], s["logits"], s["choice"], s["gate"], bias=s["bias"])
+        if kind == "route":
+            return {"choice": s["choice"], "gate": s["gate"]}
+        kfac.kfac_route_grad(ctx, s["router"], s["logits"], s["choice"], s["dgate"], s["dlogits"])
+        return {"choice": s["choice"], "gate": s["gate"], "dlogits": s["dlogits"]}
+    if kind.startswith("combine"):
+        kfac.kfac_combine(ctx, s["y"], s["gate"], s["out"], residual=s["residual"])
+        if kind == "combine":
+            return {"out": s["out"]}
+        kfac.kfac_combine_grad(ctx, s["y"], s["gate"], s["dout"], s["dresult"], s["dgate"])
+        return {"out": s["out"], "dy": s["dresult"], "dgate": s["dgate"]}
+    if kind.startswith("norm"):
+        kfac.kfac_rms_norm(ctx, s["x"], s["gamma"], EPS, s["out"], residual=s["residual"], h=s["h"], q=s["q"], scales=s["scales"])
+        out = {"h": s["h"], "y": s["out"]}
+        if kind == "norm":
+            return out
+        if case["kept"]:
+            kfac.kfac_restore(ctx, s["q"], s["scales"], s["back"])
+            out["kept"] = s["back"]
+        kfac.kfac_rms_norm_grad(ctx, s["dy"], s["h"], s["gamma"], EPS, s["dh"], dstream=s["dstream"], dgamma=s["dgamma"], F=s["F"], decay=0.0)
+        return dict(out, dh=s["dh"], dgamma=s["dgamma"], F=s["F"])
+    if kind == "keep":
+        kfac.kfac_keep(ctx, s["x"], s["q"], s["scales"])
+        kfac.kfac_restore(ctx, s["q"], s["scales"], s["back"])
+        return {"kept": s["back"], "scales": s["scales"]}
+    if kind == "kept_weights":
+        kfac.kfac_expert_grad_weight_kept(ctx, s["layer"], s["order"], s["offsets"], s["q"], s["scales"], s["dy"], s["dW"], fan=case["fan"])
+        return {"dW": s["dW"]}
+    kfac.kfac_stats_expert_kept(ctx, s["layer"], s["order"], s["offsets"], s["q"], s["scales"], None, 0.0, s["A"], None, fan=case["fan"])
+    return {"A": s["A"]}
+
+
+def _plain_route(case, logits, bias):
+    """(choice, gate): experts in the order of their rank, equal ones by number."""
+    n, E = logits.shape
+    k, groups, best = case["fan"], case["groups"], case["group_best"]
+    open_ = logits > -math.inf
+    exact_scores = bias is not None or (groups > 1 and best > 1)
+    rank = logits.double()
+    if exact_scores:
+        rank = torch.sigmoid(rank) if case["scores"] == "sigmoid" else torch.softmax(rank, 1)
+        if bias is not None:
+            rank = rank + bias.double()
+    rank = torch.where(open_, rank, -math.inf)
+    if groups > 1:
+        top = torch.sort(rank.view(n, groups, E // groups), dim=2, descending=True).values[:, :, :best]
+        of_group = torch.where(top > -math.inf, top, 0.0).sum(2)
+        of_group = torch.where(top[:, :, 0] > -math.inf, of_group, -math.inf)
+        kept = torch.sort(of_group, dim=1, descending=True, stable=True).indices[:, :case["top_groups"]]
+        in_kept = torch.zeros(n, groups, dtype=torch.bool, device="cuda").scatter_(1, kept, True)
+        rank = torch.where(in_kept.repeat_interleave(E // groups, 1), rank, -math.inf)
+    ordered = torch.sort(rank, dim=1, descending=True, stable=True)
+    choice, there = ordered.indices[:, :k], ordered.values[:, :k] > -math.inf
+    x = logits.float()
+    picked = x.gather(1, choice)
+    if case["scores"] == "sigmoid":
+        gate = torch.where(there, torch.sigmoid(picked), 0.0)
+    else:
+        high = torch.where(there[:, :1], x.amax(1, keepdim=True), 0.0)
+        gate = torch.where(there, torch.exp(picked - high) / torch.exp(x - high).sum(1, keepdim=True), 0.0)
+    if case["renormalise"]:
+        gate = gate / torch.where(there[:, :1], gate.sum(1, keepdim=True), 1.0)
+    return torch.where(there, choice, -1), gate * case["scale"]
+
+
+def _plain_route_grad(case, logits, choice, dgate):
+    x, there, at = logits.float(), choice >= 0, choice.clamp(min=0)
+    picked = x.gather(1, at)
+    if case["scores"] == "sigmoid":
+        score = torch.where(there, torch.sigmoid(picked), 0.0)
+    else:
+        high = torch.where(there[:, :1], x.amax(1, keepdim=True), 0.0)
+        all_ = torch.where(there[:, :1], torch.exp(x - high), 0.0)
+        all_ = all_ / torch.where(there[:, :1], all_.sum(1, keepdim=True), 1.0)
+        score = torch.where(there, all_.gather(1, at), 0.0)
+    d = torch.where(there, dgate, 0.0) * case["scale"]
+    if case["renormalise"]:
+        total = torch.where(there[:, :1], score.sum(1, keepdim=True), 1.0)
+        d = torch.where(there, (d - (d * score).sum(1, keepdim=True) / total) / total, 0.0)
+    dx = torch.zeros_like(x)
+    if case["scores"] == "sigmoid":
+        return dx.scatter_add_(1, at, d * score * (1.0 - score))
+    return dx.scatter_add_(1, at, d * score) - all_ * (d * score).sum(1, keepdim=True)
+
+
+def _run_plain(s):
+    case = s["case"]
+    kind, dtype = case["kind"], TYPES[case["dtype"]]
+    if kind.startswith("route"):
+        choice, gate = _plain_route(case, s["logits"], s["bias"])
+        out = {"choice": choice.reshape(-1).to(torch.int32), "gate": gate}
+        if kind == "route_training":
+            out["dlogits"] = _plain_route_grad(case, s["logits"], choice, s["dgate"]).to(dtype)
+        return out
+    if kind.startswith("combine"):
+        n, k, d, stream = case["tokens"], case["fan"], case["dim"], TYPES[case["stream"]]
+        y, gate = s["y"].float().reshape(n, k, d), s["gate"]
+        out = {"out": (s["residual"].float() + (gate[:, :, None] * y).sum(1)).to(stream)}
+        if kind == "combine_training":
+            dout = s["dout"].float()
+            out["dy"] = (gate[:, :, None] * dout[:, None, :]).reshape(n * k, d).to(dtype)
+            out["dgate"] = (y * dout[:, None, :]).sum(2)
+        return out
+    if kind.startswith("norm"):
+        n, stream, gamma = case["tokens"], TYPES[case["stream"]], s["gamma"]
+        h = (s["x"].float() + s["residual"].float()).to(stream)
+        hf = h.float()
+        r = torch.rsqrt(hf.square().mean(1, keepdim=True) + EPS)
+        y = hf * r * gamma
+        out = {"h": h, "y": y.to(dtype)}
+        if kind == "norm_training":
+            if case["kept"]:
+                out["kept"] = _from_8_bits(*_to_8_bits(y)).to(torch.bfloat16)
+            dy, unit = s["dy"].float(), hf * r
+            g = dy * gamma
+            out["dh"] = (s["dstream"].float() + r * (g - unit * (g * unit).mean(1, keepdim=True))).to(stream)
+            per_token = dy * unit
+            out["dgamma"], out["F"] = per_token.sum(0), per_token.square().sum(0) / n
+        return out
+    if kind == "keep":
+        q, scales = _to_8_bits(s["x"].float())
+        return {"kept": _from_8_bits(q, scales).to(dtype), "scales": scales}
+    # the rows of every expert, padded to the longest
+    fan, E, b, order, offsets = case["fan"], case["experts"], case["bias"], s["order"], s["offsets"]
+    at = offsets[:E, None] + torch.arange(s["longest"], device="cuda", dtype=torch.int32)
+    there = at < offsets[1:, None]
+    slot = order[at.clamp(max=order.numel() - 1)]
+    xs = _from_8_bits(s["q"], s["scales"])[slot // fan] * there[:, :, None]
+    if b:
+        xs = torch.cat([xs, there[:, :, None].float()], 2)
+    if kind == "kept_weights":
+        return {"dW": torch.matmul((s["dy"][slot].float() * there[:, :, None]).transpose(1, 2), xs)}
+    return {"A": torch.matmul(xs.transpose(1, 2), xs) / (offsets[1:] - offsets[:-1]).clamp(min=1).float()[:, None, None]}
+
+
+# ---------------------------------------------------------------------------------------------- in 64 bits
+def _exact_values(q, scales):
+    """What bytes of e4m3 stand for, from their fields."""
+    byte = q.view(torch.uint8).to(torch.int64)
+    sign, field, low = 1.0 - 2.0 * (byte >> 7).double(), (byte >> 3) & 15, (byte & 7).double()
+    v = torch.where(field == 0, low * 2.0 ** -9, (8.0 + low) * torch.exp2((field - 10).double()))
+    power = torch.exp2(scales.double() - 127.0).repeat_interleave(32, 1)[:, :q.shape[1]]
+    return sign * v * power
+
+
+def _nearest_8_bits(v):
+    """Values in 64 bits rounded to e4m3 under the scale of their 32, as values in 64 bits; and the scales' exponents."""
+    rows, cols = v.shape
+    blocks = (cols + 31) // 32
+    high = torch.zeros(rows, blocks * 32, dtype=torch.float64, device="cuda")
+    high[:, :cols] = v.abs()
+    high = high.view(rows, blocks, 32).amax(2)
+    e = torch.full_like(high, -117.0)
+    for step in range(-116, 120):
+        e = torch.where(high > 448.0 * 2.0 ** (step - 1), float(step), e)
+    power = torch.exp2(e).repeat_interleave(32, 1)[:, :cols]
+    u = v / power
+    binade = torch.floor(torch.log2(u.abs().clamp(min=2.0 ** -20))).clamp(min=-6.0)
+    binade = torch.where(torch.exp2(binade) > u.abs(), (binade - 1).clamp(min=-6.0), binade)
+    step = torch.exp2(binade - 3.0)
+    return torch.round(u / step) * step * power, e      # (round: halves to even)
+
+
+def _exact_route(case, s):
+    x = s["logits"].double()
+    n, E = x.shape
+    k, groups, f64 = case["fan"], case["groups"], dict(dtype=torch.float64, device="cuda")
+    sigmoid = case["scores"] == "sigmoid"
+    shut = torch.isneginf(x)
+    e = torch.where(shut, torch.zeros((), **f64), torch.exp(x if not sigmoid else -x.abs()))
+    if sigmoid:
+        score = torch.where(x >= 0, 1.0 / (1.0 + e), e / (1.0 + e))
+    else:
+        score = e / e.sum(1, keepdim=True).clamp(min=1e-300)
+    score = torch.where(shut, 0.0, score)
+    rank = x.clone() if s["bias"] is None and (groups == 1 or case["group_best"] == 1) else score + (0.0 if s["bias"] is None else s["bias"].double())
+    rank[shut] = -math.inf
+    numbers = torch.arange(E, device="cuda").expand(n, E)
+
+    def take_best(values, ids, limit):
+        high = values.amax(1, keepdim=True)
+        first = torch.where(values == high, ids, limit).amin(1, keepdim=True)
+        return high, first
+
+    if groups > 1:
+        left = rank.view(n * groups, E // groups).clone()
+        inside = torch.arange(E // groups, device="cuda").expand_as(left)
+        total, any_ = torch.zeros(n * groups, 1, **f64), None
+        for _ in range(case["group_best"]):
+            high, first = take_best(left, inside, E)
+            any_ = high > -math.inf if any_ is None else any_
+            total = total + torch.where(high > -math.inf, high, 0.0)
+            left.scatter_(1, first, -math.inf)
+        total = torch.where(any_, total, -math.inf).view(n, groups)
+        open_groups = torch.zeros(n, groups, dtype=torch.bool, device="cuda")
+        which = torch.arange(groups, device="cuda").expand(n, groups)
+        taken = torch.zeros(n, groups, dtype=torch.bool, device="cuda")
+        for _ in range(case["top_groups"]):
+            _, first = take_best(torch.where(taken, -math.inf, total), torch.where(taken, groups, which), groups)
+            first = first.clamp(max=groups - 1)
+            taken.scatter_(1, first, True)
+            open_groups.scatter_(1, first, True)
+        rank = rank.masked_fill(~open_groups[:, torch.arange(E, device="cuda") // (E // groups)], -math.inf)
+    chosen = []
+    for _ in range(k):
+        high, first = take_best(rank, numbers, E - 1)
+        chosen.append(torch.where(high > -math.inf, first, -1))
+        rank = rank.scatter(1, first, -math.inf)
+    chosen = torch.cat(chosen, 1)
+    there, at = chosen >= 0, chosen.clamp(min=0)
+    mine = torch.where(there, score.gather(1, at), 0.0)
+    total = mine.sum(1, keepdim=True)
+    total = torch.where(total > 0, total, 1.0) if case["renormalise"] else torch.ones_like(total)
+    out = {"choice": None, "gate": case["scale"] * mine / total}
+    if case["kind"] == "route_training":
+        up = case["scale"] * torch.where(there, s["dgate"].double(), 0.0)
+        dscore = up / total
+        if case["renormalise"]:
+            dscore = torch.where(there, dscore - (up * mine).sum(1, keepdim=True) / total ** 2, 0.0)
+        full = torch.zeros(n, E, **f64).scatter_add_(1, at, dscore)
+        out["dlogits"] = full * score * (1.0 - score) if sigmoid else score * (full - (full * score).sum(1, keepdim=True))
+    return out
+
+
+def exact(case, seed):
+    s = _inputs(case, seed)
+    kind, f64 = case["kind"], torch.float64
+    if kind.startswith("route"):
+        return _exact_route(case, s)
+    if kind.startswith("combine"):
+        n, k, d = case["tokens"], case["fan"], case["dim"]
+        out = s["residual"].to(f64)
+        dy, dgate = torch.empty(n, k, d, dtype=f64, device="cuda"), torch.empty(n, k, dtype=f64, device="cuda")
+        for j in range(k):
+            mine, weight = s["y"][j::k].to(f64), s["gate"][:, j:j + 1].to(f64)
+            out = out + weight * mine
+            if kind == "combine_training":
+                up = s["dout"].to(f64)
+                dy[:, j], dgate[:, j] = weight * up, (mine * up).sum(1)
+        return {"out": out} if kind == "combine" else {"out": out, "dy": dy.view(n * k, d), "dgate": dgate}
+    if kind.startswith("norm"):
+        stream = TYPES[case["stream"]]
+        h = s["x"].to(f64) + s["residual"].to(f64)
+        out = {"h": h}
+        h = h.float().to(stream).to(f64)                   # the norm is that of the stream as it is written
+        length = torch.sqrt((h * h).sum(1, keepdim=True) / case["dim"] + EPS)
+        unit, gamma = h / length, s["gamma"].to(f64)
+        out["y"] = unit * gamma
+        if kind == "norm":
+            return out
+        if case["kept"]:
+            out["kept"] = _nearest_8_bits(unit * gamma)[0]
+        dy = s["dy"].to(f64)
+        along = (dy * gamma * unit).sum(1, keepdim=True) / case["dim"]
+        out["dh"] = s["dstream"].to(f64) + (dy * gamma - along * unit) / length
+        out["dgamma"], out["F"] = (dy * unit).sum(0), ((dy * unit) ** 2).sum(0) / case["tokens"]
+        return out
+    if kind == "keep":
+        return {"kept": _nearest_8_bits(s["x"].to(f64))[0], "scales": None}
+    fan, E, ci, co, b = case["fan"], case["experts"], case["c_in"], case["c_out"], case["bias"]
+    values = _exact_values(s["q"], s["scales"])
+    result = torch.zeros(E, co if kind == "kept_weights" else ci + b, ci + b, dtype=f64, device="cuda")
+    for e in range(E):
+        mine = torch.nonzero(s["choice"] == e).reshape(-1)
+        if not mine.numel():
+            continue
+        x = values[mine // fan]
+        if b:
+            x = torch.cat([x, torch.ones(x.shape[0], 1, dtype=f64, device="cuda")], 1)
+        result[e] = s["dy"][mine].to(f64).T @ x if kind == "kept_weights" else x.T @ x / mine.numel()
+    return {"dW": result} if kind == "kept_weights" else {"A": result}
