@@ -288,7 +288,7 @@ def prepare(case, seed):
         else:
             E, ci, co, b = case["experts"], case["c_in"], case["c_out"], case["bias"]
             layer = (1, ci, co, 1, 1, 0, 1, 1, b)
-            need = kfac.kfac_kept_workspace_bytes(layer, E, case["tokens"] * case["fan"])
+            need = kfac.kfac_kept_workspace_bytes(layer, E, case["tokens"] * case["fan"], case["fan"])
             if kind == "kept_weights":
                 s["dW"] = torch.empty(E, co, ci + b, **new)
             else:
