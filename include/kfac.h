@@ -539,6 +539,124 @@ kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t expert
                               float *G_ema);
 
 /*
+ * Around the products of experts: which experts a token goes to, the join of their results, the norm in front of them, and
+ * activations kept in 8 bits until the backward pass and the statistics have read them.  The rules of the token and expert
+ * layers hold here too.
+ */
+
+/*
+ * Routing.  For every token t with logits l[t, :]:
+ *   scores   s_e = exp(l_e) / sum_i exp(l_i), or sigmoid(l_e)
+ *   ranks    r_e = s_e + bias[e], compared as if formed in 64 bits; without a bias the order of the logits.  Equal ranks: the
+ *            lower number first.  An expert whose logit or bias is -infinity is closed.
+ *   groups   experts / groups adjacent experts form a group; its rank is the sum of its group_best (1 or 2) best r_e (as above; of one
+ *            logit, if there is no bias and group_best = 1), of what it has if fewer are open.  The top_groups best groups take part.
+ *   choice[t * fan + j]   the expert with the j-th best rank among them; -1 where no open one is left (kfac_segments puts these last,
+ *            kfac_expert_forward writes zeros)
+ *   gate[t * fan + j]     scale * s_e, without the bias; renormalise != 0: scale * s_e / (sum of the chosen s); 0 for a choice of -1
+ * A NaN among a token's logits or the ranks, or a softmax over a logit of +infinity, makes all its choices -1 and all its gates NaN.
+ * logits: dev [n, experts] of `type`, rows ld apart; bias: dev [experts] fp32 or NULL; choice: dev [n * fan] int32; gate: dev
+ * [n, fan] fp32.  Scores and sums in fp32 (ranks that are too near to each other for that in 64 bits).
+ */
+typedef enum { KFAC_ROUTE_SOFTMAX = 0, KFAC_ROUTE_SIGMOID = 1 } kfac_route_scores;
+typedef struct {
+    int32_t experts;       /* 1 .. 1024 */
+    int32_t fan;           /* 1 .. 32 experts a token goes to, at most those of top_groups groups */
+    int32_t groups;        /* 1: no groups; a divisor of experts */
+    int32_t top_groups;    /* 1 .. groups */
+    int32_t group_best;    /* 1 or 2 */
+    int32_t scores;        /* kfac_route_scores */
+    int32_t renormalise;   /* 0 or 1 */
+    float scale;
+} kfac_router;
+kfac_status kfac_route(kfac_ctx *ctx, const kfac_router *router, int32_t n, kfac_dtype type, const void *logits, int64_t ld, const float *bias,
+                       int32_t *choice, float *gate);
+/*
+ * Its gradient: dlogits[t, :] from dgate[t, :], with the choices taken as given (the ranks have none).
+ *   softmax, not renormalised   dl_e = s_e (u_e - sum_j u_j s_j),  u_e = scale * sum of dgate over the choices of e
+ *   sigmoid, not renormalised   dl_e = u_e s_e (1 - s_e)
+ *   renormalised                dl_e = sum over the choices j of e of scale w_j (dgate_j - sum_i dgate_i w_i), w_j = s_j / (sum of the
+ *                               chosen s); of sigmoids times (1 - s_e)
+ * A choice outside [0, experts) and what stands in its dgate have no part; a token without another one gets zeros.  dlogits: dev [n, experts] of `type`, rows ldd apart,
+ * every element is written; choice and dgate as kfac_route writes choice and gate.
+ */
+kfac_status kfac_route_grad(kfac_ctx *ctx, const kfac_router *router, int32_t n, kfac_dtype type, const void *logits, int64_t ld,
+                            const int32_t *choice, const float *dgate, void *dlogits, int64_t ldd);
+
+/*
+ * The join of the results of a token's experts.  n choices, choice t * fan + j is the j-th of token t:
+ *   out[t, :] = residual[t, :] + sum_j gate[t * fan + j] * y[t * fan + j, :]
+ * y: dev [n, dim] of `type`; gate: dev [n] fp32, or NULL for ones (dx of kfac_expert_grad_input is summed to the gradient of x that
+ * way); residual (or NULL) and out: dev [n / fan, dim] of out_type.  Sums in fp32 in the order of j, the residual last; one
+ * rounding.  out may be residual itself (same rows).
+ */
+kfac_status kfac_combine(kfac_ctx *ctx, int32_t n, int32_t fan, int32_t dim, kfac_dtype type, const void *y, int64_t ldy, const float *gate,
+                         kfac_dtype out_type, const void *residual, int64_t ldr, void *out, int64_t ldo);
+/*
+ * Its gradients:  dy[t * fan + j, :] = gate[t * fan + j] * dout[t, :]  (dev [n, dim] of `type`),
+ * dgate[t * fan + j] = sum_c dout[t, c] * y[t * fan + j, c]  (dev [n] fp32).  Either may be NULL: then dgate and y, or dy and gate, are
+ * not touched; gate = NULL as above.  The gradient of the residual is dout itself.
+ */
+kfac_status kfac_combine_grad(kfac_ctx *ctx, int32_t n, int32_t fan, int32_t dim, kfac_dtype type, const void *y, int64_t ldy, const float *gate,
+                              kfac_dtype out_type, const void *dout, int64_t ldd, void *dy, int64_t lddy, float *dgate);
+
+/*
+ * Activations in 8 bits.  A row is cut into blocks of 32 adjacent elements (the last may be shorter); a block has one scale 2^e, the
+ * least e in [-117, 119] for which its largest finite magnitude is at most 448 * 2^e, and holds the elements / 2^e as e4m3 (OCP FP8:
+ * four significant bits, 448 at most, 2^-9 at least), rounded to nearest, ties to even.  A scale is kept as the byte e + 127.
+ * Infinities and NaN are held as NaN and do not reach others of their block; magnitudes above 448 * 2^119 are held as that.  What is
+ * held is exact in bf16, q * 2^e.
+ * q: dev [rows, cols] bytes, rows ldq apart; scales: dev [rows, ceil(cols / 32)] bytes, rows lds apart.  kfac_restore gives
+ * the values back as `type`; both take any scale byte e + 127 from 10 to 246.
+ */
+kfac_status kfac_keep(kfac_ctx *ctx, int64_t rows, int32_t cols, kfac_dtype type, const void *x, int64_t ldx, uint8_t *q, int64_t ldq,
+                      uint8_t *scales, int64_t lds);
+kfac_status kfac_restore(kfac_ctx *ctx, int64_t rows, int32_t cols, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds,
+                         kfac_dtype type, void *x, int64_t ldx);
+
+/*
+ * kfac_expert_grad_weight and kfac_stats_expert for inputs x that were kept in 8 bits: q dev [n / fan, c_in] bytes and their scales, as
+ * kfac_keep or kfac_rms_norm write them; `type` is that of dy and grad_out.  Results are those of the plain calls for the values that
+ * the bytes stand for.  Dense layers: experts = 1, order = NULL, offsets = {0, n}.  Workspace: kfac_kept_workspace_bytes (0 for invalid
+ * arguments; never less for larger n or fewer choices a row).
+ */
+size_t kfac_kept_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan);
+kfac_status kfac_expert_grad_weight_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type,
+                                         const int32_t *order, const int32_t *offsets, const uint8_t *q, int64_t ldq, const uint8_t *scales,
+                                         int64_t lds, const void *dy, int64_t ldy, float *dW);
+kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype in,
+                                   const int32_t *order, const int32_t *offsets, const uint8_t *q, int64_t ldq, const uint8_t *scales,
+                                   int64_t lds, const void *grad_out, int64_t ldg, float decay, float *A_ema, float *G_ema);
+
+/*
+ * Root-mean-square norm of a residual stream, 1 <= dim <= 16384:
+ *   h[t, :] = x[t, :] + residual[t, :], rounded to stream_type;  without a residual (NULL) the norm is that of x, h is NULL and
+ *             stream_type is `type`
+ *   y[t, c] = gamma[c] h[t, c] / sqrt(mean_c h[t, c]^2 + eps)
+ * x: dev [n, dim] of `type`; residual, h: dev [n, dim] of stream_type; gamma: dev [dim] fp32; y: dev [n, dim] of `type`, or NULL;
+ * q, scales: y (before its rounding to `type`) in 8 bits as by kfac_keep, or both NULL; at least one of y and q.  Sums in fp32.
+ * h may be residual itself, and x if the types agree; y may be x if it is not h (same rows each).
+ */
+kfac_status kfac_rms_norm(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type, const void *x, int64_t ldx, kfac_dtype stream_type,
+                          const void *residual, int64_t ldr, void *h, int64_t ldh, const float *gamma, float eps, void *y, int64_t ldy,
+                          uint8_t *q, int64_t ldq, uint8_t *scales, int64_t lds);
+/*
+ * Its gradients.  With r = 1 / sqrt(mean_c h^2 + eps), u = r h, g = gamma dy:
+ *   dh[t, :]  = dstream[t, :] + r (g - u mean_c(g u))       the gradient of x and of the residual; dstream (or NULL): that of h from elsewhere
+ *   dgamma[c] = sum_t dy[t, c] u[t, c]
+ *   F_ema[c] <- decay F_ema[c] + (1 - decay) / n sum_t (dy[t, c] u[t, c])^2     the diagonal of gamma's Fisher matrix (Sec. 4.2, per unit), for
+ *               per-sample gradients dy as in kfac_stats; decay = 0 does not read it; n = 0 leaves it
+ * dy: dev [n, dim] of `type`; h: dev [n, dim] of stream_type, what the norm was taken of; dstream, dh: dev [n, dim] of stream_type;
+ * dgamma, F_ema: dev [dim] fp32, either may be NULL.  dh may be NULL; it may be dstream itself, or dy if the types agree (same rows).
+ * Sums in fp32 in an order that depends on n and dim only.  Workspace: kfac_rms_norm_workspace_bytes (0 for invalid arguments; never less
+ * for larger n or dim), none if dgamma and F_ema are NULL.
+ */
+size_t kfac_rms_norm_workspace_bytes(int32_t n, int32_t dim);
+kfac_status kfac_rms_norm_grad(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type, const void *dy, int64_t lddy, kfac_dtype stream_type,
+                               const void *h, int64_t ldh, const float *gamma, float eps, const void *dstream, int64_t ldr, void *dh,
+                               int64_t lddh, float *dgamma, float decay, float *F_ema);
+
+/*
  * Optional per-launch timing for benchmarks (not part of the method).  While enabled,
  * every kernel launch of this context is bracketed by HIP events on the context's stream.
  * kfac_profile_read waits for the stream, copies up to max_entries records (in launch
@@ -551,14 +669,16 @@ typedef enum {
     KFAC_K_GEMM_F32 = 0, KFAC_K_GEMM_BF16 = 1, KFAC_K_GEMM_REDUCE = 2, KFAC_K_PATCH = 3, KFAC_K_TRACE = 4,
     KFAC_K_COPY_DAMP = 5, KFAC_K_LEAF_INVERSE = 6, KFAC_K_ZERO = 7, KFAC_K_BN_UNIT = 8, KFAC_K_BN_REDUCE = 9,
     KFAC_K_PAD = 10, KFAC_K_ASSEMBLE = 11, KFAC_K_BORDER = 12, KFAC_K_STALENESS = 13, KFAC_K_PACK = 14, KFAC_K_UPDATE = 15, KFAC_K_BN_FULL = 16, KFAC_K_LAYOUT = 17, KFAC_K_GEMM_F32_SPLIT = 18,
-    KFAC_K_SEGMENTS = 19, KFAC_K_EMBEDDING = 20, KFAC_K_DROPOUT = 21, KFAC_K_EXPERT = 22
+    KFAC_K_SEGMENTS = 19, KFAC_K_EMBEDDING = 20, KFAC_K_DROPOUT = 21, KFAC_K_EXPERT = 22,
+    KFAC_K_ROUTE = 23, KFAC_K_COMBINE = 24, KFAC_K_NORM = 25, KFAC_K_KEEP = 26
 } kfac_kernel;
 
 typedef struct {
     int32_t kernel;    /* kfac_kernel */
     int32_t variant;   /* GEMM: 0 = 128x128 tiles, 1 = 64x64 tiles, 2 / 3 = 32x32 / 64x64 without LDS staging,
                         * 4 = the displaced products of one image together.  Embedding: 0 = lookup, 1 and 2 = the passes of
-                        * its gradient; experts: 0 = forward, 1 = grad_input, 2 = grad_weight, 3 = factors */
+                        * its gradient; experts: 0 = forward, 1 = grad_input, 2 = grad_weight, 3 = factors; route, combine:
+                        * 1 = gradient; norm: 1 and 2 = the passes of its gradient; keep: 1 = restore */
     int32_t workgroups;   /* 0: not reported (token and expert layers) */
     float ms;
     double flops;

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libkfac_hip.so")
 SOURCES = ["kfac_api.hip", "gemm_nt.hip", "gemm_direct.hip", "patch.hip", "corr.hip", "inverse.hip", "bn.hip", "stale.hip", "pack.hip", "update.hip", "bn_full.hip", "layout.hip",
-           "segments.hip", "embedding.hip", "dropout.hip", "expert.hip", "token_api.hip"]
+           "segments.hip", "embedding.hip", "dropout.hip", "expert.hip", "token_api.hip",
+           "route.hip", "combine.hip", "keep.hip", "rms_norm.hip", "block_api.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-unknown-warning-option", "-Wno-null-pointer-arithmetic"]

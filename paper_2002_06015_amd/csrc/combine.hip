@@ -1,0 +1,139 @@
+// The join of the results of a token's experts, out = residual + sum_j gate_j y_j, and its gradients dy_j = gate_j dout,
+// dgate_j = <dout, y_j>.
+//
+// Sums in fp32 in the order of j, one rounding; the products of a gate's gradient are added up by one wave (or one workgroup) in an
+// order that depends on the row's length only.  Both are bound by memory: every element is read or written once.
+#include <algorithm>
+
+#include "elements.h"
+#include "token_internal.h"
+
+namespace kfac {
+
+namespace {
+
+// A thread: eight elements of a token's row.
+template <typename T, typename S>
+__global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsigned per_row, unsigned long long units)
+{
+    for (unsigned long long u = (unsigned long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (unsigned long long)gridDim.x * 256) {
+        const long long token = (long long)(u / per_row);
+        const int c = 8 * (int)(u - token * per_row), there = a.dim - c;
+        float sum[8], v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum[q] = 0.f;
+        const T *y = (const T *)a.y + token * a.fan * a.ldy + c;
+        for (int j = 0; j < a.fan; ++j) {
+            load8(y + j * a.ldy, there, v);
+            const float g = a.gate ? a.gate[token * a.fan + j] : 1.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] = fmaf(g, v[q], sum[q]);
+        }
+        if (a.r) {
+            load8((const S *)a.r + token * a.ldr + c, there, v);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] += v[q];
+        }
+        store8((S *)a.out + token * a.ldo + c, there, sum);
+    }
+}
+
+// THREADS threads for FAN choices of a token.
+template <typename T, typename S, int THREADS, int FAN>
+__global__ __launch_bounds__(256) void combine_grad_kernel(const CombineArgs a)
+{
+    __shared__ float parts[4 * FAN];
+    const int me = threadIdx.x % THREADS, lane = threadIdx.x & 63;
+    const int sets = (a.fan + FAN - 1) / FAN;   // of choices, a token
+    const long long all = (long long)a.tokens * sets, stripe = (long long)gridDim.x * (256 / THREADS);
+    for (long long set = (long long)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS; set < all; set += stripe) {
+        const long long token = sets == 1 ? set : set / sets;
+        const int j0 = sets == 1 ? 0 : FAN * (int)(set - token * sets);
+        const S *dout = (const S *)a.dout + token * a.ldd;
+        const long long choice = token * a.fan + j0;
+        float g[FAN], dot[FAN];
+#pragma unroll
+        for (int j = 0; j < FAN; ++j) {
+            g[j] = a.gate && a.dy && j0 + j < a.fan ? a.gate[choice + j] : 1.f;
+            dot[j] = 0.f;
+        }
+        for (int c = 8 * me; c < a.dim; c += 8 * THREADS) {
+            float d[8], v[8];
+            load8(dout + c, a.dim - c, d);
+#pragma unroll
+            for (int j = 0; j < FAN; ++j) {
+                if (j0 + j >= a.fan) break;
+                if (a.dgate) {
+                    load8((const T *)a.y + (choice + j) * a.ldy + c, a.dim - c, v);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) dot[j] = fmaf(d[q], v[q], dot[j]);
+                }
+                if (a.dy) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = g[j] * d[q];
+                    store8((T *)a.dy + (choice + j) * a.lddy + c, a.dim - c, v);
+                }
+            }
+        }
+        if (!a.dgate) continue;
+#pragma unroll
+        for (int j = 0; j < FAN; ++j)
+            for (int o = 32; o > 0; o >>= 1) dot[j] += __shfl_xor(dot[j], o);
+        if constexpr (THREADS == 64) {
+#pragma unroll
+            for (int j = 0; j < FAN; ++j)
+                if (lane == j && j0 + j < a.fan) a.dgate[choice + j] = dot[j];
+        } else {
+            __syncthreads();
+            if (lane == 0)
+#pragma unroll
+                for (int j = 0; j < FAN; ++j) parts[(threadIdx.x >> 6) * FAN + j] = dot[j];
+            __syncthreads();
+            if (threadIdx.x < FAN && j0 + (int)threadIdx.x < a.fan)
+                a.dgate[choice + threadIdx.x] = parts[threadIdx.x] + parts[FAN + threadIdx.x] + parts[2 * FAN + threadIdx.x] + parts[3 * FAN + threadIdx.x];
+        }
+    }
+}
+
+template <typename T, typename S>
+hipError_t run(const CombineArgs &a, hipStream_t s)
+{
+    const unsigned per_row = (unsigned)(a.dim + 7) / 8;
+    const unsigned long long units = (unsigned long long)a.tokens * per_row, wgs = (units + 255) / 256;
+    combine_kernel<T, S><<<dim3((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20))), dim3(256), 0, s>>>(a, per_row, units);
+    return hipGetLastError();
+}
+
+template <typename T, typename S, int THREADS>
+hipError_t run_grad(const CombineArgs &a, hipStream_t s)
+{
+    constexpr int per = 256 / THREADS;
+    const long long sets = (long long)a.tokens * (a.fan <= 2 ? 1 : (a.fan + 3) / 4);
+    const dim3 grid((unsigned)std::min((sets + per - 1) / per, 1LL << 20)), block(256);   // a launch takes less than 2^32 threads
+    if (a.fan <= 1) combine_grad_kernel<T, S, THREADS, 1><<<grid, block, 0, s>>>(a);
+    else if (a.fan <= 2) combine_grad_kernel<T, S, THREADS, 2><<<grid, block, 0, s>>>(a);
+    else combine_grad_kernel<T, S, THREADS, 4><<<grid, block, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, typename S>
+hipError_t run_grad(const CombineArgs &a, hipStream_t s)
+{
+    return a.tokens >= 4096 || a.dim <= 512 ? run_grad<T, S, 64>(a, s) : run_grad<T, S, 256>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_combine(const CombineArgs &a, int bf16, int out_bf16, hipStream_t s)
+{
+    if (bf16) return out_bf16 ? run<bf16_bits, bf16_bits>(a, s) : run<bf16_bits, float>(a, s);
+    return out_bf16 ? run<float, bf16_bits>(a, s) : run<float, float>(a, s);
+}
+
+hipError_t launch_combine_grad(const CombineArgs &a, int bf16, int out_bf16, hipStream_t s)
+{
+    if (bf16) return out_bf16 ? run_grad<bf16_bits, bf16_bits>(a, s) : run_grad<bf16_bits, float>(a, s);
+    return out_bf16 ? run_grad<float, bf16_bits>(a, s) : run_grad<float, float>(a, s);
+}
+
+}  // namespace kfac

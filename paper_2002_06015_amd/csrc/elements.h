@@ -1,0 +1,145 @@
+// Eight adjacent elements of a row, in memory as fp32, bf16 or e4m3, in registers as fp32.  Any alignment to whole elements.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+namespace kfac {
+
+typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned short ushort8_u __attribute__((ext_vector_type(8), aligned(2)));
+typedef unsigned uint2_u __attribute__((ext_vector_type(2), aligned(1)));
+typedef unsigned short bf16_bits;
+
+template <typename T> struct Element;
+template <> struct Element<float> {
+    static __device__ __forceinline__ float get(const float *p) { return *p; }
+    static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
+    static __device__ __forceinline__ float round(float v) { return v; }
+};
+template <> struct Element<bf16_bits> {
+    static __device__ __forceinline__ float get(const bf16_bits *p) { return __uint_as_float((unsigned)*p << 16); }
+    static __device__ __forceinline__ void put(bf16_bits *p, float v) { *p = __builtin_bit_cast(bf16_bits, (__bf16)v); }
+    static __device__ __forceinline__ float round(float v) { return (float)(__bf16)v; }
+};
+
+// The first `there` of eight; zeros behind them.
+template <typename T>
+__device__ __forceinline__ void load8(const T *__restrict__ p, int there, float (&v)[8])
+{
+    if (there >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            const ushort8_u r = *(const ushort8_u *)p;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((unsigned)r[j] << 16);
+        } else {
+            const float4_u a = *(const float4_u *)p, b = *(const float4_u *)(p + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < there ? Element<T>::get(p + j) : 0.f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *__restrict__ p, int there, const float (&v)[8])
+{
+    if (there >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            ushort8_u r;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[j] = __builtin_bit_cast(bf16_bits, (__bf16)v[j]);
+            *(ushort8_u *)p = r;
+        } else {
+            float4_u a, b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { a[j] = v[j]; b[j] = v[4 + j]; }
+            *(float4_u *)p = a;
+            *(float4_u *)(p + 4) = b;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < there) Element<T>::put(p + j, v[j]);
+    }
+}
+
+// ---- blocks of 32 in 8 bits: lanes 4 i .. 4 i + 3 of a wave hold a block, eight elements each ------------
+// What a block's scale goes by: the bits of its largest finite magnitude.
+__device__ __forceinline__ unsigned finite_bits(float v)
+{
+    const unsigned a = __float_as_uint(v) & 0x7FFFFFFFu;
+    return a < 0x7F800000u ? a : 0u;
+}
+template <int CTRL>
+__device__ __forceinline__ unsigned from_lane(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+
+// e + 127 for the least e in [-117, 119] with magnitude <= 448 2^e (448 = 1.75 2^8)
+__device__ __forceinline__ int scale_byte(unsigned magnitude)
+{
+    const int e = (int)(magnitude >> 23) - 8 + ((magnitude & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return min(max(e, 127 - 117), 127 + 119);
+}
+__device__ __forceinline__ float power_of_two(int byte) { return __uint_as_float((unsigned)byte << 23); }
+
+// All lanes of a wave call it.  v: zeros behind the row's end.  Returns the block's scale byte; q: the eight bytes.
+__device__ __forceinline__ int to_8_bits(const float (&v)[8], uint2_u &q)
+{
+    unsigned high = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) high = max(high, finite_bits(v[j]));
+    high = max(high, from_lane<0xB1>(high));   // quad_perm 1 0 3 2
+    high = max(high, from_lane<0x4E>(high));   // quad_perm 2 3 0 1
+    const int byte = scale_byte(high);
+    const float inverse = power_of_two(254 - byte);
+    float u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float w = v[j] * inverse;
+        u[j] = (__float_as_uint(v[j]) & 0x7F800000u) == 0x7F800000u ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_fmed3f(w, -448.f, 448.f);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * j], u[4 * j + 1], 0, false);
+        q[j] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(u[4 * j + 2], u[4 * j + 3], r, true);
+    }
+    return byte;
+}
+
+// The values of eight bytes under a scale.
+__device__ __forceinline__ void from_8_bits(const uint2_u &q, int byte, float (&v)[8])
+{
+    const float scale = power_of_two(byte);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[j], true);
+        v[4 * j] = lo[0] * scale;
+        v[4 * j + 1] = lo[1] * scale;
+        v[4 * j + 2] = hi[0] * scale;
+        v[4 * j + 3] = hi[1] * scale;
+    }
+}
+
+// The first `there` of eight bytes.
+__device__ __forceinline__ void store_bytes(unsigned char *p, int there, const uint2_u &q)
+{
+    if (there >= 8) {
+        *(uint2_u *)p = q;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < there) p[j] = (unsigned char)(q[j >> 2] >> (8 * (j & 3)));
+    }
+}
+__device__ __forceinline__ uint2_u load_bytes(const unsigned char *p, int there)
+{
+    if (there >= 8) return *(const uint2_u *)p;
+    uint2_u q = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < there) q[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
+    return q;
+}
+
+}  // namespace kfac

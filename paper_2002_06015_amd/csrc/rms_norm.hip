@@ -1,0 +1,261 @@
+// Root-mean-square norm of a residual stream, and its gradients.
+//
+//   h = x + residual,  r = 1 / sqrt(mean h^2 + eps),  u = r h,  y = gamma u
+//   dh = dstream + r (g - u mean(g u)),  g = gamma dy;   dgamma = sum over tokens of dy u;   F = mean over tokens of (dy u)^2
+// h is rounded to the type of the stream before the norm is taken of it, so that the gradient, which reads the written h, belongs to
+// exactly what was computed; everything else is fp32, rounded once.  A row is read once and stays in the registers of the
+// wave (or workgroup) that has it.  Columns are summed over a workgroup's rows in its registers, then over the workgroups in the order
+// of their numbers by a second launch.  Bound by memory.
+#include <algorithm>
+
+#include "elements.h"
+#include "token_internal.h"
+
+namespace kfac {
+
+namespace {
+
+// The sum over the THREADS threads of a row, in all of them.
+template <int THREADS, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float *parts)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o);
+    if constexpr (THREADS > 64) {
+        constexpr int W = THREADS / 64;
+        __syncthreads();   // what was there has been read
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) parts[i * W + (threadIdx.x >> 6)] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) v[i] += parts[i * W + w];
+        }
+    }
+}
+
+__device__ __forceinline__ float inverse_root(float squares, int dim, float eps) { return 1.f / sqrtf(squares / (float)dim + eps); }
+
+// THREADS threads a row, CH chunks of eight elements each; workgroups of at least 256 threads.
+template <typename T, typename S, int THREADS, int CH>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(const NormArgs a)
+{
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    __shared__ float parts[THREADS / 64];
+    const int me = threadIdx.x % THREADS;
+    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS; row < a.n; row += (long long)gridDim.x * ROWS) {
+        float h[CH][8], sum[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = 8 * (me + THREADS * k), there = a.dim - c;
+            load8((const T *)a.x + row * a.ldx + c, there, h[k]);
+            if (a.r) {
+                float r[8];
+                load8((const S *)a.r + row * a.ldr + c, there, r);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[k][j] = Element<S>::round(h[k][j] + r[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[0] = fmaf(h[k][j], h[k][j], sum[0]);
+        }
+        row_sums<THREADS>(sum, parts);
+        const float r = inverse_root(sum[0], a.dim, a.eps);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = 8 * (me + THREADS * k), there = a.dim - c;
+            if (a.h) store8((S *)a.h + row * a.ldh + c, there, h[k]);
+            float g[8];
+            load8(a.gamma + c, there, g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] *= h[k][j] * r;
+            if (a.y) store8((T *)a.y + row * a.ldy + c, there, g);
+            if (a.q) {
+                uint2_u q;
+                const int byte = to_8_bits(g, q);
+                if (there > 0) store_bytes(a.q + row * a.ldq + c, there, q);
+                if (there > 0 && (threadIdx.x & 3) == 0) a.scales[row * a.lds + c / 32] = (unsigned char)byte;
+            }
+        }
+    }
+}
+
+// The rows `part`, part + parts, ...; COLUMNS: sums of the columns too.
+template <typename T, typename S, int THREADS, int CH, bool COLUMNS>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kernel(const NormGradArgs a)
+{
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    __shared__ float parts[2 * (THREADS / 64)], columns[COLUMNS && ROWS > 1 ? 8 * 256 : 1];
+    const int me = threadIdx.x % THREADS, stripe = gridDim.x * ROWS;
+    float first[COLUMNS ? CH : 1][8], second[COLUMNS ? CH : 1][8];
+    if constexpr (COLUMNS)
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) first[k][j] = second[k][j] = 0.f;
+    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS; row < a.n; row += stripe) {
+        float h[CH][8], d[CH][8], sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = 8 * (me + THREADS * k), there = a.dim - c;
+            load8((const S *)a.h + row * a.ldh + c, there, h[k]);
+            load8((const T *)a.dy + row * a.lddy + c, there, d[k]);
+            float g[8];
+            load8(a.gamma + c, there, g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sums[0] = fmaf(h[k][j], h[k][j], sums[0]);
+                sums[1] = fmaf(g[j] * d[k][j], h[k][j], sums[1]);
+            }
+        }
+        row_sums<THREADS>(sums, parts);
+        const float r = inverse_root(sums[0], a.dim, a.eps), along = r * r * (sums[1] / (float)a.dim);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = 8 * (me + THREADS * k), there = a.dim - c;
+            if constexpr (COLUMNS)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float p = d[k][j] * (h[k][j] * r);
+                    first[k][j] += p;
+                    second[k][j] = fmaf(p, p, second[k][j]);
+                }
+            if (a.dh) {
+                float g[8], o[8];
+                load8(a.gamma + c, there, g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = 0.f;
+                if (a.r) load8((const S *)a.r + row * a.ldr + c, there, o);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = fmaf(r, g[j] * d[k][j] - h[k][j] * along, o[j]);
+                store8((S *)a.dh + row * a.lddh + c, there, o);
+            }
+        }
+    }
+    if constexpr (COLUMNS) {
+        float *const out = a.partial + 2LL * blockIdx.x * a.dim;
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const int c = 8 * (me + THREADS * k);
+                float *const v = which ? second[k] : first[k];
+                if constexpr (ROWS > 1) {   // element j of thread t at 256 j + t
+                    __syncthreads();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) columns[256 * j + threadIdx.x] = v[j];
+                    __syncthreads();
+                    if ((int)threadIdx.x >= THREADS) continue;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int w = 1; w < ROWS; ++w) v[j] += columns[256 * j + THREADS * w + threadIdx.x];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < a.dim) out[(long long)which * a.dim + c + j] = v[j];
+            }
+    }
+}
+
+// 32 columns a workgroup, 32 threads a column: the parts one after the other, then the threads.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const NormGradArgs a, int parts)
+{
+    __shared__ float sums[2][32][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float v[2] = {0.f, 0.f};
+    if (c < a.dim)
+        for (int p = group; p < parts; p += 32) {
+            v[0] += a.partial[2LL * p * a.dim + c];
+            v[1] += a.partial[(2LL * p + 1) * a.dim + c];
+        }
+    sums[0][group][lane] = v[0];
+    sums[1][group][lane] = v[1];
+    __syncthreads();
+    if (group < 2 && c < a.dim) {
+        float total = 0.f;
+#pragma unroll
+        for (int q = 0; q < 32; ++q) total += sums[group][q][lane];
+        if (group == 0) {
+            if (a.dgamma) a.dgamma[c] = total;
+        } else if (a.F && a.n > 0) {
+            const float mean = total / (float)a.n;
+            a.F[c] = a.decay == 0.f ? mean : fmaf(1.f - a.decay, mean, a.decay * a.F[c]);
+        }
+    }
+}
+
+// A launch takes less than 2^32 threads; the kernels go on from there.
+unsigned workgroups(int n, int rows) { return (unsigned)std::min((n + rows - 1) / rows, 1 << 20); }
+
+template <typename T, typename S, int THREADS, int CH>
+hipError_t run(const NormArgs &a, hipStream_t s)
+{
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    norm_kernel<T, S, THREADS, CH><<<dim3(workgroups(a.n, ROWS)), dim3(THREADS < 256 ? 256 : THREADS), 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, typename S>
+hipError_t run(const NormArgs &a, hipStream_t s)
+{
+    if (a.dim <= 512) return run<T, S, 64, 1>(a, s);
+    if (a.dim <= 1024) return run<T, S, 64, 2>(a, s);
+    if (a.dim <= 2048) return run<T, S, 64, 4>(a, s);
+    if (a.dim <= 4096) return run<T, S, 256, 2>(a, s);
+    if (a.dim <= 8192) return run<T, S, 256, 4>(a, s);
+    return run<T, S, 1024, 2>(a, s);
+}
+
+int rows_at_once(int dim) { return dim <= 2048 ? 4 : 1; }
+
+template <typename T, typename S, int THREADS, int CH>
+hipError_t run_grad(const NormGradArgs &a, hipStream_t s)
+{
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    const dim3 block(THREADS < 256 ? 256 : THREADS);
+    if (a.dgamma || a.F) norm_grad_kernel<T, S, THREADS, CH, true><<<dim3((unsigned)norm_parts(a.n, a.dim)), block, 0, s>>>(a);
+    else norm_grad_kernel<T, S, THREADS, CH, false><<<dim3(workgroups(a.n, ROWS)), block, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, typename S>
+hipError_t run_grad(const NormGradArgs &a, hipStream_t s)
+{
+    if (a.dim <= 512) return run_grad<T, S, 64, 1>(a, s);
+    if (a.dim <= 1024) return run_grad<T, S, 64, 2>(a, s);
+    if (a.dim <= 2048) return run_grad<T, S, 64, 4>(a, s);
+    if (a.dim <= 4096) return run_grad<T, S, 256, 2>(a, s);
+    if (a.dim <= 8192) return run_grad<T, S, 256, 4>(a, s);
+    return run_grad<T, S, 1024, 2>(a, s);
+}
+
+}  // namespace
+
+int norm_parts(int n, int dim)
+{
+    const int rows = rows_at_once(dim), most = (n + 4 * rows - 1) / (4 * rows);   // four rows at least for a row of sums
+    return most < 1 ? 1 : most > 512 ? 512 : most;
+}
+
+hipError_t launch_norm(const NormArgs &a, int bf16, int stream_bf16, hipStream_t s)
+{
+    if (bf16) return stream_bf16 ? run<bf16_bits, bf16_bits>(a, s) : run<bf16_bits, float>(a, s);
+    return stream_bf16 ? run<float, bf16_bits>(a, s) : run<float, float>(a, s);
+}
+
+hipError_t launch_norm_grad(const NormGradArgs &a, int bf16, int stream_bf16, hipStream_t s)
+{
+    if (bf16) return stream_bf16 ? run_grad<bf16_bits, bf16_bits>(a, s) : run_grad<bf16_bits, float>(a, s);
+    return stream_bf16 ? run_grad<float, bf16_bits>(a, s) : run_grad<float, float>(a, s);
+}
+
+hipError_t launch_norm_join(const NormGradArgs &a, hipStream_t s)
+{
+    norm_join_kernel<<<dim3((unsigned)((a.dim + 31) / 32)), dim3(1024), 0, s>>>(a, norm_parts(a.n, a.dim));
+    return hipGetLastError();
+}
+
+}  // namespace kfac

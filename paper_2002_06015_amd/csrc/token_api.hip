@@ -4,53 +4,11 @@
 
 #include <algorithm>
 
-#include "token_internal.h"
+#include "token_args.h"
 
 using namespace kfac;
 
 namespace {
-
-constexpr int kMaxPositions = 1 << 30, kMaxDim = 1 << 20, kMaxExperts = 1 << 16;
-
-bool type_ok(kfac_dtype t) { return t == KFAC_F32 || t == KFAC_BF16; }
-size_t esize(kfac_dtype t) { return t == KFAC_BF16 ? 2 : 4; }
-
-// Bytes that a call touches: one piece of `row` bytes every `ld` bytes from p to p + size; ld = 0: one piece.  Empty: touches nothing.
-struct Range {
-    const char *p;
-    size_t size, row, ld;
-    Range(const void *p_ = nullptr, size_t size_ = 0, size_t row_ = 0, size_t ld_ = 0) : p((const char *)p_), size(size_), row(ld_ ? row_ : size_), ld(ld_) {}
-};
-Range matrix(const void *p, long long rows, long long cols, long long ld, size_t es)
-{
-    if (!p || rows <= 0) return Range();
-    return Range(p, (size_t)((rows - 1) * ld + cols) * es, (size_t)cols * es, rows > 1 && ld > cols ? (size_t)ld * es : 0);
-}
-// Columns beside each other in one wider tensor are apart though their ranges meet: with the same distance of rows (or one piece on
-// one side) the two sets of pieces are compared inside one distance.
-bool overlap(const Range &a, const Range &b)
-{
-    if (!a.size || !b.size || a.p >= b.p + b.size || b.p >= a.p + a.size) return false;
-    if (a.ld != b.ld && a.ld && b.ld) return true;
-    const size_t ld = a.ld ? a.ld : b.ld;
-    if (!ld) return true;
-    const size_t at = a.p <= b.p ? (size_t)(b.p - a.p) % ld : (ld - (size_t)(a.p - b.p) % ld) % ld;   // of b's pieces behind a's
-    return at < a.row || at + b.row > ld;
-}
-// rows that lie ld elements apart: offsets, in bytes too, stay far inside 64 bits
-bool spread_ok(long long rows, long long ld)
-{
-    constexpr long long most = 1LL << 40;
-    return ld <= most && (rows <= 1 || ld <= most / rows);
-}
-bool aligned(const void *p, size_t es) { return (uintptr_t)p % es == 0; }
-
-// One launch between the profiler's events
-template <typename F>
-bool timed(kfac_ctx *ctx, int kernel, int variant, double flops, double bytes, F launch)
-{
-    return profile_begin(ctx, kernel, variant, flops, bytes) && launch() == hipSuccess && profile_end(ctx);
-}
 
 bool segments_ok(int32_t n, int32_t num) { return n >= 0 && n <= kMaxPositions && num >= 1 && num < (1 << 30); }
 
@@ -100,6 +58,77 @@ bool run_expert(kfac_ctx *ctx, ExpertOp op, const ExpertArgs &a, kfac_dtype type
 {
     const CtxView c = ctx_view(ctx);
     return timed(ctx, KFAC_K_EXPERT, (int)op, flops, bytes, [&] { return launch_expert(op, a, type == KFAC_BF16, c.fp32_planes, c.stream); });
+}
+
+// The checks of kfac_expert_grad_weight and kfac_stats_expert, and what they launch.  in: what x is read from, one or two tensors.
+struct Inputs { Range a, b; };
+Inputs plain_inputs(const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type, const void *x, int64_t ldx)
+{
+    return L && fan >= 1 && n > 0 && ldx >= L->c_in && ldx <= kMaxPositions ? Inputs{matrix(x, n / fan, L->c_in, ldx, esize(type)), Range{}} : Inputs{};
+}
+Inputs kept_inputs(const kfac_layer *L, int32_t n, int32_t fan, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds)
+{
+    return {matrix(q, n / fan, L->c_in, ldq, 1), matrix(scales, n / fan, (L->c_in + 31) / 32, lds, 1)};
+}
+kfac_status weight_args(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type, const int32_t *order,
+                        const int32_t *offsets, const Inputs &in, const void *x, int64_t ldx, const void *dy, int64_t ldy, float *dW, ExpertArgs &a)
+{
+    if (!expert_ok(ctx, L, experts, n, fan, type, offsets) || !aligned(order, 4) || !dW || !aligned(dW, 4)) return KFAC_ERR_INVALID;
+    if (ldx < L->c_in || ldy < L->c_out || ldx > kMaxPositions || ldy > kMaxPositions) return KFAC_ERR_INVALID;
+    const size_t es = esize(type);
+    if (n > 0 && (!x || !dy || !aligned(x, es) || !aligned(dy, es))) return KFAC_ERR_INVALID;
+    const Range out = matrix(dW, (long long)experts * L->c_out, L->c_in + L->bias, L->c_in + L->bias, 4);
+    if (overlap(out, in.a) || overlap(out, in.b) || overlap(out, matrix(dy, n, L->c_out, ldy, es))) return KFAC_ERR_INVALID;
+    a = expert_args(L, experts, n, fan, order, offsets);
+    a.x = x; a.ldx = ldx; a.dy = dy; a.ldy = ldy; a.dW = dW;
+    return KFAC_OK;
+}
+kfac_status run_weight(kfac_ctx *ctx, const ExpertArgs &a, kfac_dtype type)
+{
+    return run_expert(ctx, EXPERT_GRAD_WEIGHT, a, type, 2.0 * a.n * a.ci * a.co,
+                      esize(type) * (double)a.n * (a.ci / (double)a.fan + a.co) + 4.0 * a.experts * a.co * (a.ci + a.bias)) ? KFAC_OK : KFAC_ERR_DEVICE;
+}
+
+kfac_status stats_args(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype in, const int32_t *order,
+                       const int32_t *offsets, const Inputs &from, const void *x, int64_t ldx, const void *grad_out, int64_t ldg, float decay,
+                       float *A_ema, float *G_ema, ExpertArgs &a)
+{
+    if (!expert_ok(ctx, L, experts, n, fan, in, offsets) || !aligned(order, 4)) return KFAC_ERR_INVALID;
+    if (!(decay >= 0.f && decay < 1.f) || (!A_ema && !G_ema) || !aligned(A_ema, 4) || !aligned(G_ema, 4)) return KFAC_ERR_INVALID;
+    const size_t es = esize(in);
+    if (A_ema && (ldx < L->c_in || ldx > kMaxPositions || (n > 0 && (!x || !aligned(x, es))))) return KFAC_ERR_INVALID;
+    if (G_ema && (ldg < L->c_out || ldg > kMaxPositions || (n > 0 && (!grad_out || !aligned(grad_out, es))))) return KFAC_ERR_INVALID;
+    const long long dA = L->c_in + L->bias, dG = L->c_out;
+    const Range rg = G_ema ? matrix(grad_out, n, L->c_out, ldg, es) : Range{}, A = matrix(A_ema, experts * dA, dA, dA, 4),
+                G = matrix(G_ema, experts * dG, dG, dG, 4);
+    if (overlap(A, G) || overlap(A, rg) || overlap(G, rg)) return KFAC_ERR_INVALID;
+    if (A_ema && (overlap(A, from.a) || overlap(A, from.b) || overlap(G, from.a) || overlap(G, from.b))) return KFAC_ERR_INVALID;
+    a = expert_args(L, experts, n, fan, order, offsets);
+    a.x = x; a.ldx = ldx; a.dy = grad_out; a.ldy = ldg;
+    a.A = A_ema; a.G = G_ema; a.decay = decay;
+    return KFAC_OK;
+}
+kfac_status run_stats(kfac_ctx *ctx, const ExpertArgs &a, kfac_dtype in)
+{
+    const double dA = a.ci + a.bias, dG = a.co, fa = a.A ? dA * dA : 0.0, fg = a.G ? dG * dG : 0.0, es = esize(in);
+    const double read = (a.A ? es * a.n / a.fan * a.ci : 0.0) + (a.G ? es * a.n * a.co : 0.0);
+    return run_expert(ctx, EXPERT_STATS, a, in, a.n * (fa + fg), read + 4.0 * a.experts * (fa + fg)) ? KFAC_OK : KFAC_ERR_DEVICE;
+}
+
+// Inputs of experts that were kept in 8 bits; in the workspace as values, rows a whole number of 16-byte chunks apart.
+int64_t kept_row(const kfac_layer *L) { return ((int64_t)L->c_in + 63) / 64 * 64; }
+size_t kept_bytes(const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type) { return (size_t)(n / fan) * kept_row(L) * esize(type); }
+bool kept_ok(const kfac_layer *L, int32_t n, int32_t fan, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds)
+{
+    return ldq >= L->c_in && lds >= (L->c_in + 31) / 32 && ldq <= kMaxPositions && lds <= kMaxPositions && (n == 0 || (q && scales));
+}
+bool restore_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds)
+{
+    KeepArgs k{};
+    k.rows = n / fan; k.cols = L->c_in; k.back = ctx_view(ctx).ws; k.ldx = kept_row(L);
+    k.q = const_cast<uint8_t *>(q); k.ldq = ldq; k.scales = const_cast<uint8_t *>(scales); k.lds = lds;   // (only read)
+    return timed(ctx, KFAC_K_KEEP, 1, 0.0, (double)k.rows * k.cols * (esize(type) + 1 + 1.0 / 32),
+                 [&] { return launch_restore(k, type == KFAC_BF16, ctx_view(ctx).stream); });
 }
 
 }  // namespace
@@ -256,38 +285,54 @@ kfac_status kfac_expert_grad_input(kfac_ctx *ctx, const kfac_layer *L, int32_t e
 kfac_status kfac_expert_grad_weight(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type, const int32_t *order,
                                     const int32_t *offsets, const void *x, int64_t ldx, const void *dy, int64_t ldy, float *dW)
 {
-    if (!expert_ok(ctx, L, experts, n, fan, type, offsets) || !aligned(order, 4) || !dW || !aligned(dW, 4)) return KFAC_ERR_INVALID;
-    if (ldx < L->c_in || ldy < L->c_out || ldx > kMaxPositions || ldy > kMaxPositions) return KFAC_ERR_INVALID;
-    const size_t es = esize(type);
-    if (n > 0 && (!x || !dy || !aligned(x, es) || !aligned(dy, es))) return KFAC_ERR_INVALID;
-    const Range out = matrix(dW, (long long)experts * L->c_out, L->c_in + L->bias, L->c_in + L->bias, 4);
-    if (overlap(out, matrix(x, n / fan, L->c_in, ldx, es)) || overlap(out, matrix(dy, n, L->c_out, ldy, es))) return KFAC_ERR_INVALID;
-    ExpertArgs a = expert_args(L, experts, n, fan, order, offsets);
-    a.x = x; a.ldx = ldx; a.dy = dy; a.ldy = ldy; a.dW = dW;
-    return run_expert(ctx, EXPERT_GRAD_WEIGHT, a, type, 2.0 * n * L->c_in * L->c_out,
-                      es * (double)n * (L->c_in / (double)fan + L->c_out) + 4.0 * experts * L->c_out * (L->c_in + L->bias)) ? KFAC_OK : KFAC_ERR_DEVICE;
+    ExpertArgs a;
+    const kfac_status st = weight_args(ctx, L, experts, n, fan, type, order, offsets, plain_inputs(L, n, fan, type, x, ldx), x, ldx, dy, ldy, dW, a);
+    return st == KFAC_OK ? run_weight(ctx, a, type) : st;
 }
 
 kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype in, const int32_t *order,
                               const int32_t *offsets, const void *x, int64_t ldx, const void *grad_out, int64_t ldg, float decay, float *A_ema,
                               float *G_ema)
 {
-    if (!expert_ok(ctx, L, experts, n, fan, in, offsets) || !aligned(order, 4)) return KFAC_ERR_INVALID;
-    if (!(decay >= 0.f && decay < 1.f) || (!A_ema && !G_ema) || !aligned(A_ema, 4) || !aligned(G_ema, 4)) return KFAC_ERR_INVALID;
-    const size_t es = esize(in);
-    if (A_ema && (ldx < L->c_in || ldx > kMaxPositions || (n > 0 && (!x || !aligned(x, es))))) return KFAC_ERR_INVALID;
-    if (G_ema && (ldg < L->c_out || ldg > kMaxPositions || (n > 0 && (!grad_out || !aligned(grad_out, es))))) return KFAC_ERR_INVALID;
-    const long long dA = L->c_in + L->bias, dG = L->c_out;
-    const Range rx = A_ema ? matrix(x, n / fan, L->c_in, ldx, es) : Range{}, rg = G_ema ? matrix(grad_out, n, L->c_out, ldg, es) : Range{},
-                A = matrix(A_ema, experts * dA, dA, dA, 4), G = matrix(G_ema, experts * dG, dG, dG, 4);
-    if (overlap(A, G) || overlap(A, rx) || overlap(A, rg) || overlap(G, rx) || overlap(G, rg)) return KFAC_ERR_INVALID;
+    ExpertArgs a;
+    const kfac_status st = stats_args(ctx, L, experts, n, fan, in, order, offsets, plain_inputs(L, n, fan, in, x, ldx), x, ldx, grad_out, ldg, decay,
+                                      A_ema, G_ema, a);
+    return st == KFAC_OK && n > 0 ? run_stats(ctx, a, in) : st;   // (n = 0: no expert has rows)
+}
+
+size_t kfac_kept_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan)
+{
+    return experts_ok(L, experts, n) && fan >= 1 && n % fan == 0 ? std::max<size_t>(256, kept_bytes(L, n, fan, KFAC_F32)) : 0;
+}
+
+kfac_status kfac_expert_grad_weight_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type,
+                                         const int32_t *order, const int32_t *offsets, const uint8_t *q, int64_t ldq, const uint8_t *scales,
+                                         int64_t lds, const void *dy, int64_t ldy, float *dW)
+{
+    if (!expert_ok(ctx, L, experts, n, fan, type, offsets) || !kept_ok(L, n, fan, q, ldq, scales, lds)) return KFAC_ERR_INVALID;
+    const CtxView c = ctx_view(ctx);
+    ExpertArgs a;
+    const kfac_status st = weight_args(ctx, L, experts, n, fan, type, order, offsets, kept_inputs(L, n, fan, q, ldq, scales, lds), c.ws, kept_row(L), dy, ldy, dW, a);
+    if (st != KFAC_OK) return st;
+    if (kept_bytes(L, n, fan, type) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    if (n > 0 && !restore_kept(ctx, L, n, fan, type, q, ldq, scales, lds)) return KFAC_ERR_DEVICE;
+    return run_weight(ctx, a, type);
+}
+
+kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype in,
+                                   const int32_t *order, const int32_t *offsets, const uint8_t *q, int64_t ldq, const uint8_t *scales,
+                                   int64_t lds, const void *grad_out, int64_t ldg, float decay, float *A_ema, float *G_ema)
+{
+    if (!expert_ok(ctx, L, experts, n, fan, in, offsets) || (A_ema && !kept_ok(L, n, fan, q, ldq, scales, lds))) return KFAC_ERR_INVALID;
+    const CtxView c = ctx_view(ctx);
+    ExpertArgs a;
+    const kfac_status st = stats_args(ctx, L, experts, n, fan, in, order, offsets, A_ema ? kept_inputs(L, n, fan, q, ldq, scales, lds) : Inputs{}, c.ws,
+                                      kept_row(L), grad_out, ldg, decay, A_ema, G_ema, a);
+    if (st != KFAC_OK) return st;
     if (n == 0) return KFAC_OK;   // no expert has rows
-    ExpertArgs a = expert_args(L, experts, n, fan, order, offsets);
-    a.x = x; a.ldx = ldx; a.dy = grad_out; a.ldy = ldg;
-    a.A = A_ema; a.G = G_ema; a.decay = decay;
-    const double fa = A_ema ? (double)dA * dA : 0.0, fg = G_ema ? (double)dG * dG : 0.0;
-    return run_expert(ctx, EXPERT_STATS, a, in, n * (fa + fg), (double)rx.size + rg.size + 4.0 * experts * (fa + fg)) ? KFAC_OK
-                                                                                                                               : KFAC_ERR_DEVICE;
+    if (A_ema && kept_bytes(L, n, fan, in) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    if (A_ema && !restore_kept(ctx, L, n, fan, in, q, ldq, scales, lds)) return KFAC_ERR_DEVICE;
+    return run_stats(ctx, a, in);
 }
 
 }  // extern "C"

@@ -95,4 +95,75 @@ enum ExpertOp { EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, EXPERT_ST
 // planes: how fp32 operands are multiplied (bf16 != 0: not used)
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s);
 
+// ---- routing -------------------------------------------------------------------------------------------
+constexpr int kMaxRouted = 1024, kMaxFan = 32;
+struct RouteArgs {
+    int n, experts, fan, groups, top_groups, group_best, sigmoid, renormalise;
+    float scale;
+    const void *logits;
+    long long ld;
+    const float *bias;            // may be nullptr
+    int *choice;
+    float *gate;
+    const float *dgate;           // of the gradient
+    void *dlogits;
+    long long ldd;
+};
+hipError_t launch_route(const RouteArgs &a, int bf16, hipStream_t s);
+hipError_t launch_route_grad(const RouteArgs &a, int bf16, hipStream_t s);
+
+// ---- the join of the experts' results ------------------------------------------------------------------
+struct CombineArgs {
+    int tokens, fan, dim;
+    const void *y, *r, *dout;     // r may be nullptr
+    long long ldy, ldr, ldd;
+    const float *gate;            // may be nullptr
+    void *out, *dy;               // dy may be nullptr
+    long long ldo, lddy;
+    float *dgate;                 // may be nullptr
+};
+hipError_t launch_combine(const CombineArgs &a, int bf16, int out_bf16, hipStream_t s);
+hipError_t launch_combine_grad(const CombineArgs &a, int bf16, int out_bf16, hipStream_t s);
+
+// ---- activations in 8 bits -----------------------------------------------------------------------------
+struct KeepArgs {
+    long long rows;
+    int cols;
+    const void *x;                // of kfac_keep
+    void *back;                   // of kfac_restore
+    long long ldx;
+    unsigned char *q, *scales;
+    long long ldq, lds;
+};
+hipError_t launch_keep(const KeepArgs &a, int bf16, hipStream_t s);
+hipError_t launch_restore(const KeepArgs &a, int bf16, hipStream_t s);
+
+// ---- root-mean-square norm -----------------------------------------------------------------------------
+constexpr int kMaxNorm = 16384;
+struct NormArgs {
+    int n, dim;
+    const void *x, *r;            // r may be nullptr
+    void *h, *y;                  // either may be nullptr
+    const float *gamma;
+    float eps;
+    long long ldx, ldr, ldh, ldy;
+    unsigned char *q, *scales;    // may be nullptr
+    long long ldq, lds;
+};
+struct NormGradArgs {
+    int n, dim;
+    const void *dy, *h, *r;       // r: the stream's own gradient, may be nullptr
+    void *dh;                     // may be nullptr
+    long long lddy, ldh, ldr, lddh;
+    const float *gamma;
+    float eps;
+    float *dgamma, *F;            // either may be nullptr
+    float decay;
+    float *partial;               // [parts][2][dim], not read or written if both are nullptr
+};
+hipError_t launch_norm(const NormArgs &a, int bf16, int stream_bf16, hipStream_t s);
+int norm_parts(int n, int dim);   // never fewer for more rows or columns
+hipError_t launch_norm_grad(const NormGradArgs &a, int bf16, int stream_bf16, hipStream_t s);
+hipError_t launch_norm_join(const NormGradArgs &a, hipStream_t s);
+
 }  // namespace kfac

@@ -31,11 +31,14 @@ EXPORTS = [
     "kfac_staleness", "kfac_staleness_static", "kfac_next_interval", "kfac_refresh_init", "kfac_refresh_due", "kfac_refresh_advance",
     "kfac_segments_workspace_bytes", "kfac_segments", "kfac_embedding", "kfac_embedding_workspace_bytes", "kfac_embedding_grad", "kfac_dropout",
     "kfac_expert_workspace_bytes", "kfac_expert_forward", "kfac_expert_grad_input", "kfac_expert_grad_weight", "kfac_stats_expert",
+    "kfac_route", "kfac_route_grad", "kfac_combine", "kfac_combine_grad", "kfac_keep", "kfac_restore",
+    "kfac_kept_workspace_bytes", "kfac_expert_grad_weight_kept", "kfac_stats_expert_kept",
+    "kfac_rms_norm", "kfac_rms_norm_workspace_bytes", "kfac_rms_norm_grad",
 ]
 
 KERNEL_NAMES = ["gemm_f32", "gemm_bf16", "gemm_reduce", "patch", "trace", "copy_damp", "leaf_inverse", "zero",
                 "bn_unit", "bn_reduce", "pad", "assemble", "border", "staleness", "pack", "update", "bn_full", "layout", "gemm_f32_split",
-                "segments", "embedding", "dropout", "expert"]
+                "segments", "embedding", "dropout", "expert", "route", "combine", "norm", "keep"]
 
 
 class kfac_profile_entry(ctypes.Structure):
@@ -169,6 +172,20 @@ def lib() -> ctypes.CDLL:
         L.kfac_expert_grad_input.argtypes = [vp, vp, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp, i64]
         L.kfac_expert_grad_weight.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp]
         L.kfac_stats_expert.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, f32, vp, vp]
+        L.kfac_route.argtypes = [vp, vp, i32, typ, vp, i64, vp, vp, vp]
+        L.kfac_route_grad.argtypes = [vp, vp, i32, typ, vp, i64, vp, vp, vp, i64]
+        L.kfac_combine.argtypes = [vp, i32, i32, i32, typ, vp, i64, vp, typ, vp, i64, vp, i64]
+        L.kfac_combine_grad.argtypes = [vp, i32, i32, i32, typ, vp, i64, vp, typ, vp, i64, vp, i64, vp]
+        L.kfac_keep.argtypes = [vp, i64, i32, typ, vp, i64, vp, i64, vp, i64]
+        L.kfac_restore.argtypes = [vp, i64, i32, vp, i64, vp, i64, typ, vp, i64]
+        L.kfac_kept_workspace_bytes.restype = sz
+        L.kfac_kept_workspace_bytes.argtypes = [vp, i32, i32, i32]
+        L.kfac_expert_grad_weight_kept.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.kfac_stats_expert_kept.argtypes = [vp, vp, i32, i32, i32, typ, vp, vp, vp, i64, vp, i64, vp, i64, f32, vp, vp]
+        L.kfac_rms_norm.argtypes = [vp, i32, i32, typ, vp, i64, typ, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, i64]
+        L.kfac_rms_norm_workspace_bytes.restype = sz
+        L.kfac_rms_norm_workspace_bytes.argtypes = [i32, i32]
+        L.kfac_rms_norm_grad.argtypes = [vp, i32, i32, typ, vp, i64, typ, vp, i64, vp, f32, vp, i64, vp, i64, vp, f32, vp]
         _lib = L
     return _lib
 
@@ -753,6 +770,211 @@ def kfac_stats_expert(ctx: Context, layer, order: Optional[torch.Tensor], offset
                                  _floats(A_ema, experts * dA * dA, "A_ema"), _floats(G_ema, experts * L.c_out * L.c_out, "G_ema"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_stats_expert")
+
+
+# ---------------------------------------------------------------- around the products of experts
+KFAC_ROUTE_SOFTMAX, KFAC_ROUTE_SIGMOID = 0, 1
+
+
+class kfac_router(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("experts", "fan", "groups", "top_groups", "group_best", "scores", "renormalise")] + \
+               [("scale", ctypes.c_float)]
+
+
+def router(experts: int, fan: int, groups: int = 1, top_groups: int = 1, group_best: int = 1, scores: int = KFAC_ROUTE_SOFTMAX,
+           renormalise: bool = True, scale: float = 1.0) -> kfac_router:
+    """How tokens choose their experts."""
+    return kfac_router(int(experts), int(fan), int(groups), int(top_groups), int(group_best), int(scores), int(renormalise), float(scale))
+
+
+def _here(ctx: Context, *tensors: Optional[torch.Tensor]) -> None:
+    device = ctx.workspace.get_device()
+    if torch.cuda.current_device() != device:
+        raise ValueError("the current device must be that of the context, cuda:%d" % device)
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("tensors must be on the device of the context, cuda:%d" % device)
+
+
+def _view(t: Optional[torch.Tensor], rows: int, cols: int, dtype, what: str) -> tuple:
+    """Pointer and distance of the rows; nothing for None."""
+    return (None, 0) if t is None else (t.data_ptr(), _rows_of(t, rows, cols, dtype, what))
+
+
+def _choices(t: torch.Tensor, n: int, what: str) -> int:
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+        raise ValueError("%s must be a contiguous int32 device tensor of %d elements" % (what, n))
+    return t.data_ptr()
+
+
+def kfac_route(ctx: Context, router: kfac_router, logits: torch.Tensor, choice: torch.Tensor, gate: torch.Tensor,
+               bias: Optional[torch.Tensor] = None) -> None:
+    """choice: int32 [n * fan], the experts of every token (-1: none left); gate: float32 [n, fan]; logits [n, experts]."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n, experts]")
+    n, E, fan = logits.shape[0], router.experts, router.fan
+    _here(ctx, logits, choice, gate, bias)
+    st = lib().kfac_route(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(),
+                          _rows_of(logits, n, E, logits.dtype, "logits"), _floats(bias, E, "bias"), _choices(choice, n * fan, "choice"),
+                          _floats(gate, n * fan, "gate"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_route")
+
+
+def kfac_route_grad(ctx: Context, router: kfac_router, logits: torch.Tensor, choice: torch.Tensor, dgate: torch.Tensor,
+                    dlogits: torch.Tensor) -> None:
+    """dlogits [n, experts], of the type of the logits, from dgate: float32 [n, fan]."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n, experts]")
+    n, E, fan = logits.shape[0], router.experts, router.fan
+    _here(ctx, logits, choice, dgate, dlogits)
+    st = lib().kfac_route_grad(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(),
+                               _rows_of(logits, n, E, logits.dtype, "logits"), _choices(choice, n * fan, "choice"), _floats(dgate, n * fan, "dgate"),
+                               dlogits.data_ptr(), _rows_of(dlogits, n, E, logits.dtype, "dlogits"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_route_grad")
+
+
+def _fan(n: int, tokens: int) -> int:
+    """Choices of a token."""
+    if n % tokens if tokens else n:
+        raise ValueError("%d choices are not the same number for each of %d tokens" % (n, tokens))
+    return n // tokens if n else 1
+
+
+def kfac_combine(ctx: Context, y: torch.Tensor, gate: Optional[torch.Tensor], out: torch.Tensor, residual: Optional[torch.Tensor] = None) -> None:
+    """out[t] = residual[t] + sum over the choices of token t of gate * y; y [n, dim], out and residual [tokens, dim], gate float32 [n]
+    or None for ones.  out may be residual."""
+    if y.dim() != 2 or out.dim() != 2:
+        raise ValueError("y must be [n, dim] and out [tokens, dim]")
+    (n, dim), tokens = y.shape, out.shape[0]
+    _here(ctx, y, gate, out, residual)
+    pr, ldr = _view(residual, tokens, dim, out.dtype, "residual")
+    st = lib().kfac_combine(ctx.handle, n, _fan(n, tokens), dim, _type_of(y, "y"), y.data_ptr(), _rows_of(y, n, dim, y.dtype, "y"),
+                            _floats(gate, n, "gate"), _type_of(out, "out"), pr, ldr, out.data_ptr(), _rows_of(out, tokens, dim, out.dtype, "out"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_combine")
+
+
+def kfac_combine_grad(ctx: Context, y: Optional[torch.Tensor], gate: Optional[torch.Tensor], dout: torch.Tensor, dy: Optional[torch.Tensor],
+                      dgate: Optional[torch.Tensor]) -> None:
+    """dy = gate * dout [n, dim] and dgate = <dout, y> float32 [n]; what is None is skipped (and y is not read without dgate)."""
+    src = dy if dy is not None else y
+    if src is None or src.dim() != 2 or dout.dim() != 2 or (dgate is None and dy is None) or (dgate is not None and y is None):
+        raise ValueError("dy or dgate is needed, dgate needs y; y and dy must be [n, dim], dout [tokens, dim]")
+    (n, dim), tokens = src.shape, dout.shape[0]
+    _here(ctx, y, gate, dout, dy, dgate)
+    py, ldy = _view(y if dgate is not None else None, n, dim, src.dtype, "y")
+    pd, lddy = _view(dy, n, dim, src.dtype, "dy")
+    st = lib().kfac_combine_grad(ctx.handle, n, _fan(n, tokens), dim, _type_of(src, "y"), py, ldy, _floats(gate, n, "gate"), _type_of(dout, "dout"),
+                                 dout.data_ptr(), _rows_of(dout, tokens, dim, dout.dtype, "dout"), pd, lddy, _floats(dgate, n, "dgate"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_combine_grad")
+
+
+def _bytes(q: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> tuple:
+    """Pointers and distances of the rows of activations in 8 bits."""
+    return q.data_ptr(), _rows_of(q, rows, cols, torch.float8_e4m3fn, "q"), scales.data_ptr(), _rows_of(scales, rows, (cols + 31) // 32, torch.uint8, "scales")
+
+
+def kfac_keep(ctx: Context, x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor) -> None:
+    """x [rows, cols] in 8 bits: q float8_e4m3fn [rows, cols], scales uint8 [rows, ceil(cols / 32)]."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    _here(ctx, x, q, scales)
+    st = lib().kfac_keep(ctx.handle, rows, cols, _type_of(x, "x"), x.data_ptr(), _rows_of(x, rows, cols, x.dtype, "x"), *_bytes(q, scales, rows, cols))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_keep")
+
+
+def kfac_restore(ctx: Context, q: torch.Tensor, scales: torch.Tensor, x: torch.Tensor) -> None:
+    """The values that q and its scales stand for, float32 or bfloat16."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    _here(ctx, x, q, scales)
+    st = lib().kfac_restore(ctx.handle, rows, cols, *_bytes(q, scales, rows, cols), _type_of(x, "x"), x.data_ptr(), _rows_of(x, rows, cols, x.dtype, "x"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_restore")
+
+
+def kfac_kept_workspace_bytes(layer, experts: int, n: int, fan: int = 1) -> int:
+    L = kfac_layer(*[int(v) for v in layer])
+    return int(lib().kfac_kept_workspace_bytes(ctypes.addressof(L), int(experts), int(n), int(fan)))
+
+
+def kfac_expert_grad_weight_kept(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
+                                 dy: torch.Tensor, dW: torch.Tensor, fan: int = 1) -> None:
+    """kfac_expert_grad_weight for inputs that were kept in 8 bits: q [n // fan, c_in] with its scales."""
+    n = dy.shape[0]
+    L, experts, po, pf = _expert(layer, order, offsets, n)
+    _here(ctx, order, offsets, q, scales, dy, dW)
+    typ = _type_of(dy, "dy")
+    st = lib().kfac_expert_grad_weight_kept(ctx.handle, ctypes.addressof(L), experts, n, int(fan), typ, po, pf,
+                                            *_bytes(q, scales, n // max(1, int(fan)), L.c_in), dy.data_ptr(),
+                                            _rows_of(dy, n, L.c_out, dy.dtype, "dy"), _floats(dW, experts * L.c_out * (L.c_in + L.bias), "dW"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_expert_grad_weight_kept")
+
+
+def kfac_stats_expert_kept(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
+                           grad_out: Optional[torch.Tensor], decay: float, A_ema: torch.Tensor, G_ema: Optional[torch.Tensor], fan: int = 1) -> None:
+    """kfac_stats_expert for inputs that were kept in 8 bits; G_ema None: grad_out is not read."""
+    fan = int(fan)
+    if G_ema is not None and grad_out is None:
+        raise ValueError("a factor needs its input")
+    n = order.numel() if order is not None else grad_out.shape[0] if grad_out is not None else q.shape[0] * fan
+    L, experts, po, pf = _expert(layer, order, offsets, n)
+    _here(ctx, order, offsets, q, scales, grad_out, A_ema, G_ema)
+    dA = L.c_in + L.bias
+    pg, ldg = (None, 0) if G_ema is None else (grad_out.data_ptr(), _rows_of(grad_out, n, L.c_out, grad_out.dtype, "grad_out"))
+    st = lib().kfac_stats_expert_kept(ctx.handle, ctypes.addressof(L), experts, n, fan, KFAC_BF16 if G_ema is None else _type_of(grad_out, "grad_out"),
+                                      po, pf, *_bytes(q, scales, n // max(1, fan), L.c_in), pg, ldg, float(decay),
+                                      _floats(A_ema, experts * dA * dA, "A_ema"), _floats(G_ema, experts * L.c_out * L.c_out, "G_ema"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_stats_expert_kept")
+
+
+def kfac_rms_norm(ctx: Context, x: torch.Tensor, gamma: torch.Tensor, eps: float, y: Optional[torch.Tensor], residual: Optional[torch.Tensor] = None,
+                  h: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None) -> None:
+    """h = x + residual (both or neither), y = gamma h / sqrt(mean h^2 + eps), and the same in 8 bits if q and scales are given."""
+    if x.dim() != 2:
+        raise ValueError("x must be [n, dim]")
+    n, dim = x.shape
+    if (residual is None) != (h is None) or (q is None) != (scales is None):
+        raise ValueError("residual and h, and q and scales, go together")
+    _here(ctx, x, gamma, y, residual, h, q, scales)
+    typ = _type_of(x, "x")
+    stream = typ if residual is None else _type_of(residual, "residual")
+    pr, ldr = _view(residual, n, dim, None if residual is None else residual.dtype, "residual")
+    ph, ldh = _view(h, n, dim, None if residual is None else residual.dtype, "h")
+    py, ldy = _view(y, n, dim, x.dtype, "y")
+    st = lib().kfac_rms_norm(ctx.handle, n, dim, typ, x.data_ptr(), _rows_of(x, n, dim, x.dtype, "x"), stream, pr, ldr, ph, ldh,
+                             _floats(gamma, dim, "gamma"), float(eps), py, ldy, *((None, 0, None, 0) if q is None else _bytes(q, scales, n, dim)))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_rms_norm")
+
+
+def kfac_rms_norm_workspace_bytes(n: int, dim: int) -> int:
+    return int(lib().kfac_rms_norm_workspace_bytes(int(n), int(dim)))
+
+
+def kfac_rms_norm_grad(ctx: Context, dy: torch.Tensor, h: torch.Tensor, gamma: torch.Tensor, eps: float, dh: Optional[torch.Tensor],
+                       dstream: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None, F: Optional[torch.Tensor] = None,
+                       decay: float = 0.0) -> None:
+    """dh = dstream + the norm's gradient; dgamma: float32 [dim]; F: float32 [dim], running average of the diagonal factor of gamma."""
+    if dy.dim() != 2:
+        raise ValueError("dy must be [n, dim]")
+    n, dim = dy.shape
+    _here(ctx, dy, h, gamma, dh, dstream, dgamma, F)
+    pr, ldr = _view(dstream, n, dim, h.dtype, "dstream")
+    ph, lddh = _view(dh, n, dim, h.dtype, "dh")
+    st = lib().kfac_rms_norm_grad(ctx.handle, n, dim, _type_of(dy, "dy"), dy.data_ptr(), _rows_of(dy, n, dim, dy.dtype, "dy"), _type_of(h, "h"),
+                                  h.data_ptr(), _rows_of(h, n, dim, h.dtype, "h"), _floats(gamma, dim, "gamma"), float(eps), pr, ldr, ph, lddh,
+                                  _floats(dgamma, dim, "dgamma"), float(decay), _floats(F, dim, "F"))
+    if st != KFAC_OK:
+        raise KfacError(st, "kfac_rms_norm_grad")
 
 
 def kfac_profile_enable(ctx: Context, on: bool) -> None:

@@ -1,0 +1,256 @@
+"""Activations in 8 bits on the GPU: bytes exactly as the format says, and the products of experts that read them.
+
+Tolerances of the products: as of the products of the values, (m + 8) 2^-24 of the sum of the magnitudes of m terms."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks as B
+from oracle import tokens as T
+from paper_2002_06015_amd import kfac, workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+E4M3 = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    c = kfac.Context([wl.fc_layer(2, 64, 32)], workspace_bytes=256)
+    yield c
+    c.close()
+
+
+def _rows(a, dtype, pad=0, fill=float("nan")):
+    t = torch.full((a.shape[0] + 1, a.shape[1] + pad), fill, dtype=dtype, device="cuda")
+    t[:-1, :a.shape[1]] = torch.from_numpy(np.ascontiguousarray(a)).to(dtype)
+    return t[:-1, :a.shape[1]], t
+
+
+def _values(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _bytes(n, dim, pad=0):
+    q = torch.full((n + 1, dim + pad), 7, dtype=torch.uint8, device="cuda")
+    s = torch.full((n + 1, (dim + 31) // 32 + pad), 9, dtype=torch.uint8, device="cuda")
+    return q.view(E4M3)[:n, :dim], s[:n, :(dim + 31) // 32], q, s
+
+
+def _same_values(a, b):
+    """Equal, NaN where the other has one."""
+    return bool((np.isnan(a) == np.isnan(b)).all() and (a[~np.isnan(a)] == b[~np.isnan(b)]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 31, 0), (2, 32, 0), (3, 33, 1), (5, 8, 0), (7, 515, 3), (64, 1024, 0), (33, 1001, 8), (2, 20000, 0), (1000, 40, 0)])
+def test_keep_and_restore(ctx, rows, cols, pad, dtype):
+    rng = np.random.default_rng(rows + cols)
+    x = rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-12, 12, (rows, 1))
+    t, _ = _rows(x, dtype, pad)
+    q, s, qw, sw = _bytes(rows, cols, pad)
+    kfac.kfac_keep(ctx, t, q, s)
+    torch.cuda.synchronize()
+    rq, rs = B.keep(_values(t))
+    assert np.array_equal(q.view(torch.uint8).cpu().numpy(), rq) and np.array_equal(s.cpu().numpy(), rs)
+    assert bool((qw[-1] == 7).all()) and bool((qw[:, cols:] == 7).all()) and bool((sw[-1] == 9).all()) and bool((sw[:, (cols + 31) // 32:] == 9).all())
+    for out in (F32, BF16):
+        back, whole = _rows(np.zeros((rows, cols)), out, pad, 5.0)
+        kfac.kfac_restore(ctx, q, s, back)
+        assert np.array_equal(_values(back), B.restore(rq, rs))
+        assert bool((whole[-1] == 5.0).all()) and bool((whole[:, cols:] == 5.0).all())
+    again, scales, _, _ = _bytes(rows, cols)     # what was held once is held exactly
+    kfac.kfac_keep(ctx, back, again, scales)
+    back2 = torch.empty(rows, cols, dtype=BF16, device="cuda")
+    kfac.kfac_restore(ctx, again, scales, back2)
+    assert torch.equal(back2, back.contiguous())
+
+
+def test_every_byte_and_every_tie(ctx):
+    """All finite values under scales from one end to the other, the middles between neighbours and what lies next to them."""
+    v = B.e4m3_values()[:127]
+    middle = (v[1:] + v[:-1]) / 2
+    x = np.concatenate([v, middle, np.nextafter(middle.astype(np.float32), np.float32(1e9)), np.nextafter(middle.astype(np.float32), np.float32(0))])
+    x = np.concatenate([x, -x])
+    x = np.concatenate([x, np.zeros(-len(x) % 31)]).reshape(-1, 31)
+    x = np.concatenate([np.full((len(x), 1), 448.0), x], 1).reshape(1, -1)       # the first of every block sets its scale
+    t = torch.from_numpy(np.concatenate([x * 2.0 ** e for e in (-117, -100, -9, 0, 3, 60, 119)]).astype(np.float32)).cuda()
+    q, s, _, _ = _bytes(*t.shape)
+    kfac.kfac_keep(ctx, t, q, s)
+    rq, rs = B.keep(_values(t))
+    assert np.array_equal(s.cpu().numpy(), rs) and np.array_equal(q.view(torch.uint8).cpu().numpy(), rq)
+    table = torch.arange(256, dtype=torch.int32).to(torch.uint8).cuda().repeat(237, 1).view(E4M3)
+    scales = torch.arange(10, 247, dtype=torch.int32).to(torch.uint8).cuda()[:, None].repeat(1, 8).contiguous()
+    for out in (F32, BF16):
+        back = torch.empty(237, 256, dtype=out, device="cuda")
+        kfac.kfac_restore(ctx, table, scales, back)
+        with np.errstate(over="ignore"):
+            want = B.restore(table.view(torch.uint8).cpu().numpy(), scales.cpu().numpy())
+        assert _same_values(_values(back), want)
+
+
+def test_values_at_the_ends(ctx):
+    x = np.zeros((6, 64), dtype=np.float32)
+    x[0, 0] = 3.4e38
+    x[0, 1] = 1.0
+    x[1, :] = 1e-40                                    # subnormal
+    x[2, 0], x[2, 1], x[2, 40] = np.inf, 2.0, -np.inf
+    x[3, 5], x[3, 6] = np.nan, 3.0
+    x[4, :] = -0.0
+    x[5, :32], x[5, 32:] = np.nan, np.inf
+    t = torch.from_numpy(x).cuda()
+    q, s, _, _ = _bytes(6, 64)
+    kfac.kfac_keep(ctx, t, q, s)
+    rq, rs = B.keep(x.astype(np.float64))
+    got, sc = q.view(torch.uint8).cpu().numpy(), s.cpu().numpy()
+    assert np.array_equal(sc, rs)
+    nan = (rq & 0x7F) == 0x7F
+    assert np.array_equal((got & 0x7F) == 0x7F, nan) and np.array_equal(got[~nan], rq[~nan])
+    back = torch.empty(6, 64, device="cuda")
+    kfac.kfac_restore(ctx, q, s, back)
+    assert float(back[0, 0]) == 448 * 2.0 ** 119 and float(back[2, 1]) == 2.0 and float(back[3, 6]) == 3.0
+
+
+def test_views_and_columns_of_one_tensor(ctx):
+    x = torch.randn(50, 96, device="cuda")
+    q, s, _, _ = _bytes(50, 64)
+    kfac.kfac_keep(ctx, x[:, 32:], q, s)
+    wide = torch.zeros(50, 200, dtype=torch.uint8, device="cuda")
+    kfac.kfac_keep(ctx, x[:, 32:], wide[:, 1:65].view(E4M3), wide[:, 70:72])
+    assert torch.equal(wide[:, 1:65], q.view(torch.uint8)) and torch.equal(wide[:, 70:72], s) and not wide[:, 65:70].any() and not wide[:, 72:].any()
+
+
+SHAPES = [  # tokens, fan, experts, c_in, c_out, bias, kind, pad
+    (1, 1, 1, 1, 1, 0, "even", 0), (3, 2, 16, 128, 72, 0, "even", 0), (5, 1, 3, 7, 9, 1, "even", 3), (33, 1, 4, 515, 33, 1, "skew", 0), (64, 4, 8, 256, 128, 0, "skew", 8),
+    (130, 2, 5, 100, 257, 1, "drop", 0), (300, 1, 2, 384, 512, 0, "one", 0), (90, 1, 3, 40, 48, 1, "none", 0), (1031, 2, 6, 192, 320, 1, "skew", 0),
+    (700, 1, 4, 264, 520, 1, "drop", 8), (4111, 1, 1, 96, 64, 1, "even", 0), (9001, 1, 1, 65, 130, 0, "even", 1), (6000, 2, 2, 256, 256, 1, "skew", 0),
+    (2051, 1, 3, 1024, 1032, 1, "skew", 0),
+]
+
+
+def _setup(shape, dtype):
+    tokens, fan, E, ci, co, bias, kind, pad = shape
+    n = tokens * fan
+    rng = np.random.default_rng(tokens + 3 * ci + co)
+    if kind == "skew":
+        p = 1.0 / np.arange(1, E + 1) ** 1.5
+        choice = rng.choice(E, n, p=p / p.sum())
+        choice[choice == 1] = 0
+    else:
+        choice = {"one": lambda: np.full(n, E - 1), "none": lambda: np.full(n, -1), "drop": lambda: rng.integers(-1, E + 1, n),
+                  "even": lambda: rng.integers(0, E, n)}[kind]()
+    layer = wl.fc_layer(1, ci, co, bias)
+    need = max(kfac.kfac_kept_workspace_bytes(layer, E, n, fan), kfac.kfac_segments_workspace_bytes(n, E))
+    c = kfac.Context([layer], workspace_bytes=need)
+    order, offsets = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    kfac.kfac_segments(c, torch.from_numpy(choice.astype(np.int32)).cuda(), E, order, offsets)
+    q, s, _, _ = _bytes(tokens, ci, pad)
+    loud = np.where(rng.random(ci) < 0.1, 30.0, 1.0)
+    rq, rs = B.keep((rng.standard_normal((tokens, ci)) * loud).astype(np.float32).astype(np.float64))
+    q.view(torch.uint8).copy_(torch.from_numpy(rq))
+    s.copy_(torch.from_numpy(rs))
+    dy, _ = _rows(rng.standard_normal((n, co)), dtype, pad)
+    longest = int(np.bincount(choice[(choice >= 0) & (choice < E)], minlength=1).max())
+    return c, layer, choice, order, offsets, q, s, B.restore(rq, rs), dy, longest, rng
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=["x".join(str(v) for v in s) for s in SHAPES])
+def test_products(shape, dtype):
+    tokens, fan, E, ci, co, bias, kind, pad = shape
+    c, layer, choice, order, offsets, q, s, x, dy, longest, rng = _setup(shape, dtype)
+    buf = torch.full((E * co * (ci + bias) + 8,), 5.0, device="cuda")
+    dW = buf[:-8].view(E, co, ci + bias)
+    kfac.kfac_expert_grad_weight_kept(c, layer, order, offsets, q, s, dy, dW, fan=fan)
+    torch.cuda.synchronize()
+    ref, mag = T.expert_grad_weight(choice, x, _values(dy), E, bias, fan)
+    assert (np.abs(_values(dW) - ref) <= (longest + 8) * 2.0 ** -24 * mag + 1e-40).all() and bool((buf[-8:] == 5.0).all())
+    refA, magA, count = T.expert_factors(choice, x, E, bias, fan)
+    refG, magG, _ = T.expert_factors(choice, _values(dy), E, 0, 1)
+    for decay in (0.0, 0.9):
+        A0, G0 = rng.standard_normal((E, ci + bias, ci + bias)).astype(np.float32), rng.standard_normal((E, co, co)).astype(np.float32)
+        A0, G0 = A0 + A0.transpose(0, 2, 1), G0 + G0.transpose(0, 2, 1)
+        if decay == 0.0:
+            A0[count > 0], G0[count > 0] = np.nan, np.nan
+        d = float(np.float32(decay))
+        for with_G in (False, True):
+            A, G = torch.from_numpy(A0).cuda(), torch.from_numpy(G0).cuda() if with_G else None
+            kfac.kfac_stats_expert_kept(c, layer, order, offsets, q, s, dy if with_G else None, decay, A, G, fan=fan)
+            torch.cuda.synchronize()
+            for got, old, ref, mag in ((A, A0, refA, magA),) + (((G, G0, refG, magG),) if with_G else ()):
+                g = got.cpu().numpy()
+                for e in range(E):
+                    if count[e] == 0:
+                        assert np.array_equal(g[e], old[e])
+                        continue
+                    before = np.zeros_like(ref[e]) if decay == 0.0 else old[e].astype(np.float64)
+                    want, m = d * before + (1 - d) * ref[e], d * np.abs(before) + (1 - d) * mag[e]
+                    assert (np.abs(g[e] - want) <= (longest + 12) * 2.0 ** -24 * m + 1e-40).all()
+                    assert np.array_equal(g[e], g[e].T)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_dense_layers_and_the_fp32_instruction(dtype):
+    """One expert that has all rows, in the order they stand; contexts that ask for the fp32 matrix instruction."""
+    rng = np.random.default_rng(1)
+    layer, n = wl.fc_layer(1, 72, 40, 1), 333
+    rq, rs = B.keep(rng.standard_normal((n, 72)))
+    q, s = torch.from_numpy(rq).cuda().view(E4M3), torch.from_numpy(rs).cuda()
+    dy = torch.from_numpy(rng.standard_normal((n, 40))).to(dtype).cuda()
+    offsets = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    x = B.restore(rq, rs)
+    for opts in (None, kfac.options(fp32_products=kfac.KFAC_PRODUCTS_FP32_MFMA)):
+        c = kfac.Context([layer], workspace_bytes=kfac.kfac_kept_workspace_bytes(layer, 1, n), opts=opts)
+        dW, A = torch.empty(1, 40, 73, device="cuda"), torch.empty(1, 73, 73, device="cuda")
+        kfac.kfac_expert_grad_weight_kept(c, layer, None, offsets, q, s, dy, dW)
+        kfac.kfac_stats_expert_kept(c, layer, None, offsets, q, s, None, 0.0, A, None)
+        ref, mag = T.expert_grad_weight(np.zeros(n, dtype=int), x, _values(dy), 1, 1, 1)
+        assert (np.abs(_values(dW) - ref) <= (n + 8) * 2.0 ** -24 * mag).all()
+        ref, mag, _ = T.expert_factors(np.zeros(n, dtype=int), x, 1, 1, 1)
+        assert (np.abs(_values(A) - ref) <= (n + 12) * 2.0 ** -24 * mag).all()
+        c.close()
+
+
+def test_no_rows():
+    layer = wl.fc_layer(1, 72, 40, 1)
+    c = kfac.Context([layer], workspace_bytes=kfac.kfac_kept_workspace_bytes(layer, 2, 0))
+    q, s, dy = torch.empty(0, 72, dtype=E4M3, device="cuda"), torch.empty(0, 3, dtype=torch.uint8, device="cuda"), torch.empty(0, 40, device="cuda")
+    order, offsets = torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    dW, A = torch.full((2, 40, 73), 5.0, device="cuda"), torch.full((2, 73, 73), 5.0, device="cuda")
+    kfac.kfac_expert_grad_weight_kept(c, layer, order, offsets, q, s, dy, dW)
+    kfac.kfac_stats_expert_kept(c, layer, order, offsets, q, s, None, 0.0, A, None)
+    assert not dW.any() and bool((A == 5.0).all())
+    c.close()
+
+
+def test_values_that_are_not_finite_stay_in_their_column():
+    layer, n = wl.fc_layer(1, 64, 64, 0), 100
+    x = torch.randn(n, 64, device="cuda")
+    x[10, 7] = float("inf")
+    c = kfac.Context([layer], workspace_bytes=kfac.kfac_kept_workspace_bytes(layer, 1, n))
+    q, s = torch.empty(n, 64, dtype=E4M3, device="cuda"), torch.empty(n, 2, dtype=torch.uint8, device="cuda")
+    kfac.kfac_keep(c, x, q, s)
+    dW = torch.empty(1, 64, 64, device="cuda")
+    kfac.kfac_expert_grad_weight_kept(c, layer, None, torch.tensor([0, n], dtype=torch.int32, device="cuda"), q, s, torch.randn(n, 64, device="cuda").bfloat16(), dW)
+    bad = torch.isnan(dW[0])
+    assert bad[:, 7].all() and not bad[:, :7].any() and not bad[:, 8:].any()
+    c.close()
+
+
+def test_binding_refuses(ctx):
+    x = torch.zeros(4, 40, device="cuda")
+    q, s, _, _ = _bytes(4, 40)
+    for bad in (dict(q=q.view(torch.uint8)), dict(scales=s[:, :1]), dict(scales=s.int()), dict(x=x.half()), dict(x=x[:, :33]), dict(q=q[:3])):
+        for fn in (kfac.kfac_keep, kfac.kfac_restore):
+            with pytest.raises(ValueError):
+                fn(**{**dict(ctx=ctx, x=x, q=q, scales=s), **bad})
+    layer = wl.fc_layer(1, 1024, 64, 0)
+    big, scales, _, _ = _bytes(64, 1024)
+    with pytest.raises(kfac.KfacError) as e:
+        kfac.kfac_expert_grad_weight_kept(ctx, layer, None, torch.tensor([0, 64], dtype=torch.int32, device="cuda"), big, scales,
+                                          torch.zeros(64, 64, device="cuda"), torch.empty(1, 64, 1024, device="cuda"))
+    assert e.value.status == kfac.KFAC_ERR_WORKSPACE
