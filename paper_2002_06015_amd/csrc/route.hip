@@ -12,22 +12,56 @@ namespace kfac {
 
 namespace {
 
-constexpr int kPer = kMaxRouted / 64;   // experts a lane, at most
-
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
 
-template <typename V>
-__device__ __forceinline__ V wave_sum(V v)
+// ---- over LANES adjacent lanes (16: a row of the data-parallel moves, or the whole wave), all of them active ----
+template <int CTRL, typename V>
+__device__ __forceinline__ V moved(V v)
+{
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int LANES, typename V, typename F>
+__device__ __forceinline__ V over_lanes(V v, F f)
+{
+    v = f(v, moved<0xB1>(v));    // quad_perm 1 0 3 2
+    v = f(v, moved<0x4E>(v));    // quad_perm 2 3 0 1
+    v = f(v, moved<0x141>(v));   // the other quad of eight
+    v = f(v, moved<0x140>(v));   // the other eight of sixteen
+    if constexpr (LANES == 64) {
+        v = f(v, __shfl_xor(v, 16));
+        v = f(v, __shfl_xor(v, 32));
+    }
+    return v;
+}
+template <int LANES> __device__ __forceinline__ float sum_of(float v) { return over_lanes<LANES>(v, [](float a, float b) { return a + b; }); }
+template <int LANES> __device__ __forceinline__ float max_of(float v) { return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES> __device__ __forceinline__ float min_of(float v) { return over_lanes<LANES>(v, [](float a, float b) { return fminf(a, b); }); }
+template <int LANES> __device__ __forceinline__ unsigned max_of(unsigned v) { return over_lanes<LANES>(v, [](unsigned a, unsigned b) { return max(a, b); }); }
+// of the next lane
+template <int LANES, typename V>
+__device__ __forceinline__ V next_lane(V v)
+{
+    if constexpr (LANES == 16) return moved<0x101>(v);   // row_shl 1
+    else return __shfl(v, (threadIdx.x + 1) & 63);
+}
+
+// The weights w_j = s_j / (sum of the chosen s) of renormalised gates, in the lanes j that hold a chosen logit (there).
+template <int LANES>
+__device__ __forceinline__ float weight(bool sigmoids, float l, bool there)
+{
+    const float m = max_of<LANES>(there ? l : -INFINITY);
+    float e;
+    if (sigmoids && m >= -60.f) e = there ? sigmoid(l) : 0.f;
+    else e = there ? expf(l - m) : 0.f;
+    return e / sum_of<LANES>(e);
+}
+
+// ---- in 64 bits: any number of experts and groups -------------------------------------------------------
+__device__ __forceinline__ double wave_sum(double v)
 {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-__device__ __forceinline__ float wave_max(float v)
-{
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-
 // The best (rank, lowest number) of the wave's lanes; number < 0: none.
 __device__ __forceinline__ void best_of_wave(double &rank, int &number)
 {
@@ -37,140 +71,295 @@ __device__ __forceinline__ void best_of_wave(double &rank, int &number)
         if (n >= 0 && (number < 0 || r > rank || (r == rank && n < number))) { rank = r; number = n; }
     }
 }
+// LDS accesses of a wave take place in order: only the compiler has to keep them so.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// The weights w_j = s_j / (sum of the chosen s) of renormalised gates, in the lanes j that hold a chosen logit (there).
-__device__ __forceinline__ float weight(bool sigmoids, float l, bool there)
+// One token by a whole wave; lane i holds experts i, i + 64, ...; ranks: LDS, 64 PER of the wave's own.
+template <typename T, int PER>
+__device__ __forceinline__ void route_exactly(const RouteArgs &a, long long token, double *ranks)
 {
-    const float m = wave_max(there ? l : -INFINITY);
-    float e;
-    if (sigmoids && m >= -60.f) e = there ? sigmoid(l) : 0.f;
-    else e = there ? expf(l - m) : 0.f;
-    return e / wave_sum(e);
+    const int lane = threadIdx.x & 63;
+    const T *logits = (const T *)a.logits + token * a.ld;
+    double rank[PER];
+    bool bad = false;
+    float high = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 64 * i;
+        rank[i] = -INFINITY;
+        if (e < a.experts) {
+            const float l = Element<T>::get(logits + e);
+            rank[i] = l;
+            bad |= l != l || (!a.sigmoid && l == INFINITY);
+            high = fmaxf(high, l);
+        }
+    }
+    high = max_of<64>(high);
+    const bool sums = a.groups > 1 && a.group_best > 1;
+    if (a.bias || sums) {
+        double total = 0.0;
+        if (!a.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (rank[i] > -INFINITY) total += exp(rank[i] - (double)high);
+            total = wave_sum(total);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (rank[i] > -INFINITY) {
+                double s = a.sigmoid ? 1.0 / (1.0 + exp(-rank[i])) : exp(rank[i] - (double)high) / total;
+                if (a.bias) s += (double)a.bias[lane + 64 * i];
+                bad |= s != s;
+                rank[i] = s;
+            }
+    }
+    if (a.groups > 1) {
+        const int size = a.experts / a.groups;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) ranks[lane + 64 * i] = rank[i];
+        in_order();
+        double of[PER];   // the ranks of groups lane, lane + 64, ...
+        unsigned open = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int g = lane + 64 * i;
+            double one = -INFINITY, two = -INFINITY;
+            if (g < a.groups)
+                for (int q = 0; q < size; ++q) {
+                    const double r = ranks[g * size + q];
+                    if (r > one) { two = one; one = r; }
+                    else if (r > two) two = r;
+                }
+            of[i] = a.group_best > 1 && two > -INFINITY ? one + two : one;
+        }
+        in_order();
+        for (int k = 0; k < a.top_groups; ++k) {
+            double best = -INFINITY;
+            int number = -1;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (!(open >> i & 1) && of[i] > best) { best = of[i]; number = lane + 64 * i; }
+            best_of_wave(best, number);
+            if (number < 0) break;
+            if ((number & 63) == lane) open |= 1u << (number >> 6);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) ranks[lane + 64 * i] = open >> i & 1 ? 1.0 : 0.0;   // (of groups now)
+        in_order();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = lane + 64 * i;
+            if (e < a.experts && ranks[e / size] == 0.0) rank[i] = -INFINITY;
+            else if (e < a.experts && sums && !a.bias) rank[i] = Element<T>::get(logits + e);
+        }
+        in_order();
+    }
+    bad = __ballot(bad) != 0;
+    int mine = -1;
+    for (int k = 0; k < a.fan; ++k) {
+        double best = -INFINITY;
+        int number = -1;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (rank[i] > best) { best = rank[i]; number = lane + 64 * i; }
+        best_of_wave(best, number);
+        if (bad || number < 0) break;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (number == lane + 64 * i) rank[i] = -INFINITY;
+        if (lane == k) mine = number;
+    }
+    const bool there = mine >= 0;
+    const float l = there ? Element<T>::get(logits + mine) : 0.f;
+    float gate;
+    if (a.renormalise) {
+        gate = weight<64>(a.sigmoid, l, there);
+    } else if (a.sigmoid) {
+        gate = sigmoid(l);
+    } else {
+        float sum = 0.f;
+        for (int e = lane; e < a.experts; e += 64) sum += expf(Element<T>::get(logits + e) - high);
+        gate = expf(l - high) / sum_of<64>(sum);
+    }
+    if (lane < a.fan) {
+        a.choice[token * a.fan + lane] = mine;
+        a.gate[token * a.fan + lane] = bad ? __uint_as_float(0x7FC00000u) : there ? a.scale * gate : 0.f;
+    }
 }
 
-// One wave a token; lane i holds experts i, i + 64, ...
 template <typename T>
-__global__ __launch_bounds__(256) void route_kernel(const RouteArgs a)
+__global__ __launch_bounds__(256) void route_general_kernel(const RouteArgs a)
 {
     __shared__ double ranks[4][kMaxRouted];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool by_score = a.bias || (a.groups > 1 && a.group_best > 1);
-    for (long long token = (long long)blockIdx.x * 4 + wave; token - wave < a.n; token += 4LL * gridDim.x) {
-        if (token < a.n) {
-            const T *logits = (const T *)a.logits + token * a.ld;
-            double rank[kPer];
-            bool bad = false;
-            float high = -INFINITY;
+    for (long long token = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); token < a.n; token += 4LL * gridDim.x)
+        route_exactly<T, kMaxRouted / 64>(a, token, ranks[threadIdx.x >> 6]);
+}
+
+// ---- LANES lanes a token, EPL experts a lane -------------------------------------------------------------
+// Lane i holds the `per` experts from i per on.  Ranks are formed in fp32 and brought into whole numbers: 31 bits, below them the
+// experts' numbers from behind, so that the largest is the choice and all of them differ.  The best one below M is M + max(key - M)
+// in wrapping arithmetic: an element costs a subtraction and half a maximum in each round.  Where two neighbours among the chosen (and
+// the first that is not chosen) are nearer than the error of their ranks, and not exactly equal, the wave does the token again in 64 bits; so
+// it does with ranks that are not finite.  Groups need to be whole lanes.
+// 65536 tokens 256 experts bf16, sigmoids, a bias, 4 of 8 groups, fan 8: see the launch.
+template <typename T, int N>
+__device__ __forceinline__ void load_logits(const T *p, int there, float (&v)[N])
+{
+    typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    if (there >= N) {
+        if constexpr (N == 8) {
+            load8(p, 8, v);
+        } else if constexpr (N == 1) {
+            v[0] = Element<T>::get(p);
+        } else {
+            const vec r = *(const vec *)p;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int e = lane + 64 * i;
-                rank[i] = -INFINITY;
-                if (e < a.experts) {
-                    const float l = Element<T>::get(logits + e);
-                    rank[i] = l;
-                    bad |= l != l || (!a.sigmoid && l == INFINITY);
-                    high = fmaxf(high, l);
-                }
-            }
-            high = wave_max(high);
-            double total = 0.0;
-            if (by_score) {
-                if (!a.sigmoid) {
-#pragma unroll
-                    for (int i = 0; i < kPer; ++i)
-                        if (rank[i] > -INFINITY) total += exp(rank[i] - (double)high);
-                    total = wave_sum(total);
-                }
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int e = lane + 64 * i;
-                    if (rank[i] > -INFINITY) {
-                        double s = a.sigmoid ? 1.0 / (1.0 + exp(-rank[i])) : exp(rank[i] - (double)high) / total;
-                        if (a.bias) s += (double)a.bias[e];
-                        bad |= s != s;
-                        rank[i] = s;
-                    }
-                }
-            }
-            if (a.groups > 1) {
-                const int size = a.experts / a.groups;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (lane + 64 * i < a.experts) ranks[wave][lane + 64 * i] = rank[i];
-                __builtin_amdgcn_wave_barrier();
-                __threadfence_block();
-                // lanes take groups in turn; the ranks of groups replace those of their first experts afterwards
-                double group_rank[kPer];
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int g = lane + 64 * i;
-                    double one = -INFINITY, two = -INFINITY;
-                    if (g < a.groups)
-                        for (int q = 0; q < size; ++q) {
-                            const double r = ranks[wave][g * size + q];
-                            if (r > one) { two = one; one = r; }
-                            else if (r > two) two = r;
-                        }
-                    group_rank[i] = a.group_best > 1 && two > -INFINITY ? one + two : one;
-                }
-                unsigned open = 0;   // of the lane's groups
-                for (int k = 0; k < a.top_groups; ++k) {
-                    double best = -INFINITY;
-                    int number = -1;
-#pragma unroll
-                    for (int i = 0; i < kPer; ++i)
-                        if (!(open >> i & 1) && group_rank[i] > best) { best = group_rank[i]; number = lane + 64 * i; }
-                    best_of_wave(best, number);
-                    if (number < 0) break;
-                    if ((number & 63) == lane) open |= 1u << (number >> 6);
-                }
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (lane + 64 * i < a.groups) ranks[wave][lane + 64 * i] = open >> i & 1 ? 1.0 : 0.0;
-                __builtin_amdgcn_wave_barrier();
-                __threadfence_block();
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int e = lane + 64 * i;
-                    if (e < a.experts && ranks[wave][e / size] == 0.0) rank[i] = -INFINITY;
-                }
-                __builtin_amdgcn_wave_barrier();
-            }
-            bad = __ballot(bad) != 0;
-            int mine = -1;
-            for (int k = 0; k < a.fan; ++k) {
-                double best = -INFINITY;
-                int number = -1;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (rank[i] > best) { best = rank[i]; number = lane + 64 * i; }
-                best_of_wave(best, number);
-                if (bad || number < 0) break;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (number == lane + 64 * i) rank[i] = -INFINITY;
-                if (lane == k) mine = number;
-            }
-            const bool there = mine >= 0;
-            const float l = there ? Element<T>::get(logits + mine) : 0.f;
-            float gate;
-            if (a.renormalise) {
-                gate = weight(a.sigmoid, l, there);
-            } else if (a.sigmoid) {
-                gate = sigmoid(l);
-            } else {
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (lane + 64 * i < a.experts) sum += expf(Element<T>::get(logits + lane + 64 * i) - high);
-                gate = expf(l - high) / wave_sum(sum);
-            }
-            if (lane < a.fan) {
-                a.choice[token * a.fan + lane] = mine;
-                a.gate[token * a.fan + lane] = bad ? __uint_as_float(0x7FC00000u) : there ? a.scale * gate : 0.f;
+            for (int j = 0; j < N; ++j) {
+                const T one = r[j];
+                v[j] = Element<T>::get(&one);
             }
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = j < there ? Element<T>::get(p + j) : -INFINITY;
+    }
+}
+
+template <typename T, int LANES, int EPL>
+__global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5 : 2) void route_kernel(const RouteArgs a, int per)
+{
+    constexpr int ALL = LANES * EPL, IB = ALL <= 16 ? 4 : ALL <= 32 ? 5 : ALL <= 64 ? 6 : ALL <= 128 ? 7 : ALL <= 256 ? 8 : ALL <= 512 ? 9 : 10;
+    constexpr int ROWS = 256 / LANES, N = EPL < 8 ? EPL : 8, PER = (ALL + 63) / 64;
+    __shared__ double ranks[4][64 * PER];
+    const int lane = threadIdx.x & 63, sub = lane & (LANES - 1), first = sub * per;
+    const bool sums = a.groups > 1 && a.group_best > 1, by_score = a.bias || sums;
+    for (long long base = (long long)blockIdx.x * ROWS; base < a.n; base += (long long)gridDim.x * ROWS) {
+        const long long mine_at = base + threadIdx.x / LANES, token = mine_at < a.n ? mine_at : a.n - 1;   // (all lanes take part)
+        const T *logits = (const T *)a.logits + token * a.ld;
+        const int there = min(per, a.experts - first);
+        float l[EPL], k[EPL];
+#pragma unroll
+        for (int i = 0; i < EPL; i += N) {
+            float v[N];
+            load_logits(logits + first + i, there - i, v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) l[i + j] = v[j];
+        }
+        bool again = false;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            again |= l[i] != l[i];
+            k[i] = l[i];
+        }
+        float high = l[0];
+#pragma unroll
+        for (int i = 1; i < EPL; ++i) high = fmaxf(high, l[i]);
+        high = max_of<LANES>(high);
+        again |= high == INFINITY;
+        float total = 1.f, error = 0.f;
+        if (!a.sigmoid && (by_score || !a.renormalise)) {
+            total = 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                const float e = l[i] > -INFINITY ? __expf(l[i] - high) : 0.f;
+                total += e;
+                if (by_score) k[i] = e;
+            }
+            total = sum_of<LANES>(total);
+        }
+        if (by_score) {
+            // errors: sigmoids below 2^-21 (the argument's rounding is multiplied by s (1 - s)), softmaxes below 2^-19 of the largest
+            const float share = 1.f / total;
+            error = a.sigmoid ? 0x1p-21f : 0x1p-19f * share;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.f + __expf(-l[i])) : k[i] * share;
+                if (a.bias && i < there) s += a.bias[first + i];
+                s = l[i] > -INFINITY ? s : -INFINITY;
+                again |= s != s;
+                k[i] = s;
+            }
+        }
+        if (a.groups > 1) {
+            float one = -INFINITY, two = -INFINITY, largest = 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                two = fmaxf(two, fminf(one, k[i]));
+                one = fmaxf(one, k[i]);
+            }
+            const int lanes = LANES / a.groups;   // of a group
+            for (int o = 1; o < lanes; o <<= 1) {
+                const float p = __shfl_xor(one, o), q = __shfl_xor(two, o);
+                two = fmaxf(fmaxf(two, q), fminf(one, p));
+                one = fmaxf(one, p);
+            }
+            const float of = a.group_best > 1 && two > -INFINITY ? one + two : one;
+            int better = 0;
+            for (int d = lanes; d < LANES; d += lanes) {
+                const int other = (sub + d) & (LANES - 1);
+                const float r = __shfl(of, lane - sub + other);
+                better += r > of || (r == of && other < sub) ? 1 : 0;
+            }
+            const bool open = better < a.top_groups;
+            if (by_score) {
+                const float low = min_of<LANES>(open ? of : INFINITY), next = max_of<LANES>(open ? -INFINITY : of);
+                largest = fmaxf(fabsf(low), fabsf(next));
+                again |= next > -INFINITY && !(low - next > 4.f * error + 0x1p-21f * largest);
+            }
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) k[i] = !open ? -INFINITY : sums && !a.bias ? l[i] : k[i];
+            if (sums && !a.bias) error = 0.f;
+        }
+        // whole numbers: 1024 at the least of the lanes' best ones, which the `fan` best and the next one mostly reach (where fewer lanes than
+        // that are open: at the least open one), but 64 below the best at most; what is further below is 1
+        float best = k[0];
+#pragma unroll
+        for (int i = 1; i < EPL; ++i) best = fmaxf(best, k[i]);
+        float low = best > -INFINITY ? best : INFINITY;
+        if (a.groups > 1 && a.top_groups * (LANES / a.groups) <= a.fan)
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) low = k[i] > -INFINITY ? fminf(low, k[i]) : low;
+        const float top = max_of<LANES>(best);
+        low = fmaxf(min_of<LANES>(low), top - 64.f);
+        again |= top == INFINITY;
+        constexpr float steps = (float)((1u << (IB < 8 ? 23 : 31 - IB)) - 2048);   // (24 bits: each is formed with less than one of error)
+        const float step = top > low ? fminf(steps / (top - low), 0x1p100f) : 0.f;
+        const unsigned margin = error > 0.f ? (unsigned)fminf(2.f * (error + 0x1p-23f * fmaxf(fabsf(top), fabsf(low))) * step, steps) + 4u : 0u;
+        unsigned key[EPL];
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            const unsigned q = (unsigned)fmaxf(fmaf(k[i] - low, step, 1024.f), 1.f);
+            key[i] = k[i] > -INFINITY ? (q << IB) + (unsigned)(ALL - 1 - first - i) : 0u;
+        }
+        unsigned mine = 0, M = 0x80000000u;
+        for (int r = 0; r <= a.fan; ++r) {
+            unsigned far = key[0] - M;
+#pragma unroll
+            for (int i = 1; i < EPL; ++i) far = max(far, key[i] - M);
+            far = max_of<LANES>(far);
+            M = M == 0 ? 0 : M + far;
+            mine = sub == r ? M : mine;
+        }
+        const int e = ALL - 1 - (int)(mine & (ALL - 1));
+        const float chosen = mine ? Element<T>::get(logits + e) : 0.f, added = mine && a.bias ? a.bias[e] : 0.f;
+        const unsigned next = next_lane<LANES>(mine);
+        const bool equal = chosen == next_lane<LANES>(chosen) && added == next_lane<LANES>(added);
+        again |= sub < a.fan && next != 0 && (mine >> IB) - (next >> IB) <= margin && !equal;
+        const unsigned long long rows = __ballot(again);
+        const bool mine_again = (rows >> (lane - sub) & (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1)) != 0;
+        const bool chosen_one = mine != 0 && sub < a.fan;
+        float gate;
+        if (a.renormalise) gate = weight<LANES>(a.sigmoid, chosen, chosen_one);
+        else gate = a.sigmoid ? sigmoid(chosen) : expf(chosen - high) / total;
+        if (sub < a.fan && mine_at < a.n && !mine_again) {
+            a.choice[token * a.fan + sub] = chosen_one ? e : -1;
+            a.gate[token * a.fan + sub] = chosen_one ? a.scale * gate : 0.f;
+        }
+        if (rows)
+            for (int r = 0; r < 64 / LANES; ++r) {
+                const long long t = base + (threadIdx.x >> 6) * (64 / LANES) + r;
+                if ((rows >> (LANES * r) & (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1)) && t < a.n) route_exactly<T, PER>(a, t, ranks[threadIdx.x >> 6]);
+            }
     }
 }
 
@@ -189,7 +378,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a)
         const bool any = __ballot(there) != 0;
         float part = 0.f, common = 0.f, high = 0.f, share = 0.f;   // of the lane's choice; what all experts lose (softmax); their score
         if (a.renormalise) {
-            const float w = weight(a.sigmoid, l, there), mean = wave_sum(there ? up * w : 0.f);
+            const float w = weight<64>(a.sigmoid, l, there), mean = sum_of<64>(there ? up * w : 0.f);
             part = there ? w * (up - mean) : 0.f;
             if (a.sigmoid) part *= sigmoid(-l);
         } else if (a.sigmoid) {
@@ -197,12 +386,12 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a)
         } else if (any) {
             high = -INFINITY;
             for (int e = lane; e < a.experts; e += 64) high = fmaxf(high, Element<T>::get(logits + e));
-            high = wave_max(high);
+            high = max_of<64>(high);
             float sum = 0.f;
             for (int e = lane; e < a.experts; e += 64) sum += expf(Element<T>::get(logits + e) - high);
-            share = 1.f / wave_sum(sum);
+            share = 1.f / sum_of<64>(sum);
             part = there ? up * (expf(l - high) * share) : 0.f;
-            common = wave_sum(part);
+            common = sum_of<64>(part);
         }
         for (int e0 = 0; e0 < a.experts; e0 += 64) {
             const int e = e0 + lane;
@@ -220,20 +409,41 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a)
     }
 }
 
-template <typename K>
-hipError_t run(K kernel, const RouteArgs &a, hipStream_t s)
+// A launch takes less than 2^32 threads; the kernels go on from there.
+dim3 workgroups(int n, int rows) { return dim3((unsigned)min((n + rows - 1) / rows, 1 << 20)); }
+
+template <typename T, int LANES, int EPL>
+hipError_t run(const RouteArgs &a, hipStream_t s)
 {
-    const int wgs = (a.n + 3) / 4;
-    kernel<<<dim3((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20))), dim3(256), 0, s>>>(a);
+    route_kernel<T, LANES, EPL><<<workgroups(a.n, 256 / LANES), dim3(256), 0, s>>>(a, (a.experts + LANES - 1) / LANES);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run(const RouteArgs &a, hipStream_t s)
+{
+    const int lanes = a.experts <= 256 ? 16 : 64, per = (a.experts + lanes - 1) / lanes;
+    if (a.fan >= lanes || (a.groups > 1 && (lanes % a.groups || a.experts % lanes))) {
+        route_general_kernel<T><<<workgroups(a.n, 4), dim3(256), 0, s>>>(a);
+        return hipGetLastError();
+    }
+    if (lanes == 64) return per <= 8 ? run<T, 64, 8>(a, s) : run<T, 64, 16>(a, s);
+    if (per <= 1) return run<T, 16, 1>(a, s);
+    if (per <= 2) return run<T, 16, 2>(a, s);
+    if (per <= 4) return run<T, 16, 4>(a, s);
+    return per <= 8 ? run<T, 16, 8>(a, s) : run<T, 16, 16>(a, s);
+}
+
+template <typename T>
+hipError_t run_grad(const RouteArgs &a, hipStream_t s)
+{
+    route_grad_kernel<T><<<workgroups(a.n, 4), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_route(const RouteArgs &a, int bf16, hipStream_t s) { return bf16 ? run(route_kernel<bf16_bits>, a, s) : run(route_kernel<float>, a, s); }
-hipError_t launch_route_grad(const RouteArgs &a, int bf16, hipStream_t s)
-{
-    return bf16 ? run(route_grad_kernel<bf16_bits>, a, s) : run(route_grad_kernel<float>, a, s);
-}
+hipError_t launch_route(const RouteArgs &a, int bf16, hipStream_t s) { return bf16 ? run<bf16_bits>(a, s) : run<float>(a, s); }
+hipError_t launch_route_grad(const RouteArgs &a, int bf16, hipStream_t s) { return bf16 ? run_grad<bf16_bits>(a, s) : run_grad<float>(a, s); }
 
 }  // namespace kfac
