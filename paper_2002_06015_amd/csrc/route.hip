@@ -78,7 +78,8 @@ __device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ
 template <typename T, int PER>
 __device__ __forceinline__ void route_exactly(const RouteArgs &a, long long token, double *ranks)
 {
-    const int lane = threadIdx.x & 63;
+    int lane = threadIdx.x & 63, groups = a.groups;
+    asm("" : "+v"(lane), "+s"(groups));   // (what hangs on these is not to be worked out ahead of a rare call)
     const T *logits = (const T *)a.logits + token * a.ld;
     double rank[PER];
     bool bad = false;
@@ -95,7 +96,7 @@ __device__ __forceinline__ void route_exactly(const RouteArgs &a, long long toke
         }
     }
     high = max_of<64>(high);
-    const bool sums = a.groups > 1 && a.group_best > 1;
+    const bool sums = groups > 1 && a.group_best > 1;
     if (a.bias || sums) {
         double total = 0.0;
         if (!a.sigmoid) {
@@ -113,8 +114,8 @@ __device__ __forceinline__ void route_exactly(const RouteArgs &a, long long toke
                 rank[i] = s;
             }
     }
-    if (a.groups > 1) {
-        const int size = a.experts / a.groups;
+    if (groups > 1) {
+        const int size = a.experts / groups;
 #pragma unroll
         for (int i = 0; i < PER; ++i) ranks[lane + 64 * i] = rank[i];
         in_order();
@@ -124,7 +125,7 @@ __device__ __forceinline__ void route_exactly(const RouteArgs &a, long long toke
         for (int i = 0; i < PER; ++i) {
             const int g = lane + 64 * i;
             double one = -INFINITY, two = -INFINITY;
-            if (g < a.groups)
+            if (g < groups)
                 for (int q = 0; q < size; ++q) {
                     const double r = ranks[g * size + q];
                     if (r > one) { two = one; one = r; }
@@ -226,7 +227,7 @@ __device__ __forceinline__ void load_logits(const T *p, int there, float (&v)[N]
 }
 
 template <typename T, int LANES, int EPL>
-__global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5 : 2) void route_kernel(const RouteArgs a, int per)
+__global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5 : 2) void route_kernel(const RouteArgs a, int per, int group_lanes)
 {
     constexpr int ALL = LANES * EPL, IB = ALL <= 16 ? 4 : ALL <= 32 ? 5 : ALL <= 64 ? 6 : ALL <= 128 ? 7 : ALL <= 256 ? 8 : ALL <= 512 ? 9 : 10;
     constexpr int ROWS = 256 / LANES, N = EPL < 8 ? EPL : 8, PER = (ALL + 63) / 64;
@@ -271,13 +272,26 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
             // errors: sigmoids below 2^-21 (the argument's rounding is multiplied by s (1 - s)), softmaxes below 2^-19 of the largest
             const float share = 1.f / total;
             error = a.sigmoid ? 0x1p-21f : 0x1p-19f * share;
+            if (a.sigmoid) {
+#pragma unroll
+                for (int i = 0; i < EPL; ++i) k[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < EPL; ++i) k[i] *= share;
+            }
+            if (a.bias) {
+#pragma unroll
+                for (int i = 0; i < EPL; i += N) {
+                    float v[N];
+                    load_logits(a.bias + first + i, there - i, v);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) k[i + j] += v[j];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < EPL; ++i) {
-                float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.f + __expf(-l[i])) : k[i] * share;
-                if (a.bias && i < there) s += a.bias[first + i];
-                s = l[i] > -INFINITY ? s : -INFINITY;
-                again |= s != s;
-                k[i] = s;
+                k[i] = l[i] > -INFINITY ? k[i] : -INFINITY;
+                again |= k[i] != k[i];
             }
         }
         if (a.groups > 1) {
@@ -287,15 +301,14 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
                 two = fmaxf(two, fminf(one, k[i]));
                 one = fmaxf(one, k[i]);
             }
-            const int lanes = LANES / a.groups;   // of a group
-            for (int o = 1; o < lanes; o <<= 1) {
+            for (int o = 1; o < group_lanes; o <<= 1) {
                 const float p = __shfl_xor(one, o), q = __shfl_xor(two, o);
                 two = fmaxf(fmaxf(two, q), fminf(one, p));
                 one = fmaxf(one, p);
             }
             const float of = a.group_best > 1 && two > -INFINITY ? one + two : one;
             int better = 0;
-            for (int d = lanes; d < LANES; d += lanes) {
+            for (int d = group_lanes; d < LANES; d += group_lanes) {
                 const int other = (sub + d) & (LANES - 1);
                 const float r = __shfl(of, lane - sub + other);
                 better += r > of || (r == of && other < sub) ? 1 : 0;
@@ -316,7 +329,7 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
 #pragma unroll
         for (int i = 1; i < EPL; ++i) best = fmaxf(best, k[i]);
         float low = best > -INFINITY ? best : INFINITY;
-        if (a.groups > 1 && a.top_groups * (LANES / a.groups) <= a.fan)
+        if (a.groups > 1 && a.top_groups * group_lanes <= a.fan)
 #pragma unroll
             for (int i = 0; i < EPL; ++i) low = k[i] > -INFINITY ? fminf(low, k[i]) : low;
         const float top = max_of<LANES>(best);
@@ -415,7 +428,7 @@ dim3 workgroups(int n, int rows) { return dim3((unsigned)min((n + rows - 1) / ro
 template <typename T, int LANES, int EPL>
 hipError_t run(const RouteArgs &a, hipStream_t s)
 {
-    route_kernel<T, LANES, EPL><<<workgroups(a.n, 256 / LANES), dim3(256), 0, s>>>(a, (a.experts + LANES - 1) / LANES);
+    route_kernel<T, LANES, EPL><<<workgroups(a.n, 256 / LANES), dim3(256), 0, s>>>(a, (a.experts + LANES - 1) / LANES, LANES / a.groups);
     return hipGetLastError();
 }
 
