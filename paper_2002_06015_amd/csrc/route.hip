@@ -226,6 +226,32 @@ __device__ __forceinline__ void load_logits(const T *p, int there, float (&v)[N]
     }
 }
 
+template <typename T, int N>
+__device__ __forceinline__ void store_logits(T *p, int there, const float (&v)[N])
+{
+    typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    if (there >= N) {
+        if constexpr (N == 8) {
+            store8(p, 8, v);
+        } else if constexpr (N == 1) {
+            Element<T>::put(p, v[0]);
+        } else {
+            vec r;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                T one;
+                Element<T>::put(&one, v[j]);
+                r[j] = one;
+            }
+            *(vec *)p = r;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < there) Element<T>::put(p + j, v[j]);
+    }
+}
+
 template <typename T, int LANES, int EPL>
 __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5 : 2) void route_kernel(const RouteArgs a, int per, int group_lanes)
 {
@@ -376,49 +402,87 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
     }
 }
 
-// One wave a token.
-template <typename T>
+// ---- gradient -------------------------------------------------------------------------------------------
+// LANES lanes a token; lane i < fan works on choice i, then every lane on chunks of N adjacent experts.  A row of zeros with the
+// choices' parts in their places is put together in LDS (an expert that is there twice gets the sum in the order of the choices).
+// Bound by memory and the launch: see there.
+template <typename T, int LANES, int EPL>
 __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    for (long long token = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); token < a.n; token += 4LL * gridDim.x) {
+    constexpr int ROWS = 256 / LANES, N = EPL < 8 ? EPL : 8, ALL = LANES * EPL;
+    __shared__ __attribute__((aligned(16))) float rows[ROWS][ALL];
+    const int lane = threadIdx.x & 63, sub = lane & (LANES - 1);
+    float *const row = rows[threadIdx.x / LANES];
+    for (long long base = (long long)blockIdx.x * ROWS; base < a.n; base += (long long)gridDim.x * ROWS) {
+        const long long at = base + threadIdx.x / LANES, token = at < a.n ? at : a.n - 1;   // (all lanes take part)
         const T *logits = (const T *)a.logits + token * a.ld;
-        T *out = (T *)a.dlogits + token * a.ldd;
-        int mine = lane < a.fan ? a.choice[token * a.fan + lane] : -1;
+        int mine = sub < a.fan ? a.choice[token * a.fan + sub] : -1;
         const bool there = mine >= 0 && mine < a.experts;
-        const float l = there ? Element<T>::get(logits + mine) : 0.f, up = there ? a.scale * a.dgate[token * a.fan + lane] : 0.f;
         if (!there) mine = -1;
-        const bool any = __ballot(there) != 0;
-        float part = 0.f, common = 0.f, high = 0.f, share = 0.f;   // of the lane's choice; what all experts lose (softmax); their score
+        const float up = there ? a.scale * a.dgate[token * a.fan + sub] : 0.f;
+        float part = 0.f, common = 0.f, s[EPL];   // of the lane's choice; what all experts lose; their scores (softmax)
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) s[i] = 0.f;
         if (a.renormalise) {
-            const float w = weight<64>(a.sigmoid, l, there), mean = sum_of<64>(there ? up * w : 0.f);
+            const float l = there ? Element<T>::get(logits + mine) : 0.f, w = weight<LANES>(a.sigmoid, l, there), mean = sum_of<LANES>(there ? up * w : 0.f);
             part = there ? w * (up - mean) : 0.f;
             if (a.sigmoid) part *= sigmoid(-l);
         } else if (a.sigmoid) {
+            const float l = there ? Element<T>::get(logits + mine) : 0.f;
             part = up * sigmoid(l) * sigmoid(-l);
-        } else if (any) {
-            high = -INFINITY;
-            for (int e = lane; e < a.experts; e += 64) high = fmaxf(high, Element<T>::get(logits + e));
-            high = max_of<64>(high);
-            float sum = 0.f;
-            for (int e = lane; e < a.experts; e += 64) sum += expf(Element<T>::get(logits + e) - high);
-            share = 1.f / sum_of<64>(sum);
+        } else {
+            float high = -INFINITY, total = 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; i += N) {
+                const int e = (i / N * LANES + sub) * N;
+                float v[N];
+                load_logits(logits + e, a.experts - e, v);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    s[i + j] = v[j];
+                    high = fmaxf(high, v[j]);
+                }
+            }
+            high = max_of<LANES>(high);
+            const float l = there ? Element<T>::get(logits + mine) : 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                s[i] = s[i] == -INFINITY ? 0.f : expf(s[i] - high);
+                total += s[i];
+            }
+            const float share = 1.f / sum_of<LANES>(total);
+            const bool any = max_of<LANES>(there ? 1u : 0u) != 0;   // a token without a choice gets zeros, whatever its logits
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) s[i] = any ? s[i] * share : 0.f;
             part = there ? up * (expf(l - high) * share) : 0.f;
-            common = sum_of<64>(part);
+            common = sum_of<LANES>(part);
         }
-        for (int e0 = 0; e0 < a.experts; e0 += 64) {
-            const int e = e0 + lane;
-            float sum = 0.f;
-            for (int j = 0; j < a.fan; ++j) {
-                const int c = __shfl(mine, j);
-                const float p = __shfl(part, j);
-                sum += c == e ? p : 0.f;
-            }
-            if (e < a.experts) {
-                if (share != 0.f) sum -= common * (expf(Element<T>::get(logits + e) - high) * share);
-                Element<T>::put(out + e, sum);
-            }
+        // the sum over equal choices, by the first of them
+        float sum = 0.f;
+        bool first = there;
+        for (int j = 0; j < a.fan; ++j) {
+            const int c = __shfl(mine, lane - sub + j);
+            const float p = __shfl(part, lane - sub + j);
+            sum += c == mine ? p : 0.f;
+            first = first && !(j < sub && c == mine);
         }
+        in_order();
+#pragma unroll
+        for (int i = 0; i < EPL; i += N)
+#pragma unroll
+            for (int j = 0; j < N; ++j) row[(i / N * LANES + sub) * N + j] = 0.f;
+        in_order();
+        if (first) row[mine] = sum;
+        in_order();
+#pragma unroll
+        for (int i = 0; i < EPL; i += N) {
+            const int e = (i / N * LANES + sub) * N;
+            float v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = row[e + j] - common * s[i + j];
+            if (at < a.n) store_logits((T *)a.dlogits + token * a.ldd + e, a.experts - e, v);
+        }
+        in_order();
     }
 }
 
@@ -447,11 +511,22 @@ hipError_t run(const RouteArgs &a, hipStream_t s)
     return per <= 8 ? run<T, 16, 8>(a, s) : run<T, 16, 16>(a, s);
 }
 
+template <typename T, int LANES, int EPL>
+hipError_t run_grad(const RouteArgs &a, hipStream_t s)
+{
+    route_grad_kernel<T, LANES, EPL><<<workgroups(a.n, 256 / LANES), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t run_grad(const RouteArgs &a, hipStream_t s)
 {
-    route_grad_kernel<T><<<workgroups(a.n, 4), dim3(256), 0, s>>>(a);
-    return hipGetLastError();
+    const int lanes = a.experts <= 256 && a.fan <= 16 ? 16 : 64, per = (a.experts + lanes - 1) / lanes;
+    if (lanes == 64) return per <= 4 ? run_grad<T, 64, 4>(a, s) : per <= 8 ? run_grad<T, 64, 8>(a, s) : run_grad<T, 64, 16>(a, s);
+    if (per <= 1) return run_grad<T, 16, 1>(a, s);
+    if (per <= 2) return run_grad<T, 16, 2>(a, s);
+    if (per <= 4) return run_grad<T, 16, 4>(a, s);
+    return per <= 8 ? run_grad<T, 16, 8>(a, s) : run_grad<T, 16, 16>(a, s);
 }
 
 }  // namespace
