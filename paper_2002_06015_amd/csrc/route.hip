@@ -62,114 +62,121 @@ __device__ __forceinline__ double wave_sum(double v)
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-// The best (rank, lowest number) of the wave's lanes; number < 0: none.
-__device__ __forceinline__ void best_of_wave(double &rank, int &number)
+template <int CTRL>
+__device__ __forceinline__ double max_moved(double v)
 {
-    for (int o = 32; o > 0; o >>= 1) {
-        const double r = __shfl_xor(rank, o);
-        const int n = __shfl_xor(number, o);
-        if (n >= 0 && (number < 0 || r > rank || (r == rank && n < number))) { rank = r; number = n; }
-    }
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = moved<CTRL>((unsigned)b), hi = moved<CTRL>((unsigned)(b >> 32));
+    return fmax(v, __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo));
+}
+// The best (rank, lowest number) of the wave's lanes, -1 if all are -infinity.
+__device__ __forceinline__ int best_of_wave(double rank, int number)
+{
+    double m = max_moved<0x140>(max_moved<0x141>(max_moved<0x4E>(max_moved<0xB1>(rank))));
+    m = fmax(m, __shfl_xor(m, 16));
+    m = fmax(m, __shfl_xor(m, 32));
+    if (m == -INFINITY) return -1;
+    return over_lanes<64>(rank == m ? number : 0x7FFFFFFF, [](int a, int b) { return min(a, b); });
 }
 // LDS accesses of a wave take place in order: only the compiler has to keep them so.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// One token by a whole wave; lane i holds experts i, i + 64, ...; ranks: LDS, 64 PER of the wave's own.
-template <typename T, int PER>
-__device__ __forceinline__ void route_exactly(const RouteArgs &a, long long token, double *ranks)
+// One token by a whole wave; lane i looks after experts i, i + 64, ...; ranks, of, open: LDS, a.experts and twice a.groups of the wave's own.
+// (Everything stays there: the kernel that calls this in the rare case shall not need registers for it.)
+template <typename T>
+__device__ __forceinline__ void route_exactly(const RouteArgs &a, long long token, double *ranks, double *of, unsigned char *open)
 {
     int lane = threadIdx.x & 63, groups = a.groups;
     asm("" : "+v"(lane), "+s"(groups));   // (what hangs on these is not to be worked out ahead of a rare call)
     const T *logits = (const T *)a.logits + token * a.ld;
-    double rank[PER];
     bool bad = false;
     float high = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane + 64 * i;
-        rank[i] = -INFINITY;
-        if (e < a.experts) {
-            const float l = Element<T>::get(logits + e);
-            rank[i] = l;
-            bad |= l != l || (!a.sigmoid && l == INFINITY);
-            high = fmaxf(high, l);
-        }
+#pragma unroll 1
+    for (int e = lane; e < a.experts; e += 64) {
+        const float l = Element<T>::get(logits + e);
+        bad |= l != l || (!a.sigmoid && l == INFINITY);
+        high = fmaxf(high, l);
+        ranks[e] = l;
     }
     high = max_of<64>(high);
     const bool sums = groups > 1 && a.group_best > 1;
     if (a.bias || sums) {
         double total = 0.0;
         if (!a.sigmoid) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (rank[i] > -INFINITY) total += exp(rank[i] - (double)high);
+#pragma unroll 1
+            for (int e = lane; e < a.experts; e += 64) {
+                const double l = ranks[e];
+                if (l > -INFINITY) total += exp(l - (double)high);
+            }
             total = wave_sum(total);
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (rank[i] > -INFINITY) {
-                double s = a.sigmoid ? 1.0 / (1.0 + exp(-rank[i])) : exp(rank[i] - (double)high) / total;
-                if (a.bias) s += (double)a.bias[lane + 64 * i];
+#pragma unroll 1
+        for (int e = lane; e < a.experts; e += 64) {
+            const double l = ranks[e];
+            if (l > -INFINITY) {
+                const double x = exp(a.sigmoid ? -l : l - (double)high);
+                double s = a.sigmoid ? 1.0 / (1.0 + x) : x / total;
+                if (a.bias) s += (double)a.bias[e];
                 bad |= s != s;
-                rank[i] = s;
+                ranks[e] = s;
             }
+        }
     }
+    in_order();
     if (groups > 1) {
         const int size = a.experts / groups;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) ranks[lane + 64 * i] = rank[i];
-        in_order();
-        double of[PER];   // the ranks of groups lane, lane + 64, ...
-        unsigned open = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int g = lane + 64 * i;
+#pragma unroll 1
+        for (int g = lane; g < groups; g += 64) {
             double one = -INFINITY, two = -INFINITY;
-            if (g < groups)
-                for (int q = 0; q < size; ++q) {
-                    const double r = ranks[g * size + q];
-                    if (r > one) { two = one; one = r; }
-                    else if (r > two) two = r;
-                }
-            of[i] = a.group_best > 1 && two > -INFINITY ? one + two : one;
+#pragma unroll 4
+            for (int q = 0; q < size; ++q) {
+                const double r = ranks[g * size + q];
+                two = fmax(two, fmin(one, r));
+                one = fmax(one, r);
+            }
+            of[g] = a.group_best > 1 && two > -INFINITY ? one + two : one;
+            open[g] = 0;
         }
         in_order();
+#pragma unroll 1
         for (int k = 0; k < a.top_groups; ++k) {
             double best = -INFINITY;
-            int number = -1;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (!(open >> i & 1) && of[i] > best) { best = of[i]; number = lane + 64 * i; }
-            best_of_wave(best, number);
+            int number = 0;
+#pragma unroll 1
+            for (int g = lane; g < groups; g += 64)
+                if (of[g] > best) { best = of[g]; number = g; }
+            number = best_of_wave(best, number);
             if (number < 0) break;
-            if ((number & 63) == lane) open |= 1u << (number >> 6);
+            if ((number & 63) == lane) {
+                open[number] = 1;
+                of[number] = -INFINITY;
+            }
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) ranks[lane + 64 * i] = open >> i & 1 ? 1.0 : 0.0;   // (of groups now)
         in_order();
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + 64 * i;
-            if (e < a.experts && ranks[e / size] == 0.0) rank[i] = -INFINITY;
-            else if (e < a.experts && sums && !a.bias) rank[i] = Element<T>::get(logits + e);
+#pragma unroll 1
+        for (int e = lane; e < a.experts; e += 64) {
+            if (!open[e / size]) ranks[e] = -INFINITY;
+            else if (sums && !a.bias) ranks[e] = Element<T>::get(logits + e);
         }
         in_order();
     }
     bad = __ballot(bad) != 0;
     int mine = -1;
+#pragma unroll 1
     for (int k = 0; k < a.fan; ++k) {
         double best = -INFINITY;
-        int number = -1;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (rank[i] > best) { best = rank[i]; number = lane + 64 * i; }
-        best_of_wave(best, number);
+        int number = 0;
+#pragma unroll 4
+        for (int e = lane; e < a.experts; e += 64) {
+            const double r = ranks[e];
+            if (r > best) { best = r; number = e; }
+        }
+        number = best_of_wave(best, number);
         if (bad || number < 0) break;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (number == lane + 64 * i) rank[i] = -INFINITY;
+        if ((number & 63) == lane) ranks[number] = -INFINITY;
         if (lane == k) mine = number;
     }
+    in_order();
     const bool there = mine >= 0;
     const float l = there ? Element<T>::get(logits + mine) : 0.f;
     float gate;
@@ -179,6 +186,7 @@ __device__ __forceinline__ void route_exactly(const RouteArgs &a, long long toke
         gate = sigmoid(l);
     } else {
         float sum = 0.f;
+#pragma unroll 1
         for (int e = lane; e < a.experts; e += 64) sum += expf(Element<T>::get(logits + e) - high);
         gate = expf(l - high) / sum_of<64>(sum);
     }
@@ -191,17 +199,18 @@ __device__ __forceinline__ void route_exactly(const RouteArgs &a, long long toke
 template <typename T>
 __global__ __launch_bounds__(256) void route_general_kernel(const RouteArgs a)
 {
-    __shared__ double ranks[4][kMaxRouted];
-    for (long long token = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); token < a.n; token += 4LL * gridDim.x)
-        route_exactly<T, kMaxRouted / 64>(a, token, ranks[threadIdx.x >> 6]);
+    __shared__ double ranks[4][kMaxRouted], of[4][kMaxRouted];
+    __shared__ unsigned char open[4][kMaxRouted];
+    const int wave = threadIdx.x >> 6;
+    for (long long token = (long long)blockIdx.x * 4 + wave; token < a.n; token += 4LL * gridDim.x) route_exactly<T>(a, token, ranks[wave], of[wave], open[wave]);
 }
 
 // ---- LANES lanes a token, EPL experts a lane -------------------------------------------------------------
-// Lane i holds the `per` experts from i per on.  Ranks are formed in fp32 and brought into whole numbers: 31 bits, below them the
-// experts' numbers from behind, so that the largest is the choice and all of them differ.  The best one below M is M + max(key - M)
-// in wrapping arithmetic: an element costs a subtraction and half a maximum in each round.  Where two neighbours among the chosen (and
-// the first that is not chosen) are nearer than the error of their ranks, and not exactly equal, the wave does the token again in 64 bits; so
-// it does with ranks that are not finite.  Groups need to be whole lanes.
+// Lane i holds the `per` experts from i per on.  Ranks are formed in fp32 and brought into [1, 2); the bits of the fraction, with the
+// experts' numbers from behind below them, are keys that all differ, and the largest is the choice.  The best one below M is M + max(key - M)
+// in wrapping arithmetic: an element costs a subtraction and half a maximum in each round.  Where two neighbours among the chosen are
+// nearer than the error of their ranks, and not exactly equal, the chosen ones are ranked in 64 bits; where the last of them and others are, or
+// groups, or ranks are not finite, the wave does the token again in 64 bits.  Groups need to be whole lanes.
 // 65536 tokens 256 experts bf16, sigmoids, a bias, 4 of 8 groups, fan 8: see the launch.
 template <typename T, int N>
 __device__ __forceinline__ void load_logits(const T *p, int there, float (&v)[N])
@@ -253,11 +262,12 @@ __device__ __forceinline__ void store_logits(T *p, int there, const float (&v)[N
 }
 
 template <typename T, int LANES, int EPL>
-__global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5 : 2) void route_kernel(const RouteArgs a, int per, int group_lanes)
+__global__ __launch_bounds__(256, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route_kernel(const RouteArgs a, int per, int group_lanes)
 {
     constexpr int ALL = LANES * EPL, IB = ALL <= 16 ? 4 : ALL <= 32 ? 5 : ALL <= 64 ? 6 : ALL <= 128 ? 7 : ALL <= 256 ? 8 : ALL <= 512 ? 9 : 10;
-    constexpr int ROWS = 256 / LANES, N = EPL < 8 ? EPL : 8, PER = (ALL + 63) / 64;
-    __shared__ double ranks[4][64 * PER];
+    constexpr int ROWS = 256 / LANES, N = EPL < 8 ? EPL : 8;
+    __shared__ double ranks[4][ALL], of_groups[4][LANES];   // (as many groups as lanes at most)
+    __shared__ unsigned char opened[4][LANES];
     const int lane = threadIdx.x & 63, sub = lane & (LANES - 1), first = sub * per;
     const bool sums = a.groups > 1 && a.group_best > 1, by_score = a.bias || sums;
     for (long long base = (long long)blockIdx.x * ROWS; base < a.n; base += (long long)gridDim.x * ROWS) {
@@ -274,10 +284,9 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
         }
         bool again = false;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            again |= l[i] != l[i];
-            k[i] = l[i];
-        }
+        for (int i = 0; i < EPL; ++i) k[i] = l[i];
+#pragma unroll
+        for (int i = 0; i < EPL; i += 2) again |= __builtin_isunordered(l[i], l[EPL > 1 ? i + 1 : i]);
         float high = l[0];
 #pragma unroll
         for (int i = 1; i < EPL; ++i) high = fmaxf(high, l[i]);
@@ -295,9 +304,10 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
             total = sum_of<LANES>(total);
         }
         if (by_score) {
-            // errors: sigmoids below 2^-21 (the argument's rounding is multiplied by s (1 - s)), softmaxes below 2^-19 of the largest
+            // errors: of sigmoids s (1 - s) (|l| 2^-24 + 2^-23) by the exponential, 2^-24 s by the sum, 2^-23 s by the reciprocal: below 2^-22;
+            // of softmaxes below 2^-19 of the largest
             const float share = 1.f / total;
-            error = a.sigmoid ? 0x1p-21f : 0x1p-19f * share;
+            error = a.sigmoid ? 0x1p-22f : 0x1p-19f * share;
             if (a.sigmoid) {
 #pragma unroll
                 for (int i = 0; i < EPL; ++i) k[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
@@ -312,13 +322,12 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
                     load_logits(a.bias + first + i, there - i, v);
 #pragma unroll
                     for (int j = 0; j < N; ++j) k[i + j] += v[j];
+#pragma unroll
+                    for (int j = 0; j < N; j += 2) again |= __builtin_isunordered(v[j], v[N > 1 ? j + 1 : j]);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) {
-                k[i] = l[i] > -INFINITY ? k[i] : -INFINITY;
-                again |= k[i] != k[i];
-            }
+            for (int i = 0; i < EPL; ++i) k[i] = l[i] > -INFINITY ? k[i] : -INFINITY;
         }
         if (a.groups > 1) {
             float one = -INFINITY, two = -INFINITY, largest = 0.f;
@@ -349,8 +358,8 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
             for (int i = 0; i < EPL; ++i) k[i] = !open ? -INFINITY : sums && !a.bias ? l[i] : k[i];
             if (sums && !a.bias) error = 0.f;
         }
-        // whole numbers: 1024 at the least of the lanes' best ones, which the `fan` best and the next one mostly reach (where fewer lanes than
-        // that are open: at the least open one), but 64 below the best at most; what is further below is 1
+        // [1, 1 + width): 1 + 2^-13 at the least of the lanes' best ones, which the `fan` best and the next one mostly reach (where fewer lanes
+        // than that are open: at the least open one), but 64 below the best at most; what is further below, or closed, is 1
         float best = k[0];
 #pragma unroll
         for (int i = 1; i < EPL; ++i) best = fmaxf(best, k[i]);
@@ -361,43 +370,86 @@ __global__ __launch_bounds__(256, EPL >= 16 && LANES == 16 ? 4 : LANES == 16 ? 5
         const float top = max_of<LANES>(best);
         low = fmaxf(min_of<LANES>(low), top - 64.f);
         again |= top == INFINITY;
-        constexpr float steps = (float)((1u << (IB < 8 ? 23 : 31 - IB)) - 2048);   // (24 bits: each is formed with less than one of error)
-        const float step = top > low ? fminf(steps / (top - low), 0x1p100f) : 0.f;
-        const unsigned margin = error > 0.f ? (unsigned)fminf(2.f * (error + 0x1p-23f * fmaxf(fabsf(top), fabsf(low))) * step, steps) + 4u : 0u;
+        constexpr float width = IB <= 8 ? 1.f : IB == 9 ? 0.5f : 0.25f;   // what a shift by IB leaves of a fraction
+        const float step = top > low ? fminf((width - 0x1p-10f) / (top - low), 0x1p100f) : 0x1p100f;
+        // twice the error of a rank and of its rounding, and what the map adds
+        const unsigned margin = error > 0.f ? (unsigned)(fminf(2.f * (error + 0x1p-23f * fmaxf(fabsf(top), fabsf(low))) * step, 1.f) * 0x1p23f) + 4u : 0u;
         unsigned key[EPL];
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-            const unsigned q = (unsigned)fmaxf(fmaf(k[i] - low, step, 1024.f), 1.f);
-            key[i] = k[i] > -INFINITY ? (q << IB) + (unsigned)(ALL - 1 - first - i) : 0u;
+            const float f = fmaxf(fmaf(k[i] - low, step, 1.f + 0x1p-13f), 1.f);
+            key[i] = (__float_as_uint(f) << IB) + (unsigned)(ALL - 1 - first - i);
         }
-        unsigned mine = 0, M = 0x80000000u;
+        unsigned mine = 0, M = IB <= 8 ? 0u : 0x80000000u;   // (with up to 8 bits below it a 1 of the exponent is the highest bit)
         for (int r = 0; r <= a.fan; ++r) {
             unsigned far = key[0] - M;
 #pragma unroll
             for (int i = 1; i < EPL; ++i) far = max(far, key[i] - M);
-            far = max_of<LANES>(far);
-            M = M == 0 ? 0 : M + far;
+            M += max_of<LANES>(far);
             mine = sub == r ? M : mine;
         }
+        constexpr unsigned one = 0x3F800000u << IB;   // (what is left of it)
+        const bool open = top > -INFINITY;
+        again |= open && sub < a.fan && mine - one < 1u << IB;   // closed, or too far below
         const int e = ALL - 1 - (int)(mine & (ALL - 1));
-        const float chosen = mine ? Element<T>::get(logits + e) : 0.f, added = mine && a.bias ? a.bias[e] : 0.f;
+        const bool real = sub <= a.fan && e < a.experts;   // (the numbers behind a.experts are closed, too)
+        const float chosen = real ? Element<T>::get(logits + e) : 0.f, added = real && a.bias ? a.bias[e] : 0.f;
         const unsigned next = next_lane<LANES>(mine);
         const bool equal = chosen == next_lane<LANES>(chosen) && added == next_lane<LANES>(added);
-        again |= sub < a.fan && next != 0 && (mine >> IB) - (next >> IB) <= margin && !equal;
+        const bool close = open && sub < a.fan && (mine >> IB) - (next >> IB) <= margin;
+        const unsigned long long lanes_of_row = (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1) << (lane - sub);
+        const unsigned long long edges = __ballot(close && sub == a.fan - 1);
+        if (edges) {   // the last choice and the first that is none: whatever is as near as that has to be equal
+            const int last = lane - sub + a.fan - 1;
+            const unsigned edge = __shfl(mine, last) >> IB;
+            const float l0 = __shfl(chosen, last), b0 = __shfl(added, last);
+#pragma unroll
+            for (int i = 0; i < EPL; ++i)
+                if ((edges & lanes_of_row) && (key[i] >> IB) - edge + margin <= 2 * margin) {
+                    const bool in = i < there;
+                    again |= !in || Element<T>::get(logits + (in ? first + i : 0)) != l0 || (a.bias && a.bias[in ? first + i : 0] != b0);
+                }
+        }
+        int place = sub;
+        if (__ballot(close && sub < a.fan - 1 && !equal)) {   // the chosen ones in 64 bits, their places counted
+            double rank = chosen;
+            if (error > 0.f) {
+                double all = 1.0;
+                if (!a.sigmoid) {
+                    all = 0.0;
+#pragma unroll 1
+                    for (int q = sub; q < a.experts; q += LANES) {
+                        const float x = Element<T>::get(logits + q);
+                        if (x > -INFINITY) all += exp((double)x - (double)high);
+                    }
+                    for (int o = LANES / 2; o > 0; o >>= 1) all += __shfl_xor(all, o);
+                }
+                const double x = exp(a.sigmoid ? -(double)chosen : (double)chosen - (double)high);
+                rank = (a.sigmoid ? 1.0 / (1.0 + x) : x / all) + (double)added;
+            }
+            int better = 0;
+            for (int q = 0; q < a.fan; ++q) {
+                const double r = __shfl(rank, lane - sub + q);
+                const int number = __shfl(e, lane - sub + q);
+                better += r > rank || (r == rank && number < e) ? 1 : 0;
+            }
+            if (sub < a.fan) place = better;
+        }
         const unsigned long long rows = __ballot(again);
-        const bool mine_again = (rows >> (lane - sub) & (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1)) != 0;
-        const bool chosen_one = mine != 0 && sub < a.fan;
+        const bool mine_again = (rows & lanes_of_row) != 0;
+        const bool chosen_one = open && place < a.fan;
         float gate;
         if (a.renormalise) gate = weight<LANES>(a.sigmoid, chosen, chosen_one);
         else gate = a.sigmoid ? sigmoid(chosen) : expf(chosen - high) / total;
-        if (sub < a.fan && mine_at < a.n && !mine_again) {
-            a.choice[token * a.fan + sub] = chosen_one ? e : -1;
-            a.gate[token * a.fan + sub] = chosen_one ? a.scale * gate : 0.f;
+        if (place < a.fan && mine_at < a.n && !mine_again) {
+            a.choice[token * a.fan + place] = chosen_one ? e : -1;
+            a.gate[token * a.fan + place] = chosen_one ? a.scale * gate : 0.f;
         }
         if (rows)
             for (int r = 0; r < 64 / LANES; ++r) {
                 const long long t = base + (threadIdx.x >> 6) * (64 / LANES) + r;
-                if ((rows >> (LANES * r) & (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1)) && t < a.n) route_exactly<T, PER>(a, t, ranks[threadIdx.x >> 6]);
+                if ((rows >> (LANES * r) & (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1)) && t < a.n)
+                    route_exactly<T>(a, t, ranks[threadIdx.x >> 6], of_groups[threadIdx.x >> 6], opened[threadIdx.x >> 6]);
             }
     }
 }
@@ -487,7 +539,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a)
 }
 
 // A launch takes less than 2^32 threads; the kernels go on from there.
-dim3 workgroups(int n, int rows) { return dim3((unsigned)min((n + rows - 1) / rows, 1 << 20)); }
+dim3 workgroups(int n, int rows, int most = 1 << 20) { return dim3((unsigned)min((n + rows - 1) / rows, most)); }
 
 template <typename T, int LANES, int EPL>
 hipError_t run(const RouteArgs &a, hipStream_t s)

@@ -202,3 +202,32 @@ def test_binding_refuses(ctx):
             kfac.kfac_route(**{**dict(ctx=ctx, router=r, logits=x, choice=choice, gate=gate), **bad})
     with pytest.raises(kfac.KfacError):
         kfac.kfac_route(ctx, kfac.router(8, 9), x, torch.zeros(36, dtype=torch.int32, device="cuda"), torch.zeros(4, 9, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("E,groups,top,best", [(8, 1, 1, 1), (64, 8, 4, 2), (64, 8, 2, 1), (256, 8, 4, 2), (256, 1, 1, 1), (512, 8, 3, 2)])
+def test_many_equal_ranks(ctx, E, groups, top, best, dtype):
+    """Few different logits and biases: runs of equal ranks that reach over the last choice, with other ranks right behind them, and groups that are
+    equal; every lane of the kernel may hold the largest one."""
+    rng = np.random.default_rng(E + groups)
+    n, fan = 600, min(7, top * E // groups)
+    grid = rng.integers(0, 3, (n, E)) / 4.0
+    grid[:100] = np.where(rng.random((100, E)) < 0.9, 0.5, 0.25)
+    fine = grid + rng.integers(0, 2, (n, E)) * 2.0 ** -22           # (in fp32: neighbours that differ by a few of its steps)
+    for logits in (grid, fine):
+        for bias in (None, np.zeros(E), rng.integers(0, 2, E) * 0.25):
+            for scores in (0, 1):
+                _run(ctx, logits, bias, rng.standard_normal((n, fan)), dtype, 0, scores=scores, fan=fan, groups=groups, top_groups=top, group_best=best)
+
+
+@pytest.mark.parametrize("scores", [0, 1])
+def test_closed_by_the_lowest_value_of_the_type(ctx, scores):
+    """Masks of -3.4e38 instead of -infinity: such experts are open, and come last."""
+    rng = np.random.default_rng(12)
+    for E in (16, 64, 256):
+        logits = rng.standard_normal((80, E))
+        logits[rng.random((80, E)) < 0.5] = -np.finfo(np.float32).max
+        logits[0] = -np.finfo(np.float32).max
+        logits[1, 3:] = -np.finfo(np.float32).max
+        _run(ctx, logits, None, rng.standard_normal((80, 4)), F32, 0, scores=scores, fan=4, renormalise=scores == 0)
+        _run(ctx, logits, 0.1 * rng.standard_normal(E), rng.standard_normal((80, 4)), F32, 0, scores=scores, fan=4, groups=4, top_groups=2, group_best=2)
