@@ -14,6 +14,7 @@
 // 8-byte groups addressed by lanes i / 4, i / 4 + 4, i / 4 + 8, i / 4 + 12).
 // fp32 operands are the exact sum of three bf16 values; of the nine products the six above 2^-24 are formed (h h, h m, m h,
 // m m, h l, l h), all accumulated in fp32.  Contexts that ask for the fp32 matrix instruction get it.
+#include <algorithm>
 #include <type_traits>
 
 #include "gemm_tiles.h"
@@ -345,6 +346,74 @@ __device__ __forceinline__ bool expert_share(int slots, int tiles, int &e, int &
     return local < tiles;
 }
 
+// Tile `local` of an expert's, for the contractions over rows.
+template <int OP, int BM, int BN>
+__device__ __forceinline__ void row_tile(const ExpertArgs &a, int tiles_j, int local, Tile &t)
+{
+    t.g = false;
+    if constexpr (OP == EXPERT_GRAD_WEIGHT) {
+        banded(local, (a.co + BM - 1) / BM, tiles_j, t.ti, t.tj);
+        t.I = a.co;
+        t.J = a.ci;
+    } else {
+        static_assert(BM == BN, "the triangle has square tiles");
+        const int na = a.A ? triangle_tiles<BM>(a.ci) : 0;
+        t.g = local >= na;
+        tri_decode(t.g ? local - na : local, t.ti, t.tj);
+        t.I = t.J = t.g ? a.co : a.ci;
+    }
+}
+
+// Contractions over rows in pieces (up to 64 experts): the rows of an expert that has more than a.piece of them are cut into equal parts, and
+// the parts of all experts are taken up in the order of their lengths, so that the last ones to run are short ones.  Lane e of every wave
+// knows expert e's.
+struct Pieces {
+    int begin, len, count, rows;   // of the expert; its pieces and their rows (the last has what is left)
+    int first, slot;               // places of its first piece: in the order of lengths; among the pieces of experts with several
+    int split;                     // experts before it that have several
+};
+template <int OP>
+__device__ __forceinline__ Pieces pieces_of(const ExpertArgs &a)
+{
+    const int lane = threadIdx.x & 63;
+    Pieces p{};
+    if (lane < a.experts) {
+        segment(a, lane, p.begin, p.len);
+        const int want = (p.len + a.piece - 1) / a.piece;
+        p.rows = want > 1 ? ((p.len + want - 1) / want + 63) / 64 * 64 : p.len;
+        p.count = want > 1 ? (p.len + p.rows - 1) / p.rows : OP == EXPERT_GRAD_WEIGHT || p.len > 0 ? 1 : 0;   // (weights without rows become zero)
+    }
+    for (int e = 0; e < a.experts; ++e) {
+        const int rows = __builtin_amdgcn_readlane(p.rows, e), count = __builtin_amdgcn_readlane(p.count, e);
+        p.first += rows > p.rows || (rows == p.rows && e < lane) ? count : 0;
+        if (e < lane && count > 1) { p.slot += count; ++p.split; }
+    }
+    return p;
+}
+// slot: where the tile's sums go, -1: straight into the result
+template <int OP, int BM, int BN>
+__device__ __forceinline__ bool find_piece(const ExpertArgs &a, int tiles_j, int tiles, Tile &t, int &slot)
+{
+    const Pieces p = pieces_of<OP>(a);
+    const int at = blockIdx.x / tiles, local = blockIdx.x - at * tiles;
+    const unsigned long long has = __ballot(at >= p.first && at < p.first + p.count);
+    if (!has) return false;
+    const int e = __ffsll(has) - 1;
+    const int rows = __builtin_amdgcn_readlane(p.rows, e), count = __builtin_amdgcn_readlane(p.count, e), q = at - __builtin_amdgcn_readlane(p.first, e);
+    t.e = e;
+    t.len = __builtin_amdgcn_readlane(p.len, e);
+    t.begin = __builtin_amdgcn_readlane(p.begin, e) + q * rows;
+    t.K = min(rows, t.len - q * rows);
+    const int place = __builtin_amdgcn_readlane(p.slot, e) + q;
+    if (count > 1 && place >= a.most) return false;   // (offsets that no sort makes: segments that overlap)
+    slot = count > 1 ? place * tiles + local : -1;
+    row_tile<OP, BM, BN>(a, tiles_j, local, t);
+    return true;
+}
+// What a tile's sums take in the workspace: the sums in the order of the kernel's registers, then those of its rows.
+template <int BM, int BN>
+__host__ __device__ constexpr long long slot_floats() { return (long long)BM * BN + BM; }
+
 template <int OP, int BM, int BN>
 __device__ __forceinline__ bool find_work(const ExpertArgs &a, int tiles_j, int total, Tile &t)
 {
@@ -496,7 +565,7 @@ __device__ __forceinline__ floatx4 add_up(const bf16x8 &i, const floatx4 &c)
 
 // GROUPS of four waves share a tile: each takes every GROUPS-th step of the contraction, the sums are added up in the groups' order.
 // FP32: with the fp32 matrix instruction, whose four k of step v are 16 u + 4 q + v of the lanes 16 q .. 16 q + 15.
-template <typename T, bool FP32, int OP, int EDGE, int GROUPS>
+template <typename T, bool FP32, int OP, int EDGE, int GROUPS, bool PIECES>
 __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_general_kernel(const ExpertArgs a, int tiles_j, int total)
 {
     typedef std::conditional_t<FP32, float, bf16_t> E;   // what is in LDS
@@ -512,7 +581,12 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
     const int wi = wave >> 1, wj = wave & 1;
     E *const tile_a = lds + group * 2 * NP * PLANE, *const tile_b = tile_a + NP * PLANE;
     Tile t;
-    if (!find_work<OP, EDGE, EDGE>(a, tiles_j, total, t)) return;
+    int slot = -1;
+    if constexpr (PIECES) {
+        if (!find_piece<OP, EDGE, EDGE>(a, tiles_j, total, t, slot)) return;
+    } else {
+        if (!find_work<OP, EDGE, EDGE>(a, tiles_j, total, t)) return;
+    }
 
     Staged<T, ACROSS_A, GATHER_A, BK, EDGE> sa;
     Staged<T, ACROSS_B, GATHER_B, BK, EDGE> sb;
@@ -620,6 +694,17 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
                     for (int j = 0; j < NB; ++j) acc[i][j] += *(const floatx4 *)(part + row * LD + wj * (EDGE / 2) + 16 * j + 4 * (lane >> 4));
                 }
         }
+    }
+    if (PIECES && slot >= 0) {
+        if (group > 0) return;
+        float *const out = a.partial + slot * slot_floats<EDGE, EDGE>();
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) *(floatx4 *)(out + 4 * ((i * NB + j) * 256 + tid)) = acc[i][j];
+            if (sums && lane < 16) out[EDGE * EDGE + wi * (EDGE / 2) + 16 * i + lane] = row_sum[i][0];
+        }
+        return;
     }
     // lane -> row lane % 16 of a block, columns 4 (lane / 16) .. + 3
     constexpr bool SAME = OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT;   // results of the operands' type
@@ -766,7 +851,7 @@ struct Direct {
     }
 };
 
-template <int OP, int BM, int BN, int WI, int WJ, bool SUMS>
+template <int OP, int BM, int BN, int WI, int WJ, bool SUMS, bool PIECES>
 __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const ExpertArgs a, int tiles_j, int total)
 {
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
@@ -778,7 +863,12 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
     Tile t;
-    if (!find_work<OP, BM, BN>(a, tiles_j, total, t)) return;
+    int slot = -1;
+    if constexpr (PIECES) {
+        if (!find_piece<OP, BM, BN>(a, tiles_j, total, t, slot)) return;
+    } else {
+        if (!find_work<OP, BM, BN>(a, tiles_j, total, t)) return;
+    }
 
     typedef Direct<ACROSS_A, GATHER_A, BM, THREADS> DirectA;
     typedef Direct<ACROSS_B, GATHER_B, BN, THREADS> DirectB;
@@ -905,6 +995,20 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     if constexpr (SUMS)
 #pragma unroll
         for (int i = 0; i < NI; ++i) row_sum[i] += __shfl_xor(row_sum[i], 32);   // the other 8 of 16 k
+    if (PIECES && slot >= 0) {
+        float *const out = a.partial + slot * slot_floats<BM, BN>();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(floatx4 *)(out + 4 * (((i * NJ + j) * 4 + g) * THREADS + tid)) =
+                        floatx4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+            if (sums && lane < 32) out[BM * BN + wi * TI + 32 * i + lane] = row_sum[i];
+        }
+        return;
+    }
     // lane -> row lane % 32 of a block, columns 8 g + 4 (lane / 32) .. + 3 for its 16 sums in fours
     constexpr int SIZE = OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT ? 2 : 4;
     constexpr int PART = BM * (BN + 8) * SIZE <= (int)sizeof(lds) ? BM : BM / 2;
@@ -925,6 +1029,65 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     if (sums && lane < 32)
 #pragma unroll
         for (int i = 0; i < NI; ++i) store_sum<OP>(a, t, t.ti * BM + wi * TI + 32 * i + lane, row_sum[i]);
+}
+
+// ---- the pieces' sums together ---------------------------------------------------------------------------
+// Experts with several pieces: a thread adds up four adjacent sums of a tile over the pieces, in their order, and stores them as the kernels do.
+// Bound by memory, and few: the pieces are as long as they can be with every CU at work.
+template <int OP, bool DIRECT, int BM, int BN, int WI, int WJ>
+__global__ __launch_bounds__(256) void expert_join_kernel(const ExpertArgs a, int tiles_j, int tiles)
+{
+    constexpr int PARTS = BM * BN / 1024, THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ;
+    const Pieces p = pieces_of<OP>(a);
+    const int of = blockIdx.x / (tiles * PARTS), rest = blockIdx.x - of * tiles * PARTS, local = rest / PARTS, part = rest - local * PARTS;
+    const unsigned long long has = __ballot(p.count > 1 && p.split == of);
+    if (!has) return;
+    Tile t;
+    t.e = __ffsll(has) - 1;
+    t.len = __builtin_amdgcn_readlane(p.len, t.e);
+    const int count = __builtin_amdgcn_readlane(p.count, t.e), place = __builtin_amdgcn_readlane(p.slot, t.e);
+    if (place + count > a.most) return;
+    row_tile<OP, BM, BN>(a, tiles_j, local, t);
+    const float *from = a.partial + ((long long)place * tiles + local) * slot_floats<BM, BN>();
+    const long long apart = tiles * slot_floats<BM, BN>();
+    const int quad = part * 256 + threadIdx.x, q = quad / THREADS, tid = quad % THREADS, lane = tid & 63, wi = (tid >> 6) / WJ, wj = (tid >> 6) % WJ;
+    floatx4 v = *(const floatx4 *)(from + 4 * quad);
+#pragma unroll 4
+    for (int k = 1; k < count; ++k) v += *(const floatx4 *)(from + k * apart + 4 * quad);
+    int row, col;
+    if constexpr (DIRECT) {
+        constexpr int NJ = TJ / 32;
+        row = wi * TI + 32 * (q / 4 / NJ) + (lane & 31);
+        col = wj * TJ + 32 * (q / 4 % NJ) + 8 * (q % 4) + 4 * (lane >> 5);
+    } else {
+        constexpr int NJ = TJ / 16;
+        row = wi * TI + 16 * (q / NJ) + (lane & 15);
+        col = wj * TJ + 16 * (q % NJ) + 4 * (lane >> 4);
+    }
+    row += t.ti * BM;
+    col += t.tj * BN;
+    if (row < t.I) {
+        if constexpr (OP == EXPERT_GRAD_WEIGHT) {
+            store4<float>(a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias) + col, t.J - col, v);
+        } else {
+            const int d = t.g ? a.co : a.ci + a.bias;
+            float *const M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
+            const float alpha = (1.f - a.decay) / (float)t.len;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (col + r <= row) {   // the lower triangle and its mirror image
+                    float *const out = M + (long long)row * d + col + r;
+                    const float w = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *out, v[r]);
+                    *out = w;
+                    M[(long long)(col + r) * d + row] = w;
+                }
+        }
+    }
+    if (a.bias && !t.g && t.tj == 0 && part == 0 && threadIdx.x < BM) {
+        float sum = 0.f;
+        for (int k = 0; k < count; ++k) sum += from[k * apart + BM * BN + threadIdx.x];
+        store_sum<OP>(a, t, t.ti * BM + (int)threadIdx.x, sum);
+    }
 }
 
 // Operands that go straight to LDS: whole 16-byte chunks, offsets of 32 bits, choices that the division by `fan` is exact for.
@@ -967,8 +1130,8 @@ hipError_t run_direct(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     const long long wgs = count_tiles<BM, BN>(op, a, tj);
     const dim3 grid((unsigned)wgs), block(64 * WI * WJ);
     switch (op) {
-        case EXPERT_FORWARD: expert_direct_kernel<EXPERT_FORWARD, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
-        case EXPERT_GRAD_INPUT: expert_direct_kernel<EXPERT_GRAD_INPUT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_FORWARD: expert_direct_kernel<EXPERT_FORWARD, BM, BN, WI, WJ, false, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
+        case EXPERT_GRAD_INPUT: expert_direct_kernel<EXPERT_GRAD_INPUT, BM, BN, WI, WJ, false, false><<<grid, block, 0, s>>>(a, tj, (int)wgs); break;
         default: return hipErrorInvalidValue;   // (run_direct_rows has the others)
     }
     return hipGetLastError();
@@ -982,11 +1145,11 @@ hipError_t run_direct_rows(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     const long long wgs = count_tiles<BM, BN>(op, a, tj);
     const dim3 grid((unsigned)wgs), block(64 * WI * WJ);
     if (op == EXPERT_GRAD_WEIGHT) {
-        if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-        else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+        if (a.bias) expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, true, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+        else expert_direct_kernel<EXPERT_GRAD_WEIGHT, BM, BN, WI, WJ, false, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
     } else {
-        if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, true><<<grid, block, 0, s>>>(a, tj, (int)wgs);
-        else expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+        if (a.bias) expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, true, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
+        else expert_direct_kernel<EXPERT_STATS, BM, BN, WI, WJ, false, false><<<grid, block, 0, s>>>(a, tj, (int)wgs);
     }
     return hipGetLastError();
 }
@@ -996,7 +1159,7 @@ hipError_t run_general(const ExpertArgs &a, hipStream_t s)
 {
     int tj;
     const long long wgs = count_tiles<EDGE, EDGE>(OP, a, tj);
-    expert_general_kernel<T, FP32, OP, EDGE, GROUPS><<<dim3((unsigned)wgs), dim3(256 * GROUPS), 0, s>>>(a, tj, (int)wgs);
+    expert_general_kernel<T, FP32, OP, EDGE, GROUPS, false><<<dim3((unsigned)wgs), dim3(256 * GROUPS), 0, s>>>(a, tj, (int)wgs);
     return hipGetLastError();
 }
 
@@ -1029,6 +1192,67 @@ hipError_t general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
     return hipErrorInvalidValue;
 }
 
+// ---- contractions over rows in pieces -------------------------------------------------------------------
+// Every CU shall have work and the pieces shall be few (their sums go to memory and back): as many rows as a tile has if all of them went
+// evenly to `slots` workgroups, 512 at least.
+int piece_rows(long long n, int tiles, int slots)
+{
+    const long long even = std::min((n * tiles + slots - 1) / slots, n);
+    return (int)std::max(512LL, (even + 63) / 64 * 64);
+}
+template <int OP, int BM, int BN>
+int row_tiles(const ExpertArgs &a, int &tiles_j)
+{
+    tiles_j = (a.ci + BN - 1) / BN;
+    if (OP == EXPERT_GRAD_WEIGHT) return (a.co + BM - 1) / BM * tiles_j;
+    return (a.A ? triangle_tiles<BM>(a.ci) : 0) + (a.G ? triangle_tiles<BM>(a.co) : 0);
+}
+
+template <ExpertOp OP, bool DIRECT, int BM, int BN, int WI, int WJ, typename Launch>
+hipError_t run_pieces(ExpertArgs a, int slots, hipStream_t s, Launch launch)
+{
+    int tj;
+    const int tiles = row_tiles<OP, BM, BN>(a, tj);
+    a.piece = piece_rows(a.n, tiles, slots);
+    a.most = (int)(2LL * a.n / a.piece);   // pieces of experts with several: each is longer than half of a.piece
+    launch(a, dim3((unsigned)((a.n / a.piece + a.experts) * tiles)), tj, tiles);
+    if (a.n > a.piece)   // at most n / piece experts have several
+        expert_join_kernel<OP, DIRECT, BM, BN, WI, WJ><<<dim3((unsigned)(a.n / a.piece) * tiles * (BM * BN / 1024)), dim3(256), 0, s>>>(a, tj, tiles);
+    return hipGetLastError();
+}
+
+template <ExpertOp OP, int BM, int BN, int WI, int WJ>
+hipError_t run_direct_pieces(const ExpertArgs &a, int slots, hipStream_t s)
+{
+    return run_pieces<OP, true, BM, BN, WI, WJ>(a, slots, s, [&](const ExpertArgs &p, dim3 grid, int tj, int tiles) {
+        if (p.bias) expert_direct_kernel<OP, BM, BN, WI, WJ, true, true><<<grid, dim3(64 * WI * WJ), 0, s>>>(p, tj, tiles);
+        else expert_direct_kernel<OP, BM, BN, WI, WJ, false, true><<<grid, dim3(64 * WI * WJ), 0, s>>>(p, tj, tiles);
+    });
+}
+template <typename T, bool FP32, ExpertOp OP, int EDGE, int GROUPS>
+hipError_t run_general_pieces(const ExpertArgs &a, int slots, hipStream_t s)
+{
+    return run_pieces<OP, false, EDGE, EDGE, 2, 2>(a, slots, s, [&](const ExpertArgs &p, dim3 grid, int tj, int tiles) {
+        expert_general_kernel<T, FP32, OP, EDGE, GROUPS, true><<<grid, dim3(256 * GROUPS), 0, s>>>(p, tj, tiles);
+    });
+}
+
+template <ExpertOp OP>
+hipError_t pieces(const ExpertArgs &a, bool bf16, bool planes, hipStream_t s)
+{
+    int tj;
+    if (bf16 && direct_ok(OP, a)) {
+        if (a.experts * row_tiles<OP, 256, 256>(a, tj) >= 512) return run_direct_pieces<OP, 256, 256, 4, 2>(a, 128, s);
+        return run_direct_pieces<OP, 128, 128, 2, 2>(a, 512, s);
+    }
+    if (a.experts * row_tiles<OP, 128, 128>(a, tj) >= 512) {
+        if (bf16) return run_general_pieces<bf16_t, false, OP, 128, 1>(a, 512, s);
+        return planes ? run_general_pieces<float, false, OP, 128, 1>(a, 512, s) : run_general_pieces<float, true, OP, 128, 1>(a, 512, s);
+    }
+    if (bf16) return run_general_pieces<bf16_t, false, OP, 64, 2>(a, 1024, s);
+    return planes ? run_general_pieces<float, false, OP, 64, 2>(a, 1024, s) : run_general_pieces<float, true, OP, 64, 2>(a, 1024, s);
+}
+
 }  // namespace
 
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s)
@@ -1050,6 +1274,21 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes
     }
     if (bf16) return general<bf16_t, false>(op, a, s);
     return planes ? general<float, false>(op, a, s) : general<float, true>(op, a, s);
+}
+
+size_t expert_pieces_bytes(int experts, int n, int ci, int co)
+{
+    if (experts > 64) return 0;
+    // n / 256 pieces at most (of A and G: 2 triangles with their diagonals), 1024 tiles of 128 x 128 at most (256 and 2048 of the others)
+    const size_t longer = (size_t)std::max(ci, co), edge = (longer + 255) / 256 * 256;
+    const size_t piece = 2 * edge * edge * sizeof(float) / 64 * 65, most = (size_t)1024 * (128 * 128 / 64 * 65) * sizeof(float);
+    return std::min((size_t)(n / 256) * piece, most);
+}
+
+hipError_t launch_expert_pieces(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s)
+{
+    if (a.experts > 64) return launch_expert(op, a, bf16, planes, s);
+    return op == EXPERT_GRAD_WEIGHT ? pieces<EXPERT_GRAD_WEIGHT>(a, bf16, planes, s) : pieces<EXPERT_STATS>(a, bf16, planes, s);
 }
 
 }  // namespace kfac

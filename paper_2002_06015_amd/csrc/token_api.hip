@@ -57,7 +57,9 @@ ExpertArgs expert_args(const kfac_layer *L, int32_t experts, int32_t n, int32_t 
 bool run_expert(kfac_ctx *ctx, ExpertOp op, const ExpertArgs &a, kfac_dtype type, double flops, double bytes)
 {
     const CtxView c = ctx_view(ctx);
-    return timed(ctx, KFAC_K_EXPERT, (int)op, flops, bytes, [&] { return launch_expert(op, a, type == KFAC_BF16, c.fp32_planes, c.stream); });
+    return timed(ctx, KFAC_K_EXPERT, (int)op, flops, bytes, [&] {
+        return (a.partial ? launch_expert_pieces : launch_expert)(op, a, type == KFAC_BF16, c.fp32_planes, c.stream);
+    });
 }
 
 // The checks of kfac_expert_grad_weight and kfac_stats_expert, and what they launch.  in: what x is read from, one or two tensors.
@@ -117,7 +119,10 @@ kfac_status run_stats(kfac_ctx *ctx, const ExpertArgs &a, kfac_dtype in)
 
 // Inputs of experts that were kept in 8 bits; in the workspace as values, rows a whole number of 16-byte chunks apart.
 int64_t kept_row(const kfac_layer *L) { return ((int64_t)L->c_in + 63) / 64 * 64; }
-size_t kept_bytes(const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type) { return (size_t)(n / fan) * kept_row(L) * esize(type); }
+size_t kept_bytes(const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type)
+{
+    return ((size_t)(n / fan) * kept_row(L) * esize(type) + 255) / 256 * 256;
+}
 bool kept_ok(const kfac_layer *L, int32_t n, int32_t fan, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds)
 {
     return ldq >= L->c_in && lds >= (L->c_in + 31) / 32 && ldq <= kMaxPositions && lds <= kMaxPositions && (n == 0 || (q && scales));
@@ -302,7 +307,7 @@ kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t expert
 
 size_t kfac_kept_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan)
 {
-    return experts_ok(L, experts, n) && fan >= 1 && n % fan == 0 ? std::max<size_t>(256, kept_bytes(L, n, fan, KFAC_F32)) : 0;
+    return experts_ok(L, experts, n) && fan >= 1 && n % fan == 0 ? std::max<size_t>(256, kept_bytes(L, n, fan, KFAC_F32) + expert_pieces_bytes(experts, n, L->c_in, L->c_out)) : 0;
 }
 
 kfac_status kfac_expert_grad_weight_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type,
@@ -314,7 +319,9 @@ kfac_status kfac_expert_grad_weight_kept(kfac_ctx *ctx, const kfac_layer *L, int
     ExpertArgs a;
     const kfac_status st = weight_args(ctx, L, experts, n, fan, type, order, offsets, kept_inputs(L, n, fan, q, ldq, scales, lds), c.ws, kept_row(L), dy, ldy, dW, a);
     if (st != KFAC_OK) return st;
-    if (kept_bytes(L, n, fan, type) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    const size_t values = kept_bytes(L, n, fan, type);
+    if (values + expert_pieces_bytes(experts, n, L->c_in, L->c_out) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    a.partial = (float *)(c.ws + values);
     if (n > 0 && !restore_kept(ctx, L, n, fan, type, q, ldq, scales, lds)) return KFAC_ERR_DEVICE;
     return run_weight(ctx, a, type);
 }
@@ -330,7 +337,9 @@ kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t e
                                       kept_row(L), grad_out, ldg, decay, A_ema, G_ema, a);
     if (st != KFAC_OK) return st;
     if (n == 0) return KFAC_OK;   // no expert has rows
-    if (A_ema && kept_bytes(L, n, fan, in) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    const size_t values = A_ema ? kept_bytes(L, n, fan, in) : 0;
+    if (values + expert_pieces_bytes(experts, n, L->c_in, L->c_out) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    a.partial = (float *)(c.ws + values);
     if (A_ema && !restore_kept(ctx, L, n, fan, in, q, ldq, scales, lds)) return KFAC_ERR_DEVICE;
     return run_stats(ctx, a, in);
 }

@@ -90,10 +90,16 @@ struct ExpertArgs {
     float *dW;                    // [experts, co, ci + bias]
     float *A, *G;                 // [experts, ci + bias, ci + bias], [experts, co, co]
     float decay;
+    float *partial;               // sums of pieces (launch_expert_pieces), expert_pieces_bytes of them
+    int piece, most;              // rows that an expert has at most if they are not cut, places for pieces (set by it)
 };
 enum ExpertOp { EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, EXPERT_STATS };
 // planes: how fp32 operands are multiplied (bf16 != 0: not used)
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s);
+
+// The contractions over rows (gradient of the weights, factors) with long experts cut into pieces.
+size_t expert_pieces_bytes(int experts, int n, int ci, int co);   // never less for more rows, experts up to 64 or channels
+hipError_t launch_expert_pieces(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s);
 
 // ---- routing -------------------------------------------------------------------------------------------
 constexpr int kMaxRouted = 1024, kMaxFan = 32;

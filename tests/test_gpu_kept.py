@@ -215,6 +215,69 @@ def test_dense_layers_and_the_fp32_instruction(dtype):
         c.close()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("E,ci,co,bias", [(1, 64, 64, 1), (3, 128, 256, 0), (64, 72, 40, 1), (65, 72, 40, 1), (2, 1000, 130, 1), (40, 1024, 1024, 1)])
+def test_long_experts_in_pieces(E, ci, co, bias, dtype):
+    """Experts of one row, of no rows, of 511 to 513, of many thousands: the same sums as of the values brought back, to the rounding of the order in
+    which they are added up (errors of both: (rows + 8) 2^-24 of the magnitudes)."""
+    rng = np.random.default_rng(E + ci)
+    lengths = [9000, 511, 0, 512, 513, 1, 1025][:E] + [int(v) for v in rng.integers(0, 200, max(0, E - 7))]
+    n = sum(lengths)
+    layer = wl.fc_layer(1, ci, co, bias)
+    choice = torch.from_numpy(rng.permutation(np.repeat(np.arange(E), lengths)).astype(np.int32)).cuda()
+    need = max(kfac.kfac_kept_workspace_bytes(layer, E, n), kfac.kfac_segments_workspace_bytes(n, E))
+    c = kfac.Context([layer], workspace_bytes=need)
+    guard = c.workspace[(c.workspace.data_ptr() + 255) // 256 * 256 - c.workspace.data_ptr() + need:]
+    guard.fill_(77)
+    order, offsets = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    kfac.kfac_segments(c, choice, E, order, offsets)
+    x = torch.from_numpy(rng.standard_normal((n, ci)).astype(np.float32)).cuda()
+    q, s, _, _ = _bytes(n, ci)
+    kfac.kfac_keep(c, x, q, s)
+    v = torch.empty(n, ci, dtype=dtype, device="cuda")
+    kfac.kfac_restore(c, q, s, v)
+    dy = torch.from_numpy(rng.standard_normal((n, co)).astype(np.float32)).cuda().to(dtype)
+    new = lambda d, e: [torch.full((E, d, e), 3.0, device="cuda") for _ in range(2)]  # noqa: E731
+    (W1, W2), (A1, A2), (G1, G2) = new(co, ci + bias), new(ci + bias, ci + bias), new(co, co)
+    kfac.kfac_expert_grad_weight(c, layer, order, offsets, v, dy, W1)
+    kfac.kfac_expert_grad_weight_kept(c, layer, order, offsets, q, s, dy, W2)
+    kfac.kfac_stats_expert(c, layer, order, offsets, v, dy, 0.25, A1, G1)
+    kfac.kfac_stats_expert_kept(c, layer, order, offsets, q, s, dy, 0.25, A2, G2)
+    magW, magA, magG = torch.empty_like(W1), torch.empty_like(A1), torch.empty_like(G1)
+    kfac.kfac_expert_grad_weight(c, layer, order, offsets, v.abs(), dy.abs(), magW)
+    kfac.kfac_stats_expert(c, layer, order, offsets, v.abs(), dy.abs(), 0.0, magA, magG)
+    torch.cuda.synchronize()
+    rows = torch.tensor(lengths, device="cuda", dtype=torch.float64)[:, None, None]
+    for a, b, m, old in ((W1, W2, magW, 0.0), (A1, A2, magA, 3.0), (G1, G2, magG, 3.0)):
+        m = torch.where(rows > 0, m.double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+        assert bool(((a.double() - b.double()).abs() <= 2.01 * (rows + 12) * 2.0 ** -24 * (m + old)).all())
+    assert torch.equal(A2, A2.transpose(1, 2)) and torch.equal(G2, G2.transpose(1, 2))
+    again = torch.empty_like(W2)
+    kfac.kfac_expert_grad_weight_kept(c, layer, order, offsets, q, s, dy, again)
+    assert torch.equal(again, W2) and bool((guard == 77).all())
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_offsets_that_overlap_stay_inside_the_workspace(dtype):
+    """Offsets that no sort makes: every second expert has all rows."""
+    layer, E, n = wl.fc_layer(1, 64, 64, 1), 8, 3000
+    need = kfac.kfac_kept_workspace_bytes(layer, E, n)
+    c = kfac.Context([layer], workspace_bytes=need)
+    base = (c.workspace.data_ptr() + 255) // 256 * 256 - c.workspace.data_ptr()
+    c.workspace[base + need:].fill_(77)
+    q, s, _, _ = _bytes(n, 64)
+    kfac.kfac_keep(c, torch.randn(n, 64, device="cuda"), q, s)
+    dy = torch.randn(n, 64, device="cuda").to(dtype)
+    offsets = torch.tensor([0, n, 0, n, 0, n, 0, n, 0], dtype=torch.int32, device="cuda")
+    whole = torch.full((E * 64 * 65 + 8,), 5.0, device="cuda")
+    kfac.kfac_expert_grad_weight_kept(c, layer, None, offsets, q, s, dy, whole[:-8].view(E, 64, 65))
+    kfac.kfac_stats_expert_kept(c, layer, None, offsets, q, s, None, 0.0, torch.empty(E, 65, 65, device="cuda"), None)
+    torch.cuda.synchronize()
+    assert bool((whole[-8:] == 5.0).all()) and bool((c.workspace[base + need:] == 77).all())
+    c.close()
+
+
 def test_no_rows():
     layer = wl.fc_layer(1, 72, 40, 1)
     c = kfac.Context([layer], workspace_bytes=kfac.kfac_kept_workspace_bytes(layer, 2, 0))
