@@ -357,14 +357,12 @@ __device__ __forceinline__ void row_tile(const ExpertArgs &a, int tiles_j, int l
         t.J = a.ci;
     } else {
         static_assert(BM == BN, "the triangle has square tiles");
-        const int na = a.A ? triangle_tiles<BM>(a.ci) : 0;
-        t.g = local >= na;
-        tri_decode(t.g ? local - na : local, t.ti, t.tj);
-        t.I = t.J = t.g ? a.co : a.ci;
+        tri_decode(local, t.ti, t.tj);
+        t.I = t.J = a.ci;
     }
 }
 
-// Contractions over rows in pieces (up to 64 experts): the rows of an expert that has more than a.piece of them are cut into equal parts, and
+// Contractions over rows in pieces (up to 64 experts; of the statistics factor A alone; x sorted: row s is that of the choice at place s): the rows of an expert that has more than a.piece of them are cut into equal parts, and
 // the parts of all experts are taken up in the order of their lengths, so that the last ones to run are short ones.  Lane e of every wave
 // knows expert e's.
 struct Pieces {
@@ -395,9 +393,11 @@ template <int OP, int BM, int BN>
 __device__ __forceinline__ bool find_piece(const ExpertArgs &a, int tiles_j, int tiles, Tile &t, int &slot)
 {
     const Pieces p = pieces_of<OP>(a);
-    const int at = blockIdx.x / tiles, local = blockIdx.x - at * tiles;
+    // of every piece an XCD has an eighth of the tiles, or it has whole pieces, in turn forth and back
+    const int x = blockIdx.x & 7, i = blockIdx.x >> 3, per = a.whole_pieces ? tiles : (tiles + 7) / 8;
+    const int round = i / per, at = !a.whole_pieces ? round : 8 * round + (round & 1 ? 7 - x : x), local = (a.whole_pieces ? 0 : x * per) + i - round * per;
     const unsigned long long has = __ballot(at >= p.first && at < p.first + p.count);
-    if (!has) return false;
+    if (!has || local >= tiles) return false;
     const int e = __ffsll(has) - 1;
     const int rows = __builtin_amdgcn_readlane(p.rows, e), count = __builtin_amdgcn_readlane(p.count, e), q = at - __builtin_amdgcn_readlane(p.first, e);
     t.e = e;
@@ -572,8 +572,9 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
     constexpr int BK = sizeof(T) == 2 ? 64 : 32, NP = sizeof(T) == 2 || FP32 ? 1 : 3;
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
-    constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
-    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
+    constexpr int GATHER_X = PIECES ? 0 : 2;
+    constexpr int GATHER_A = OP == EXPERT_FORWARD ? 2 : OP == EXPERT_STATS ? GATHER_X : 1;
+    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? GATHER_X : 0;
     constexpr int PLANE = EDGE * BK, NB = EDGE / 32;   // NB x NB blocks of 16 x 16 a wave
     __shared__ __attribute__((aligned(16))) E lds[GROUPS * 2 * NP * PLANE];
     const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -590,7 +591,7 @@ __global__ __launch_bounds__(256 * GROUPS, EDGE == 128 ? 2 : 4) void expert_gene
 
     Staged<T, ACROSS_A, GATHER_A, BK, EDGE> sa;
     Staged<T, ACROSS_B, GATHER_B, BK, EDGE> sb;
-    const T *We = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw, *x = (const T *)a.x, *dy = (const T *)a.dy;
+    const T *We = (const T *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw, *x = (const T *)a.x + (PIECES ? t.begin * a.ldx : 0), *dy = (const T *)a.dy;
     if constexpr (OP == EXPERT_FORWARD) sa.init(a, x, a.ldx, a.fan, t.begin, t.ti * EDGE, t.I, t.K, first, tid);
     else if constexpr (OP == EXPERT_STATS) sa.init(a, t.g ? dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * EDGE, t.I, t.K, first, tid);
     else sa.init(a, dy, a.ldy, 1, t.begin, t.ti * EDGE, t.I, t.K, first, tid);
@@ -856,8 +857,9 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
 {
     constexpr bool ACROSS_A = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS;
     constexpr bool ACROSS_B = OP != EXPERT_FORWARD;
-    constexpr int GATHER_A = OP == EXPERT_FORWARD || OP == EXPERT_STATS ? 2 : 1;
-    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? 2 : 0;
+    constexpr int GATHER_X = PIECES ? 0 : 2;
+    constexpr int GATHER_A = OP == EXPERT_FORWARD ? 2 : OP == EXPERT_STATS ? GATHER_X : 1;
+    constexpr int GATHER_B = OP == EXPERT_GRAD_WEIGHT || OP == EXPERT_STATS ? GATHER_X : 0;
     constexpr int THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ, NI = TI / 32, NJ = TJ / 32, PLACE = (BM + BN) * 32;
     __shared__ __attribute__((aligned(1024))) bf16_t lds[kPlaces * PLACE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -875,13 +877,13 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
     constexpr int LA = 2 * DirectA::CH, LOADS = LA + 2 * DirectB::CH;   // a thread's, a step
     DirectA da;
     DirectB db;
-    const bf16_t *We = (const bf16_t *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw;
-    if constexpr (OP == EXPERT_FORWARD) da.init(a, a.x, a.ldx, a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
-    else if constexpr (OP == EXPERT_STATS) da.init(a, t.g ? a.dy : a.x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
+    const bf16_t *We = (const bf16_t *)a.W + (long long)min(t.e, a.experts - 1) * a.co * a.ldw, *x = (const bf16_t *)a.x + (PIECES ? t.begin * a.ldx : 0);
+    if constexpr (OP == EXPERT_FORWARD) da.init(a, x, a.ldx, a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) da.init(a, t.g ? (const bf16_t *)a.dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.ti * BM, t.I, t.K, tid);
     else da.init(a, a.dy, a.ldy, 1, t.begin, t.ti * BM, t.I, t.K, tid);
     if constexpr (OP == EXPERT_FORWARD || OP == EXPERT_GRAD_INPUT) db.init(a, We, a.ldw, 1, 0, t.tj * BN, t.J, t.K, tid);
-    else if constexpr (OP == EXPERT_STATS) db.init(a, t.g ? a.dy : a.x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
-    else db.init(a, a.x, a.ldx, a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
+    else if constexpr (OP == EXPERT_STATS) db.init(a, t.g ? (const bf16_t *)a.dy : x, t.g ? a.ldy : a.ldx, t.g ? 1 : a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
+    else db.init(a, x, a.ldx, a.fan, t.begin, t.tj * BN, t.J, t.K, tid);
     const bool sums = SUMS && wants_sums<OP>(a, t, wj);
 
     floatx16 acc[NI][NJ];
@@ -967,9 +969,10 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
             const bool more = s + 2 < whole;
             wait_lds();   // everyone has read the first half of step s: its place and the one before it are free
             half(fa[0], fb[0], behind(1), fa[1], fb[1], std::true_type{}, more, s, behind(4));
-            fetch(s + 3);
+            if (!PIECES) fetch(s + 3);
             if (more) wait_loads<LOADS>();   // step s + 1 is there
             else wait_loads<0>();
+            if (PIECES) fetch(s + 3);        // (the wait is for scalar loads, too: these have half a step)
             half(fa[1], fb[1], behind(2), fa[0], fb[0], std::false_type{}, false, s, 0);   // (what is read behind the last step is not used)
             place = behind(2);
         }
@@ -1070,8 +1073,8 @@ __global__ __launch_bounds__(256) void expert_join_kernel(const ExpertArgs a, in
         if constexpr (OP == EXPERT_GRAD_WEIGHT) {
             store4<float>(a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias) + col, t.J - col, v);
         } else {
-            const int d = t.g ? a.co : a.ci + a.bias;
-            float *const M = (t.g ? a.G : a.A) + (long long)t.e * d * d;
+            const int d = a.ci + a.bias;
+            float *const M = a.A + (long long)t.e * d * d;
             const float alpha = (1.f - a.decay) / (float)t.len;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -1083,7 +1086,7 @@ __global__ __launch_bounds__(256) void expert_join_kernel(const ExpertArgs a, in
                 }
         }
     }
-    if (a.bias && !t.g && t.tj == 0 && part == 0 && threadIdx.x < BM) {
+    if (a.bias && t.tj == 0 && part == 0 && threadIdx.x < BM) {
         float sum = 0.f;
         for (int k = 0; k < count; ++k) sum += from[k * apart + BM * BN + threadIdx.x];
         store_sum<OP>(a, t, t.ti * BM + (int)threadIdx.x, sum);
@@ -1205,7 +1208,7 @@ int row_tiles(const ExpertArgs &a, int &tiles_j)
 {
     tiles_j = (a.ci + BN - 1) / BN;
     if (OP == EXPERT_GRAD_WEIGHT) return (a.co + BM - 1) / BM * tiles_j;
-    return (a.A ? triangle_tiles<BM>(a.ci) : 0) + (a.G ? triangle_tiles<BM>(a.co) : 0);
+    return triangle_tiles<BM>(a.ci);
 }
 
 template <ExpertOp OP, bool DIRECT, int BM, int BN, int WI, int WJ, typename Launch>
@@ -1215,7 +1218,9 @@ hipError_t run_pieces(ExpertArgs a, int slots, hipStream_t s, Launch launch)
     const int tiles = row_tiles<OP, BM, BN>(a, tj);
     a.piece = piece_rows(a.n, tiles, slots);
     a.most = (int)(2LL * a.n / a.piece);   // pieces of experts with several: each is longer than half of a.piece
-    launch(a, dim3((unsigned)((a.n / a.piece + a.experts) * tiles)), tj, tiles);
+    a.whole_pieces = tiles <= slots / 8;   // then there are eight pieces at least
+    const int most = a.n / a.piece + a.experts;
+    launch(a, dim3((unsigned)(a.whole_pieces ? (most + 7) / 8 * 8 * tiles : most * ((tiles + 7) / 8 * 8))), tj, tiles);
     if (a.n > a.piece)   // at most n / piece experts have several
         expert_join_kernel<OP, DIRECT, BM, BN, WI, WJ><<<dim3((unsigned)(a.n / a.piece) * tiles * (BM * BN / 1024)), dim3(256), 0, s>>>(a, tj, tiles);
     return hipGetLastError();
@@ -1279,15 +1284,14 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes
 size_t expert_pieces_bytes(int experts, int n, int ci, int co)
 {
     if (experts > 64) return 0;
-    // n / 256 pieces at most (of A and G: 2 triangles with their diagonals), 1024 tiles of 128 x 128 at most (256 and 2048 of the others)
-    const size_t longer = (size_t)std::max(ci, co), edge = (longer + 255) / 256 * 256;
-    const size_t piece = 2 * edge * edge * sizeof(float) / 64 * 65, most = (size_t)1024 * (128 * 128 / 64 * 65) * sizeof(float);
+    // n / 256 pieces at most, 1024 tiles of 128 x 128 at most (256 and 2048 of the others)
+    const size_t i = ((size_t)ci + 255) / 256 * 256, o = ((size_t)co + 255) / 256 * 256;
+    const size_t piece = i * std::max(i, o) * sizeof(float) / 64 * 65, most = (size_t)1024 * (128 * 128 / 64 * 65) * sizeof(float);
     return std::min((size_t)(n / 256) * piece, most);
 }
 
 hipError_t launch_expert_pieces(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s)
 {
-    if (a.experts > 64) return launch_expert(op, a, bf16, planes, s);
     return op == EXPERT_GRAD_WEIGHT ? pieces<EXPERT_GRAD_WEIGHT>(a, bf16, planes, s) : pieces<EXPERT_STATS>(a, bf16, planes, s);
 }
 

@@ -34,8 +34,13 @@ __global__ __launch_bounds__(256) void restore_kernel(const KeepArgs a, unsigned
         const unsigned long long row = u / per_row;
         const int c = 8 * (int)(u - row * per_row), there = a.cols - c;
         if (there <= 0) continue;   // (a row has whole blocks of threads)
+        long long from = (long long)row;
+        if (a.gather) {
+            const int choice = a.order ? a.order[row] : (int)row;
+            from = (unsigned)min(max(choice, 0), (int)a.rows - 1) / (unsigned)a.fan;
+        }
         float v[8];
-        from_8_bits(load_bytes(a.q + row * a.ldq + c, there), a.scales[row * a.lds + c / 32], v);
+        from_8_bits(load_bytes(a.q + from * a.ldq + c, there), a.scales[from * a.lds + c / 32], v);
         store8((T *)a.back + row * a.ldx + c, there, v);
     }
 }

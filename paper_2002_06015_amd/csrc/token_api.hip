@@ -117,23 +117,35 @@ kfac_status run_stats(kfac_ctx *ctx, const ExpertArgs &a, kfac_dtype in)
     return run_expert(ctx, EXPERT_STATS, a, in, a.n * (fa + fg), read + 4.0 * a.experts * (fa + fg)) ? KFAC_OK : KFAC_ERR_DEVICE;
 }
 
-// Inputs of experts that were kept in 8 bits; in the workspace as values, rows a whole number of 16-byte chunks apart.
+// Inputs of experts that were kept in 8 bits; in the workspace as values, rows a whole number of 16-byte chunks apart: sorted by place for up to
+// kPieceExperts experts (the products then cut long experts into pieces, whose sums follow), by token for more.
 int64_t kept_row(const kfac_layer *L) { return ((int64_t)L->c_in + 63) / 64 * 64; }
-size_t kept_bytes(const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type)
+size_t kept_bytes(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type)
 {
-    return ((size_t)(n / fan) * kept_row(L) * esize(type) + 255) / 256 * 256;
+    return ((size_t)(experts <= kPieceExperts ? n : n / fan) * kept_row(L) * esize(type) + 255) / 256 * 256;
+}
+size_t kept_scratch(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type)
+{
+    return kept_bytes(L, experts, n, fan, type) + (experts <= kPieceExperts ? expert_pieces_bytes(experts, n, L->c_in, L->c_out) : 0);
 }
 bool kept_ok(const kfac_layer *L, int32_t n, int32_t fan, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds)
 {
     return ldq >= L->c_in && lds >= (L->c_in + 31) / 32 && ldq <= kMaxPositions && lds <= kMaxPositions && (n == 0 || (q && scales));
 }
-bool restore_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t n, int32_t fan, kfac_dtype type, const uint8_t *q, int64_t ldq, const uint8_t *scales, int64_t lds)
+// Brings them there and sends the product after them.
+kfac_status run_kept(kfac_ctx *ctx, ExpertOp op, ExpertArgs a, const kfac_layer *L, kfac_dtype type, const uint8_t *q, int64_t ldq, const uint8_t *scales,
+                     int64_t lds)
 {
+    const CtxView c = ctx_view(ctx);
     KeepArgs k{};
-    k.rows = n / fan; k.cols = L->c_in; k.back = ctx_view(ctx).ws; k.ldx = kept_row(L);
+    const bool pieces = a.experts <= kPieceExperts;
+    k.gather = pieces; k.order = a.order; k.fan = a.fan;
+    k.rows = pieces ? a.n : a.n / a.fan; k.cols = L->c_in; k.back = c.ws; k.ldx = kept_row(L);
     k.q = const_cast<uint8_t *>(q); k.ldq = ldq; k.scales = const_cast<uint8_t *>(scales); k.lds = lds;   // (only read)
-    return timed(ctx, KFAC_K_KEEP, 1, 0.0, (double)k.rows * k.cols * (esize(type) + 1 + 1.0 / 32),
-                 [&] { return launch_restore(k, type == KFAC_BF16, ctx_view(ctx).stream); });
+    if (k.rows > 0 && !timed(ctx, KFAC_K_KEEP, 1, 0.0, (double)k.rows * k.cols * (esize(type) + 1 + 1.0 / 32),
+                             [&] { return launch_restore(k, type == KFAC_BF16, c.stream); })) return KFAC_ERR_DEVICE;
+    if (pieces) a.partial = (float *)(c.ws + kept_bytes(L, a.experts, a.n, a.fan, type));
+    return op == EXPERT_GRAD_WEIGHT ? run_weight(ctx, a, type) : run_stats(ctx, a, type);
 }
 
 }  // namespace
@@ -307,7 +319,7 @@ kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t expert
 
 size_t kfac_kept_workspace_bytes(const kfac_layer *L, int32_t experts, int32_t n, int32_t fan)
 {
-    return experts_ok(L, experts, n) && fan >= 1 && n % fan == 0 ? std::max<size_t>(256, kept_bytes(L, n, fan, KFAC_F32) + expert_pieces_bytes(experts, n, L->c_in, L->c_out)) : 0;
+    return experts_ok(L, experts, n) && fan >= 1 && n % fan == 0 ? std::max<size_t>(256, kept_scratch(L, experts, n, fan, KFAC_F32)) : 0;
 }
 
 kfac_status kfac_expert_grad_weight_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype type,
@@ -319,11 +331,8 @@ kfac_status kfac_expert_grad_weight_kept(kfac_ctx *ctx, const kfac_layer *L, int
     ExpertArgs a;
     const kfac_status st = weight_args(ctx, L, experts, n, fan, type, order, offsets, kept_inputs(L, n, fan, q, ldq, scales, lds), c.ws, kept_row(L), dy, ldy, dW, a);
     if (st != KFAC_OK) return st;
-    const size_t values = kept_bytes(L, n, fan, type);
-    if (values + expert_pieces_bytes(experts, n, L->c_in, L->c_out) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
-    a.partial = (float *)(c.ws + values);
-    if (n > 0 && !restore_kept(ctx, L, n, fan, type, q, ldq, scales, lds)) return KFAC_ERR_DEVICE;
-    return run_weight(ctx, a, type);
+    if (kept_scratch(L, experts, n, fan, type) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    return run_kept(ctx, EXPERT_GRAD_WEIGHT, a, L, type, q, ldq, scales, lds);
 }
 
 kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t experts, int32_t n, int32_t fan, kfac_dtype in,
@@ -337,11 +346,15 @@ kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t e
                                       kept_row(L), grad_out, ldg, decay, A_ema, G_ema, a);
     if (st != KFAC_OK) return st;
     if (n == 0) return KFAC_OK;   // no expert has rows
-    const size_t values = A_ema ? kept_bytes(L, n, fan, in) : 0;
-    if (values + expert_pieces_bytes(experts, n, L->c_in, L->c_out) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
-    a.partial = (float *)(c.ws + values);
-    if (A_ema && !restore_kept(ctx, L, n, fan, in, q, ldq, scales, lds)) return KFAC_ERR_DEVICE;
-    return run_stats(ctx, a, in);
+    if (A_ema && kept_scratch(L, experts, n, fan, in) > c.ws_bytes) return KFAC_ERR_WORKSPACE;
+    if (G_ema) {   // as ever: its input was not kept
+        ExpertArgs g = a;
+        g.A = nullptr;
+        const kfac_status done = run_stats(ctx, g, in);
+        if (done != KFAC_OK || !A_ema) return done;
+    }
+    a.G = nullptr;
+    return run_kept(ctx, EXPERT_STATS, a, L, in, q, ldq, scales, lds);
 }
 
 }  // extern "C"

@@ -91,14 +91,16 @@ struct ExpertArgs {
     float *A, *G;                 // [experts, ci + bias, ci + bias], [experts, co, co]
     float decay;
     float *partial;               // sums of pieces (launch_expert_pieces), expert_pieces_bytes of them
-    int piece, most;              // rows that an expert has at most if they are not cut, places for pieces (set by it)
+    int piece, most, whole_pieces;   // set by it: rows that an expert has at most if they are not cut, places for pieces, whether an XCD has whole ones
 };
 enum ExpertOp { EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, EXPERT_STATS };
 // planes: how fp32 operands are multiplied (bf16 != 0: not used)
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s);
 
-// The contractions over rows (gradient of the weights, factors) with long experts cut into pieces.
-size_t expert_pieces_bytes(int experts, int n, int ci, int co);   // never less for more rows, experts up to 64 or channels
+// The contractions over rows (gradient of the weights, factor A) for up to kPieceExperts experts, long ones cut into pieces; x is sorted: row s
+// belongs to the choice at place s.
+constexpr int kPieceExperts = 64;
+size_t expert_pieces_bytes(int experts, int n, int ci, int co);   // never less for more rows, experts or channels
 hipError_t launch_expert_pieces(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s);
 
 // ---- routing -------------------------------------------------------------------------------------------
@@ -135,6 +137,9 @@ hipError_t launch_combine_grad(const CombineArgs &a, int bf16, int out_bf16, hip
 struct KeepArgs {
     long long rows;
     int cols;
+    bool gather;                  // of launch_restore: row s is that of the choice order[s] (or s), choice / fan
+    const int *order;
+    int fan;
     const void *x;                // of kfac_keep
     void *back;                   // of kfac_restore
     long long ldx;
