@@ -8,6 +8,7 @@ namespace kfac {
 typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned short ushort8_u __attribute__((ext_vector_type(8), aligned(2)));
 typedef unsigned uint2_u __attribute__((ext_vector_type(2), aligned(1)));
+typedef unsigned uint4_u __attribute__((ext_vector_type(4), aligned(1)));
 typedef unsigned short bf16_bits;
 
 template <typename T> struct Element;
@@ -83,15 +84,9 @@ __device__ __forceinline__ int scale_byte(unsigned magnitude)
 }
 __device__ __forceinline__ float power_of_two(int byte) { return __uint_as_float((unsigned)byte << 23); }
 
-// All lanes of a wave call it.  v: zeros behind the row's end.  Returns the block's scale byte; q: the eight bytes.
-__device__ __forceinline__ int to_8_bits(const float (&v)[8], uint2_u &q)
+// Eight elements over a scale.
+__device__ __forceinline__ void in_8_bits(const float (&v)[8], int byte, uint2_u &q)
 {
-    unsigned high = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) high = max(high, finite_bits(v[j]));
-    high = max(high, from_lane<0xB1>(high));   // quad_perm 1 0 3 2
-    high = max(high, from_lane<0x4E>(high));   // quad_perm 2 3 0 1
-    const int byte = scale_byte(high);
     const float inverse = power_of_two(254 - byte);
     float u[8];
 #pragma unroll
@@ -104,6 +99,33 @@ __device__ __forceinline__ int to_8_bits(const float (&v)[8], uint2_u &q)
         int r = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * j], u[4 * j + 1], 0, false);
         q[j] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(u[4 * j + 2], u[4 * j + 3], r, true);
     }
+}
+
+// All lanes of a wave call these.  v: zeros behind the row's end.  They return the block's scale byte; q: the bytes.
+__device__ __forceinline__ int to_8_bits(const float (&v)[8], uint2_u &q)
+{
+    unsigned high = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) high = max(high, finite_bits(v[j]));
+    high = max(high, from_lane<0xB1>(high));   // quad_perm 1 0 3 2
+    high = max(high, from_lane<0x4E>(high));   // quad_perm 2 3 0 1
+    const int byte = scale_byte(high);
+    in_8_bits(v, byte, q);
+    return byte;
+}
+
+// Sixteen elements a lane: lanes 2 i and 2 i + 1 hold a block.
+__device__ __forceinline__ int to_8_bits(const float (&v)[2][8], uint2_u (&q)[2])
+{
+    unsigned high = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) high = max(high, finite_bits(v[h][j]));
+    high = max(high, from_lane<0xB1>(high));   // quad_perm 1 0 3 2
+    const int byte = scale_byte(high);
+    in_8_bits(v[0], byte, q[0]);
+    in_8_bits(v[1], byte, q[1]);
     return byte;
 }
 
@@ -140,6 +162,28 @@ __device__ __forceinline__ uint2_u load_bytes(const unsigned char *p, int there)
     for (int j = 0; j < 8; ++j)
         if (j < there) q[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
     return q;
+}
+
+// The same of sixteen.
+__device__ __forceinline__ void store_bytes(unsigned char *p, int there, const uint2_u (&q)[2])
+{
+    if (there >= 16) {
+        *(uint4_u *)p = uint4_u{q[0][0], q[0][1], q[1][0], q[1][1]};
+    } else {
+        store_bytes(p, there, q[0]);
+        store_bytes(p + 8, there - 8, q[1]);
+    }
+}
+__device__ __forceinline__ void load_bytes(const unsigned char *p, int there, uint2_u (&q)[2])
+{
+    if (there >= 16) {
+        const uint4_u r = *(const uint4_u *)p;
+        q[0] = uint2_u{r[0], r[1]};
+        q[1] = uint2_u{r[2], r[3]};
+    } else {
+        q[0] = load_bytes(p, there);
+        q[1] = load_bytes(p + 8, there - 8);
+    }
 }
 
 }  // namespace kfac

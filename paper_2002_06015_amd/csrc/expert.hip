@@ -1035,12 +1035,13 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
 }
 
 // ---- the pieces' sums together ---------------------------------------------------------------------------
-// Experts with several pieces: a thread adds up four adjacent sums of a tile over the pieces, in their order, and stores them as the kernels do.
+// Experts with several pieces: a thread adds up four times four adjacent sums of a tile over the pieces, in their order, and stores them as the
+// kernels do.
 // Bound by memory, and few: the pieces are as long as they can be with every CU at work.
 template <int OP, bool DIRECT, int BM, int BN, int WI, int WJ>
 __global__ __launch_bounds__(256) void expert_join_kernel(const ExpertArgs a, int tiles_j, int tiles)
 {
-    constexpr int PARTS = BM * BN / 1024, THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ;
+    constexpr int QUADS = 4, PARTS = BM * BN / (1024 * QUADS), THREADS = 64 * WI * WJ, TI = BM / WI, TJ = BN / WJ;   // QUADS a thread
     const Pieces p = pieces_of<OP>(a);
     const int of = blockIdx.x / (tiles * PARTS), rest = blockIdx.x - of * tiles * PARTS, local = rest / PARTS, part = rest - local * PARTS;
     const unsigned long long has = __ballot(p.count > 1 && p.split == of);
@@ -1053,37 +1054,41 @@ __global__ __launch_bounds__(256) void expert_join_kernel(const ExpertArgs a, in
     row_tile<OP, BM, BN>(a, tiles_j, local, t);
     const float *from = a.partial + ((long long)place * tiles + local) * slot_floats<BM, BN>();
     const long long apart = tiles * slot_floats<BM, BN>();
-    const int quad = part * 256 + threadIdx.x, q = quad / THREADS, tid = quad % THREADS, lane = tid & 63, wi = (tid >> 6) / WJ, wj = (tid >> 6) % WJ;
-    floatx4 v = *(const floatx4 *)(from + 4 * quad);
-#pragma unroll 4
-    for (int k = 1; k < count; ++k) v += *(const floatx4 *)(from + k * apart + 4 * quad);
-    int row, col;
-    if constexpr (DIRECT) {
-        constexpr int NJ = TJ / 32;
-        row = wi * TI + 32 * (q / 4 / NJ) + (lane & 31);
-        col = wj * TJ + 32 * (q / 4 % NJ) + 8 * (q % 4) + 4 * (lane >> 5);
-    } else {
-        constexpr int NJ = TJ / 16;
-        row = wi * TI + 16 * (q / NJ) + (lane & 15);
-        col = wj * TJ + 16 * (q % NJ) + 4 * (lane >> 4);
-    }
-    row += t.ti * BM;
-    col += t.tj * BN;
-    if (row < t.I) {
-        if constexpr (OP == EXPERT_GRAD_WEIGHT) {
-            store4<float>(a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias) + col, t.J - col, v);
+    floatx4 sum[QUADS];
+#pragma unroll
+    for (int u = 0; u < QUADS; ++u) sum[u] = *(const floatx4 *)(from + 4 * ((part * QUADS + u) * 256 + threadIdx.x));
+    for (int k = 1; k < count; ++k)
+#pragma unroll
+        for (int u = 0; u < QUADS; ++u) sum[u] += *(const floatx4 *)(from + k * apart + 4 * ((part * QUADS + u) * 256 + threadIdx.x));
+#pragma unroll
+    for (int u = 0; u < QUADS; ++u) {
+        const int quad = (part * QUADS + u) * 256 + threadIdx.x, q = quad / THREADS, tid = quad % THREADS, lane = tid & 63, wi = (tid >> 6) / WJ, wj = (tid >> 6) % WJ;
+        int row, col;
+        if constexpr (DIRECT) {
+            constexpr int NJ = TJ / 32;
+            row = wi * TI + 32 * (q / 4 / NJ) + (lane & 31);
+            col = wj * TJ + 32 * (q / 4 % NJ) + 8 * (q % 4) + 4 * (lane >> 5);
         } else {
-            const int d = a.ci + a.bias;
-            float *const M = a.A + (long long)t.e * d * d;
+            constexpr int NJ = TJ / 16;
+            row = wi * TI + 16 * (q / NJ) + (lane & 15);
+            col = wj * TJ + 16 * (q % NJ) + 4 * (lane >> 4);
+        }
+        row += t.ti * BM;
+        col += t.tj * BN;
+        if (row >= t.I) continue;
+        if constexpr (OP == EXPERT_GRAD_WEIGHT) {
+            store4<float>(a.dW + ((long long)t.e * a.co + row) * (a.ci + a.bias) + col, t.J - col, sum[u]);
+        } else {
+            const int d = a.ci + a.bias, below = min(row + 1 - col, 4);   // the lower triangle and its mirror image
+            float *const M = a.A + (long long)t.e * d * d, *const out = M + (long long)row * d + col;
             const float alpha = (1.f - a.decay) / (float)t.len;
+            floatx4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = blend(a.decay, alpha, a.decay != 0.f && r < below ? out[r] : 0.f, sum[u][r]);
+            store4<float>(out, below, v);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (col + r <= row) {   // the lower triangle and its mirror image
-                    float *const out = M + (long long)row * d + col + r;
-                    const float w = blend(a.decay, alpha, a.decay == 0.f ? 0.f : *out, v[r]);
-                    *out = w;
-                    M[(long long)(col + r) * d + row] = w;
-                }
+                if (r < below && col + r < row) M[(long long)(col + r) * d + row] = v[r];
         }
     }
     if (a.bias && t.tj == 0 && part == 0 && threadIdx.x < BM) {
@@ -1222,7 +1227,7 @@ hipError_t run_pieces(ExpertArgs a, int slots, hipStream_t s, Launch launch)
     const int most = a.n / a.piece + a.experts;
     launch(a, dim3((unsigned)(a.whole_pieces ? (most + 7) / 8 * 8 * tiles : most * ((tiles + 7) / 8 * 8))), tj, tiles);
     if (a.n > a.piece)   // at most n / piece experts have several
-        expert_join_kernel<OP, DIRECT, BM, BN, WI, WJ><<<dim3((unsigned)(a.n / a.piece) * tiles * (BM * BN / 1024)), dim3(256), 0, s>>>(a, tj, tiles);
+        expert_join_kernel<OP, DIRECT, BM, BN, WI, WJ><<<dim3((unsigned)(a.n / a.piece) * tiles * (BM * BN / 4096)), dim3(256), 0, s>>>(a, tj, tiles);
     return hipGetLastError();
 }
 

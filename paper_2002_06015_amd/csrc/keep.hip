@@ -3,6 +3,8 @@
 // 2^e is the least power with max |x| <= 448 2^e over the block's finite elements, so nothing is cut off and an element above
 // 2^-6 of that range is held to four bits (half a step: 2^-4 of it).  Scaling by a power of two is exact: the one rounding is the
 // conversion, and what is held, q 2^e with e >= -117, is exact in bf16 and fp32.  Both directions are bound by memory.
+#include <algorithm>
+
 #include "elements.h"
 #include "token_internal.h"
 
@@ -10,47 +12,58 @@ namespace kfac {
 
 namespace {
 
-// A thread: eight elements of a row; four adjacent threads: a block.  Threads behind the last one do their part with zeros, so that the
-// lanes of a block are all there.
+// 2^log threads a row (workgroups of 256: several rows, or a row in several steps), sixteen elements a thread; two adjacent threads: a block.
+// Threads behind a row's end or the last row do their part with zeros, so that the lanes of a block are all there.
 template <typename T>
-__global__ __launch_bounds__(256) void keep_kernel(const KeepArgs a, unsigned per_row, unsigned long long units)
+__global__ __launch_bounds__(256) void keep_kernel(const KeepArgs a, int log)
 {
-    for (unsigned long long first = (unsigned long long)blockIdx.x * 256; first < units; first += (unsigned long long)gridDim.x * 256) {
-        const unsigned long long u = first + threadIdx.x, row = u / per_row;
-        const int c = 8 * (int)(u - row * per_row), there = u < units ? a.cols - c : 0;
-        float v[8];
-        load8((const T *)a.x + row * a.ldx + c, there, v);
-        uint2_u q;
-        const int byte = to_8_bits(v, q);
-        if (there > 0) store_bytes(a.q + row * a.ldq + c, there, q);
-        if (there > 0 && (threadIdx.x & 3) == 0) a.scales[row * a.lds + c / 32] = (unsigned char)byte;
+    const long long stripe = (long long)gridDim.x << (8 - log);
+    for (long long r0 = (long long)blockIdx.x << (8 - log); r0 < a.rows; r0 += stripe) {
+        const long long row = r0 + (threadIdx.x >> log);
+        for (int c0 = 0; c0 < a.cols; c0 += 16 << log) {
+            const int c = c0 + 16 * (int)(threadIdx.x & ((1 << log) - 1)), there = row < a.rows ? a.cols - c : 0;
+            float v[2][8];
+            load8((const T *)a.x + row * a.ldx + c, there, v[0]);
+            load8((const T *)a.x + row * a.ldx + c + 8, there - 8, v[1]);
+            uint2_u q[2];
+            const int byte = to_8_bits(v, q);
+            if (there > 0) store_bytes(a.q + row * a.ldq + c, there, q);
+            if (there > 0 && (threadIdx.x & 1) == 0) a.scales[row * a.lds + c / 32] = (unsigned char)byte;
+        }
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void restore_kernel(const KeepArgs a, unsigned per_row, unsigned long long units)
+__global__ __launch_bounds__(256) void restore_kernel(const KeepArgs a, int log)
 {
-    for (unsigned long long u = (unsigned long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (unsigned long long)gridDim.x * 256) {
-        const unsigned long long row = u / per_row;
-        const int c = 8 * (int)(u - row * per_row), there = a.cols - c;
-        if (there <= 0) continue;   // (a row has whole blocks of threads)
-        long long from = (long long)row;
+    const long long stripe = (long long)gridDim.x << (8 - log);
+    for (long long row = ((long long)blockIdx.x << (8 - log)) + (threadIdx.x >> log); row < a.rows; row += stripe) {
+        long long from = row;
         if (a.gather) {
             const int choice = a.order ? a.order[row] : (int)row;
             from = (unsigned)min(max(choice, 0), (int)a.rows - 1) / (unsigned)a.fan;
         }
-        float v[8];
-        from_8_bits(load_bytes(a.q + from * a.ldq + c, there), a.scales[from * a.lds + c / 32], v);
-        store8((T *)a.back + row * a.ldx + c, there, v);
+        for (int c = 16 * (int)(threadIdx.x & ((1 << log) - 1)); c < a.cols; c += 16 << log) {
+            uint2_u q[2];
+            load_bytes(a.q + from * a.ldq + c, a.cols - c, q);
+            const int byte = a.scales[from * a.lds + c / 32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+                from_8_bits(q[h], byte, v);
+                store8((T *)a.back + row * a.ldx + c + 8 * h, a.cols - c - 8 * h, v);
+            }
+        }
     }
 }
 
 template <typename K>
 hipError_t run(K kernel, const KeepArgs &a, hipStream_t s)
 {
-    const unsigned per_row = 4u * (unsigned)((a.cols + 31) / 32);
-    const unsigned long long units = (unsigned long long)a.rows * per_row, wgs = (units + 255) / 256;
-    kernel<<<dim3((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20))), dim3(256), 0, s>>>(a, per_row, units);
+    int log = 1;
+    while (log < 8 && (16 << log) < a.cols) ++log;
+    const long long wgs = (a.rows + (256 >> log) - 1) >> (8 - log);
+    kernel<<<dim3((unsigned)std::min(wgs, 1LL << 20)), dim3(256), 0, s>>>(a, log);
     return hipGetLastError();
 }
 
