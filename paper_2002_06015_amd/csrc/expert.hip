@@ -1202,11 +1202,16 @@ hipError_t general(ExpertOp op, const ExpertArgs &a, hipStream_t s)
 
 // ---- contractions over rows in pieces -------------------------------------------------------------------
 // Every CU shall have work and the pieces shall be few (their sums go to memory and back): as many rows as a tile has if all of them went
-// evenly to `slots` workgroups, 512 at least.
-int piece_rows(long long n, int tiles, int slots)
+// evenly to `slots` workgroups, 512 at least, and more if the sums had no room.  128 x 128, two a CU, 512 slots: factors of 32768 rows 1024
+// channels in one expert 82 us, in 16 uneven ones 108 (384: 96 and 110, 768: 82 and 113, 1024: 85 and 120); of the same in tiles of 256 x 256
+// 99 and 117.
+int most_pieces(long long n, int experts, int piece) { return (int)std::min(2 * n / piece, n / piece + experts); }   // of experts with several: each is longer than half a piece
+int piece_rows(long long n, int experts, int tiles, int slots, size_t slot_bytes, size_t room)
 {
     const long long even = std::min((n * tiles + slots - 1) / slots, n);
-    return (int)std::max(512LL, (even + 63) / 64 * 64);
+    long long rows = std::max(512LL, (even + 63) / 64 * 64);
+    while (rows < n && (size_t)most_pieces(n, experts, (int)rows) * tiles * slot_bytes > room) rows += std::max(64LL, rows / 16 / 64 * 64);
+    return (int)rows;
 }
 template <int OP, int BM, int BN>
 int row_tiles(const ExpertArgs &a, int &tiles_j)
@@ -1221,9 +1226,9 @@ hipError_t run_pieces(ExpertArgs a, int slots, hipStream_t s, Launch launch)
 {
     int tj;
     const int tiles = row_tiles<OP, BM, BN>(a, tj);
-    a.piece = piece_rows(a.n, tiles, slots);
-    a.most = (int)(2LL * a.n / a.piece);   // pieces of experts with several: each is longer than half of a.piece
-    a.whole_pieces = tiles <= slots / 8;   // then there are eight pieces at least
+    a.piece = piece_rows(a.n, a.experts, tiles, slots, slot_floats<BM, BN>() * sizeof(float), expert_pieces_bytes(a.experts, a.n, a.ci, a.co));
+    a.most = a.n > a.piece ? most_pieces(a.n, a.experts, a.piece) : 0;
+    a.whole_pieces = BM < 256 && tiles <= slots / 8;   // then there are eight pieces at least (dense factors above: 101 us in eighths; weights in tiles of 256: 134 whole, 116)
     const int most = a.n / a.piece + a.experts;
     launch(a, dim3((unsigned)(a.whole_pieces ? (most + 7) / 8 * 8 * tiles : most * ((tiles + 7) / 8 * 8))), tj, tiles);
     if (a.n > a.piece)   // at most n / piece experts have several
@@ -1252,7 +1257,9 @@ hipError_t pieces(const ExpertArgs &a, bool bf16, bool planes, hipStream_t s)
 {
     int tj;
     if (bf16 && direct_ok(OP, a)) {
-        if (a.experts * row_tiles<OP, 256, 256>(a, tj) >= 512) return run_direct_pieces<OP, 256, 256, 4, 2>(a, 128, s);
+        // 256 x 256, one a CU, needs long contractions for what it does not overlap: with 2048 rows for each CU on (weights 1024 -> 2048 of 16384 rows
+        // in one expert 89 us, 109 with 128 x 128; in 16 uneven ones 116 and 154)
+        if ((long long)a.n * row_tiles<OP, 256, 256>(a, tj) >= 2048 * 256) return run_direct_pieces<OP, 256, 256, 4, 2>(a, 256, s);
         return run_direct_pieces<OP, 128, 128, 2, 2>(a, 512, s);
     }
     if (a.experts * row_tiles<OP, 128, 128>(a, tj) >= 512) {
@@ -1264,6 +1271,15 @@ hipError_t pieces(const ExpertArgs &a, bool bf16, bool planes, hipStream_t s)
 }
 
 }  // namespace
+
+size_t expert_pieces_bytes(int experts, int n, int ci, int co)
+{
+    if (experts > 64) return 0;
+    // room for n / 256 pieces or for about 64 MiB of them
+    const size_t i = ((size_t)ci + 255) / 256 * 256, o = ((size_t)co + 255) / 256 * 256;
+    const size_t piece = i * std::max(i, o) * sizeof(float) / 64 * 65, most = (size_t)1024 * (128 * 128 / 64 * 65) * sizeof(float);
+    return std::min((size_t)(n / 256) * piece, most);
+}
 
 hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s)
 {
@@ -1284,15 +1300,6 @@ hipError_t launch_expert(ExpertOp op, const ExpertArgs &a, int bf16, bool planes
     }
     if (bf16) return general<bf16_t, false>(op, a, s);
     return planes ? general<float, false>(op, a, s) : general<float, true>(op, a, s);
-}
-
-size_t expert_pieces_bytes(int experts, int n, int ci, int co)
-{
-    if (experts > 64) return 0;
-    // n / 256 pieces at most, 1024 tiles of 128 x 128 at most (256 and 2048 of the others)
-    const size_t i = ((size_t)ci + 255) / 256 * 256, o = ((size_t)co + 255) / 256 * 256;
-    const size_t piece = i * std::max(i, o) * sizeof(float) / 64 * 65, most = (size_t)1024 * (128 * 128 / 64 * 65) * sizeof(float);
-    return std::min((size_t)(n / 256) * piece, most);
 }
 
 hipError_t launch_expert_pieces(ExpertOp op, const ExpertArgs &a, int bf16, bool planes, hipStream_t s)
