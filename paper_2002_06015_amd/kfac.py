@@ -302,6 +302,7 @@ class Context:
         if st != KFAC_OK:
             raise KfacError(st, "kfac_create")
         self.handle = handle
+        self.device = self.workspace.get_device()
 
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle.value:
@@ -787,23 +788,29 @@ def router(experts: int, fan: int, groups: int = 1, top_groups: int = 1, group_b
     return kfac_router(int(experts), int(fan), int(groups), int(top_groups), int(group_best), int(scores), int(renormalise), float(scale))
 
 
-def _here(ctx: Context, *tensors: Optional[torch.Tensor]) -> None:
-    device = ctx.workspace.get_device()
+# A decoding step's calls take about as long on the host as on the device: these look at each property once.
+def _device(ctx: Context) -> int:
+    device = ctx.device
     if torch.cuda.current_device() != device:
         raise ValueError("the current device must be that of the context, cuda:%d" % device)
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("tensors must be on the device of the context, cuda:%d" % device)
+    return device
 
 
-def _view(t: Optional[torch.Tensor], rows: int, cols: int, dtype, what: str) -> tuple:
-    """Pointer and distance of the rows; nothing for None."""
-    return (None, 0) if t is None else (t.data_ptr(), _rows_of(t, rows, cols, dtype, what))
+def _mat(device: int, t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
+    """The distance of the rows of a [rows, cols] tensor on the device whose rows are contiguous."""
+    if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != device:
+        raise ValueError("%s must be a tensor of %s and shape [%d, %d] on cuda:%d, got %s %s on %s" % (what, dtype, rows, cols, device, t.dtype, tuple(t.shape), t.device))
+    if t.is_contiguous():
+        return cols
+    if rows > 0 and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols)):
+        raise ValueError("%s must have contiguous rows" % what)
+    return t.stride(0) if rows > 1 else cols
 
 
-def _choices(t: torch.Tensor, n: int, what: str) -> int:
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
-        raise ValueError("%s must be a contiguous int32 device tensor of %d elements" % (what, n))
+def _flat(device: int, t: torch.Tensor, numel: int, dtype, what: str) -> int:
+    """The address of a contiguous tensor on the device."""
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor of %s with %d elements on cuda:%d" % (what, dtype, numel, device))
     return t.data_ptr()
 
 
@@ -812,11 +819,10 @@ def kfac_route(ctx: Context, router: kfac_router, logits: torch.Tensor, choice: 
     """choice: int32 [n * fan], the experts of every token (-1: none left); gate: float32 [n, fan]; logits [n, experts]."""
     if logits.dim() != 2:
         raise ValueError("logits must be [n, experts]")
-    n, E, fan = logits.shape[0], router.experts, router.fan
-    _here(ctx, logits, choice, gate, bias)
-    st = lib().kfac_route(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(),
-                          _rows_of(logits, n, E, logits.dtype, "logits"), _floats(bias, E, "bias"), _choices(choice, n * fan, "choice"),
-                          _floats(gate, n * fan, "gate"))
+    n, E, fan, dev, dtype = logits.shape[0], router.experts, router.fan, _device(ctx), logits.dtype
+    st = _lib.kfac_route(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(), _mat(dev, logits, n, E, dtype, "logits"),
+                         None if bias is None else _flat(dev, bias, E, torch.float32, "bias"), _flat(dev, choice, n * fan, torch.int32, "choice"),
+                         _flat(dev, gate, n * fan, torch.float32, "gate"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_route")
 
@@ -826,11 +832,10 @@ def kfac_route_grad(ctx: Context, router: kfac_router, logits: torch.Tensor, cho
     """dlogits [n, experts], of the type of the logits, from dgate: float32 [n, fan]."""
     if logits.dim() != 2:
         raise ValueError("logits must be [n, experts]")
-    n, E, fan = logits.shape[0], router.experts, router.fan
-    _here(ctx, logits, choice, dgate, dlogits)
-    st = lib().kfac_route_grad(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(),
-                               _rows_of(logits, n, E, logits.dtype, "logits"), _choices(choice, n * fan, "choice"), _floats(dgate, n * fan, "dgate"),
-                               dlogits.data_ptr(), _rows_of(dlogits, n, E, logits.dtype, "dlogits"))
+    n, E, fan, dev, dtype = logits.shape[0], router.experts, router.fan, _device(ctx), logits.dtype
+    st = _lib.kfac_route_grad(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(), _mat(dev, logits, n, E, dtype, "logits"),
+                              _flat(dev, choice, n * fan, torch.int32, "choice"), _flat(dev, dgate, n * fan, torch.float32, "dgate"),
+                              dlogits.data_ptr(), _mat(dev, dlogits, n, E, dtype, "dlogits"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_route_grad")
 
@@ -847,11 +852,13 @@ def kfac_combine(ctx: Context, y: torch.Tensor, gate: Optional[torch.Tensor], ou
     or None for ones.  out may be residual."""
     if y.dim() != 2 or out.dim() != 2:
         raise ValueError("y must be [n, dim] and out [tokens, dim]")
-    (n, dim), tokens = y.shape, out.shape[0]
-    _here(ctx, y, gate, out, residual)
-    pr, ldr = _view(residual, tokens, dim, out.dtype, "residual")
-    st = lib().kfac_combine(ctx.handle, n, _fan(n, tokens), dim, _type_of(y, "y"), y.data_ptr(), _rows_of(y, n, dim, y.dtype, "y"),
-                            _floats(gate, n, "gate"), _type_of(out, "out"), pr, ldr, out.data_ptr(), _rows_of(out, tokens, dim, out.dtype, "out"))
+    (n, dim), tokens, dev, dtype, stream = y.shape, out.shape[0], _device(ctx), y.dtype, out.dtype
+    pr = ldr = 0
+    if residual is not None:
+        pr, ldr = residual.data_ptr(), _mat(dev, residual, tokens, dim, stream, "residual")
+    st = _lib.kfac_combine(ctx.handle, n, _fan(n, tokens), dim, _type_of(y, "y"), y.data_ptr(), _mat(dev, y, n, dim, dtype, "y"),
+                           None if gate is None else _flat(dev, gate, n, torch.float32, "gate"), _type_of(out, "out"), pr, ldr,
+                           out.data_ptr(), _mat(dev, out, tokens, dim, stream, "out"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_combine")
 
@@ -862,28 +869,31 @@ def kfac_combine_grad(ctx: Context, y: Optional[torch.Tensor], gate: Optional[to
     src = dy if dy is not None else y
     if src is None or src.dim() != 2 or dout.dim() != 2 or (dgate is None and dy is None) or (dgate is not None and y is None):
         raise ValueError("dy or dgate is needed, dgate needs y; y and dy must be [n, dim], dout [tokens, dim]")
-    (n, dim), tokens = src.shape, dout.shape[0]
-    _here(ctx, y, gate, dout, dy, dgate)
-    py, ldy = _view(y if dgate is not None else None, n, dim, src.dtype, "y")
-    pd, lddy = _view(dy, n, dim, src.dtype, "dy")
-    st = lib().kfac_combine_grad(ctx.handle, n, _fan(n, tokens), dim, _type_of(src, "y"), py, ldy, _floats(gate, n, "gate"), _type_of(dout, "dout"),
-                                 dout.data_ptr(), _rows_of(dout, tokens, dim, dout.dtype, "dout"), pd, lddy, _floats(dgate, n, "dgate"))
+    (n, dim), tokens, dev, dtype = src.shape, dout.shape[0], _device(ctx), src.dtype
+    py = ldy = pd = lddy = pg = 0
+    if dgate is not None:
+        py, ldy, pg = y.data_ptr(), _mat(dev, y, n, dim, dtype, "y"), _flat(dev, dgate, n, torch.float32, "dgate")
+    if dy is not None:
+        pd, lddy = dy.data_ptr(), _mat(dev, dy, n, dim, dtype, "dy")
+    st = _lib.kfac_combine_grad(ctx.handle, n, _fan(n, tokens), dim, _type_of(src, "y"), py, ldy,
+                                None if gate is None else _flat(dev, gate, n, torch.float32, "gate"), _type_of(dout, "dout"),
+                                dout.data_ptr(), _mat(dev, dout, tokens, dim, dout.dtype, "dout"), pd, lddy, pg)
     if st != KFAC_OK:
         raise KfacError(st, "kfac_combine_grad")
 
 
-def _bytes(q: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> tuple:
+def _bytes(dev: int, q: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> tuple:
     """Pointers and distances of the rows of activations in 8 bits."""
-    return q.data_ptr(), _rows_of(q, rows, cols, torch.float8_e4m3fn, "q"), scales.data_ptr(), _rows_of(scales, rows, (cols + 31) // 32, torch.uint8, "scales")
+    return (q.data_ptr(), _mat(dev, q, rows, cols, torch.float8_e4m3fn, "q"), scales.data_ptr(),
+            _mat(dev, scales, rows, (cols + 31) // 32, torch.uint8, "scales"))
 
 
 def kfac_keep(ctx: Context, x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor) -> None:
     """x [rows, cols] in 8 bits: q float8_e4m3fn [rows, cols], scales uint8 [rows, ceil(cols / 32)]."""
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
-    rows, cols = x.shape
-    _here(ctx, x, q, scales)
-    st = lib().kfac_keep(ctx.handle, rows, cols, _type_of(x, "x"), x.data_ptr(), _rows_of(x, rows, cols, x.dtype, "x"), *_bytes(q, scales, rows, cols))
+    (rows, cols), dev = x.shape, _device(ctx)
+    st = _lib.kfac_keep(ctx.handle, rows, cols, _type_of(x, "x"), x.data_ptr(), _mat(dev, x, rows, cols, x.dtype, "x"), *_bytes(dev, q, scales, rows, cols))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_keep")
 
@@ -892,9 +902,8 @@ def kfac_restore(ctx: Context, q: torch.Tensor, scales: torch.Tensor, x: torch.T
     """The values that q and its scales stand for, float32 or bfloat16."""
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
-    rows, cols = x.shape
-    _here(ctx, x, q, scales)
-    st = lib().kfac_restore(ctx.handle, rows, cols, *_bytes(q, scales, rows, cols), _type_of(x, "x"), x.data_ptr(), _rows_of(x, rows, cols, x.dtype, "x"))
+    (rows, cols), dev = x.shape, _device(ctx)
+    st = _lib.kfac_restore(ctx.handle, rows, cols, *_bytes(dev, q, scales, rows, cols), _type_of(x, "x"), x.data_ptr(), _mat(dev, x, rows, cols, x.dtype, "x"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_restore")
 
@@ -907,13 +916,11 @@ def kfac_kept_workspace_bytes(layer, experts: int, n: int, fan: int = 1) -> int:
 def kfac_expert_grad_weight_kept(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
                                  dy: torch.Tensor, dW: torch.Tensor, fan: int = 1) -> None:
     """kfac_expert_grad_weight for inputs that were kept in 8 bits: q [n // fan, c_in] with its scales."""
-    n = dy.shape[0]
+    n, dev = dy.shape[0], _device(ctx)
     L, experts, po, pf = _expert(layer, order, offsets, n)
-    _here(ctx, order, offsets, q, scales, dy, dW)
-    typ = _type_of(dy, "dy")
-    st = lib().kfac_expert_grad_weight_kept(ctx.handle, ctypes.addressof(L), experts, n, int(fan), typ, po, pf,
-                                            *_bytes(q, scales, n // max(1, int(fan)), L.c_in), dy.data_ptr(),
-                                            _rows_of(dy, n, L.c_out, dy.dtype, "dy"), _floats(dW, experts * L.c_out * (L.c_in + L.bias), "dW"))
+    st = _lib.kfac_expert_grad_weight_kept(ctx.handle, ctypes.addressof(L), experts, n, int(fan), _type_of(dy, "dy"), po, pf,
+                                           *_bytes(dev, q, scales, n // max(1, int(fan)), L.c_in), dy.data_ptr(), _mat(dev, dy, n, L.c_out, dy.dtype, "dy"),
+                                           _flat(dev, dW, experts * L.c_out * (L.c_in + L.bias), torch.float32, "dW"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_expert_grad_weight_kept")
 
@@ -921,17 +928,18 @@ def kfac_expert_grad_weight_kept(ctx: Context, layer, order: Optional[torch.Tens
 def kfac_stats_expert_kept(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
                            grad_out: Optional[torch.Tensor], decay: float, A_ema: torch.Tensor, G_ema: Optional[torch.Tensor], fan: int = 1) -> None:
     """kfac_stats_expert for inputs that were kept in 8 bits; G_ema None: grad_out is not read."""
-    fan = int(fan)
+    fan, dev = int(fan), _device(ctx)
     if G_ema is not None and grad_out is None:
         raise ValueError("a factor needs its input")
     n = order.numel() if order is not None else grad_out.shape[0] if grad_out is not None else q.shape[0] * fan
     L, experts, po, pf = _expert(layer, order, offsets, n)
-    _here(ctx, order, offsets, q, scales, grad_out, A_ema, G_ema)
     dA = L.c_in + L.bias
-    pg, ldg = (None, 0) if G_ema is None else (grad_out.data_ptr(), _rows_of(grad_out, n, L.c_out, grad_out.dtype, "grad_out"))
-    st = lib().kfac_stats_expert_kept(ctx.handle, ctypes.addressof(L), experts, n, fan, KFAC_BF16 if G_ema is None else _type_of(grad_out, "grad_out"),
-                                      po, pf, *_bytes(q, scales, n // max(1, fan), L.c_in), pg, ldg, float(decay),
-                                      _floats(A_ema, experts * dA * dA, "A_ema"), _floats(G_ema, experts * L.c_out * L.c_out, "G_ema"))
+    typ, pg, ldg, pG = KFAC_BF16, 0, 0, 0
+    if G_ema is not None:
+        typ, pg, ldg = _type_of(grad_out, "grad_out"), grad_out.data_ptr(), _mat(dev, grad_out, n, L.c_out, grad_out.dtype, "grad_out")
+        pG = _flat(dev, G_ema, experts * L.c_out * L.c_out, torch.float32, "G_ema")
+    st = _lib.kfac_stats_expert_kept(ctx.handle, ctypes.addressof(L), experts, n, fan, typ, po, pf, *_bytes(dev, q, scales, n // max(1, fan), L.c_in), pg, ldg,
+                                     float(decay), _flat(dev, A_ema, experts * dA * dA, torch.float32, "A_ema"), pG)
     if st != KFAC_OK:
         raise KfacError(st, "kfac_stats_expert_kept")
 
@@ -941,17 +949,19 @@ def kfac_rms_norm(ctx: Context, x: torch.Tensor, gamma: torch.Tensor, eps: float
     """h = x + residual (both or neither), y = gamma h / sqrt(mean h^2 + eps), and the same in 8 bits if q and scales are given."""
     if x.dim() != 2:
         raise ValueError("x must be [n, dim]")
-    n, dim = x.shape
     if (residual is None) != (h is None) or (q is None) != (scales is None):
         raise ValueError("residual and h, and q and scales, go together")
-    _here(ctx, x, gamma, y, residual, h, q, scales)
-    typ = _type_of(x, "x")
-    stream = typ if residual is None else _type_of(residual, "residual")
-    pr, ldr = _view(residual, n, dim, None if residual is None else residual.dtype, "residual")
-    ph, ldh = _view(h, n, dim, None if residual is None else residual.dtype, "h")
-    py, ldy = _view(y, n, dim, x.dtype, "y")
-    st = lib().kfac_rms_norm(ctx.handle, n, dim, typ, x.data_ptr(), _rows_of(x, n, dim, x.dtype, "x"), stream, pr, ldr, ph, ldh,
-                             _floats(gamma, dim, "gamma"), float(eps), py, ldy, *((None, 0, None, 0) if q is None else _bytes(q, scales, n, dim)))
+    (n, dim), dev, dtype, typ = x.shape, _device(ctx), x.dtype, _type_of(x, "x")
+    stream, pr, ldr, ph, ldh, py, ldy, pq, ldq, ps, lds = typ, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0
+    if residual is not None:
+        stream, pr, ldr = _type_of(residual, "residual"), residual.data_ptr(), _mat(dev, residual, n, dim, residual.dtype, "residual")
+        ph, ldh = h.data_ptr(), _mat(dev, h, n, dim, residual.dtype, "h")
+    if y is not None:
+        py, ldy = y.data_ptr(), _mat(dev, y, n, dim, dtype, "y")
+    if q is not None:
+        pq, ldq, ps, lds = _bytes(dev, q, scales, n, dim)
+    st = _lib.kfac_rms_norm(ctx.handle, n, dim, typ, x.data_ptr(), _mat(dev, x, n, dim, dtype, "x"), stream, pr, ldr, ph, ldh,
+                            _flat(dev, gamma, dim, torch.float32, "gamma"), eps, py, ldy, pq, ldq, ps, lds)
     if st != KFAC_OK:
         raise KfacError(st, "kfac_rms_norm")
 
@@ -966,13 +976,16 @@ def kfac_rms_norm_grad(ctx: Context, dy: torch.Tensor, h: torch.Tensor, gamma: t
     """dh = dstream + the norm's gradient; dgamma: float32 [dim]; F: float32 [dim], running average of the diagonal factor of gamma."""
     if dy.dim() != 2:
         raise ValueError("dy must be [n, dim]")
-    n, dim = dy.shape
-    _here(ctx, dy, h, gamma, dh, dstream, dgamma, F)
-    pr, ldr = _view(dstream, n, dim, h.dtype, "dstream")
-    ph, lddh = _view(dh, n, dim, h.dtype, "dh")
-    st = lib().kfac_rms_norm_grad(ctx.handle, n, dim, _type_of(dy, "dy"), dy.data_ptr(), _rows_of(dy, n, dim, dy.dtype, "dy"), _type_of(h, "h"),
-                                  h.data_ptr(), _rows_of(h, n, dim, h.dtype, "h"), _floats(gamma, dim, "gamma"), float(eps), pr, ldr, ph, lddh,
-                                  _floats(dgamma, dim, "dgamma"), float(decay), _floats(F, dim, "F"))
+    (n, dim), dev, stream = dy.shape, _device(ctx), h.dtype
+    pr = ldr = ph = lddh = 0
+    if dstream is not None:
+        pr, ldr = dstream.data_ptr(), _mat(dev, dstream, n, dim, stream, "dstream")
+    if dh is not None:
+        ph, lddh = dh.data_ptr(), _mat(dev, dh, n, dim, stream, "dh")
+    st = _lib.kfac_rms_norm_grad(ctx.handle, n, dim, _type_of(dy, "dy"), dy.data_ptr(), _mat(dev, dy, n, dim, dy.dtype, "dy"), _type_of(h, "h"),
+                                 h.data_ptr(), _mat(dev, h, n, dim, stream, "h"), _flat(dev, gamma, dim, torch.float32, "gamma"), eps, pr, ldr, ph, lddh,
+                                 0 if dgamma is None else _flat(dev, dgamma, dim, torch.float32, "dgamma"), decay,
+                                 0 if F is None else _flat(dev, F, dim, torch.float32, "F"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_rms_norm_grad")
 
