@@ -13,7 +13,7 @@ namespace kfac {
 namespace {
 
 // A thread: eight elements of a token's row.
-template <typename T, typename S>
+template <typename T, typename S, bool SHORT>
 __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsigned per_row, unsigned long long units)
 {
     for (unsigned long long u = (unsigned long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (unsigned long long)gridDim.x * 256) {
@@ -22,15 +22,29 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsig
         float sum[8], v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum[q] = 0.f;
-        const T *y = (const T *)a.y + token * a.fan * a.ldy + c;
-        for (int j = 0; j < a.fan; ++j) {
-            load8(y + j * a.ldy, there, v);
-            const float g = a.gate ? a.gate[token * a.fan + j] : 1.f;
+        const T *y = (const T *)a.y + token * a.fan * a.ldy;
+        const float *gate = a.gate + token * a.fan;
+        Raw8<S> res;
+        if (a.r) res.template load<SHORT>((const S *)a.r + token * a.ldr, c, a.dim);
+        for (int j0 = 0; j0 < a.fan; j0 += 4) {   // four rows in flight
+            Raw8<T> raw[4];
+            float g[4];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) sum[q] = fmaf(g, v[q], sum[q]);
+            for (int j = 0; j < 4; ++j)
+                if (j0 + j < a.fan) {
+                    raw[j].template load<SHORT>(y + (j0 + j) * a.ldy, c, a.dim);
+                    g[j] = a.gate ? gate[j0 + j] : 1.f;
+                }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j0 + j < a.fan) {
+                    raw[j].get(v);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) sum[q] = fmaf(g[j], v[q], sum[q]);
+                }
         }
         if (a.r) {
-            load8((const S *)a.r + token * a.ldr + c, there, v);
+            res.get(v);
 #pragma unroll
             for (int q = 0; q < 8; ++q) sum[q] += v[q];
         }
@@ -39,7 +53,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsig
 }
 
 // THREADS threads for FAN choices of a token.
-template <typename T, typename S, int THREADS, int FAN>
+template <typename T, typename S, int THREADS, int FAN, bool SHORT>
 __global__ __launch_bounds__(256) void combine_grad_kernel(const CombineArgs a)
 {
     __shared__ float parts[4 * FAN];
@@ -59,12 +73,19 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(const CombineArgs a)
         }
         for (int c = 8 * me; c < a.dim; c += 8 * THREADS) {
             float d[8], v[8];
-            load8(dout + c, a.dim - c, d);
+            Raw8<S> raw_d;
+            Raw8<T> raw_y[FAN];
+            raw_d.template load<SHORT>(dout, c, a.dim);
+            if (a.dgate)
+#pragma unroll
+                for (int j = 0; j < FAN; ++j)
+                    if (j0 + j < a.fan) raw_y[j].template load<SHORT>((const T *)a.y + (choice + j) * a.ldy, c, a.dim);
+            raw_d.get(d);
 #pragma unroll
             for (int j = 0; j < FAN; ++j) {
                 if (j0 + j >= a.fan) break;
                 if (a.dgate) {
-                    load8((const T *)a.y + (choice + j) * a.ldy + c, a.dim - c, v);
+                    raw_y[j].get(v);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) dot[j] = fmaf(d[q], v[q], dot[j]);
                 }
@@ -100,26 +121,29 @@ hipError_t run(const CombineArgs &a, hipStream_t s)
 {
     const unsigned per_row = (unsigned)(a.dim + 7) / 8;
     const unsigned long long units = (unsigned long long)a.tokens * per_row, wgs = (units + 255) / 256;
-    combine_kernel<T, S><<<dim3((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20))), dim3(256), 0, s>>>(a, per_row, units);
+    const dim3 grid((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)));
+    if (a.dim < 8) combine_kernel<T, S, true><<<grid, dim3(256), 0, s>>>(a, per_row, units);
+    else combine_kernel<T, S, false><<<grid, dim3(256), 0, s>>>(a, per_row, units);
     return hipGetLastError();
 }
 
-template <typename T, typename S, int THREADS>
+template <typename T, typename S, int THREADS, bool SHORT>
 hipError_t run_grad(const CombineArgs &a, hipStream_t s)
 {
     constexpr int per = 256 / THREADS;
     const long long sets = (long long)a.tokens * (a.fan <= 2 ? 1 : (a.fan + 3) / 4);
     const dim3 grid((unsigned)std::min((sets + per - 1) / per, 1LL << 20)), block(256);   // a launch takes less than 2^32 threads
-    if (a.fan <= 1) combine_grad_kernel<T, S, THREADS, 1><<<grid, block, 0, s>>>(a);
-    else if (a.fan <= 2) combine_grad_kernel<T, S, THREADS, 2><<<grid, block, 0, s>>>(a);
-    else combine_grad_kernel<T, S, THREADS, 4><<<grid, block, 0, s>>>(a);
+    if (a.fan <= 1) combine_grad_kernel<T, S, THREADS, 1, SHORT><<<grid, block, 0, s>>>(a);
+    else if (a.fan <= 2) combine_grad_kernel<T, S, THREADS, 2, SHORT><<<grid, block, 0, s>>>(a);
+    else combine_grad_kernel<T, S, THREADS, 4, SHORT><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <typename T, typename S>
 hipError_t run_grad(const CombineArgs &a, hipStream_t s)
 {
-    return a.tokens >= 4096 || a.dim <= 512 ? run_grad<T, S, 64>(a, s) : run_grad<T, S, 256>(a, s);
+    if (a.dim < 8) return run_grad<T, S, 64, true>(a, s);
+    return a.tokens >= 4096 || a.dim <= 512 ? run_grad<T, S, 64, false>(a, s) : run_grad<T, S, 256, false>(a, s);
 }
 
 }  // namespace

@@ -23,24 +23,65 @@ template <> struct Element<bf16_bits> {
     static __device__ __forceinline__ float round(float v) { return (float)(__bf16)v; }
 };
 
-// The first `there` of eight; zeros behind them.
+// Eight elements of a row from place c on, zeros behind its end.  load() has no branches and only sends the loads out: where the row ends
+// inside the eight, or before them, its last eight are loaded, and get() moves them.  (A branch around a load, or a conversion next to it, makes
+// every load wait for the one before it.)  SHORT: rows of less than eight elements, one by one.
 template <typename T>
-__device__ __forceinline__ void load8(const T *__restrict__ p, int there, float (&v)[8])
-{
-    if (there >= 8) {
+struct Raw8 {
+    float4_u a, b;   // bf16: the 16 bytes are in a
+    int back;
+    template <bool SHORT>
+    __device__ __forceinline__ void load(const T *row, int c, int cols)
+    {
+        if constexpr (SHORT) {
+            back = 0;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? Element<T>::get(row + c + j) : 0.f;
+            if constexpr (sizeof(T) == 2) {
+                ushort8_u r;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) r[j] = (bf16_bits)(__float_as_uint(v[j]) >> 16);
+                a = __builtin_bit_cast(float4_u, r);
+            } else {
+                a = float4_u{v[0], v[1], v[2], v[3]};
+                b = float4_u{v[4], v[5], v[6], v[7]};
+            }
+        } else {
+            const int from = min(c, cols - 8);
+            back = min(c - from, 8);
+            if constexpr (sizeof(T) == 2) {
+                a = __builtin_bit_cast(float4_u, *(const ushort8_u *)(row + from));
+            } else {
+                a = *(const float4_u *)(row + from);
+                b = *(const float4_u *)(row + from + 4);
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
         if constexpr (sizeof(T) == 2) {
-            const ushort8_u r = *(const ushort8_u *)p;
+            const ushort8_u r = __builtin_bit_cast(ushort8_u, a);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((unsigned)r[j] << 16);
         } else {
-            const float4_u a = *(const float4_u *)p, b = *(const float4_u *)(p + 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
         }
-    } else {
+        if (back)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < there ? Element<T>::get(p + j) : 0.f;
+            for (int s = 8; s > 0; s >>= 1)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = back & s ? (j + s < 8 ? v[j + s] : 0.f) : v[j];
     }
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *__restrict__ p, float (&v)[8])
+{
+    Raw8<T> r;
+    r.template load<false>(p, 0, 8);
+    r.get(v);
 }
 
 template <typename T>

@@ -13,18 +13,21 @@ namespace kfac {
 namespace {
 
 // 2^log threads a row (workgroups of 256: several rows, or a row in several steps), sixteen elements a thread; two adjacent threads: a block.
-// Threads behind a row's end or the last row do their part with zeros, so that the lanes of a block are all there.
-template <typename T>
+// Threads behind a row's end or the last row do their part, so that the lanes of a block are all there, and store nothing.
+template <typename T, bool SHORT>
 __global__ __launch_bounds__(256) void keep_kernel(const KeepArgs a, int log)
 {
     const long long stripe = (long long)gridDim.x << (8 - log);
     for (long long r0 = (long long)blockIdx.x << (8 - log); r0 < a.rows; r0 += stripe) {
-        const long long row = r0 + (threadIdx.x >> log);
+        const long long mine = r0 + (threadIdx.x >> log), row = mine < a.rows ? mine : a.rows - 1;
         for (int c0 = 0; c0 < a.cols; c0 += 16 << log) {
-            const int c = c0 + 16 * (int)(threadIdx.x & ((1 << log) - 1)), there = row < a.rows ? a.cols - c : 0;
+            const int c = c0 + 16 * (int)(threadIdx.x & ((1 << log) - 1)), there = mine < a.rows ? a.cols - c : 0;
             float v[2][8];
-            load8((const T *)a.x + row * a.ldx + c, there, v[0]);
-            load8((const T *)a.x + row * a.ldx + c + 8, there - 8, v[1]);
+            Raw8<T> raw[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) raw[h].template load<SHORT>((const T *)a.x + row * a.ldx, c + 8 * h, a.cols);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) raw[h].get(v[h]);
             uint2_u q[2];
             const int byte = to_8_bits(v, q);
             if (there > 0) store_bytes(a.q + row * a.ldq + c, there, q);
@@ -69,7 +72,11 @@ hipError_t run(K kernel, const KeepArgs &a, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_keep(const KeepArgs &a, int bf16, hipStream_t s) { return bf16 ? run(keep_kernel<bf16_bits>, a, s) : run(keep_kernel<float>, a, s); }
+hipError_t launch_keep(const KeepArgs &a, int bf16, hipStream_t s)
+{
+    if (a.cols < 8) return bf16 ? run(keep_kernel<bf16_bits, true>, a, s) : run(keep_kernel<float, true>, a, s);
+    return bf16 ? run(keep_kernel<bf16_bits, false>, a, s) : run(keep_kernel<float, false>, a, s);
+}
 hipError_t launch_restore(const KeepArgs &a, int bf16, hipStream_t s)
 {
     return bf16 ? run(restore_kernel<bf16_bits>, a, s) : run(restore_kernel<float>, a, s);

@@ -16,6 +16,7 @@ namespace kfac {
 namespace {
 
 // The sum over the THREADS threads of a row, in all of them.
+// parts: LDS, N THREADS / 64 of the row's own
 template <int THREADS, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float *parts)
 {
@@ -28,7 +29,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *parts)
         __syncthreads();   // what was there has been read
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int i = 0; i < N; ++i) parts[i * W + (threadIdx.x >> 6)] = v[i];
+            for (int i = 0; i < N; ++i) parts[i * W + (threadIdx.x % THREADS >> 6)] = v[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -42,35 +43,46 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *parts)
 __device__ __forceinline__ float inverse_root(float squares, int dim, float eps) { return 1.f / sqrtf(squares / (float)dim + eps); }
 
 // THREADS threads a row, CH chunks of eight elements each; workgroups of at least 256 threads.
-template <typename T, typename S, int THREADS, int CH>
+template <typename T, typename S, int THREADS, int CH, bool SHORT>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(const NormArgs a)
 {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
-    __shared__ float parts[THREADS / 64];
+    __shared__ float parts[ROWS][THREADS / 64];
     const int me = threadIdx.x % THREADS;
-    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS; row < a.n; row += (long long)gridDim.x * ROWS) {
+    for (long long first = (long long)blockIdx.x * ROWS; first < a.n; first += (long long)gridDim.x * ROWS) {
+        const long long mine = first + threadIdx.x / THREADS, row = mine < a.n ? mine : a.n - 1;   // (all threads meet at the barriers)
+        const int dim = mine < a.n ? a.dim : 0;   // what is stored
         float h[CH][8], sum[1] = {0.f};
+        Raw8<T> raw_x[CH];
+        Raw8<S> raw_r[CH];
+        Raw8<float> raw_g[CH];
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = 8 * (me + THREADS * k), there = a.dim - c;
-            load8((const T *)a.x + row * a.ldx + c, there, h[k]);
+            const int c = 8 * (me + THREADS * k);
+            raw_x[k].template load<SHORT>((const T *)a.x + row * a.ldx, c, a.dim);
+            if (a.r) raw_r[k].template load<SHORT>((const S *)a.r + row * a.ldr, c, a.dim);
+            raw_g[k].template load<SHORT>(a.gamma, c, a.dim);
+        }
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            raw_x[k].get(h[k]);
             if (a.r) {
                 float r[8];
-                load8((const S *)a.r + row * a.ldr + c, there, r);
+                raw_r[k].get(r);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[k][j] = Element<S>::round(h[k][j] + r[j]);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[0] = fmaf(h[k][j], h[k][j], sum[0]);
         }
-        row_sums<THREADS>(sum, parts);
+        row_sums<THREADS>(sum, parts[threadIdx.x / THREADS]);
         const float r = inverse_root(sum[0], a.dim, a.eps);
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = 8 * (me + THREADS * k), there = a.dim - c;
+            const int c = 8 * (me + THREADS * k), there = dim - c;
             if (a.h) store8((S *)a.h + row * a.ldh + c, there, h[k]);
             float g[8];
-            load8(a.gamma + c, there, g);
+            raw_g[k].get(g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] *= h[k][j] * r;
             if (a.y) store8((T *)a.y + row * a.ldy + c, there, g);
@@ -85,11 +97,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(con
 }
 
 // The rows `part`, part + parts, ...; COLUMNS: sums of the columns too.
-template <typename T, typename S, int THREADS, int CH, bool COLUMNS>
+template <typename T, typename S, int THREADS, int CH, bool COLUMNS, bool SHORT>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kernel(const NormGradArgs a)
 {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
-    __shared__ float parts[2 * (THREADS / 64)], columns[COLUMNS && ROWS > 1 ? 8 * 256 : 1];
+    __shared__ float parts[ROWS][2 * (THREADS / 64)], columns[COLUMNS && ROWS > 1 ? 8 * 256 : 1];
     const int me = threadIdx.x % THREADS, stripe = gridDim.x * ROWS;
     float first[COLUMNS ? CH : 1][8], second[COLUMNS ? CH : 1][8];
     if constexpr (COLUMNS)
@@ -97,42 +109,64 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
         for (int k = 0; k < CH; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j) first[k][j] = second[k][j] = 0.f;
-    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS; row < a.n; row += stripe) {
-        float h[CH][8], d[CH][8], sums[2] = {0.f, 0.f};
+    // a row is on its way while the one before it is worked on
+    Raw8<S> raw_h[CH], raw_r[CH];
+    Raw8<T> raw_d[CH];
+    auto fetch = [&](long long next) {
+        const long long row = next < a.n ? next : a.n - 1;   // (all threads meet at the barriers)
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = 8 * (me + THREADS * k), there = a.dim - c;
-            load8((const S *)a.h + row * a.ldh + c, there, h[k]);
-            load8((const T *)a.dy + row * a.lddy + c, there, d[k]);
-            float g[8];
-            load8(a.gamma + c, there, g);
+            const int c = 8 * (me + THREADS * k);
+            raw_h[k].template load<SHORT>((const S *)a.h + row * a.ldh, c, a.dim);
+            raw_d[k].template load<SHORT>((const T *)a.dy + row * a.lddy, c, a.dim);
+            if (a.r && a.dh) raw_r[k].template load<SHORT>((const S *)a.r + row * a.ldr, c, a.dim);
+        }
+    };
+    float gamma[CH][8];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = 8 * (me + THREADS * k);
+        Raw8<float> raw;
+        raw.template load<SHORT>(a.gamma, c, a.dim);
+        raw.get(gamma[k]);
+    }
+    const int mine = threadIdx.x / THREADS;
+    if (a.n > 0) fetch((long long)blockIdx.x * ROWS + mine);
+    for (long long row0 = (long long)blockIdx.x * ROWS; row0 < a.n; row0 += stripe) {
+        const long long row = row0 + mine;
+        const int dim = row < a.n ? a.dim : 0;
+        float h[CH][8], d[CH][8], o[CH][8], sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            raw_h[k].get(h[k]);
+            raw_d[k].get(d[k]);
+            if (a.r && a.dh) raw_r[k].get(o[k]);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[k][j] = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 sums[0] = fmaf(h[k][j], h[k][j], sums[0]);
-                sums[1] = fmaf(g[j] * d[k][j], h[k][j], sums[1]);
+                sums[1] = fmaf(gamma[k][j] * d[k][j], h[k][j], sums[1]);
             }
         }
-        row_sums<THREADS>(sums, parts);
+        fetch(row + stripe);
+        row_sums<THREADS>(sums, parts[mine]);
         const float r = inverse_root(sums[0], a.dim, a.eps), along = r * r * (sums[1] / (float)a.dim);
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = 8 * (me + THREADS * k), there = a.dim - c;
-            if constexpr (COLUMNS)
+            const int c = 8 * (me + THREADS * k);
+            if (COLUMNS && dim > 0)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float p = d[k][j] * (h[k][j] * r);
                     first[k][j] += p;
                     second[k][j] = fmaf(p, p, second[k][j]);
                 }
-            if (a.dh) {
-                float g[8], o[8];
-                load8(a.gamma + c, there, g);
+            if (a.dh && dim > c) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = 0.f;
-                if (a.r) load8((const S *)a.r + row * a.ldr + c, there, o);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = fmaf(r, g[j] * d[k][j] - h[k][j] * along, o[j]);
-                store8((S *)a.dh + row * a.lddh + c, there, o);
+                for (int j = 0; j < 8; ++j) o[k][j] = fmaf(r, gamma[k][j] * d[k][j] - h[k][j] * along, o[k][j]);
+                store8((S *)a.dh + row * a.lddh + c, dim - c, o[k]);
             }
         }
     }
@@ -192,43 +226,46 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const NormGradArgs a, i
 // A launch takes less than 2^32 threads; the kernels go on from there.
 unsigned workgroups(int n, int rows) { return (unsigned)std::min((n + rows - 1) / rows, 1 << 20); }
 
-template <typename T, typename S, int THREADS, int CH>
+template <typename T, typename S, int THREADS, int CH, bool SHORT = false>
 hipError_t run(const NormArgs &a, hipStream_t s)
 {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
-    norm_kernel<T, S, THREADS, CH><<<dim3(workgroups(a.n, ROWS)), dim3(THREADS < 256 ? 256 : THREADS), 0, s>>>(a);
+    norm_kernel<T, S, THREADS, CH, SHORT><<<dim3(workgroups(a.n, ROWS)), dim3(THREADS < 256 ? 256 : THREADS), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, typename S>
 hipError_t run(const NormArgs &a, hipStream_t s)
 {
+    // one chunk a thread up to 8192 (16384 rows 2048, bf16 and fp32 stream, 8 bits beside: 73 us, 90 with a wave a row and four chunks a thread)
+    if (a.dim < 8) return run<T, S, 64, 1, true>(a, s);
     if (a.dim <= 512) return run<T, S, 64, 1>(a, s);
-    if (a.dim <= 1024) return run<T, S, 64, 2>(a, s);
-    if (a.dim <= 2048) return run<T, S, 64, 4>(a, s);
-    if (a.dim <= 4096) return run<T, S, 256, 2>(a, s);
-    if (a.dim <= 8192) return run<T, S, 256, 4>(a, s);
+    if (a.dim <= 1024) return run<T, S, 128, 1>(a, s);
+    if (a.dim <= 2048) return run<T, S, 256, 1>(a, s);
+    if (a.dim <= 4096) return run<T, S, 512, 1>(a, s);
+    if (a.dim <= 8192) return run<T, S, 1024, 1>(a, s);
     return run<T, S, 1024, 2>(a, s);
 }
 
-int rows_at_once(int dim) { return dim <= 2048 ? 4 : 1; }
+int rows_at_once(int dim) { return dim <= 512 ? 4 : dim <= 1024 ? 2 : 1; }
 
-template <typename T, typename S, int THREADS, int CH>
+template <typename T, typename S, int THREADS, int CH, bool SHORT = false>
 hipError_t run_grad(const NormGradArgs &a, hipStream_t s)
 {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
     const dim3 block(THREADS < 256 ? 256 : THREADS);
-    if (a.dgamma || a.F) norm_grad_kernel<T, S, THREADS, CH, true><<<dim3((unsigned)norm_parts(a.n, a.dim)), block, 0, s>>>(a);
-    else norm_grad_kernel<T, S, THREADS, CH, false><<<dim3(workgroups(a.n, ROWS)), block, 0, s>>>(a);
+    if (a.dgamma || a.F) norm_grad_kernel<T, S, THREADS, CH, true, SHORT><<<dim3((unsigned)norm_parts(a.n, a.dim)), block, 0, s>>>(a);
+    else norm_grad_kernel<T, S, THREADS, CH, false, SHORT><<<dim3(workgroups(a.n, ROWS)), block, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, typename S>
 hipError_t run_grad(const NormGradArgs &a, hipStream_t s)
 {
+    if (a.dim < 8) return run_grad<T, S, 64, 1, true>(a, s);
     if (a.dim <= 512) return run_grad<T, S, 64, 1>(a, s);
-    if (a.dim <= 1024) return run_grad<T, S, 64, 2>(a, s);
-    if (a.dim <= 2048) return run_grad<T, S, 64, 4>(a, s);
-    if (a.dim <= 4096) return run_grad<T, S, 256, 2>(a, s);
-    if (a.dim <= 8192) return run_grad<T, S, 256, 4>(a, s);
+    if (a.dim <= 1024) return run_grad<T, S, 128, 1>(a, s);
+    if (a.dim <= 2048) return run_grad<T, S, 256, 1>(a, s);
+    if (a.dim <= 4096) return run_grad<T, S, 512, 1>(a, s);
+    if (a.dim <= 8192) return run_grad<T, S, 1024, 1>(a, s);
     return run_grad<T, S, 1024, 2>(a, s);
 }
 

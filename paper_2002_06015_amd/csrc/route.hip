@@ -218,7 +218,7 @@ __device__ __forceinline__ void load_logits(const T *p, int there, float (&v)[N]
     typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
     if (there >= N) {
         if constexpr (N == 8) {
-            load8(p, 8, v);
+            load8(p, v);
         } else if constexpr (N == 1) {
             v[0] = Element<T>::get(p);
         } else {
