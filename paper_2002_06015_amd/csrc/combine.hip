@@ -12,13 +12,15 @@ namespace kfac {
 
 namespace {
 
-// A thread: eight elements of a token's row.
-template <typename T, typename S, bool SHORT>
-__global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsigned per_row, unsigned long long units)
+// 2^log threads a token (workgroups of 256: several tokens, or a token in several steps), eight elements a thread, FAN choices' rows in flight
+// (EXACT: a token has as many).
+template <typename T, typename S, int FAN, bool EXACT, bool SHORT>
+__global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, int log)
 {
-    for (unsigned long long u = (unsigned long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (unsigned long long)gridDim.x * 256) {
-        const long long token = (long long)(u / per_row);
-        const int c = 8 * (int)(u - token * per_row), there = a.dim - c;
+    const long long stripe = (long long)gridDim.x << (8 - log);
+    for (long long token = ((long long)blockIdx.x << (8 - log)) + (threadIdx.x >> log); token < a.tokens; token += stripe)
+      for (int c = 8 * (int)(threadIdx.x & ((1 << log) - 1)); c < a.dim; c += 8 << log) {
+        const int there = a.dim - c;
         float sum[8], v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum[q] = 0.f;
@@ -26,18 +28,18 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsig
         const float *gate = a.gate + token * a.fan;
         Raw8<S> res;
         if (a.r) res.template load<SHORT>((const S *)a.r + token * a.ldr, c, a.dim);
-        for (int j0 = 0; j0 < a.fan; j0 += 4) {   // four rows in flight
-            Raw8<T> raw[4];
-            float g[4];
+        for (int j0 = 0; j0 < (EXACT ? FAN : a.fan); j0 += FAN) {
+            Raw8<T> raw[FAN];
+            float g[FAN];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j0 + j < a.fan) {
+            for (int j = 0; j < FAN; ++j)
+                if (EXACT || j0 + j < a.fan) {
                     raw[j].template load<SHORT>(y + (j0 + j) * a.ldy, c, a.dim);
                     g[j] = a.gate ? gate[j0 + j] : 1.f;
                 }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j0 + j < a.fan) {
+            for (int j = 0; j < FAN; ++j)
+                if (EXACT || j0 + j < a.fan) {
                     raw[j].get(v);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) sum[q] = fmaf(g[j], v[q], sum[q]);
@@ -52,7 +54,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, unsig
     }
 }
 
-// THREADS threads for FAN choices of a token.
+// THREADS threads for FAN choices of a token, whose rows are in flight together (four of them: 2051 x 4 x 1001 fp32 18 us instead of 15).
 template <typename T, typename S, int THREADS, int FAN, bool SHORT>
 __global__ __launch_bounds__(256) void combine_grad_kernel(const CombineArgs a)
 {
@@ -119,11 +121,14 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(const CombineArgs a)
 template <typename T, typename S>
 hipError_t run(const CombineArgs &a, hipStream_t s)
 {
-    const unsigned per_row = (unsigned)(a.dim + 7) / 8;
-    const unsigned long long units = (unsigned long long)a.tokens * per_row, wgs = (units + 255) / 256;
-    const dim3 grid((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)));
-    if (a.dim < 8) combine_kernel<T, S, true><<<grid, dim3(256), 0, s>>>(a, per_row, units);
-    else combine_kernel<T, S, false><<<grid, dim3(256), 0, s>>>(a, per_row, units);
+    int log = 0;
+    while (log < 8 && (8 << log) < a.dim) ++log;
+    const long long wgs = ((long long)a.tokens + (256 >> log) - 1) >> (8 - log);
+    const dim3 grid((unsigned)std::min(wgs, 1LL << 20));   // a launch takes less than 2^32 threads
+    if (a.dim < 8) combine_kernel<T, S, 1, false, true><<<grid, dim3(256), 0, s>>>(a, log);
+    else if (a.fan == 1) combine_kernel<T, S, 1, true, false><<<grid, dim3(256), 0, s>>>(a, log);
+    else if (a.fan == 2) combine_kernel<T, S, 2, true, false><<<grid, dim3(256), 0, s>>>(a, log);
+    else combine_kernel<T, S, 4, false, false><<<grid, dim3(256), 0, s>>>(a, log);
     return hipGetLastError();
 }
 
@@ -131,11 +136,10 @@ template <typename T, typename S, int THREADS, bool SHORT>
 hipError_t run_grad(const CombineArgs &a, hipStream_t s)
 {
     constexpr int per = 256 / THREADS;
-    const long long sets = (long long)a.tokens * (a.fan <= 2 ? 1 : (a.fan + 3) / 4);
+    const long long sets = (long long)a.tokens * ((a.fan + 1) / 2);
     const dim3 grid((unsigned)std::min((sets + per - 1) / per, 1LL << 20)), block(256);   // a launch takes less than 2^32 threads
     if (a.fan <= 1) combine_grad_kernel<T, S, THREADS, 1, SHORT><<<grid, block, 0, s>>>(a);
-    else if (a.fan <= 2) combine_grad_kernel<T, S, THREADS, 2, SHORT><<<grid, block, 0, s>>>(a);
-    else combine_grad_kernel<T, S, THREADS, 4, SHORT><<<grid, block, 0, s>>>(a);
+    else combine_grad_kernel<T, S, THREADS, 2, SHORT><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -143,7 +147,10 @@ template <typename T, typename S>
 hipError_t run_grad(const CombineArgs &a, hipStream_t s)
 {
     if (a.dim < 8) return run_grad<T, S, 64, true>(a, s);
-    return a.tokens >= 4096 || a.dim <= 512 ? run_grad<T, S, 64, false>(a, s) : run_grad<T, S, 256, false>(a, s);
+    // A wave for a pair of choices where it has two steps at most and there are enough (2051 x 4 x 1001 fp32: 15 us, 19 with a workgroup; 20000 x 1
+    // x 512: 14 and 20), otherwise a workgroup (32768 x 2 x 2048 bf16: 116 us, 122 with a wave; 1024 x 2 x 4096: 8 and 11).
+    const long long sets = (long long)a.tokens * ((a.fan + 1) / 2);
+    return a.dim <= 512 || (a.dim <= 1024 && sets >= 4096) ? run_grad<T, S, 64, false>(a, s) : run_grad<T, S, 256, false>(a, s);
 }
 
 }  // namespace
