@@ -1,12 +1,15 @@
 """A small token model trained with the natural gradient: embedding, dropout, experts with a residual, a read-out layer.
 
-    python examples/token_experts.py [--steps 30] [--dtype bf16]
+    python examples/token_experts.py [--steps 30] [--dtype bf16] [--norm] [--kept]
 
 The model learns a fixed map from tokens to tokens.  Every row h of the dropped-out embedding goes to two of the experts, chosen by
 a fixed random projection, z = h + sum_j gate_j W_{e_j} h, and the read-out layer scores the classes.  Each layer has Kronecker
 factors of its inputs and of the gradients at its outputs: the embedding a diagonal A (token frequencies) and a dense G, an expert
-those of the rows that it received, the read-out those of a fully-connected layer.  The library does everything that touches the
-embedding, the experts and the factors; the read-out's products, the softmax and the routing scores are torch's.
+those of the rows that it received, the read-out those of a fully-connected layer.  With --norm the experts and the projection see the
+root-mean-square norm of h, the projection is trained as a fully-connected layer and the norm's scale with the diagonal of its Fisher
+matrix; with --kept the experts' inputs are held in 8 bits for their gradients and factors.  The library does everything that
+touches the embedding, the routing, the experts, the norm and the factors; the products of the read-out and of the projection and the
+softmax are torch's.
 """
 from __future__ import annotations
 
@@ -20,14 +23,16 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2002_06015_amd import kfac, workloads as wl  # noqa: E402
 
 FAN = 2
+EPS = 1e-5
 
 
 class Model:
-    def __init__(self, vocab=512, dim=64, experts=8, classes=512, tokens=4096, dtype=torch.float32, p=0.1, seed=0):
+    def __init__(self, vocab=512, dim=64, experts=8, classes=512, tokens=4096, dtype=torch.float32, p=0.1, seed=0, norm=False, kept=False):
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
         self.gen, self.vocab, self.dim, self.experts, self.classes, self.tokens = g, vocab, dim, experts, classes, tokens
         self.dtype, self.p, self.seed, self.step_no, self.scale = dtype, p, seed, 0, dim ** 0.5
+        self.norm, self.kept = norm, kept
         new = dict(device="cuda")
         n = tokens * FAN
         self.expert_layer, self.out_layer = wl.fc_layer(1, dim, dim, 0), wl.fc_layer(tokens, dim, classes, 0)
@@ -35,9 +40,10 @@ class Model:
         self.table_g, self.table_layer = wl.fc_layer(tokens, 1, dim, 0), wl.fc_layer(1, dim, vocab, 0)
         rand = lambda *s: torch.randn(*s, generator=g, **new)  # noqa: E731
         self.table, self.W, self.Wout = rand(vocab, dim) / self.scale, rand(experts, dim, dim) * 0.5 / self.scale, rand(classes, dim) / self.scale
-        self.router = rand(dim, experts)
+        self.router = rand(dim, experts).t().contiguous()       # [experts, dim]
+        self.gamma, self.route = torch.ones(dim, **new), kfac.router(experts, FAN)
         self.target_of = torch.randperm(max(vocab, classes), generator=g, **new)[:vocab] % classes
-        self.previous = [w.clone() for w in (self.table, self.W, self.Wout)]
+        self.previous = [w.clone() for w in (self.table, self.W, self.Wout, self.router)]
         # running averages and inverses
         self.A_table = torch.zeros(vocab, **new)
         self.A = [torch.zeros(experts, dim, dim, **new), torch.zeros(dim, dim, **new), torch.zeros(1, 1, **new)]
@@ -52,40 +58,70 @@ class Model:
         self.dtable, self.dW = torch.empty(vocab, dim, **new), torch.empty(experts, dim, dim, **new)
         self.order, self.offsets = torch.empty(n, dtype=torch.int32, **new), torch.empty(experts + 1, dtype=torch.int32, **new)
         self.all_rows = torch.tensor([0, vocab], dtype=torch.int32, **new)
+        self.choice, self.gate = torch.empty(n, dtype=torch.int32, **new), torch.empty(tokens, FAN, **new)
+        self.z, self.dh, self.dgate = torch.empty(tokens, dim, **new), torch.empty(tokens, dim, **new), torch.empty(tokens, FAN, **new)
         self.layers = [self.expert_layer] * experts + [self.out_layer, self.table_g]
+        # the norm, its scale's gradient and Fisher diagonal; the projection as a layer; inputs in 8 bits
+        self.hn, self.u = torch.empty(tokens, dim, dtype=dtype, **new), self.h
+        self.dgamma, self.F, self.dscore = torch.empty(dim, **new), torch.zeros(dim, **new), torch.empty(tokens, experts, **new)
+        self.q, self.scales = torch.empty(tokens, dim, dtype=torch.float8_e4m3fn, **new), torch.empty(tokens, (dim + 31) // 32, dtype=torch.uint8, **new)
+        self.route_layer = wl.fc_layer(tokens, dim, experts, 0)
+        self.A_route, self.G_route = torch.zeros(dim, dim, **new), torch.zeros(experts, experts, **new)
+        self.Ai_route, self.Gi_route = torch.zeros_like(self.A_route), torch.zeros_like(self.G_route)
         need = max(kfac.kfac_workspace_bytes(self.layers), kfac.kfac_workspace_bytes([self.out_layer, self.table_layer]),
                    kfac.kfac_embedding_workspace_bytes(tokens, vocab, dim), kfac.kfac_segments_workspace_bytes(n, experts),
-                   kfac.kfac_expert_workspace_bytes(self.expert_layer, experts, n))
+                   kfac.kfac_expert_workspace_bytes(self.expert_layer, experts, n), kfac.kfac_workspace_bytes([self.route_layer]),
+                   kfac.kfac_rms_norm_workspace_bytes(tokens, dim), kfac.kfac_kept_workspace_bytes(self.expert_layer, experts, n, FAN))
         self.ctx = kfac.Context([self.expert_layer], workspace_bytes=need)
 
     def forward(self, ids):
         """The classes' scores [tokens, classes]."""
         kfac.kfac_embedding(self.ctx, ids, self.table, self.scale, self.x0)
         kfac.kfac_dropout(self.ctx, self.x0, self.p, self.seed, self.step_no, self.h)
-        score = self.h.float() @ self.router
-        best = score.topk(FAN, dim=1)
-        self.gate, self.choice = best.values.softmax(1), best.indices.to(torch.int32).reshape(-1)
+        if self.norm:
+            kfac.kfac_rms_norm(self.ctx, self.h, self.gamma, EPS, self.hn, q=self.q if self.kept else None, scales=self.scales if self.kept else None)
+            self.u = self.hn
+        elif self.kept:
+            kfac.kfac_keep(self.ctx, self.h, self.q, self.scales)
+        self.score = self.u.float() @ self.router.T
+        kfac.kfac_route(self.ctx, self.route, self.score, self.choice, self.gate)
         kfac.kfac_segments(self.ctx, self.choice, self.experts, self.order, self.offsets)
         self.Wd = self.W.to(self.dtype)
-        kfac.kfac_expert_forward(self.ctx, self.expert_layer, self.order, self.offsets, self.h, self.Wd, self.y, fan=FAN)
-        self.z = self.h.float() + (self.gate[:, :, None] * self.y.float().view(self.tokens, FAN, self.dim)).sum(1)
+        kfac.kfac_expert_forward(self.ctx, self.expert_layer, self.order, self.offsets, self.u, self.Wd, self.y, fan=FAN)
+        kfac.kfac_combine(self.ctx, self.y, self.gate, self.z, residual=self.h.float())
         return self.z @ self.Wout.T
 
     def backward(self, ids, dlogits):
         """Gradients of the table, the experts and the read-out from those of every token's loss at its scores, summed over tokens."""
         dz = dlogits @ self.Wout
         self.dWout = dlogits.T @ self.z
-        self.dy.copy_((self.gate[:, :, None] * dz[:, None, :]).view(-1, self.dim))
+        kfac.kfac_combine_grad(self.ctx, self.y, self.gate, dz, self.dy, self.dgate if self.norm else None)
         kfac.kfac_expert_grad_input(self.ctx, self.expert_layer, self.order, self.offsets, self.dy, self.Wd, self.dx)
-        kfac.kfac_expert_grad_weight(self.ctx, self.expert_layer, self.order, self.offsets, self.h, self.dy, self.dW, fan=FAN)
-        dh = (dz + self.dx.float().view(self.tokens, FAN, self.dim).sum(1)).to(self.dtype)
+        if self.kept:
+            kfac.kfac_expert_grad_weight_kept(self.ctx, self.expert_layer, self.order, self.offsets, self.q, self.scales, self.dy, self.dW, fan=FAN)
+        else:
+            kfac.kfac_expert_grad_weight(self.ctx, self.expert_layer, self.order, self.offsets, self.u, self.dy, self.dW, fan=FAN)
+        if self.norm:
+            kfac.kfac_route_grad(self.ctx, self.route, self.score, self.choice, self.dgate, self.dscore)
+            self.drouter = self.dscore.T @ self.u.float()
+            kfac.kfac_combine(self.ctx, self.dx, None, self.dh, residual=self.dscore @ self.router)
+            du, dh, decay = self.dh.to(self.dtype), dz.to(self.dtype), 0.0 if self.step_no == 0 else 0.95
+            kfac.kfac_rms_norm_grad(self.ctx, du, self.h, self.gamma, EPS, dh, dstream=dh, dgamma=self.dgamma, F=self.F, decay=decay)
+        else:
+            kfac.kfac_combine(self.ctx, self.dx, None, self.dh, residual=dz)
+            dh = self.dh.to(self.dtype)
         kfac.kfac_dropout(self.ctx, dh, self.p, self.seed, self.step_no, self.dx0)
         decay = 0.0 if self.step_no == 0 else 0.95
         kfac.kfac_embedding_grad(self.ctx, ids, self.dx0, self.scale, self.dtable, A_diag=self.A_table, decay=decay)
         return decay
 
     def statistics(self, dlogits, decay):
-        kfac.kfac_stats_expert(self.ctx, self.expert_layer, self.order, self.offsets, self.h, self.dy, decay, self.A[0], self.G[0], fan=FAN)
+        if self.kept:
+            kfac.kfac_stats_expert_kept(self.ctx, self.expert_layer, self.order, self.offsets, self.q, self.scales, self.dy, decay, self.A[0], self.G[0], fan=FAN)
+        else:
+            kfac.kfac_stats_expert(self.ctx, self.expert_layer, self.order, self.offsets, self.u, self.dy, decay, self.A[0], self.G[0], fan=FAN)
+        if self.norm:
+            kfac.kfac_stats(self.ctx, [self.route_layer], kfac.KFAC_F32, [self.u.float()], [self.dscore], decay, False, [self.A_route], [self.G_route])
         kfac.kfac_stats(self.ctx, [self.out_layer, self.table_g], kfac.KFAC_F32, [self.z, None], [dlogits, self.dx0.float() * self.scale], decay, False,
                         [self.A[1], None], [self.G[1], self.G[2]])
         self.A[2].copy_(self.A_table.mean().view(1, 1))      # the mean of the diagonal: what the split of the damping asks of A
@@ -113,6 +149,12 @@ class Model:
         kfac.kfac_expert_forward(c, self.expert_layer, None, self.all_rows, rows, self.Gi[2][None], U_table)
         kfac.kfac_update_weights(c, self.layers[:E] + [self.out_layer, self.table_layer], U + [U_table], eta, momentum, False, 0.0,
                                  list(self.W) + [self.Wout, self.table], list(self.previous[1]) + [self.previous[2], self.previous[0]])
+        if self.norm:   # the projection as a layer, the scale over the diagonal of its Fisher matrix
+            kfac.kfac_invert(c, [self.route_layer], [self.A_route], [self.G_route], gamma, [self.Ai_route], [self.Gi_route])
+            U = [torch.empty_like(self.router)]
+            kfac.kfac_precondition(c, [self.route_layer], [self.Gi_route], [self.Ai_route], [self.drouter / self.tokens], U)
+            kfac.kfac_update_weights(c, [self.route_layer], U, eta, momentum, False, 0.0, [self.router], [self.previous[3]])
+            self.gamma -= eta * (self.dgamma / self.tokens) / (self.F + gamma * gamma)
         self.step_no += 1
         return loss
 
@@ -131,6 +173,8 @@ if __name__ == "__main__":
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=30)
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="bf16")
+    ap.add_argument("--norm", action="store_true")
+    ap.add_argument("--kept", action="store_true")
     a = ap.parse_args()
-    for i, v in enumerate(train(a.steps, dtype=torch.float32 if a.dtype == "f32" else torch.bfloat16)):
+    for i, v in enumerate(train(a.steps, dtype=torch.float32 if a.dtype == "f32" else torch.bfloat16, norm=a.norm, kept=a.kept)):
         print("step %3d  loss %.4f" % (i, v))
