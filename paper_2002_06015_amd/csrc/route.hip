@@ -209,9 +209,12 @@ __global__ __launch_bounds__(256) void route_general_kernel(const RouteArgs a)
 // Lane i holds the `per` experts from i per on.  Ranks are formed in fp32 and brought into [1, 2); the bits of the fraction, with the
 // experts' numbers from behind below them, are keys that all differ, and the largest is the choice.  The best one below M is M + max(key - M)
 // in wrapping arithmetic: an element costs a subtraction and half a maximum in each round.  Where two neighbours among the chosen are
-// nearer than the error of their ranks, and not exactly equal, the chosen ones are ranked in 64 bits; where the last of them and others are, or
-// groups, or ranks are not finite, the wave does the token again in 64 bits.  Groups need to be whole lanes.
-// 65536 tokens 256 experts bf16, sigmoids, a bias, 4 of 8 groups, fan 8: see the launch.
+// nearer than the error of their ranks, and not exactly equal, the chosen ones are ranked in 64 bits, together with the first that is no choice if
+// that one alone is as near to the last; where more are, or groups, or ranks are not finite, the wave does the token again in 64 bits (11 us for
+// one token, much of it code that no cache holds yet; without the rank of the first that is no choice a launch that ends with such a token
+// took 47 us instead of 40).  Groups need to be whole lanes.
+// Bound by its vector instructions: 65536 tokens, 256 experts, bf16, fan 8: sigmoids with a bias and the best 4 of 8 groups 39 us, softmax alone
+// 27 us, for 34 MB of logits.  A workgroup is one wave: 32768 tokens, 512 experts 48 us, 52 with four.
 template <typename T, int N>
 __device__ __forceinline__ void load_logits(const T *p, int there, float (&v)[N])
 {
@@ -262,12 +265,12 @@ __device__ __forceinline__ void store_logits(T *p, int there, const float (&v)[N
 }
 
 template <typename T, int LANES, int EPL>
-__global__ __launch_bounds__(256, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route_kernel(const RouteArgs a, int per, int group_lanes)
+__global__ __launch_bounds__(64, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route_kernel(const RouteArgs a, int per, int group_lanes)
 {
     constexpr int ALL = LANES * EPL, IB = ALL <= 16 ? 4 : ALL <= 32 ? 5 : ALL <= 64 ? 6 : ALL <= 128 ? 7 : ALL <= 256 ? 8 : ALL <= 512 ? 9 : 10;
-    constexpr int ROWS = 256 / LANES, N = EPL < 8 ? EPL : 8;
-    __shared__ double ranks[4][ALL], of_groups[4][LANES];   // (as many groups as lanes at most)
-    __shared__ unsigned char opened[4][LANES];
+    constexpr int ROWS = 64 / LANES, N = EPL < 8 ? EPL : 8;
+    __shared__ double ranks[1][ALL], of_groups[1][LANES];   // (as many groups as lanes at most)
+    __shared__ unsigned char opened[1][LANES];
     const int lane = threadIdx.x & 63, sub = lane & (LANES - 1), first = sub * per;
     const bool sums = a.groups > 1 && a.group_best > 1, by_score = a.bias || sums;
     for (long long base = (long long)blockIdx.x * ROWS; base < a.n; base += (long long)gridDim.x * ROWS) {
@@ -399,19 +402,26 @@ __global__ __launch_bounds__(256, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void rout
         const bool close = open && sub < a.fan && (mine >> IB) - (next >> IB) <= margin;
         const unsigned long long lanes_of_row = (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1) << (lane - sub);
         const unsigned long long edges = __ballot(close && sub == a.fan - 1);
-        if (edges) {   // the last choice and the first that is none: whatever is as near as that has to be equal
+        bool swaps = false;   // the first that is no choice may belong among them
+        if (edges) {   // the last choice and the first that is none: whatever is as near as that is equal, or that one is alone
             const int last = lane - sub + a.fan - 1;
-            const unsigned edge = __shfl(mine, last) >> IB;
+            const unsigned edge = __shfl(mine, last), after = __shfl(next, last);
             const float l0 = __shfl(chosen, last), b0 = __shfl(added, last);
+            bool differs = false, others = after - one < 1u << IB;   // (that one is closed)
 #pragma unroll
             for (int i = 0; i < EPL; ++i)
-                if ((edges & lanes_of_row) && (key[i] >> IB) - edge + margin <= 2 * margin) {
+                if ((edges & lanes_of_row) && (key[i] >> IB) - (edge >> IB) + margin <= 2 * margin) {
                     const bool in = i < there;
-                    again |= !in || Element<T>::get(logits + (in ? first + i : 0)) != l0 || (a.bias && a.bias[in ? first + i : 0] != b0);
+                    differs |= !in || Element<T>::get(logits + (in ? first + i : 0)) != l0 || (a.bias && a.bias[in ? first + i : 0] != b0);
+                    others |= key[i] - one < after - one;
                 }
+            differs = (__ballot(differs) & lanes_of_row) != 0;
+            others = (__ballot(others) & lanes_of_row) != 0;
+            again |= differs && others;
+            swaps = differs && !others;
         }
         int place = sub;
-        if (__ballot(close && sub < a.fan - 1 && !equal)) {   // the chosen ones in 64 bits, their places counted
+        if (__ballot((close && sub < a.fan - 1 && !equal) || swaps)) {   // the chosen ones in 64 bits, their places counted
             double rank = chosen;
             if (error > 0.f) {
                 double all = 1.0;
@@ -428,12 +438,13 @@ __global__ __launch_bounds__(256, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void rout
                 rank = (a.sigmoid ? 1.0 / (1.0 + x) : x / all) + (double)added;
             }
             int better = 0;
-            for (int q = 0; q < a.fan; ++q) {
+            const int ranked = a.fan + (swaps ? 1 : 0);
+            for (int q = 0; q <= a.fan; ++q) {
                 const double r = __shfl(rank, lane - sub + q);
                 const int number = __shfl(e, lane - sub + q);
-                better += r > rank || (r == rank && number < e) ? 1 : 0;
+                better += q < ranked && (r > rank || (r == rank && number < e)) ? 1 : 0;
             }
-            if (sub < a.fan) place = better;
+            if (sub < ranked) place = better;
         }
         const unsigned long long rows = __ballot(again);
         const bool mine_again = (rows & lanes_of_row) != 0;
@@ -457,7 +468,8 @@ __global__ __launch_bounds__(256, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void rout
 // ---- gradient -------------------------------------------------------------------------------------------
 // LANES lanes a token; lane i < fan works on choice i, then every lane on chunks of N adjacent experts.  A row of zeros with the
 // choices' parts in their places is put together in LDS (an expert that is there twice gets the sum in the order of the choices).
-// Bound by memory and the launch: see there.
+// Bound by memory: 65536 tokens, 256 experts, bf16, renormalised: 15.7 us for the 34 MB that it writes and the lines of the chosen logits (55
+// before rows were put together in LDS).
 template <typename T, int LANES, int EPL>
 __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a)
 {
@@ -544,13 +556,15 @@ dim3 workgroups(int n, int rows, int most = 1 << 20) { return dim3((unsigned)min
 template <typename T, int LANES, int EPL>
 hipError_t run(const RouteArgs &a, hipStream_t s)
 {
-    route_kernel<T, LANES, EPL><<<workgroups(a.n, 256 / LANES), dim3(256), 0, s>>>(a, (a.experts + LANES - 1) / LANES, LANES / a.groups);
+    route_kernel<T, LANES, EPL><<<workgroups(a.n, 64 / LANES), dim3(64), 0, s>>>(a, (a.experts + LANES - 1) / LANES, LANES / a.groups);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t run(const RouteArgs &a, hipStream_t s)
 {
+    // sixteen lanes as far as sixteen experts a lane stay in registers: four tokens share the wave's moves between lanes (65536 tokens
+    // of 256 experts 39 and 27 us, a token a wave 76 and 52)
     const int lanes = a.experts <= 256 ? 16 : 64, per = (a.experts + lanes - 1) / lanes;
     if (a.fan >= lanes || (a.groups > 1 && (lanes % a.groups || a.experts % lanes))) {
         route_general_kernel<T><<<workgroups(a.n, 4), dim3(256), 0, s>>>(a);

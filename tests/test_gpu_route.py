@@ -231,3 +231,28 @@ def test_closed_by_the_lowest_value_of_the_type(ctx, scores):
         logits[1, 3:] = -np.finfo(np.float32).max
         _run(ctx, logits, None, rng.standard_normal((80, 4)), F32, 0, scores=scores, fan=4, renormalise=scores == 0)
         _run(ctx, logits, 0.1 * rng.standard_normal(E), rng.standard_normal((80, 4)), F32, 0, scores=scores, fan=4, groups=4, top_groups=2, group_best=2)
+
+
+@pytest.mark.parametrize("scores", [0, 1])
+@pytest.mark.parametrize("E", [16, 60, 256, 512])
+@pytest.mark.parametrize("near", [2, 3, 5])
+def test_near_ranks_around_the_last_choice(ctx, near, E, scores):
+    """`near` experts whose ranks differ by less than fp32 resolves, by the rounding of a bias, with the last choice at every place among them: the
+    first expert that is no choice takes the place of any choice that it beats in 64 bits; a closed one never does."""
+    rng = np.random.default_rng(17 * near + E + scores)
+    n = 90
+    row = rng.standard_normal(E)
+    top = rng.permutation(E)[:near + 3]                             # three clearly above, then the near ones
+    row[top[:3]], row[top[3:]] = 3.0, 2.0 + 0.25 * rng.random(near)
+    row = row.astype(np.float32).astype(np.float64)
+    s = 1 / (1 + np.exp(-row)) if scores else np.exp(row - row.max()) / np.exp(row - row.max()).sum()
+    bias = np.zeros(E)
+    bias[top[:3]] = [2.0, 1.5, 1.0]
+    bias[top[3:]] = 0.75 + s[top[3]] - s[top[3:]]                   # what fp32 keeps of it decides
+    bias[[e for e in range(E) if e not in set(top)]] = -0.5
+    logits = np.tile(row, (n, 1))
+    logits[n // 3:, :] = np.where(np.isin(np.arange(E), top[:3]), logits[n // 3:, :], logits[n // 3:, :] + rng.integers(-2, 3, (n - n // 3, E)) * 2.0 ** -22)
+    logits[-1, top[4:]] = -INF                                      # the neighbours of the last choice are closed
+    for fan in range(3, min(E, near + 4)):
+        for renormalise in (True, False):
+            _run(ctx, logits, bias, rng.standard_normal((n, fan)), F32, 0, scores=scores, fan=fan, renormalise=renormalise)
