@@ -634,7 +634,8 @@ kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t e
  *             stream_type is `type`
  *   y[t, c] = gamma[c] h[t, c] / sqrt(mean_c h[t, c]^2 + eps)
  * x: dev [n, dim] of `type`; residual, h: dev [n, dim] of stream_type; gamma: dev [dim] fp32; y: dev [n, dim] of `type`, or NULL;
- * q, scales: y (before its rounding to `type`) in 8 bits as by kfac_keep, or both NULL; at least one of y and q.  Sums in fp32.
+ * q, scales: y (before its rounding to `type`) in 8 bits as by kfac_keep, or both NULL; at least one of y and q.  Sums in fp32 (a finite
+ * row whose sum of squares leaves its range, from magnitudes of 1.8e19 / sqrt(dim) on, has zeros for y).
  * h may be residual itself, and x if the types agree; y may be x if it is not h (same rows each).
  */
 kfac_status kfac_rms_norm(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type, const void *x, int64_t ldx, kfac_dtype stream_type,

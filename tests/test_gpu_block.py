@@ -236,3 +236,59 @@ def test_profile_names_the_launches():
     for want in (("norm", 0), ("route", 0), ("combine", 0), ("combine", 1), ("route", 1), ("expert", 2), ("expert", 3), ("norm", 1), ("norm", 2)):
         assert want in seen, want
     assert np.isfinite([b.dh.abs().max().item()]).all()
+
+
+@pytest.mark.parametrize("typ", [F32, BF16], ids=["f32", "bf16"])
+def test_padded_batch(typ):
+    """Tokens whose logits are all -infinity, in the middle, as whole runs and at the end: their rows are the residual's alone, and the experts' gradients
+    and factors are those of the batch without them (sums in fp32 of at most `rows` terms in two orders: rows 2^-23 of the sum of magnitudes)."""
+    T, dim, E, fan = 190, 72, 5, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    pad = torch.zeros(T, dtype=torch.bool, device="cuda")
+    pad[7], pad[50:90], pad[150:] = True, True, True
+    h, logits, dout, W = rand(T, dim).to(typ), rand(T, E), rand(T, dim).to(typ), (rand(E, dim, dim) / 8).to(typ)
+    logits[pad] = -float("inf")
+    layer, router = wl.fc_layer(1, dim, dim, 0), kfac.router(E, fan)
+    got = []
+    for rows in (slice(None), ~pad):
+        x, l, d = h[rows].contiguous(), logits[rows].contiguous(), dout[rows].contiguous()
+        t = len(x)
+        n = t * fan
+        new = lambda *s, dtype=F32: torch.full(s, 7, dtype=dtype, device="cuda")  # noqa: E731
+        need = max(kfac.kfac_segments_workspace_bytes(n, E), kfac.kfac_expert_workspace_bytes(layer, E, n), kfac.kfac_kept_workspace_bytes(layer, E, n, fan))
+        c = kfac.Context([layer], workspace_bytes=need)
+        q, s = torch.empty(t, dim, dtype=E4M3, device="cuda"), new(t, (dim + 31) // 32, dtype=torch.uint8)
+        choice, gate, order, offsets = new(n, dtype=torch.int32), new(t, fan), new(n, dtype=torch.int32), new(E + 1, dtype=torch.int32)
+        y, out, dy, dgate, dl, dx = new(n, dim, dtype=typ), new(t, dim, dtype=typ), new(n, dim, dtype=typ), new(t, fan), new(t, E), new(n, dim, dtype=typ)
+        dW, A, G = new(E, dim, dim), new(E, dim, dim), new(E, dim, dim)
+        kfac.kfac_keep(c, x, q, s)
+        kfac.kfac_route(c, router, l, choice, gate)
+        kfac.kfac_segments(c, choice, E, order, offsets)
+        kfac.kfac_expert_forward(c, layer, order, offsets, x, W, y, fan=fan)
+        kfac.kfac_combine(c, y, gate, out, residual=x)
+        kfac.kfac_combine_grad(c, y, gate, d, dy, dgate)
+        kfac.kfac_route_grad(c, router, l, choice, dgate, dl)
+        kfac.kfac_expert_grad_input(c, layer, order, offsets, dy, W, dx)
+        kfac.kfac_expert_grad_weight_kept(c, layer, order, offsets, q, s, dy, dW, fan=fan)
+        kfac.kfac_stats_expert_kept(c, layer, order, offsets, q, s, dy, 0.0, A, G, fan=fan)
+        values = new(t, dim)
+        kfac.kfac_restore(c, q, s, values)
+        torch.cuda.synchronize()
+        got.append(dict(choice=choice.view(t, fan), gate=gate, out=out, dgate=dgate, dl=dl, dx=dx.view(t, fan, dim), y=y.view(t, fan, dim), dy=dy.view(t, fan, dim),
+                        dW=dW, A=A, G=G, values=values, offsets=offsets))
+        c.close()
+    whole, real = got
+    assert bool((whole["choice"][pad] == -1).all()) and torch.equal(whole["offsets"], real["offsets"])
+    assert torch.equal(whole["out"][pad], h[pad])
+    for name in ("gate", "y", "dy", "dgate", "dl", "dx"):
+        assert bool((whole[name][pad] == 0).all()), name
+    for name in ("choice", "gate", "dy"):
+        assert torch.equal(whole[name][~pad], real[name]), name
+    e = real["choice"].long()
+    for i in range(E):
+        at, j = (e == i).nonzero(as_tuple=True)
+        v, d = real["values"][at].abs().double(), real["dy"][at, j].abs().double()
+        for name, mag in (("dW", d.t() @ v), ("A", v.t() @ v / len(at)), ("G", d.t() @ d / len(at))):
+            assert bool(((whole[name][i].double() - real[name][i].double()).abs() <= len(at) * 2.0 ** -23 * mag + 1e-30).all()), (name, i)
