@@ -766,6 +766,14 @@ __device__ __forceinline__ floatx16 mfma32(const bf16x8 &j, const bf16x8 &i, con
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(j, i, c, 0, 0, 0);
 }
 
+// c and the two bf16 values of a register, in fp32: one instruction instead of four (factors of 32768 rows in 16 experts 75.4 -> 73.2 us);
+// its roundings stay below 3 x 2^-24 of the largest, and sums of 4096 values in a row were off by as much as one by one.
+__device__ __forceinline__ float add_pair(unsigned pair, float c)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), c, false);
+}
+
 template <bool ACROSS, int GATHER, int ROWS, int THREADS>
 struct Direct {
     static constexpr int CH = ROWS * 4 / THREADS, PER = ACROSS ? ROWS / 8 : 4;   // chunks a thread and half, chunks a line
@@ -924,9 +932,16 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void expert_direct_kernel(const Ex
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int i = 0; i < NI; ++i)
+                    for (int i = 0; i < NI; ++i) {
+                        if constexpr (PIECES) {
+                            const uintx4 pairs = __builtin_bit_cast(uintx4, x[u][i]);
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) row_sum[i] += (float)x[u][i][q];
+                            for (int q = 0; q < 4; ++q) row_sum[i] = add_pair(pairs[q], row_sum[i]);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) row_sum[i] += (float)x[u][i][q];
+                        }
+                    }
     };
     const int whole = t.K / 64;
     if (whole > 0) {
