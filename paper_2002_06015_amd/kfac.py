@@ -842,8 +842,8 @@ def kfac_route_grad(ctx: Context, router: kfac_router, logits: torch.Tensor, cho
 
 def _fan(n: int, tokens: int) -> int:
     """Choices of a token."""
-    if n % tokens if tokens else n:
-        raise ValueError("%d choices are not the same number for each of %d tokens" % (n, tokens))
+    if n % tokens or not n if tokens else n:
+        raise ValueError("%d choices are not the same number for each of %d tokens, one at least" % (n, tokens))
     return n // tokens if n else 1
 
 

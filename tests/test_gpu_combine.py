@@ -129,3 +129,15 @@ def test_binding_refuses(ctx):
     for bad in (dict(dy=None, dgate=None), dict(y=None), dict(dy=y.bfloat16()), dict(dgate=gate[:5])):
         with pytest.raises(ValueError):
             kfac.kfac_combine_grad(**{**dict(ctx=ctx, y=y, gate=gate, dout=out, dy=torch.zeros_like(y), dgate=gate.clone()), **bad})
+
+
+def test_tokens_without_choices_are_refused(ctx):
+    """Nothing would be written for them; no tokens at all are fine."""
+    none, out = torch.empty(0, 8, device="cuda"), torch.full((5, 8), 3.0, device="cuda")
+    with pytest.raises(ValueError):
+        kfac.kfac_combine(ctx, none, None, out, residual=torch.zeros(5, 8, device="cuda"))
+    with pytest.raises(ValueError):
+        kfac.kfac_combine_grad(ctx, None, None, out, none, None)
+    kfac.kfac_combine(ctx, none, None, none.clone())
+    kfac.kfac_combine_grad(ctx, None, None, none, none.clone(), None)
+    assert bool((out == 3.0).all())
