@@ -444,7 +444,7 @@ __global__ __launch_bounds__(64, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route
                 const int number = __shfl(e, lane - sub + q);
                 better += q < ranked && (r > rank || (r == rank && number < e)) ? 1 : 0;
             }
-            if (sub < ranked) place = better;
+            if (open && sub < ranked) place = better;   // (a closed token beside has no ranks: of a softmax they would be NaN)
         }
         const unsigned long long rows = __ballot(again);
         const bool mine_again = (rows & lanes_of_row) != 0;
