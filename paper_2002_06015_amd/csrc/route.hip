@@ -333,7 +333,7 @@ __global__ __launch_bounds__(64, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route
             for (int i = 0; i < EPL; ++i) k[i] = l[i] > -INFINITY ? k[i] : -INFINITY;
         }
         if (a.groups > 1) {
-            float one = -INFINITY, two = -INFINITY, largest = 0.f;
+            float one = -INFINITY, two = -INFINITY;
 #pragma unroll
             for (int i = 0; i < EPL; ++i) {
                 two = fmaxf(two, fminf(one, k[i]));
@@ -353,9 +353,11 @@ __global__ __launch_bounds__(64, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route
             }
             const bool open = better < a.top_groups;
             if (by_score) {
-                const float low = min_of<LANES>(open ? of : INFINITY), next = max_of<LANES>(open ? -INFINITY : of);
-                largest = fmaxf(fabsf(low), fabsf(next));
-                again |= next > -INFINITY && !(low - next > 4.f * error + 0x1p-21f * largest);
+                // errors: of each rank `error` and 2^-24 of it, of the sum 2^-24; they go by the ranks, which may take most of each other away
+                const float magnitude = fabsf(one) + (a.group_best > 1 && two > -INFINITY ? fabsf(two) : 0.f);
+                const float off = one > -INFINITY ? 2.f * error + 0x1p-22f * magnitude : 0.f;
+                const float low = min_of<LANES>(open ? of - off : INFINITY), next = max_of<LANES>(open ? -INFINITY : of + off);
+                again |= next > -INFINITY && !(low > next);
             }
 #pragma unroll
             for (int i = 0; i < EPL; ++i) k[i] = !open ? -INFINITY : sums && !a.bias ? l[i] : k[i];
