@@ -357,7 +357,8 @@ __global__ __launch_bounds__(64, LANES == 64 ? 4 : EPL == 16 ? 5 : 6) void route
                 const float magnitude = fabsf(one) + (a.group_best > 1 && two > -INFINITY ? fabsf(two) : 0.f);
                 const float off = one > -INFINITY ? 2.f * error + 0x1p-22f * magnitude : 0.f;
                 const float low = min_of<LANES>(open ? of - off : INFINITY), next = max_of<LANES>(open ? -INFINITY : of + off);
-                again |= next > -INFINITY && !(low > next);
+                // (a sum beyond fp32's range is not that of a closed group)
+                again |= (next > -INFINITY && !(low > next)) || (one > -INFINITY && fabsf(of) == INFINITY);
             }
 #pragma unroll
             for (int i = 0; i < EPL; ++i) k[i] = !open ? -INFINITY : sums && !a.bias ? l[i] : k[i];
