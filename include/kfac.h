@@ -647,6 +647,7 @@ kfac_status kfac_rms_norm(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type
  *   dgamma[c] = sum_t dy[t, c] u[t, c]
  *   F_ema[c] <- decay F_ema[c] + (1 - decay) / n sum_t (dy[t, c] u[t, c])^2     the diagonal of gamma's Fisher matrix (Sec. 4.2, per unit), for
  *               per-sample gradients dy as in kfac_stats; decay = 0 does not read it; n = 0 leaves it
+ *               (and reads no operand: dgamma becomes zero)
  * dy: dev [n, dim] of `type`; h: dev [n, dim] of stream_type, what the norm was taken of; dstream, dh: dev [n, dim] of stream_type;
  * dgamma, F_ema: dev [dim] fp32, either may be NULL.  dh may be NULL; it may be dstream itself, or dy if the types agree (same rows).
  * Sums in fp32 in an order that depends on n and dim only.  Workspace: kfac_rms_norm_workspace_bytes (0 for invalid arguments; never less

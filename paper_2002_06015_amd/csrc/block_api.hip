@@ -208,8 +208,9 @@ kfac_status kfac_rms_norm_grad(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype
     a.n = n; a.dim = dim; a.dy = dy; a.lddy = lddy; a.h = h; a.ldh = ldh; a.r = dstream; a.ldr = ldr; a.dh = dh; a.lddh = lddh;
     a.gamma = gamma; a.eps = eps; a.dgamma = dgamma; a.F = F_ema; a.decay = decay; a.partial = (float *)c.ws;
     const double e = (double)n * dim;
-    bool ok = timed(ctx, KFAC_K_NORM, 1, 12.0 * e, e * (es + et * (1.0 + (dh ? 1.0 + (dstream != nullptr) : 0.0))),
-                    [&] { return launch_norm_grad(a, type == KFAC_BF16, stream_type == KFAC_BF16, c.stream); });
+    // (no rows: nothing to read, gamma neither; the sums of columns are zeros)
+    bool ok = n == 0 || timed(ctx, KFAC_K_NORM, 1, 12.0 * e, e * (es + et * (1.0 + (dh ? 1.0 + (dstream != nullptr) : 0.0))),
+                              [&] { return launch_norm_grad(a, type == KFAC_BF16, stream_type == KFAC_BF16, c.stream); });
     if (columns) ok = ok && timed(ctx, KFAC_K_NORM, 2, 0.0, 8.0 * norm_parts(n, dim) * dim, [&] { return launch_norm_join(a, c.stream); });
     return ok ? KFAC_OK : KFAC_ERR_DEVICE;
 }

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_grad_kerne
         raw.get(gamma[k]);
     }
     const int mine = threadIdx.x / THREADS;
-    if (a.n > 0) fetch((long long)blockIdx.x * ROWS + mine);
+    fetch((long long)blockIdx.x * ROWS + mine);
     for (long long row0 = (long long)blockIdx.x * ROWS; row0 < a.n; row0 += stripe) {
         const long long row = row0 + mine;
         const int dim = row < a.n ? a.dim : 0;
@@ -305,7 +305,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, int bf16, int stream_bf16, hi
 
 hipError_t launch_norm_join(const NormGradArgs &a, hipStream_t s)
 {
-    norm_join_kernel<<<dim3((unsigned)((a.dim + 31) / 32)), dim3(1024), 0, s>>>(a, norm_parts(a.n, a.dim));
+    norm_join_kernel<<<dim3((unsigned)((a.dim + 31) / 32)), dim3(1024), 0, s>>>(a, a.n > 0 ? norm_parts(a.n, a.dim) : 0);
     return hipGetLastError();
 }
 
