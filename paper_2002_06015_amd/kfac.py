@@ -796,6 +796,14 @@ def _device(ctx: Context) -> int:
     return device
 
 
+_MOST = (1 << 31) - 1
+
+
+def _too_large(*sizes: int):
+    """Of what the C calls take as int32: ctypes would pass the lower 32 bits."""
+    raise ValueError("sizes must be below 2^31, got %s" % (sizes,))
+
+
 def _mat(device: int, t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
     """The distance of the rows of a [rows, cols] tensor on the device whose rows are contiguous."""
     if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != device:
@@ -820,6 +828,8 @@ def kfac_route(ctx: Context, router: kfac_router, logits: torch.Tensor, choice: 
     if logits.dim() != 2:
         raise ValueError("logits must be [n, experts]")
     n, E, fan, dev, dtype = logits.shape[0], router.experts, router.fan, _device(ctx), logits.dtype
+    if n > _MOST:
+        _too_large(n)
     st = _lib.kfac_route(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(), _mat(dev, logits, n, E, dtype, "logits"),
                          None if bias is None else _flat(dev, bias, E, torch.float32, "bias"), _flat(dev, choice, n * fan, torch.int32, "choice"),
                          _flat(dev, gate, n * fan, torch.float32, "gate"))
@@ -833,6 +843,8 @@ def kfac_route_grad(ctx: Context, router: kfac_router, logits: torch.Tensor, cho
     if logits.dim() != 2:
         raise ValueError("logits must be [n, experts]")
     n, E, fan, dev, dtype = logits.shape[0], router.experts, router.fan, _device(ctx), logits.dtype
+    if n > _MOST:
+        _too_large(n)
     st = _lib.kfac_route_grad(ctx.handle, ctypes.addressof(router), n, _type_of(logits, "logits"), logits.data_ptr(), _mat(dev, logits, n, E, dtype, "logits"),
                               _flat(dev, choice, n * fan, torch.int32, "choice"), _flat(dev, dgate, n * fan, torch.float32, "dgate"),
                               dlogits.data_ptr(), _mat(dev, dlogits, n, E, dtype, "dlogits"))
@@ -853,6 +865,8 @@ def kfac_combine(ctx: Context, y: torch.Tensor, gate: Optional[torch.Tensor], ou
     if y.dim() != 2 or out.dim() != 2:
         raise ValueError("y must be [n, dim] and out [tokens, dim]")
     (n, dim), tokens, dev, dtype, stream = y.shape, out.shape[0], _device(ctx), y.dtype, out.dtype
+    if n > _MOST or dim > _MOST:
+        _too_large(n, dim)
     pr = ldr = 0
     if residual is not None:
         pr, ldr = residual.data_ptr(), _mat(dev, residual, tokens, dim, stream, "residual")
@@ -870,6 +884,8 @@ def kfac_combine_grad(ctx: Context, y: Optional[torch.Tensor], gate: Optional[to
     if src is None or src.dim() != 2 or dout.dim() != 2 or (dgate is None and dy is None) or (dgate is not None and y is None):
         raise ValueError("dy or dgate is needed, dgate needs y; y and dy must be [n, dim], dout [tokens, dim]")
     (n, dim), tokens, dev, dtype = src.shape, dout.shape[0], _device(ctx), src.dtype
+    if n > _MOST or dim > _MOST:
+        _too_large(n, dim)
     py = ldy = pd = lddy = pg = 0
     if dgate is not None:
         py, ldy, pg = y.data_ptr(), _mat(dev, y, n, dim, dtype, "y"), _flat(dev, dgate, n, torch.float32, "dgate")
@@ -893,6 +909,8 @@ def kfac_keep(ctx: Context, x: torch.Tensor, q: torch.Tensor, scales: torch.Tens
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
     (rows, cols), dev = x.shape, _device(ctx)
+    if cols > _MOST:
+        _too_large(cols)
     st = _lib.kfac_keep(ctx.handle, rows, cols, _type_of(x, "x"), x.data_ptr(), _mat(dev, x, rows, cols, x.dtype, "x"), *_bytes(dev, q, scales, rows, cols))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_keep")
@@ -903,6 +921,8 @@ def kfac_restore(ctx: Context, q: torch.Tensor, scales: torch.Tensor, x: torch.T
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
     (rows, cols), dev = x.shape, _device(ctx)
+    if cols > _MOST:
+        _too_large(cols)
     st = _lib.kfac_restore(ctx.handle, rows, cols, *_bytes(dev, q, scales, rows, cols), _type_of(x, "x"), x.data_ptr(), _mat(dev, x, rows, cols, x.dtype, "x"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_restore")
@@ -916,10 +936,12 @@ def kfac_kept_workspace_bytes(layer, experts: int, n: int, fan: int = 1) -> int:
 def kfac_expert_grad_weight_kept(ctx: Context, layer, order: Optional[torch.Tensor], offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
                                  dy: torch.Tensor, dW: torch.Tensor, fan: int = 1) -> None:
     """kfac_expert_grad_weight for inputs that were kept in 8 bits: q [n // fan, c_in] with its scales."""
-    n, dev = dy.shape[0], _device(ctx)
+    n, fan, dev = dy.shape[0], int(fan), _device(ctx)
+    if n > _MOST or fan > _MOST:
+        _too_large(n, fan)
     L, experts, po, pf = _expert(layer, order, offsets, n)
-    st = _lib.kfac_expert_grad_weight_kept(ctx.handle, ctypes.addressof(L), experts, n, int(fan), _type_of(dy, "dy"), po, pf,
-                                           *_bytes(dev, q, scales, n // max(1, int(fan)), L.c_in), dy.data_ptr(), _mat(dev, dy, n, L.c_out, dy.dtype, "dy"),
+    st = _lib.kfac_expert_grad_weight_kept(ctx.handle, ctypes.addressof(L), experts, n, fan, _type_of(dy, "dy"), po, pf,
+                                           *_bytes(dev, q, scales, n // max(1, fan), L.c_in), dy.data_ptr(), _mat(dev, dy, n, L.c_out, dy.dtype, "dy"),
                                            _flat(dev, dW, experts * L.c_out * (L.c_in + L.bias), torch.float32, "dW"))
     if st != KFAC_OK:
         raise KfacError(st, "kfac_expert_grad_weight_kept")
@@ -932,6 +954,8 @@ def kfac_stats_expert_kept(ctx: Context, layer, order: Optional[torch.Tensor], o
     if G_ema is not None and grad_out is None:
         raise ValueError("a factor needs its input")
     n = order.numel() if order is not None else grad_out.shape[0] if grad_out is not None else q.shape[0] * fan
+    if n > _MOST or fan > _MOST:
+        _too_large(n, fan)
     L, experts, po, pf = _expert(layer, order, offsets, n)
     dA = L.c_in + L.bias
     typ, pg, ldg, pG = KFAC_BF16, 0, 0, 0
@@ -952,6 +976,8 @@ def kfac_rms_norm(ctx: Context, x: torch.Tensor, gamma: torch.Tensor, eps: float
     if (residual is None) != (h is None) or (q is None) != (scales is None):
         raise ValueError("residual and h, and q and scales, go together")
     (n, dim), dev, dtype, typ = x.shape, _device(ctx), x.dtype, _type_of(x, "x")
+    if n > _MOST or dim > _MOST:
+        _too_large(n, dim)
     stream, pr, ldr, ph, ldh, py, ldy, pq, ldq, ps, lds = typ, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0
     if residual is not None:
         stream, pr, ldr = _type_of(residual, "residual"), residual.data_ptr(), _mat(dev, residual, n, dim, residual.dtype, "residual")
@@ -977,6 +1003,8 @@ def kfac_rms_norm_grad(ctx: Context, dy: torch.Tensor, h: torch.Tensor, gamma: t
     if dy.dim() != 2:
         raise ValueError("dy must be [n, dim]")
     (n, dim), dev, stream = dy.shape, _device(ctx), h.dtype
+    if n > _MOST or dim > _MOST:
+        _too_large(n, dim)
     pr = ldr = ph = lddh = 0
     if dstream is not None:
         pr, ldr = dstream.data_ptr(), _mat(dev, dstream, n, dim, stream, "dstream")
