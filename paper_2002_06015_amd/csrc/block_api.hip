@@ -178,8 +178,7 @@ kfac_status kfac_rms_norm(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type
 size_t kfac_rms_norm_workspace_bytes(int32_t n, int32_t dim)
 {
     if (n < 0 || n > kMaxPositions || dim < 1 || dim > kMaxNorm) return 0;
-    // (the number of parts may fall as rows get longer: the most that any shorter one has)
-    return std::max<size_t>(256, ((size_t)std::max(norm_parts(n, dim), dim > 1 ? norm_parts(n, 1) : 0) * 2 * dim * sizeof(float) + 255) / 256 * 256);
+    return std::max<size_t>(256, ((size_t)norm_parts(n, dim) * 2 * dim * sizeof(float) + 255) / 256 * 256);
 }
 
 kfac_status kfac_rms_norm_grad(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type, const void *dy, int64_t lddy, kfac_dtype stream_type,
