@@ -556,7 +556,8 @@ kfac_status kfac_stats_expert(kfac_ctx *ctx, const kfac_layer *L, int32_t expert
  *   gate[t * fan + j]     scale * s_e, without the bias; renormalise != 0: scale * s_e / (sum of the chosen s); 0 for a choice of -1
  * A NaN among a token's logits or the ranks, or a softmax over a logit of +infinity, makes all its choices -1 and all its gates NaN.
  * logits: dev [n, experts] of `type`, rows ld apart; bias: dev [experts] fp32 or NULL; choice: dev [n * fan] int32; gate: dev
- * [n, fan] fp32.  Scores and sums in fp32 (ranks that are too near to each other for that in 64 bits).
+ * [n, fan] fp32.  Scores and sums in fp32 (ranks that are too near to each other for that in 64 bits); a sigmoid below 2^-126 may count
+ * as 0 in its gate.
  */
 typedef enum { KFAC_ROUTE_SOFTMAX = 0, KFAC_ROUTE_SIGMOID = 1 } kfac_route_scores;
 typedef struct {
@@ -635,7 +636,8 @@ kfac_status kfac_stats_expert_kept(kfac_ctx *ctx, const kfac_layer *L, int32_t e
  *   y[t, c] = gamma[c] h[t, c] / sqrt(mean_c h[t, c]^2 + eps)
  * x: dev [n, dim] of `type`; residual, h: dev [n, dim] of stream_type; gamma: dev [dim] fp32; y: dev [n, dim] of `type`, or NULL;
  * q, scales: y (before its rounding to `type`) in 8 bits as by kfac_keep, or both NULL; at least one of y and q.  Sums in fp32 (a finite
- * row whose sum of squares leaves its range, from magnitudes of 1.8e19 / sqrt(dim) on, has zeros for y).
+ * row whose sum of squares leaves its range, from magnitudes of 1.8e19 / sqrt(dim) on, has zeros for y).  At the other end mean_c h^2 + eps has to
+ * be 2^-100 at least: with a smaller eps, or none, rows of magnitudes below 2^-50 lose bits with their squares and become infinite, NaN rows of zeros.
  * h may be residual itself, and x if the types agree; y may be x if it is not h (same rows each).
  */
 kfac_status kfac_rms_norm(kfac_ctx *ctx, int32_t n, int32_t dim, kfac_dtype type, const void *x, int64_t ldx, kfac_dtype stream_type,

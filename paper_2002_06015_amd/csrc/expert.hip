@@ -1277,6 +1277,11 @@ hipError_t pieces(const ExpertArgs &a, bool bf16, bool planes, hipStream_t s)
         if ((long long)a.n * row_tiles<OP, 256, 256>(a, tj) >= 2048 * 256) return run_direct_pieces<OP, 256, 256, 4, 2>(a, 256, s);
         return run_direct_pieces<OP, 128, 128, 2, 2>(a, 512, s);
     }
+    // 128 x 128 where the experts have 512 such tiles, 64 x 64 with two groups of waves below.  Weights in fp32, large and small: 477 and 640 us at
+    // 2048 tiles (8192 rows, two choices each), 156 and 179 at 512 (4096 rows), but 59 and 77 at 256 (2048 rows) and 392 and 545 for one expert
+    // with 128 (16384 rows), where the small ones are taken; bf16, no row aligned: 304 and 350 at 2048, 113 and 110 at 512, 365 and 434 for one
+    // expert with 128.  Factors in fp32: 258 and 274 at 576, 96 and 84 at 288, 48 and 41 at 80; bf16, no row aligned: 173 and 178 at 576, 71 and
+    // 66 at 288.
     if (a.experts * row_tiles<OP, 128, 128>(a, tj) >= 512) {
         if (bf16) return run_general_pieces<bf16_t, false, OP, 128, 1>(a, 512, s);
         return planes ? run_general_pieces<float, false, OP, 128, 1>(a, 512, s) : run_general_pieces<float, true, OP, 128, 1>(a, 512, s);
